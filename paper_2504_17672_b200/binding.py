@@ -30,6 +30,10 @@ EXPORTS = (
     "cocodc_pseudo_gradient_sum", "cocodc_outer_step_received",
     "cocodc_select_fragments_at", "cocodc_outer_step_at", "cocodc_outer_step_received_peers",
     "cocodc_scores_from_sumsq", "cocodc_bind_in_flight", "cocodc_flush_scores", "cocodc_initiate", "cocodc_initiate_at",
+    "cocodc_lm_create", "cocodc_lm_destroy", "cocodc_lm_poll_status", "cocodc_lm_launch_count",
+    "cocodc_lm_embed", "cocodc_lm_embed_grad", "cocodc_lm_embed_grad_workspace",
+    "cocodc_lm_glu", "cocodc_lm_glu_grad", "cocodc_lm_glu_grad_workspace",
+    "cocodc_lm_logprobs", "cocodc_lm_logprobs_grad",
 )
 NOALLOC_MAX_K, NOALLOC_MAX_SEGMENTS = 64, 64
 
@@ -109,11 +113,27 @@ def _load() -> ctypes.CDLL:
                                                      ctypes.POINTER(vp), i32, vp, vp, vp, i64, i64, vp, vp, vp, vp]
     lib.cocodc_poll_status.argtypes = [vp, vp]
     lib.cocodc_launch_count.argtypes = [vp]
-    lib.cocodc_launch_count.restype = i64
     lib.cocodc_status_string.argtypes = [ctypes.c_int]
-    lib.cocodc_status_string.restype = ctypes.c_char_p
+    f32, u64 = ctypes.c_float, ctypes.c_uint64
+    lib.cocodc_lm_create.argtypes = [ctypes.POINTER(vp), i32]
+    lib.cocodc_lm_destroy.argtypes = [vp]
+    lib.cocodc_lm_poll_status.argtypes = [vp, vp]
+    lib.cocodc_lm_launch_count.argtypes = [vp]
+    lib.cocodc_lm_embed.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp]
+    lib.cocodc_lm_embed_grad.argtypes = [vp, vp, i32, i64, vp, i32, i64, i64, i64, f32, i32, vp, i32, i64, vp, u64, vp]
+    lib.cocodc_lm_embed_grad_workspace.argtypes = [i64, i64, i64]
+    lib.cocodc_lm_glu.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, i64, i64, i64, vp, i64, vp, vp, i64, vp]
+    lib.cocodc_lm_glu_grad.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64,
+                                       vp, i64, vp, vp, i64, vp, u64, vp]
+    lib.cocodc_lm_glu_grad_workspace.argtypes = [i64, i64, i64]
+    lib.cocodc_lm_logprobs.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, i32, vp, vp, vp]
+    lib.cocodc_lm_logprobs_grad.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, i64, vp]
+    other = {"cocodc_launch_count": i64, "cocodc_status_string": ctypes.c_char_p, "cocodc_lm_launch_count": i64,
+             "cocodc_lm_embed_grad_workspace": u64, "cocodc_lm_glu_grad_workspace": u64}
+    for name, restype in other.items():
+        getattr(lib, name).restype = restype
     for name in EXPORTS:
-        if name not in ("cocodc_launch_count", "cocodc_status_string"):
+        if name not in other:
             getattr(lib, name).restype = ctypes.c_int
     return lib
 
@@ -344,3 +364,218 @@ class Context:
     def cocodc_poll_status(self, stream=None) -> int:
         """Waits for the stream; returns and clears the device status word."""
         return int(_lib.cocodc_poll_status(self._h, _stream(stream)))
+
+
+# ---- operators of the local step (include/cocodc_lm.h) ------------------------------------------------------------
+
+ACT_SILU, ACT_GELU = 0, 1
+LM_MAX_TOP = 32
+_ACTS = {"silu": ACT_SILU, "gelu": ACT_GELU, ACT_SILU: ACT_SILU, ACT_GELU: ACT_GELU}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
+
+
+def _matrix(t: torch.Tensor, name: str):
+    """(address, row stride) of a row-major matrix; a single row (or column) may have any stride."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, not {t.dim()}")
+    rows, cols = t.shape
+    s0, s1 = t.stride()
+    if s1 != 1 and cols > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return t.data_ptr(), (s0 if rows > 1 else max(cols, s0))
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype) -> Optional[int]:
+    """Address of a packed vector (or matrix) of n elements; None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a packed {dtype} tensor of {n} elements")
+    return t.data_ptr()
+
+
+def _ids(t: torch.Tensor, name: str, n: int):
+    if t.dtype not in _INDEX_TYPES or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a packed int32 or int64 tensor of {n} elements")
+    return t.data_ptr(), _INDEX_TYPES[t.dtype]
+
+
+class LmOps:
+    """Owns a cocodc_lm: the operators of a worker's local step on one device.
+
+    Sizes, strides and types are read from the tensors; outputs are written to the tensors that are passed.  Calls run
+    on `stream` (default: torch's current stream of the handle's device).  A workspace that is not passed is taken from
+    torch's caching allocator on that stream."""
+
+    def __init__(self, device: int = 0):
+        self._h = ctypes.c_void_p()
+        device = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+        self.device = torch.device("cuda", device.index or 0)
+        _check(_lib.cocodc_lm_create(ctypes.byref(self._h), self.device.index), "cocodc_lm_create")
+
+    def close(self) -> None:
+        if self._h:
+            _lib.cocodc_lm_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @property
+    def launch_count(self) -> int:
+        return int(_lib.cocodc_lm_launch_count(self._h))
+
+    def cocodc_lm_poll_status(self, stream=None) -> int:
+        """Waits for the stream; returns and clears the device status word."""
+        return int(_lib.cocodc_lm_poll_status(self._h, self._stream(stream)))
+
+    def _stream(self, stream) -> int:
+        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+
+    def _on_device(self, *tensors) -> None:
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"a tensor is on {t.device}, the handle on {self.device}")
+
+    def _scratch(self, workspace, need: int, stream):
+        if workspace is None:
+            if stream is None:
+                return torch.empty(max(16, need), dtype=torch.uint8, device=self.device)
+            with torch.cuda.stream(stream):
+                return torch.empty(max(16, need), dtype=torch.uint8, device=self.device)
+        self._on_device(workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        return workspace
+
+    def cocodc_lm_embed(self, table, ids, y, scale: float = 1.0, stream=None) -> None:
+        """y[t] = scale * table[ids[t]]; zeros where ids[t] < 0."""
+        self._on_device(table, ids, y)
+        (V, D), T = table.shape, ids.numel()
+        if y.shape != (T, D):
+            raise ValueError(f"y must be {T} x {D}")
+        tp, ts = _matrix(table, "table")
+        yp, ys = _matrix(y, "y")
+        ip, it = _ids(ids, "ids", T)
+        _check(_lib.cocodc_lm_embed(self._h, tp, _type(table), ts, V, D, ip, it, T, scale, yp, _type(y), ys,
+                                    self._stream(stream)), "cocodc_lm_embed")
+
+    def cocodc_lm_embed_grad(self, dy, ids, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None,
+                             stream=None) -> None:
+        """dtable[v] (+)= scale * sum of dy[t] over the t with ids[t] == v."""
+        self._on_device(dy, ids, dtable)
+        (V, D), T = dtable.shape, ids.numel()
+        if dy.shape != (T, D):
+            raise ValueError(f"dy must be {T} x {D}")
+        dp, ds = _matrix(dy, "dy")
+        gp, gs = _matrix(dtable, "dtable")
+        ip, it = _ids(ids, "ids", T)
+        w = self._scratch(workspace, _lib.cocodc_lm_embed_grad_workspace(V, D, T), stream)
+        _check(_lib.cocodc_lm_embed_grad(self._h, dp, _type(dy), ds, ip, it, T, V, D, scale, int(accumulate), gp,
+                                         _type(dtable), gs, w.data_ptr(), w.numel() * w.element_size(),
+                                         self._stream(stream)), "cocodc_lm_embed_grad")
+
+    def cocodc_lm_glu(self, x, wg, wu, h, gate=None, up=None, act="silu", stream=None) -> None:
+        """h = act(x wg^T) * (x wu^T); gate and up receive the two products (both or neither)."""
+        self._on_device(x, wg, wu, h, gate, up)
+        (T, D), F = x.shape, wg.shape[0]
+        if wg.shape != (F, D) or wu.shape != (F, D) or h.shape != (T, F) or (gate is not None and gate.shape != (T, F)) or \
+                (up is not None and up.shape != (T, F)):
+            raise ValueError(f"shapes do not fit x {T} x {D} and wg {F} x {D}")
+        kind = _one_type(x, wg, wu, h, gate, up)
+        xp, xs = _matrix(x, "x")
+        (gp, ws), (up_, us) = _matrix(wg, "wg"), _matrix(wu, "wu")
+        if ws != us and F > 1:
+            raise ValueError("wg and wu must have the same row stride")
+        hp, hs = _matrix(h, "h")
+        gt = ut = None
+        gs = gs2 = F
+        if gate is not None:
+            gt, gs = _matrix(gate, "gate")
+        if up is not None:
+            ut, gs2 = _matrix(up, "up")
+        if gate is not None and up is not None and gs != gs2 and T > 1:
+            raise ValueError("gate and up must have the same row stride")
+        _check(_lib.cocodc_lm_glu(self._h, _ACTS[act], kind, xp, xs, gp, up_, ws, T, D, F, hp, hs, gt, ut, gs,
+                                  self._stream(stream)), "cocodc_lm_glu")
+
+    def cocodc_lm_glu_grad(self, dh, gate, up, x, wg, wu, dx=None, dwg=None, dwu=None, act="silu", workspace=None,
+                           stream=None) -> None:
+        """dx, dwg, dwu of cocodc_lm_glu from dh and the gate and up that it wrote; dx, or dwg and dwu, may be None."""
+        self._on_device(dh, gate, up, x, wg, wu, dx, dwg, dwu)
+        (T, D), F = x.shape, wg.shape[0]
+        for name, t, shape in (("dh", dh, (T, F)), ("gate", gate, (T, F)), ("up", up, (T, F)), ("wg", wg, (F, D)), ("wu", wu, (F, D)),
+                               ("dx", dx, (T, D)), ("dwg", dwg, (F, D)), ("dwu", dwu, (F, D))):
+            if t is not None and t.shape != shape:
+                raise ValueError(f"{name} must be {shape[0]} x {shape[1]}")
+        kind = _one_type(x, wg, wu, dh, gate, up, dx, dwg, dwu)
+        hp, hs = _matrix(dh, "dh")
+        (gt, gs), (ut, us) = _matrix(gate, "gate"), _matrix(up, "up")
+        xp, xs = _matrix(x, "x")
+        (gp, ws), (up_, ws2) = _matrix(wg, "wg"), _matrix(wu, "wu")
+        if (gs != us and T > 1) or (ws != ws2 and F > 1):
+            raise ValueError("gate and up, and wg and wu, must have the same row stride")
+        dxp, dxs = _matrix(dx, "dx") if dx is not None else (None, D)
+        dgp, dws = _matrix(dwg, "dwg") if dwg is not None else (None, D)
+        dup, dws2 = _matrix(dwu, "dwu") if dwu is not None else (None, dws)
+        if dwg is not None and dws != dws2 and F > 1:
+            raise ValueError("dwg and dwu must have the same row stride")
+        w = self._scratch(workspace, _lib.cocodc_lm_glu_grad_workspace(T, D, F), stream)
+        _check(_lib.cocodc_lm_glu_grad(self._h, _ACTS[act], kind, hp, hs, gt, ut, gs, xp, xs, gp, up_, ws, T, D, F, dxp, dxs,
+                                       dgp, dup, dws, w.data_ptr(), w.numel() * w.element_size(), self._stream(stream)),
+               "cocodc_lm_glu_grad")
+
+    def cocodc_lm_logprobs(self, logits, targets, logp, entropy=None, lse=None, top_ids=None, top_logp=None,
+                           scale: float = 1.0, stream=None) -> None:
+        """Per row of scale * logits: log probability of targets[t] (0 where it is negative), entropy, log-sum-exp, and the
+        largest logits' ids and log probabilities (top_ids, top_logp: T x k).  targets and logp may both be None."""
+        self._on_device(logits, targets, logp, entropy, lse, top_ids, top_logp)
+        T, V = logits.shape
+        lp, ls = _matrix(logits, "logits")
+        tp, tt = _ids(targets, "targets", T) if targets is not None else (None, 0)
+        f32 = torch.float32
+        k = 0
+        if top_ids is not None:
+            if top_ids.dim() != 2 or top_ids.shape[0] != T:
+                raise ValueError("top_ids must be T x k")
+            k = top_ids.shape[1]
+        _check(_lib.cocodc_lm_logprobs(self._h, lp, _type(logits), ls, T, V, tp, tt, scale, _vector(logp, "logp", T, f32),
+                                       _vector(entropy, "entropy", T, f32), _vector(lse, "lse", T, f32), k,
+                                       _vector(top_ids, "top_ids", T * k, torch.int32) if k else None,
+                                       _vector(top_logp, "top_logp", T * k, f32) if k else None, self._stream(stream)),
+               "cocodc_lm_logprobs")
+
+    def cocodc_lm_logprobs_grad(self, logits, targets, lse, entropy, dlogp, dentropy, dlogits, scale: float = 1.0,
+                                stream=None) -> None:
+        """dlogits of cocodc_lm_logprobs given d/dlogp and d/dentropy (None for zero); dlogits may be logits itself."""
+        self._on_device(logits, targets, lse, entropy, dlogp, dentropy, dlogits)
+        T, V = logits.shape
+        if dlogits.shape != (T, V):
+            raise ValueError(f"dlogits must be {T} x {V}")
+        kind = _one_type(logits, dlogits)
+        lp, ls = _matrix(logits, "logits")
+        dp, ds = _matrix(dlogits, "dlogits")
+        tp, tt = _ids(targets, "targets", T) if targets is not None else (None, 0)
+        f32 = torch.float32
+        _check(_lib.cocodc_lm_logprobs_grad(self._h, lp, kind, ls, T, V, tp, tt, scale, _vector(lse, "lse", T, f32),
+                                            _vector(entropy, "entropy", T, f32), _vector(dlogp, "dlogp", T, f32),
+                                            _vector(dentropy, "dentropy", T, f32), dp, ds, self._stream(stream)),
+               "cocodc_lm_logprobs_grad")
+
+
+def _type(t: torch.Tensor) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"type {t.dtype} is not supported (float32, bfloat16, float16)")
+    return _TYPES[t.dtype]
+
+
+def _one_type(*tensors) -> int:
+    first = tensors[0]
+    for t in tensors:
+        if t is not None and t.dtype != first.dtype:
+            raise ValueError("the tensors must have one type")
+    return _type(first)

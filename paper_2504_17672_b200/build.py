@@ -9,11 +9,11 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIBRARY = os.path.join(_HERE, "libcocodc.so")
-HEADER = os.path.join(os.path.dirname(_HERE), "include", "cocodc.h")
+HEADERS = os.path.join(os.path.dirname(_HERE), "include", "*.h")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC", "-shared", "--threads", "0",
 ]
 
 
@@ -25,7 +25,7 @@ def _stale() -> bool:
     if not os.path.exists(LIBRARY):
         return True
     t = os.path.getmtime(LIBRARY)
-    deps = glob.glob(os.path.join(CSRC, "*")) + [HEADER]
+    deps = glob.glob(os.path.join(CSRC, "*")) + glob.glob(HEADERS)
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,0 +1,61 @@
+// Handle of the local step's operators (include/cocodc_lm.h): a status word and a launch counter.
+
+#include "lm_common.cuh"
+
+#include <new>
+
+using namespace cocodc_lm_impl;
+
+extern "C" {
+
+cocodc_status cocodc_lm_create(cocodc_lm** lm_out, int32_t device) {
+  if (!lm_out) return COCODC_ERR_INVALID_ARG;
+  *lm_out = nullptr;
+  int n_dev = 0;
+  if (cudaGetDeviceCount(&n_dev) != cudaSuccess) return COCODC_ERR_CUDA;
+  if (device < 0 || device >= n_dev) return COCODC_ERR_INVALID_ARG;
+  DeviceScope scope(device);
+  if (!scope.ok) return COCODC_ERR_CUDA;
+  cocodc_lm* lm = new (std::nothrow) cocodc_lm();
+  if (!lm) return COCODC_ERR_NOMEM;
+  lm->device = device;
+  bool ok = cudaDeviceGetAttribute(&lm->sm_count, cudaDevAttrMultiProcessorCount, device) == cudaSuccess;
+  ok = ok && cudaMalloc(&lm->d_status, sizeof(int)) == cudaSuccess;
+  ok = ok && cudaMemset(lm->d_status, 0, sizeof(int)) == cudaSuccess;
+  ok = ok && embed_prepare() && glu_prepare() && logprobs_prepare();
+  if (!ok) {
+    cudaGetLastError();
+    cudaFree(lm->d_status);
+    delete lm;
+    return COCODC_ERR_CUDA;
+  }
+  *lm_out = lm;
+  return COCODC_OK;
+}
+
+cocodc_status cocodc_lm_destroy(cocodc_lm* lm) {
+  if (!lm) return COCODC_OK;
+  DeviceScope scope(lm->device);
+  const bool ok = scope.ok && cudaFree(lm->d_status) == cudaSuccess;
+  delete lm;
+  return ok ? COCODC_OK : COCODC_ERR_CUDA;
+}
+
+cocodc_status cocodc_lm_poll_status(cocodc_lm* lm, void* stream) {
+  if (!lm) return COCODC_ERR_INVALID_ARG;
+  DeviceScope scope(lm->device);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int word = 0;
+  if (!scope.ok || cudaMemcpyAsync(&word, lm->d_status, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaStreamSynchronize(st) != cudaSuccess)
+    return COCODC_ERR_CUDA;
+  // cleared only when something was read: an error that a call on another stream records meanwhile is not lost
+  if (word != 0 && (cudaMemsetAsync(lm->d_status, 0, sizeof(int), st) != cudaSuccess ||
+                    cudaStreamSynchronize(st) != cudaSuccess))
+    return COCODC_ERR_CUDA;
+  return static_cast<cocodc_status>(word);
+}
+
+int64_t cocodc_lm_launch_count(const cocodc_lm* lm) { return lm ? (int64_t)lm->launches.load() : 0; }
+
+}  // extern "C"

@@ -1,0 +1,95 @@
+// Shared by the operators of the local step (lm_*.cu): the handle, argument checks, element types.
+#pragma once
+
+#include "../../include/cocodc_lm.h"
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstdint>
+
+struct cocodc_lm {
+  int device = 0;
+  int sm_count = 0;
+  int* d_status = nullptr;
+  std::atomic<long long> launches{0};
+};
+
+namespace cocodc_lm_impl {
+
+// Each source file opts its kernels in to the shared memory they need, once, at creation of a handle (the
+// attribute is per device and outlives the handle).
+bool embed_prepare();
+bool glu_prepare();
+bool logprobs_prepare();
+
+struct DeviceScope {
+  int prev = -1;
+  bool switched = false, ok = true;
+  explicit DeviceScope(int dev) {
+    ok = cudaGetDevice(&prev) == cudaSuccess;
+    if (ok && prev != dev) ok = switched = cudaSetDevice(dev) == cudaSuccess;
+  }
+  ~DeviceScope() { if (switched) cudaSetDevice(prev); }
+};
+
+inline cocodc_status launched(cocodc_lm* lm, int kernels = 1) {
+  lm->launches.fetch_add(kernels, std::memory_order_relaxed);
+  return cudaGetLastError() == cudaSuccess ? COCODC_OK : COCODC_ERR_CUDA;
+}
+
+inline bool known_type(int32_t t) { return t == COCODC_F32 || t == COCODC_BF16 || t == COCODC_F16; }
+inline int type_bytes(int32_t t) { return t == COCODC_F32 ? 4 : 2; }
+inline int index_bytes(int32_t t) { return t == COCODC_I32 ? 4 : 8; }
+inline bool on_boundary(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+// Rows that start on 16-byte boundaries: what vector loads and tensor maps need.
+inline bool rows_aligned(const void* p, int64_t stride, int esize) {
+  return on_boundary(p, 16) && (stride * esize) % 16 == 0;
+}
+// Sizes whose products with an element size stay far inside 64 bits.
+inline bool sane(int64_t n) { return n >= 0 && n <= (int64_t(1) << 40); }
+
+// The bytes [lo, hi) that a matrix spans; empty for no rows.
+struct Span { uintptr_t lo, hi; };
+inline Span span(const void* p, int64_t rows, int64_t stride, int64_t width, int esize) {
+  const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+  if (!p || rows < 1 || width < 1) return Span{b, b};
+  return Span{b, b + ((uintptr_t)(rows - 1) * (uintptr_t)stride + (uintptr_t)width) * (uintptr_t)esize};
+}
+inline bool meet(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
+
+// ---- device side -------------------------------------------------------------------------------
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+__device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
+
+// The token id at t as a row number: -1 for "no token", also for an id outside [0, V), which is recorded.
+__device__ __forceinline__ long long token_at(const void* ids, int is64, long long t, long long V, int* status) {
+  const long long v = is64 ? static_cast<const long long*>(ids)[t] : (long long)static_cast<const int*>(ids)[t];
+  if (v < V) return v < 0 ? -1 : v;
+  record(status, COCODC_ERR_INVALID_ARG);
+  return -1;
+}
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Calls f with a value of the C++ type that a type code stands for.
+template <typename F> bool with_type(int32_t t, F&& f) {
+  if (t == COCODC_F32) return f(float());
+  if (t == COCODC_BF16) return f(__nv_bfloat16());
+  return f(__half());
+}
+
+}  // namespace cocodc_lm_impl

@@ -1,0 +1,261 @@
+// The gated feed-forward block h = act(x Wg^T) * (x Wu^T) and its gradient (include/cocodc_lm.h).
+
+#include "lm_common.cuh"
+
+using namespace cocodc_lm_impl;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// act(g) = g * s(g) for both activations: s is the logistic function of g (SILU) or of 2z, z = sqrt(2/pi) (g + 0.044715 g^3)
+// (GELU: (1 + tanh z) / 2 is that function of 2z).  The cubic is taken at g clamped to [-30, 30], where s has long
+// been exactly 0 or 1, so that a large g cannot turn it into Inf (and its slope into 0 * Inf).
+struct Activation { float value, slope; };
+template <int ACT> __device__ __forceinline__ Activation activate(float g) {
+  float z = g, dz = 1.f;
+  if (ACT == COCODC_ACT_GELU) {
+    const float k = 2.f * 0.7978845608028654f, b = 0.044715f;
+    const float q = fminf(fmaxf(g, -30.f), 30.f);
+    z = k * (q + b * q * q * q);
+    dz = k * (1.f + 3.f * b * q * q);
+  }
+  const float s = __fdividef(1.f, 1.f + fast_exp2(-z * kLog2e));
+  return Activation{g * s, s + g * (s * (1.f - s)) * dz};
+}
+
+// ---- products of any strides and sizes: fp32 on the CUDA cores -----------------------------------
+// C[m][n] = sum over sources s < S and k < K of A_s(m, k) * B_s(n, k), 64 x 64 tiles.
+template <typename T> struct Operand {
+  const T* p;
+  long long outer, k;     // element strides of the row (m or n) and of k
+};
+constexpr int kTile = 64, kDepth = 16;
+
+template <typename T>
+__device__ __forceinline__ void load_tile(float (*dst)[kTile + 1], const Operand<T>& o, long long r0, long long rows,
+                                          long long k0, long long K) {
+  for (int i = threadIdx.x; i < kTile * kDepth; i += 256) {
+    // consecutive threads along the contiguous axis
+    const int r = o.k == 1 ? i / kDepth : i % kTile, k = o.k == 1 ? i % kDepth : i / kTile;
+    const bool in = r0 + r < rows && k0 + k < K;
+    dst[k][r] = in ? to_f32(o.p[(r0 + r) * o.outer + (k0 + k) * o.k]) : 0.f;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void accumulate(float (&c)[4][4], const Operand<T>& A, const Operand<T>& B, long long m0,
+                                           long long M, long long n0, long long N, long long K,
+                                           float (*sa)[kTile + 1], float (*sb)[kTile + 1]) {
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  for (long long k0 = 0; k0 < K; k0 += kDepth) {
+    load_tile(sa, A, m0, M, k0, K);
+    load_tile(sb, B, n0, N, k0, K);
+    __syncthreads();
+    for (int k = 0; k < kDepth; ++k)
+      for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j) c[i][j] = fmaf(sa[k][ty * 4 + i], sb[k][tx * 4 + j], c[i][j]);
+    __syncthreads();
+  }
+}
+
+template <typename T> struct PlainArgs {
+  Operand<T> a[2], b[2];
+  long long M, N, K;
+  T* out[3];              // forward: h, gate, up; otherwise out[blockIdx.z]
+  long long ld, ld_gu;
+};
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) k_glu_plain(const PlainArgs<T> p) {
+  __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
+  const long long m0 = (long long)blockIdx.x * kTile, n0 = (long long)blockIdx.y * kTile;
+  float g[4][4] = {}, u[4][4] = {};
+  accumulate(g, p.a[0], p.b[0], m0, p.M, n0, p.N, p.K, sa, sb);
+  accumulate(u, p.a[0], p.b[1], m0, p.M, n0, p.N, p.K, sa, sb);
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < 4; ++j) {
+      const long long m = m0 + threadIdx.x / 16 * 4 + i, n = n0 + threadIdx.x % 16 * 4 + j;
+      if (m >= p.M || n >= p.N) continue;
+      p.out[0][m * p.ld + n] = from_f32<T>(activate<ACT>(g[i][j]).value * u[i][j]);
+      if (p.out[1]) {
+        p.out[1][m * p.ld_gu + n] = from_f32<T>(g[i][j]);
+        p.out[2][m * p.ld_gu + n] = from_f32<T>(u[i][j]);
+      }
+    }
+}
+
+// SUM: one output, both sources added (dx); otherwise source and output z (dwg, dwu)
+template <typename T, bool SUM>
+__global__ void __launch_bounds__(256) k_product_plain(const PlainArgs<T> p) {
+  __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
+  const long long m0 = (long long)blockIdx.x * kTile, n0 = (long long)blockIdx.y * kTile;
+  const int z = blockIdx.z;
+  float c[4][4] = {};
+  accumulate(c, p.a[z], p.b[z], m0, p.M, n0, p.N, p.K, sa, sb);
+  if (SUM) accumulate(c, p.a[1], p.b[1], m0, p.M, n0, p.N, p.K, sa, sb);
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < 4; ++j) {
+      const long long m = m0 + threadIdx.x / 16 * 4 + i, n = n0 + threadIdx.x % 16 * 4 + j;
+      if (m < p.M && n < p.N) p.out[z][m * p.ld + n] = from_f32<T>(c[i][j]);
+    }
+}
+
+// ---- the element-wise part of the gradient ------------------------------------------------------
+// dg and du go to scratch of pitch F rounded up to 8 elements, so that its rows start on 16-byte boundaries.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) k_glu_slope(const T* dh, long long dh_stride, const T* gate, const T* up,
+                                                   long long gu_stride, long long rows, long long F, T* dg, T* du,
+                                                   long long pitch) {
+  const long long n = rows * F;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+    const long long t = i / F, f = i - t * F;
+    const float d = to_f32(dh[t * dh_stride + f]), u = to_f32(up[t * gu_stride + f]);
+    const Activation x = activate<ACT>(to_f32(gate[t * gu_stride + f]));
+    dg[t * pitch + f] = from_f32<T>(d * u * x.slope);
+    du[t * pitch + f] = from_f32<T>(d * x.value);
+  }
+}
+
+template <typename F> void with_glu(int32_t type, int32_t act, F&& f) {
+  if (type == COCODC_BF16) {
+    if (act == COCODC_ACT_SILU) f(__nv_bfloat16(), std::integral_constant<int, COCODC_ACT_SILU>());
+    else f(__nv_bfloat16(), std::integral_constant<int, COCODC_ACT_GELU>());
+  } else {
+    if (act == COCODC_ACT_SILU) f(__half(), std::integral_constant<int, COCODC_ACT_SILU>());
+    else f(__half(), std::integral_constant<int, COCODC_ACT_GELU>());
+  }
+}
+
+int64_t scratch_pitch(int64_t F) { return (F + 7) / 8 * 8; }
+
+bool tiles_fit(int64_t rows, int64_t cols) { return (rows + kTile - 1) / kTile <= INT32_MAX && (cols + kTile - 1) / kTile <= 65535; }
+
+}  // namespace
+
+namespace cocodc_lm_impl {
+bool glu_prepare() { return true; }
+}  // namespace cocodc_lm_impl
+
+extern "C" {
+
+cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void* x, int64_t x_stride, const void* wg,
+                            const void* wu, int64_t w_stride, int64_t T, int64_t D, int64_t F, void* h,
+                            int64_t h_stride, void* gate, void* up, int64_t gu_stride, void* stream) {
+  if (!lm || (act != COCODC_ACT_SILU && act != COCODC_ACT_GELU) || (type != COCODC_BF16 && type != COCODC_F16) ||
+      !sane(T) || !sane(D) || !sane(F) || T > INT32_MAX || D < 1 || D > INT32_MAX || F < 1 || F > INT32_MAX ||
+      x_stride < D || w_stride < D || h_stride < F || !sane(x_stride) || !sane(w_stride) || !sane(h_stride))
+    return COCODC_ERR_INVALID_ARG;
+  if ((gate == nullptr) != (up == nullptr) || (gate && (gu_stride < F || !sane(gu_stride)))) return COCODC_ERR_INVALID_ARG;
+  if (T == 0) return COCODC_OK;
+  if (!x || !wg || !wu || !h || !tiles_fit(T, F)) return COCODC_ERR_INVALID_ARG;
+  for (const void* p : {x, wg, wu, (const void*)h, (const void*)gate, (const void*)up})
+    if (!on_boundary(p, 2)) return COCODC_ERR_ALIGNMENT;
+  const Span in[3] = {span(x, T, x_stride, D, 2), span(wg, F, w_stride, D, 2), span(wu, F, w_stride, D, 2)};
+  const Span out[3] = {span(h, T, h_stride, F, 2), span(gate, T, gu_stride, F, 2), span(up, T, gu_stride, F, 2)};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 3; ++j)
+      if (meet(out[i], in[j])) return COCODC_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return COCODC_ERR_ALIAS;
+  }
+  DeviceScope scope(lm->device);
+  if (!scope.ok) return COCODC_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  with_glu(type, act, [&](auto e, auto a) {
+    using E = decltype(e);
+    PlainArgs<E> p{};
+    p.a[0] = {static_cast<const E*>(x), x_stride, 1};
+    p.b[0] = {static_cast<const E*>(wg), w_stride, 1};
+    p.b[1] = {static_cast<const E*>(wu), w_stride, 1};
+    p.M = T; p.N = F; p.K = D;
+    p.out[0] = static_cast<E*>(h);
+    p.out[1] = static_cast<E*>(gate);
+    p.out[2] = static_cast<E*>(up);
+    p.ld = h_stride;
+    p.ld_gu = gu_stride;
+    const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((F + kTile - 1) / kTile));
+    k_glu_plain<E, decltype(a)::value><<<grid, 256, 0, st>>>(p);
+  });
+  return launched(lm);
+}
+
+uint64_t cocodc_lm_glu_grad_workspace(int64_t T, int64_t D, int64_t F) {
+  if (!sane(T) || !sane(D) || !sane(F)) return 0;
+  return 16 + 2 * (uint64_t)T * (uint64_t)scratch_pitch(F) * 2;
+}
+
+cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const void* dh, int64_t dh_stride,
+                                 const void* gate, const void* up, int64_t gu_stride, const void* x, int64_t x_stride,
+                                 const void* wg, const void* wu, int64_t w_stride, int64_t T, int64_t D, int64_t F,
+                                 void* dx, int64_t dx_stride, void* dwg, void* dwu, int64_t dw_stride,
+                                 void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!lm || (act != COCODC_ACT_SILU && act != COCODC_ACT_GELU) || (type != COCODC_BF16 && type != COCODC_F16) ||
+      !sane(T) || !sane(D) || !sane(F) || T > INT32_MAX || D < 1 || D > INT32_MAX || F < 1 || F > INT32_MAX ||
+      x_stride < D || w_stride < D || dh_stride < F || gu_stride < F || !sane(x_stride) || !sane(w_stride) ||
+      !sane(dh_stride) || !sane(gu_stride) || (dx && (dx_stride < D || !sane(dx_stride))) ||
+      (dwg == nullptr) != (dwu == nullptr) || (dwg && (dw_stride < D || !sane(dw_stride))) || (!dx && !dwg))
+    return COCODC_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < cocodc_lm_glu_grad_workspace(T, D, F)) return COCODC_ERR_INVALID_ARG;
+  if (T > 0 && (!dh || !gate || !up || (dwg && !x) || (dx && (!wg || !wu)))) return COCODC_ERR_INVALID_ARG;
+  if (!tiles_fit(T, D) || !tiles_fit(F, D)) return COCODC_ERR_INVALID_ARG;
+  for (const void* p : {dh, gate, up, x, wg, wu, (const void*)dx, (const void*)dwg, (const void*)dwu})
+    if (!on_boundary(p, 2)) return COCODC_ERR_ALIGNMENT;
+  if (!on_boundary(workspace, 16)) return COCODC_ERR_ALIGNMENT;
+  const Span in[6] = {span(dh, T, dh_stride, F, 2), span(gate, T, gu_stride, F, 2), span(up, T, gu_stride, F, 2),
+                      span(x, T, x_stride, D, 2), span(wg, F, w_stride, D, 2), span(wu, F, w_stride, D, 2)};
+  const Span out[4] = {span(dx, T, dx_stride, D, 2), span(dwg, F, dw_stride, D, 2), span(dwu, F, dw_stride, D, 2),
+                       span(workspace, 1, (int64_t)workspace_bytes, (int64_t)workspace_bytes, 1)};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 6; ++j)
+      if (meet(out[i], in[j])) return COCODC_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return COCODC_ERR_ALIAS;
+  }
+  DeviceScope scope(lm->device);
+  if (!scope.ok) return COCODC_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int kernels = 0;
+  with_glu(type, act, [&](auto e, auto a) {
+    using E = decltype(e);
+    const int64_t pitch = scratch_pitch(F);
+    E* dg = static_cast<E*>(workspace);
+    E* du = dg + T * pitch;
+    if (T > 0) {
+      const long long blocks = (T * F + 255) / 256;
+      k_glu_slope<E, decltype(a)::value><<<(unsigned)(blocks < (1 << 16) ? blocks : (1 << 16)), 256, 0, st>>>(
+          static_cast<const E*>(dh), dh_stride, static_cast<const E*>(gate), static_cast<const E*>(up), gu_stride, T, F,
+          dg, du, pitch);
+      ++kernels;
+    }
+    if (dx && T > 0) {
+      PlainArgs<E> p{};
+      p.a[0] = {dg, pitch, 1};
+      p.a[1] = {du, pitch, 1};
+      p.b[0] = {static_cast<const E*>(wg), 1, w_stride};
+      p.b[1] = {static_cast<const E*>(wu), 1, w_stride};
+      p.M = T; p.N = D; p.K = F;
+      p.out[0] = static_cast<E*>(dx);
+      p.ld = dx_stride;
+      const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile));
+      k_product_plain<E, true><<<grid, 256, 0, st>>>(p);
+      ++kernels;
+    }
+    if (dwg) {
+      PlainArgs<E> p{};
+      p.a[0] = {dg, 1, pitch};
+      p.a[1] = {du, 1, pitch};
+      p.b[0] = p.b[1] = {static_cast<const E*>(x), 1, x_stride};
+      p.M = F; p.N = D; p.K = T;
+      p.out[0] = static_cast<E*>(dwg);
+      p.out[1] = static_cast<E*>(dwu);
+      p.ld = dw_stride;
+      const dim3 grid((unsigned)((F + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile), 2);
+      k_product_plain<E, false><<<grid, 256, 0, st>>>(p);
+      ++kernels;
+    }
+  });
+  return launched(lm, kernels);
+}
+
+}  // extern "C"
