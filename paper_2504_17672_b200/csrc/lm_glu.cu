@@ -1,10 +1,10 @@
 // The gated feed-forward block h = act(x Wg^T) * (x Wu^T) and its gradient (include/cocodc_lm.h).
 
-#include "lm_common.cuh"
+#include "lm_glu_tc.cuh"
 
 using namespace cocodc_lm_impl;
 
-namespace {
+namespace cocodc_lm_impl {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -23,6 +23,11 @@ template <int ACT> __device__ __forceinline__ Activation activate(float g) {
   const float s = __fdividef(1.f, 1.f + fast_exp2(-z * kLog2e));
   return Activation{g * s, s + g * (s * (1.f - s)) * dz};
 }
+template <int ACT> __device__ __forceinline__ float act_value(float g) { return activate<ACT>(g).value; }
+
+}  // namespace cocodc_lm_impl
+
+namespace {
 
 // ---- products of any strides and sizes: fp32 on the CUDA cores -----------------------------------
 // C[m][n] = sum over sources s < S and k < K of A_s(m, k) * B_s(n, k), 64 x 64 tiles.
@@ -129,12 +134,53 @@ template <typename F> void with_glu(int32_t type, int32_t act, F&& f) {
 
 int64_t scratch_pitch(int64_t F) { return (F + 7) / 8 * 8; }
 
+// ---- tensor-core path: host side ----------------------------------------------------------------
+std::atomic<EncodeTiled> g_encode{nullptr};
+
+template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t stride, int64_t rows, int64_t cols, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return g_encode.load()(map, IsBf16<E>::v ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                         const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int tiles_of(int64_t n, int tile) { return (int)((n + tile - 1) / tile); }
+
+template <typename E, int MODE, int ACT> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
+  const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices;
+  if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;
+  k_glu_tc<E, MODE, ACT><<<(unsigned)(tiles < lm->sm_count ? tiles : lm->sm_count), kTcThreads, kTcSmem, st>>>(a);
+  return launched(lm);
+}
+
 bool tiles_fit(int64_t rows, int64_t cols) { return (rows + kTile - 1) / kTile <= INT32_MAX && (cols + kTile - 1) / kTile <= 65535; }
 
 }  // namespace
 
 namespace cocodc_lm_impl {
-bool glu_prepare() { return true; }
+bool glu_prepare() {
+  if (!g_encode.load()) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || !fn) return false;
+    g_encode.store(reinterpret_cast<EncodeTiled>(fn));
+  }
+  bool ok = true;
+  const auto allow = [&](auto kernel) {
+    ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) == cudaSuccess;
+  };
+  allow(k_glu_tc<__nv_bfloat16, GLU_FWD, COCODC_ACT_SILU>);
+  allow(k_glu_tc<__nv_bfloat16, GLU_FWD, COCODC_ACT_GELU>);
+  allow(k_glu_tc<__half, GLU_FWD, COCODC_ACT_SILU>);
+  allow(k_glu_tc<__half, GLU_FWD, COCODC_ACT_GELU>);
+  allow(k_glu_tc<__nv_bfloat16, GLU_DX, 0>);
+  allow(k_glu_tc<__half, GLU_DX, 0>);
+  allow(k_glu_tc<__nv_bfloat16, GLU_DW, 0>);
+  allow(k_glu_tc<__half, GLU_DW, 0>);
+  return ok;
+}
 }  // namespace cocodc_lm_impl
 
 extern "C" {
@@ -162,8 +208,29 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool tensor = rows_aligned(x, x_stride, 2) && rows_aligned(wg, w_stride, 2) && rows_aligned(wu, w_stride, 2) &&
+                      rows_aligned(h, h_stride, 2) && (!gate || (rows_aligned(gate, gu_stride, 2) && rows_aligned(up, gu_stride, 2)));
+  cocodc_status result = COCODC_OK;
   with_glu(type, act, [&](auto e, auto a) {
     using E = decltype(e);
+    if (tensor) {
+      TcArgs c{};
+      bool ok = map_of<E>(&c.a[0], x, x_stride, T, D, kBM) && map_of<E>(&c.b[0], wg, w_stride, F, D, kBN / 2) &&
+                map_of<E>(&c.b[1], wu, w_stride, F, D, kBN / 2) && map_of<E>(&c.c[0], h, h_stride, T, F, 32);
+      if (gate) ok = ok && map_of<E>(&c.c[1], gate, gu_stride, T, F, 32) && map_of<E>(&c.c[2], up, gu_stride, T, F, 32);
+      c.m_tiles = tiles_of(T, kBM);
+      c.n_tiles = tiles_of(F, kBN / 2);
+      c.matrices = c.sources = 1;
+      c.k_blocks = tiles_of(D, kBK);
+      c.M = (int)T;
+      c.N = (int)F;
+      c.save = gate != nullptr;
+      c.out[0] = h; c.out[1] = gate; c.out[2] = up;
+      c.ld[0] = h_stride; c.ld[1] = c.ld[2] = gu_stride;
+      c.status = lm->d_status;
+      result = ok ? run_tc<E, GLU_FWD, decltype(a)::value>(lm, c, st) : COCODC_ERR_CUDA;
+      return;
+    }
     PlainArgs<E> p{};
     p.a[0] = {static_cast<const E*>(x), x_stride, 1};
     p.b[0] = {static_cast<const E*>(wg), w_stride, 1};
@@ -176,8 +243,9 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
     p.ld_gu = gu_stride;
     const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((F + kTile - 1) / kTile));
     k_glu_plain<E, decltype(a)::value><<<grid, 256, 0, st>>>(p);
+    result = launched(lm);
   });
-  return launched(lm);
+  return result;
 }
 
 uint64_t cocodc_lm_glu_grad_workspace(int64_t T, int64_t D, int64_t F) {
@@ -215,20 +283,39 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int kernels = 0;
+  const bool tensor_dx = rows_aligned(wg, w_stride, 2) && rows_aligned(wu, w_stride, 2) && rows_aligned(dx, dx_stride, 2);
+  const bool tensor_dw = rows_aligned(x, x_stride, 2) && rows_aligned(dwg, dw_stride, 2) && rows_aligned(dwu, dw_stride, 2);
+  cocodc_status result = COCODC_OK;
   with_glu(type, act, [&](auto e, auto a) {
     using E = decltype(e);
     const int64_t pitch = scratch_pitch(F);
     E* dg = static_cast<E*>(workspace);
     E* du = dg + T * pitch;
+    const auto took = [&](cocodc_status s) { if (result == COCODC_OK) result = s; };
     if (T > 0) {
       const long long blocks = (T * F + 255) / 256;
       k_glu_slope<E, decltype(a)::value><<<(unsigned)(blocks < (1 << 16) ? blocks : (1 << 16)), 256, 0, st>>>(
           static_cast<const E*>(dh), dh_stride, static_cast<const E*>(gate), static_cast<const E*>(up), gu_stride, T, F,
           dg, du, pitch);
-      ++kernels;
+      took(launched(lm));
     }
-    if (dx && T > 0) {
+    TcArgs c{};
+    c.status = lm->d_status;
+    c.N = (int)D;
+    c.n_tiles = tiles_of(D, kBN);
+    if (dx && T > 0 && tensor_dx) {
+      const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, kBM) && map_of<E>(&c.a[1], du, pitch, T, F, kBM) &&
+                      map_of<E>(&c.b[0], wg, w_stride, F, D, kBK) && map_of<E>(&c.b[1], wu, w_stride, F, D, kBK) &&
+                      map_of<E>(&c.c[0], dx, dx_stride, T, D, 32);
+      c.m_tiles = tiles_of(T, kBM);
+      c.matrices = 1;
+      c.sources = 2;
+      c.out[0] = dx;
+      c.ld[0] = dx_stride;
+      c.k_blocks = tiles_of(F, kBK);
+      c.M = (int)T;
+      took(ok ? run_tc<E, GLU_DX, 0>(lm, c, st) : COCODC_ERR_CUDA);
+    } else if (dx && T > 0) {
       PlainArgs<E> p{};
       p.a[0] = {dg, pitch, 1};
       p.a[1] = {du, pitch, 1};
@@ -239,9 +326,21 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       p.ld = dx_stride;
       const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile));
       k_product_plain<E, true><<<grid, 256, 0, st>>>(p);
-      ++kernels;
+      took(launched(lm));
     }
-    if (dwg) {
+    if (dwg && tensor_dw && T > 0) {
+      const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, kBK) && map_of<E>(&c.a[1], du, pitch, T, F, kBK) &&
+                      map_of<E>(&c.b[0], x, x_stride, T, D, kBK) && map_of<E>(&c.c[0], dwg, dw_stride, F, D, 32) &&
+                      map_of<E>(&c.c[1], dwu, dw_stride, F, D, 32);
+      c.m_tiles = tiles_of(F, kBM);
+      c.matrices = 2;
+      c.sources = 1;
+      c.out[0] = dwg; c.out[1] = dwu;
+      c.ld[0] = c.ld[1] = dw_stride;
+      c.k_blocks = tiles_of(T, kBK);
+      c.M = (int)F;
+      took(ok ? run_tc<E, GLU_DW, 0>(lm, c, st) : COCODC_ERR_CUDA);
+    } else if (dwg) {
       PlainArgs<E> p{};
       p.a[0] = {dg, 1, pitch};
       p.a[1] = {du, 1, pitch};
@@ -252,10 +351,10 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       p.ld = dw_stride;
       const dim3 grid((unsigned)((F + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile), 2);
       k_product_plain<E, false><<<grid, 256, 0, st>>>(p);
-      ++kernels;
+      took(launched(lm));
     }
   });
-  return launched(lm, kernels);
+  return result;
 }
 
 }  // extern "C"

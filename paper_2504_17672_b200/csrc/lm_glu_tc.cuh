@@ -1,0 +1,239 @@
+// Tensor-core kernel of the gated block: its forward pass and the two products of its gradient.
+//
+// Persistent, one CTA per SM, 128 x 256 output tiles (M x N), k-blocks of 64:
+//   warp 0   producer: TMA copies of the operands' tiles into a ring of shared-memory stages
+//   warp 1   issuer: tcgen05.mma of each stage into one of two TMEM accumulators of 256 columns
+//   warps 2-5 epilogue: TMEM -> registers -> activation -> shared memory -> TMA store, while the other accumulator fills
+// Forward: N = 128 columns of F, the tile's B rows are the gate's 128 weight rows followed by the up projection's, so a
+// thread of the epilogue finds gate and up of one element in its own TMEM lane and the product needs no exchange.
+// dx = dg Wg + du Wu: one accumulator, the k loop runs through both sources.  dw = d^T x: the tile index picks dg or du.
+// The operands of the gradient whose contraction runs along rows are taken MN-major as they lie in memory.
+// Ragged sizes: TMA fills what lies outside a matrix with zeros, and clips rows and whole 16-byte groups of columns
+// when it writes; the last N mod 8 columns of an output leave by ordinary stores (a copy rounds them up to 16 bytes).
+#pragma once
+
+#include "lm_mma.cuh"
+
+namespace cocodc_lm_impl {
+
+enum { GLU_FWD = 0, GLU_DX = 1, GLU_DW = 2 };
+
+struct TcArgs {
+  CUtensorMap a[2], b[2], c[3];
+  int m_tiles, n_tiles;      // of one matrix
+  int matrices;              // GLU_DW: 2
+  int k_blocks;              // of one source
+  int sources;               // GLU_DX: 2
+  int M, N;                  // rows and columns of the outputs
+  int save;                  // GLU_FWD: also write gate and up (c[1], c[2])
+  void* out[3];              // what c[] describes, for columns that a copy cannot write alone
+  long long ld[3];
+  int* status;
+};
+
+constexpr int kTcThreads = 192;
+constexpr int kBM = 128, kBN = 256, kBK = 64;
+constexpr int kStages = 4;
+constexpr unsigned kABytes = kBM * kBK * 2, kBBytes = kBN * kBK * 2, kStageBytes = kABytes + kBBytes;
+constexpr unsigned kSlab = 64 * kBK * 2;            // an MN-major operand's 64 columns of m or n: 64 k rows of 128 bytes
+constexpr unsigned kOutBytes = 32 * 128;            // one warp's staged output: 32 rows of 64 columns
+constexpr unsigned kTcSmem = 1024 + kStages * kStageBytes + 4 * 2 * kOutBytes;
+constexpr int kGroupM = 16;                         // tiles of consecutive rows that go through one column in turn
+
+struct TcShared {
+  unsigned long long full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+  unsigned tmem;
+  int stop;
+};
+
+struct TileAt { int z, m, n; };
+// Tiles in groups of kGroupM row tiles, inside a group column after column: CTAs that run together share operands in L2.
+__device__ __forceinline__ TileAt tile_at(const TcArgs& a, int tile) {
+  TileAt t;
+  const int per = a.m_tiles * a.n_tiles;
+  t.z = tile / per;
+  tile -= t.z * per;
+  const int group = tile / (kGroupM * a.n_tiles), first = group * kGroupM;
+  const int height = min(kGroupM, a.m_tiles - first);
+  tile -= group * kGroupM * a.n_tiles;
+  t.m = first + tile % height;
+  t.n = tile / height;
+  return t;
+}
+
+template <int ACT> __device__ __forceinline__ float act_value(float g);
+
+// 64 staged columns of the warp's 32 rows leave for global memory; rows and columns outside are not written.
+__device__ __forceinline__ void send(const TcArgs& a, int what, int x, int y, unsigned buf, int lane) {
+  if (x + 64 <= a.N || a.N % 8 == 0) {
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) tma_store(&a.c[what], x, y, buf);
+  } else if (y + lane < a.M) {
+    unsigned short* row = static_cast<unsigned short*>(a.out[what]) + (y + lane) * a.ld[what] + x;
+    for (int i = 0; i < a.N - x; ++i) {
+      unsigned short v;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(buf + lane * 128 + (((i / 8) ^ (lane & 7)) << 4) + i % 8 * 2));
+      row[i] = v;
+    }
+  }
+  if (lane == 0) store_commit();
+}
+// 32 columns (packed in pairs) of the thread's row into columns half*32.. of the staged tile, swizzled as the copy expects
+__device__ __forceinline__ void stage32(unsigned buf, int row, int half, const unsigned (&v)[16]) {
+  for (int q = 0; q < 4; ++q)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + row * 128 + (((half * 4 + q) ^ (row & 7)) << 4)),
+                 "r"(v[4 * q]), "r"(v[4 * q + 1]), "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
+}
+
+template <typename E, int MODE, int ACT>
+__global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant__ TcArgs a) {
+  extern __shared__ unsigned char dyn[];
+  __shared__ TcShared sh;
+  const unsigned base = (smem_addr(dyn) + 1023u) & ~1023u;
+  const unsigned staging = base + kStages * kStageBytes;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  constexpr bool a_mn = MODE == GLU_DW, b_mn = MODE != GLU_FWD;
+  const int tiles = a.m_tiles * a.n_tiles * a.matrices;
+  const int blocks = a.k_blocks * a.sources;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      bar_init(smem_addr(&sh.full[s]), 1);
+      bar_init(smem_addr(&sh.empty[s]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(smem_addr(&sh.acc_full[i]), 1);
+      bar_init(smem_addr(&sh.acc_empty[i]), 4);
+    }
+    bar_init(smem_addr(&sh.drain), 1);
+    sh.stop = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(smem_addr(&sh.tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const unsigned tmem = sh.tmem;
+  volatile int* stop = &sh.stop;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      long long it = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+        const TileAt t = tile_at(a, tile);
+        const int m0 = t.m * kBM, n0 = t.n * (MODE == GLU_FWD ? kBN / 2 : kBN);
+        for (int kb = 0; kb < blocks; ++kb, ++it) {
+          const int s = (int)(it % kStages);
+          ok = bar_wait(smem_addr(&sh.empty[s]), (unsigned)((it / kStages) & 1) ^ 1, stop);
+          if (!ok) break;
+          const unsigned full = smem_addr(&sh.full[s]), sa = base + s * kStageBytes, sb = sa + kABytes;
+          const int src = kb >= a.k_blocks, k0 = (kb - src * a.k_blocks) * kBK;
+          bar_expect(full, kStageBytes);
+          if (MODE == GLU_FWD) {
+            tma_load(sa, &a.a[0], k0, m0, full);
+            tma_load(sb, &a.b[0], k0, n0, full);
+            tma_load(sb + kBBytes / 2, &a.b[1], k0, n0, full);
+          } else {
+            if (MODE == GLU_DX) {
+              tma_load(sa, &a.a[src], k0, m0, full);
+            } else {
+              for (int i = 0; i < kBM / 64; ++i) tma_load(sa + i * kSlab, &a.a[t.z], m0 + i * 64, k0, full);
+            }
+            for (int i = 0; i < kBN / 64; ++i)
+              tma_load(sb + i * kSlab, &a.b[MODE == GLU_DX ? src : 0], n0 + i * 64, k0, full);
+          }
+        }
+      }
+      // given up: the copies in flight land before the CTA leaves its shared memory
+      if (!ok)
+        for (long long i = it > kStages ? it - kStages : 0; i < it; ++i)
+          bar_drain(smem_addr(&sh.full[i % kStages]), (unsigned)((i / kStages) & 1));
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr unsigned idesc = instr_desc<E>(kBM, kBN, a_mn, b_mn);
+      long long it = 0;
+      int turn = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++turn) {
+        const int acc = turn & 1;
+        ok = bar_wait(smem_addr(&sh.acc_empty[acc]), (unsigned)((turn >> 1) & 1) ^ 1, stop);
+        tc_fence_after();
+        for (int kb = 0; ok && kb < blocks; ++kb, ++it) {
+          const int s = (int)(it % kStages);
+          ok = bar_wait(smem_addr(&sh.full[s]), (unsigned)((it / kStages) & 1), stop);
+          if (!ok) break;
+          tc_fence_after();
+          const unsigned sa = base + s * kStageBytes, sb = sa + kABytes;
+          const unsigned long long da = tile_desc(sa, a_mn ? kSlab : 16), db = tile_desc(sb, b_mn ? kSlab : 16);
+          for (int k = 0; k < kBK / 16; ++k)   // 16 k: 32 bytes along a K-major row, 16 rows of an MN-major tile
+            tc_mma(tmem + acc * kBN, da + (unsigned)(k * (a_mn ? 2048 : 32) >> 4), db + (unsigned)(k * (b_mn ? 2048 : 32) >> 4),
+                   idesc, kb > 0 || k > 0);
+          tc_commit(smem_addr(&sh.empty[s]));
+        }
+        if (ok) tc_commit(smem_addr(&sh.acc_full[acc]));
+      }
+      if (!ok) {
+        tc_commit(smem_addr(&sh.drain));
+        bar_drain(smem_addr(&sh.drain), 0);
+      }
+    }
+  } else {
+    const int quarter = warp & 3, e = warp - 2;
+    const unsigned out = staging + e * 2 * kOutBytes;
+    int turn = 0, sent = 0;
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
+      const int acc = turn & 1;
+      const TileAt t = tile_at(a, tile);
+      const int row0 = t.m * kBM + quarter * 32, n0 = t.n * (MODE == GLU_FWD ? kBN / 2 : kBN);
+      if (!__all_sync(~0u, bar_wait(smem_addr(&sh.acc_full[acc]), (unsigned)((turn >> 1) & 1), stop))) break;
+      tc_fence_after();
+      const unsigned src = tmem + acc * kBN + ((unsigned)(quarter * 32) << 16);
+      // one staged tile of 64 columns after the other, two buffers in turn
+      const int pieces = MODE == GLU_FWD ? (a.save ? 6 : 2) : 4;
+      for (int p = 0; p < pieces; ++p) {
+        const int chunk = MODE == GLU_FWD ? (a.save ? p / 3 : p) : p, what = MODE == GLU_FWD && a.save ? p % 3 : 0;
+        const unsigned buf = out + (sent & 1) * kOutBytes;
+        const int x = n0 + chunk * 64;
+        if (x >= a.N || row0 >= a.M) continue;
+        if (lane == 0) store_wait_read<1>();
+        __syncwarp();
+        for (int half = 0; half < 2; ++half) {
+          float v[32];
+          unsigned packed[16];
+          const int col = chunk * 64 + half * 32;
+          if (MODE == GLU_FWD && what == 0) {
+            float u[32];
+            tmem_load32(v, src + col);
+            tmem_load32(u, src + kBN / 2 + col);
+            tmem_wait_loads();
+            for (int i = 0; i < 16; ++i)
+              packed[i] = pack2<E>(act_value<ACT>(v[2 * i]) * u[2 * i], act_value<ACT>(v[2 * i + 1]) * u[2 * i + 1]);
+          } else {
+            tmem_load32(v, src + col + (what == 2 ? kBN / 2 : 0));
+            tmem_wait_loads();
+            for (int i = 0; i < 16; ++i) packed[i] = pack2<E>(v[2 * i], v[2 * i + 1]);
+          }
+          stage32(buf, lane, half, packed);
+        }
+        send(a, MODE == GLU_DW ? t.z : what, x, row0, buf, lane);
+        ++sent;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&sh.acc_empty[acc]));
+    }
+    if (lane == 0) store_wait_all();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && sh.stop) record(a.status, COCODC_ERR_TIMEOUT);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+}  // namespace cocodc_lm_impl
