@@ -6,16 +6,61 @@ using namespace cocodc_lm_impl;
 
 namespace {
 
+// W elements of one type, loaded or stored as 16-byte accesses (or one of W * sizeof(T) bytes); W = 1: the element alone
+template <typename T, int W> struct Pack {
+  float v[W];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (W == 1) {
+      v[0] = to_f32(*p);
+    } else {
+      constexpr int bytes = W * (int)sizeof(T);
+      alignas(16) T e[W];
+      if constexpr (bytes == 8) *reinterpret_cast<uint2*>(e) = *reinterpret_cast<const uint2*>(p);
+      else for (int i = 0; i < bytes / 16; ++i) reinterpret_cast<uint4*>(e)[i] = reinterpret_cast<const uint4*>(p)[i];
+      for (int i = 0; i < W; ++i) v[i] = to_f32(e[i]);
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (W == 1) {
+      *p = from_f32<T>(v[0]);
+    } else {
+      constexpr int bytes = W * (int)sizeof(T);
+      alignas(16) T e[W];
+      for (int i = 0; i < W; ++i) e[i] = from_f32<T>(v[i]);
+      if constexpr (bytes == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(e);
+      else for (int i = 0; i < bytes / 16; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(e)[i];
+    }
+  }
+};
+
 // ---- lookup ------------------------------------------------------------------------------------
-template <typename TIn, typename TOut>
-__global__ void __launch_bounds__(256) k_embed(const TIn* table, long long table_stride, long long V, long long D,
-                                               const void* ids, int is64, long long T, float scale, TOut* y,
-                                               long long y_stride, int* status) {
-  const long long n = T * D;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-    const long long t = i / D, d = i - t * D;
-    const long long v = token_at(ids, is64, t, V, status);
-    y[t * y_stride + d] = from_f32<TOut>(v < 0 ? 0.f : scale * to_f32(table[v * table_stride + d]));
+// A gather: bound by memory.  A thread moves U packs of W elements, 256 apart, so that U loads are in flight; T * D / W packs
+// are numbered row by row.
+template <typename TIn, typename TOut, int W, int U>
+__global__ void __launch_bounds__(256) k_embed(const TIn* __restrict__ table, long long table_stride, long long V,
+                                               unsigned packs, const void* ids, int is64, long long T, float scale,
+                                               TOut* __restrict__ y, long long y_stride, int* status) {
+  const long long blocks = (T * packs + 256 * U - 1) / (256 * U);
+  for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const long long first = b * (256 * U), row0 = first / packs;
+    const unsigned rest = (unsigned)(first - row0 * packs) + threadIdx.x;
+    Pack<TIn, W> x[U];
+    long long v[U], t[U];
+    unsigned col[U];
+    for (int i = 0; i < U; ++i) {
+      const unsigned at = rest + i * 256, q = at / packs;
+      t[i] = row0 + q;
+      col[i] = (at - q * packs) * W;
+      v[i] = t[i] < T ? token_at(ids, is64, t[i], V, status) : -1;
+    }
+    for (int i = 0; i < U; ++i)
+      if (v[i] >= 0) x[i].load(table + v[i] * table_stride + col[i]);
+    for (int i = 0; i < U; ++i) {
+      if (t[i] >= T) continue;
+      Pack<TOut, W> out;
+      for (int k = 0; k < W; ++k) out.v[k] = v[i] < 0 ? 0.f : scale * x[i].v[k];
+      out.store(y + t[i] * y_stride + col[i]);
+    }
   }
 }
 
@@ -44,8 +89,14 @@ struct GradArgs {
   void* dtable;
   long long dtable_stride;
   int dtable_esize;
+  int dtable_wide;    // rows start on 16-byte boundaries
   int* row_start;     // [V + 1] first sorted position of every row
   int2* sorted;       // [T] (token position, row) in sorted order
+  float* partial;     // [tiles][2][padded D]: sums of the rows that a tile shares with its neighbours
+  int* arrived;       // [tiles][column blocks]: tiles that have left their part of the row that begins in the tile
+  long long n_arrived;
+  int positions;      // sorted positions of one group of a tile
+  long long pitch;    // padded D
   int* status;
 };
 
@@ -70,18 +121,29 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
   const long long t0 = warp * part, t1 = min((long long)a.T, t0 + part);
 
   for (int i = tid; i < rows * kBinPitch; i += kSortThreads) cnt[i] = 0;
+  for (long long i = (long long)blockIdx.x * kSortThreads + tid; i < a.n_arrived; i += (long long)gridDim.x * kSortThreads)
+    a.arrived[i] = 0;
   __syncthreads();
+  // calls f(position, row of this bin or -1) for the ids of the warp's part in order, four loads ahead
   int below = 0;
-  for (long long t = t0; t < t1; t += 32) {
-    const long long v = t + lane < t1 ? token_at(a.ids, a.is64, t + lane, a.V, a.status) : -1;
-    below += v >= 0 && v < lo;
-    const bool mine = v >= lo && v < lo + rows;
-    if (!__ballot_sync(~0u, mine)) continue;
-    const int r = mine ? (int)(v - lo) : -1;
-    const unsigned same = __match_any_sync(~0u, r);
-    if (mine && lane == __ffs(same) - 1) cnt[r * kBinPitch + warp] += __popc(same);
-    __syncwarp();
-  }
+  const auto walk = [&](auto&& f) {
+    for (long long t = t0; t < t1; t += 128) {
+      int r[4];
+      for (int i = 0; i < 4; ++i) {
+        const long long at = t + i * 32 + lane, v = at < t1 ? token_at(a.ids, a.is64, at, a.V, a.status) : -1;
+        below += v >= 0 && v < lo;
+        r[i] = v >= lo && v < lo + rows ? (int)(v - lo) : -1;
+      }
+      for (int i = 0; i < 4; ++i)
+        if (__ballot_sync(~0u, r[i] >= 0)) {
+          f(t + i * 32 + lane, r[i], __match_any_sync(~0u, r[i]));
+          __syncwarp();
+        }
+    }
+  };
+  walk([&](long long, int r, unsigned same) {
+    if (r >= 0 && lane == __ffs(same) - 1) cnt[r * kBinPitch + warp] += __popc(same);
+  });
   const int first = block_sum(below, scratch);
   __syncthreads();
 
@@ -111,51 +173,195 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
   }
   __syncthreads();
 
-  // rows that no token names: zeros
+  // rows that no token names: zeros, on their way while the second walk runs
   if (!a.accumulate) {
+    const bool wide = a.dtable_wide;
+    const long long bytes = a.D * a.dtable_esize, n16 = wide ? bytes / 16 : 0;
     for (int r = warp; r < rows; r += kSortWarps) {
       if (cnt[r * kBinPitch + kSortWarps]) continue;
       char* p = static_cast<char*>(a.dtable) + (lo + r) * a.dtable_stride * a.dtable_esize;
-      if (a.dtable_esize == 4) for (long long i = lane; i < a.D; i += 32) reinterpret_cast<float*>(p)[i] = 0.f;
-      else for (long long i = lane; i < a.D; i += 32) reinterpret_cast<unsigned short*>(p)[i] = 0;
+      for (long long i = lane; i < n16; i += 32) reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
+      for (long long i = n16 * 16 + lane * a.dtable_esize; i < bytes; i += 32 * a.dtable_esize) {
+        if (a.dtable_esize == 4) *reinterpret_cast<float*>(p + i) = 0.f;
+        else *reinterpret_cast<unsigned short*>(p + i) = 0;
+      }
     }
   }
 
-  for (long long t = t0; t < t1; t += 32) {
-    const long long v = t + lane < t1 ? token_at(a.ids, a.is64, t + lane, a.V, a.status) : -1;
-    const bool mine = v >= lo && v < lo + rows;
-    if (!__ballot_sync(~0u, mine)) continue;
-    const int r = mine ? (int)(v - lo) : -1;
-    const unsigned same = __match_any_sync(~0u, r);
+  walk([&](long long t, int r, unsigned same) {
     const int leader = __ffs(same) - 1;
     int base = 0;
-    if (mine && lane == leader) {
+    if (r >= 0 && lane == leader) {
       base = cnt[r * kBinPitch + warp];
       cnt[r * kBinPitch + warp] = base + __popc(same);
     }
     base = __shfl_sync(~0u, base, leader);
-    if (mine) a.sorted[base + __popc(same & ((1u << lane) - 1))] = make_int2((int)(t + lane), (int)v);
-    __syncwarp();
-  }
+    if (r >= 0) a.sorted[base + __popc(same & ((1u << lane) - 1))] = make_int2((int)t, (int)(lo + r));
+  });
 }
 
 // ---- gradient, step 2: the sums -----------------------------------------------------------------
-template <typename TIn, typename TOut>
-__global__ void __launch_bounds__(256) k_embed_sum(const GradArgs a) {
-  const int lane = threadIdx.x & 31;
-  const long long v = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (v >= a.V) return;
-  const int p0 = a.row_start[v], p1 = a.row_start[v + 1];
-  if (p0 == p1) return;
-  for (long long d = lane; d < a.D; d += 32) {
-    float s = 0.f;
-    for (int p = p0; p < p1; ++p) s += to_f32(static_cast<const TIn*>(a.dy)[a.sorted[p].x * a.dy_stride + d]);
-    TOut* out = static_cast<TOut*>(a.dtable) + v * a.dtable_stride + d;
-    *out = from_f32<TOut>(a.accumulate ? to_f32(*out) + a.scale * s : a.scale * s);
+// A CTA takes a tile of kGroups * positions consecutive entries of the sorted order, so the work is even however the
+// tokens are distributed: each of its groups of threads sums its own run of entries, one column pack per thread, and
+// starts a new sum where the row changes.  A row that lies inside one group is written at once.  Rows that cross group
+// boundaries are joined in shared memory in order; those that cross tile boundaries leave their parts in the
+// workspace, and the tile that arrives last at the row's counter adds all parts in tile order (nobody waits).
+constexpr int kGroups = 4;
+
+template <typename TIn, typename TOut, int W>
+__global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
+  extern __shared__ float part[];                       // [kGroups][2][threads of a group][W]: head, tail
+  __shared__ int pending_row[2], is_last[2];
+  const int width = blockDim.x / kGroups, group = threadIdx.x / width, c = threadIdx.x % width;
+  const long long col = ((long long)blockIdx.y * width + c) * W;
+  const bool active = col < a.D;
+  const int n = a.row_start[a.V];
+  const int tile = blockIdx.x, span = kGroups * a.positions, begin = tile * span;
+  if (begin >= n) return;
+  const TIn* dy = static_cast<const TIn*>(a.dy) + (active ? col : 0);
+  TOut* out = static_cast<TOut*>(a.dtable) + (active ? col : 0);
+
+  float acc[W];
+  const auto clear = [&] { for (int k = 0; k < W; ++k) acc[k] = 0.f; };
+  const auto write_row = [&](int row) {
+    if (!active) return;
+    Pack<TOut, W> o;
+    TOut* p = out + (long long)row * a.dtable_stride;
+    if (a.accumulate) {
+      o.load(p);
+      for (int k = 0; k < W; ++k) o.v[k] += a.scale * acc[k];
+    } else {
+      for (int k = 0; k < W; ++k) o.v[k] = a.scale * acc[k];
+    }
+    o.store(p);
+  };
+  const auto row_at = [&](int p) { return a.sorted[p].y; };
+  // entries p - 1 and p belong to one row
+  const auto joined = [&](int p) { return p > 0 && p < n && row_at(p - 1) == row_at(p); };
+  float* head = part + ((group * 2) * width + c) * W;
+  float* tail = part + ((group * 2 + 1) * width + c) * W;
+
+  const int p0 = min(n, begin + group * a.positions), p1 = min(n, p0 + a.positions);
+  if (p0 < p1) {
+    bool open = joined(p0);                              // the current sum continues a row of the group before
+    const bool goes_on = joined(p1);
+    int row = row_at(p0);
+    clear();
+    for (int p = p0; p < p1; p += 8) {
+      Pack<TIn, W> x[8];
+      int2 e[8];
+      for (int i = 0; i < 8; ++i) {
+        e[i] = p + i < p1 ? a.sorted[p + i] : make_int2(-1, row);
+        if (e[i].x >= 0) x[i].load(dy + (long long)e[i].x * a.dy_stride);
+      }
+      for (int i = 0; i < 8; ++i) {
+        if (e[i].x < 0) continue;
+        if (e[i].y != row) {
+          if (open) for (int k = 0; k < W; ++k) head[k] = acc[k];
+          else write_row(row);
+          open = false;
+          row = e[i].y;
+          clear();
+        }
+        for (int k = 0; k < W; ++k) acc[k] += x[i].v[k];
+      }
+    }
+    float* to = open ? head : goes_on ? tail : nullptr;
+    if (to) for (int k = 0; k < W; ++k) to[k] = acc[k];
+    else write_row(row);
+  }
+  if (threadIdx.x < 2) pending_row[threadIdx.x] = -1;
+  __syncthreads();
+
+  // rows that cross groups: joined in order by the first group's threads
+  if (group == 0) {
+    bool running = false, outside = false;               // a sum is open; it began in an earlier tile
+    int row = -1;
+    const auto leave = [&](int slot) {                   // slot 0: begun in an earlier tile, 1: begun here
+      if (active) {
+        float* w = a.partial + ((long long)tile * 2 + slot) * a.pitch + col;
+        for (int k = 0; k < W; ++k) w[k] = acc[k];
+      }
+      if (c == 0) pending_row[slot] = row;
+      __threadfence();
+    };
+    for (int g = 0; g < kGroups; ++g) {
+      const int q0 = begin + g * a.positions, q1 = min(n, q0 + a.positions);
+      if (q0 >= n) break;
+      const bool left = joined(q0), right = joined(q1);
+      const bool through = left && right && row_at(q0) == row_at(q1 - 1);
+      if (left) {
+        if (!running) { clear(); running = true; outside = true; row = row_at(q0); }
+        const float* h = part + ((g * 2) * width + c) * W;
+        for (int k = 0; k < W; ++k) acc[k] += h[k];
+        if (!through) {
+          if (outside) leave(0);
+          else write_row(row);
+          running = false;
+        }
+      }
+      if (right && !running) {
+        const float* h = part + ((g * 2 + 1) * width + c) * W;
+        for (int k = 0; k < W; ++k) acc[k] = h[k];
+        running = true;
+        outside = false;
+        row = row_at(q1 - 1);
+      }
+    }
+    if (running) leave(outside ? 0 : 1);
+  }
+  __syncthreads();
+
+  // rows that cross tiles: the last of their tiles to arrive adds the parts
+  if (threadIdx.x < 2) {
+    const int row = pending_row[threadIdx.x];
+    int last = 0;
+    if (row >= 0) {
+      const int first = a.row_start[row] / span, end = (a.row_start[row + 1] - 1) / span;
+      __threadfence();
+      last = atomicAdd(&a.arrived[(long long)first * gridDim.y + blockIdx.y], 1) == end - first;
+      __threadfence();
+    }
+    is_last[threadIdx.x] = last;
+  }
+  __syncthreads();
+  for (int s = 0; s < 2; ++s) {
+    if (!is_last[s]) continue;
+    const int row = pending_row[s], first = a.row_start[row] / span, parts = (a.row_start[row + 1] - 1) / span - first + 1;
+    clear();
+    const int j1 = (int)((long long)parts * (group + 1) / kGroups);
+    if (active)
+      for (int j = (int)((long long)parts * group / kGroups); j < j1; j += 4) {
+        float x[4][W];
+        for (int i = 0; i < 4; ++i)
+          if (j + i < j1) {
+            const float* w = a.partial + ((long long)(first + j + i) * 2 + (j + i == 0 ? 1 : 0)) * a.pitch + col;
+            for (int k = 0; k < W; ++k) x[i][k] = __ldcg(w + k);
+          }
+        for (int i = 0; i < 4; ++i)
+          if (j + i < j1) for (int k = 0; k < W; ++k) acc[k] += x[i][k];
+      }
+    for (int k = 0; k < W; ++k) head[k] = acc[k];
+    __syncthreads();
+    if (group == 0) {
+      for (int g = 1; g < kGroups; ++g)
+        for (int k = 0; k < W; ++k) acc[k] += part[((g * 2) * width + c) * W + k];
+      write_row(row);
+    }
+    __syncthreads();
   }
 }
 
+// Sorted entries per group: 32 amortise the boundaries; with few tokens fewer, so that there are tiles for all SMs.
+int positions_for(int64_t T) {
+  int p = 32;
+  while (p > 4 && T < (int64_t)148 * 2 * kGroups * p) p /= 2;
+  return p;
+}
+
 uint64_t up16(uint64_t n) { return (n + 15) / 16 * 16; }
+int64_t padded(int64_t D) { return (D + 7) / 8 * 8; }
+int64_t tiles_for(int64_t T) { return (T + kGroups * positions_for(T) - 1) / (kGroups * positions_for(T)); }
 
 }  // namespace
 
@@ -171,7 +377,7 @@ extern "C" {
 cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_type, int64_t table_stride, int64_t V,
                               int64_t D, const void* ids, int32_t ids_type, int64_t T, float scale, void* y,
                               int32_t y_type, int64_t y_stride, void* stream) {
-  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || !known_type(table_type) || !known_type(y_type) ||
+  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || !known_type(table_type) || !known_type(y_type) ||
       (ids_type != COCODC_I32 && ids_type != COCODC_I64) || table_stride < D || y_stride < D || !sane(table_stride) ||
       !sane(y_stride))
     return COCODC_ERR_INVALID_ARG;
@@ -185,14 +391,21 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const long long blocks = (T * D + 255) / 256;
+  const bool wide = rows_aligned(table, table_stride, es) && rows_aligned(y, y_stride, ys) && D % 8 == 0;
   with_type(table_type, [&](auto in) {
     return with_type(y_type, [&](auto out) {
       using TIn = decltype(in);
       using TOut = decltype(out);
-      k_embed<TIn, TOut><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, st>>>(
-          static_cast<const TIn*>(table), table_stride, V, D, ids, ids_type == COCODC_I64, T, scale,
-          static_cast<TOut*>(y), y_stride, lm->d_status);
+      const auto run = [&](auto kernel, int W, int U) {
+        const long long blocks = (T * (D / W) + 256 * U - 1) / (256 * U);
+        kernel<<<(unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st>>>(
+            static_cast<const TIn*>(table), table_stride, V, (unsigned)(D / W), ids, ids_type == COCODC_I64, T, scale,
+            static_cast<TOut*>(y), y_stride, lm->d_status);
+      };
+      // few packs: one per thread, so that they spread over the SMs
+      if (!wide) run(k_embed<TIn, TOut, 1, 4>, 1, 4);
+      else if (T * (D / 8) < (long long)lm->sm_count * 2048) run(k_embed<TIn, TOut, 8, 1>, 8, 1);
+      else run(k_embed<TIn, TOut, 8, 4>, 8, 4);
       return true;
     });
   });
@@ -201,14 +414,16 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
 
 uint64_t cocodc_lm_embed_grad_workspace(int64_t V, int64_t D, int64_t T) {
   if (!sane(V) || !sane(D) || !sane(T)) return 0;
-  return up16((uint64_t)(V + 1) * sizeof(int)) + up16((uint64_t)T * sizeof(int2));
+  const uint64_t tiles = (uint64_t)tiles_for(T);
+  return up16((uint64_t)(V + 1) * sizeof(int)) + up16((uint64_t)T * sizeof(int2)) + tiles * 2 * padded(D) * sizeof(float) +
+         up16(tiles * (uint64_t)((D + 31) / 32) * sizeof(int));
 }
 
 cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_type, int64_t dy_stride, const void* ids,
                                    int32_t ids_type, int64_t T, int64_t V, int64_t D, float scale, int32_t accumulate,
                                    void* dtable, int32_t dtable_type, int64_t dtable_stride, void* workspace,
                                    uint64_t workspace_bytes, void* stream) {
-  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || T > INT32_MAX || V >= INT32_MAX || !dtable ||
+  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || T > INT32_MAX || V >= INT32_MAX || !dtable ||
       !known_type(dy_type) || !known_type(dtable_type) || (ids_type != COCODC_I32 && ids_type != COCODC_I64) ||
       dy_stride < D || dtable_stride < D || !sane(dy_stride) || !sane(dtable_stride))
     return COCODC_ERR_INVALID_ARG;
@@ -238,9 +453,24 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
   a.dtable = dtable;
   a.dtable_stride = dtable_stride;
   a.dtable_esize = gs;
-  a.row_start = static_cast<int*>(workspace);
-  a.sorted = reinterpret_cast<int2*>(static_cast<char*>(workspace) + up16((uint64_t)(V + 1) * sizeof(int)));
+  const int64_t tiles = tiles_for(T);
+  char* at = static_cast<char*>(workspace);
+  const auto take = [&](uint64_t bytes) { char* p = at; at += up16(bytes); return p; };
+  a.row_start = reinterpret_cast<int*>(take((uint64_t)(V + 1) * sizeof(int)));
+  a.sorted = reinterpret_cast<int2*>(take((uint64_t)T * sizeof(int2)));
+  a.partial = reinterpret_cast<float*>(take((uint64_t)tiles * 2 * padded(D) * sizeof(float)));
+  a.arrived = reinterpret_cast<int*>(at);
   a.status = lm->d_status;
+  a.positions = positions_for(T);
+  a.pitch = padded(D);
+  a.dtable_wide = rows_aligned(dtable, dtable_stride, gs);
+  // 16 bytes of dy per thread where rows of both matrices start on 16-byte boundaries and hold whole packs
+  const int W = rows_aligned(dy, dy_stride, es) && a.dtable_wide && D % (16 / es) == 0 ? 16 / es : 1;
+  const long long packs = D / W;
+  const int width = packs >= 128 ? 128 : (int)((packs + 31) / 32 * 32);
+  const long long columns = (packs + width - 1) / width;
+  if (columns > 65535) return COCODC_ERR_INVALID_ARG;
+  a.n_arrived = tiles * columns;
   const long long per_sm = (V + lm->sm_count - 1) / lm->sm_count;
   a.bin_rows = (int)(per_sm < kMaxBinRows ? per_sm : kMaxBinRows);
   const unsigned bins = (unsigned)((V + a.bin_rows - 1) / a.bin_rows);
@@ -248,7 +478,12 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
   if (T > 0)
     with_type(dy_type, [&](auto in) {
       return with_type(dtable_type, [&](auto out) {
-        k_embed_sum<decltype(in), decltype(out)><<<(unsigned)((V + 7) / 8), 256, 0, st>>>(a);
+        using TIn = decltype(in);
+        using TOut = decltype(out);
+        const dim3 grid((unsigned)tiles, (unsigned)columns);
+        const unsigned smem = kGroups * 2 * width * W * sizeof(float);
+        if (W > 1) k_embed_sum<TIn, TOut, 16 / (int)sizeof(TIn)><<<grid, kGroups * width, smem, st>>>(a);
+        else k_embed_sum<TIn, TOut, 1><<<grid, kGroups * width, smem, st>>>(a);
         return true;
       });
     });

@@ -43,68 +43,362 @@ struct RowArgs {
   int* status;
 };
 
-__device__ __forceinline__ float block_reduce(float v, float* scratch, bool is_max) {
-  for (int o = 16; o; o >>= 1) {
-    const float w = __shfl_xor_sync(~0u, v, o);
-    v = is_max ? fmaxf(v, w) : v + w;
+// ---- sixteen bytes of a row ---------------------------------------------------------------------
+// Logits below -kFar take part in the sums as -kFar (-Inf would turn 0 * d into NaN in the entropy's sum).  That is exact
+// where their exponentials are 0 either way: where the largest logit is above -kFar / 2 and c kFar / 2 is above 200;
+// anything else goes the careful way.  kFar is a power of two, so that c * kFar is c's bits and -kFar's distance to itself is 0.
+template <typename T> struct Words;
+template <> struct Words<float> {
+  static constexpr int n = 4;
+  static constexpr float kFar = 0x1p100f;
+  float e[4];
+  __device__ __forceinline__ void set(uint4 w) {
+    const float f[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+    for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(e[i]) : "f"(f[i]), "f"(-kFar));
   }
+  static __device__ __forceinline__ uint4 far() { const unsigned v = __float_as_uint(-kFar); return make_uint4(v, v, v, v); }
+  __device__ __forceinline__ float at(int i) const { return e[i]; }
+  __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])); }
+};
+template <> struct Words<__nv_bfloat16> {
+  static constexpr int n = 8;
+  static constexpr float kFar = 0x1p100f;
+  __nv_bfloat162 e[4];
+  static __device__ __forceinline__ __nv_bfloat162 low() { return __float2bfloat162_rn(-kFar); }
+  __device__ __forceinline__ void set(uint4 w) {
+    const unsigned u[4] = {w.x, w.y, w.z, w.w};
+    for (int i = 0; i < 4; ++i) e[i] = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&u[i]), low());
+  }
+  static __device__ __forceinline__ uint4 far() {
+    const __nv_bfloat162 l = low();
+    const unsigned v = *reinterpret_cast<const unsigned*>(&l);
+    return make_uint4(v, v, v, v);
+  }
+  __device__ __forceinline__ float at(int i) const { return i & 1 ? __high2float(e[i / 2]) : __low2float(e[i / 2]); }
+  __device__ __forceinline__ float largest() const {
+    const __nv_bfloat162 m = __hmax2(__hmax2(e[0], e[1]), __hmax2(e[2], e[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+};
+template <> struct Words<__half> {
+  static constexpr int n = 8;
+  static constexpr float kFar = 0x1p15f;
+  __half2 e[4];
+  static __device__ __forceinline__ __half2 low() { return __float2half2_rn(-kFar); }
+  __device__ __forceinline__ void set(uint4 w) {
+    const unsigned u[4] = {w.x, w.y, w.z, w.w};
+    for (int i = 0; i < 4; ++i) e[i] = __hmax2_nan(*reinterpret_cast<const __half2*>(&u[i]), low());
+  }
+  static __device__ __forceinline__ uint4 far() {
+    const __half2 l = low();
+    const unsigned v = *reinterpret_cast<const unsigned*>(&l);
+    return make_uint4(v, v, v, v);
+  }
+  __device__ __forceinline__ float at(int i) const { return i & 1 ? __high2float(e[i / 2]) : __low2float(e[i / 2]); }
+  __device__ __forceinline__ float largest() const {
+    const __half2 m = __hmax2(__hmax2(e[0], e[1]), __hmax2(e[2], e[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+};
+
+// What a part of a row comes to, in base 2: m the largest logit, s = sum 2^(c (x - m)), u = sum c (x - m) 2^(c (x - m)).
+struct Stats {
+  float m, s, u;
+};
+__device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  // the offsets are bounded so that 0 * offset stays 0; a part without sum keeps its zeros
+  const float da = fmaxf((a.m == m ? 0.f : (a.m - m) * c), -1e4f), db = fmaxf((b.m == m ? 0.f : (b.m - m) * c), -1e4f);
+  const float fa = exp2f(da), fb = exp2f(db);
+  return Stats{m, a.s * fa + b.s * fb, (a.u + da * a.s) * fa + (b.u + db * b.s) * fb};
+}
+__device__ __forceinline__ Stats block_join(Stats x, float c, Stats* scratch) {
+  for (int o = 16; o; o >>= 1)
+    x = join(x, Stats{__shfl_xor_sync(~0u, x.m, o), __shfl_xor_sync(~0u, x.s, o), __shfl_xor_sync(~0u, x.u, o)}, c);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
   __syncthreads();
-  v = scratch[0];
-  for (int w = 1; w < kWarps; ++w) v = is_max ? fmaxf(v, scratch[w]) : v + scratch[w];
-  return v;
+  x = scratch[0];
+  for (int w = 1; w < kWarps; ++w) x = join(x, scratch[w], c);
+  return x;
 }
 
+// The careful way: any values, any number of them, element by element.  [j0, j1) of the row.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a) {
-  __shared__ float scratch[kWarps];
-  __shared__ unsigned long long best[kWarps];
-  const long long t = blockIdx.x;
-  const T* row = static_cast<const T*>(a.logits) + t * a.stride;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  float m = -INFINITY;
-  for (unsigned j = tid; j < a.V; j += kThreads) m = fmaxf(m, to_f32(row[j]));
-  m = block_reduce(m, scratch, true);
-  float s = 0.f, u = 0.f;
-  const float c = a.scale * kLog2e;
-  for (unsigned j = tid; j < a.V; j += kThreads) {
-    const float x = to_f32(row[j]);
-    if (x == -INFINITY) continue;
-    const float d = (x - m) * c, e = exp2f(d);
-    s += e;
-    if (e != 0.f) u += e * d;      // a far lower logit: d may be -Inf, e * d is 0
+__device__ __noinline__ Stats careful_stats(const T* row, unsigned j0, unsigned j1, float c, Stats* scratch) {
+  Stats x{-INFINITY, 0.f, 0.f};
+  bool nan = false;
+  for (unsigned j = j0 + threadIdx.x; j < j1; j += kThreads) {
+    const float v = to_f32(row[j]);
+    nan |= v != v;
+    x.m = fmaxf(x.m, v);
   }
-  s = block_reduce(s, scratch, false);
-  u = block_reduce(u, scratch, false);
-  const bool empty = m == -INFINITY && s == 0.f;
-  const float lse = empty ? -INFINITY : m * a.scale + logf(s);
-  if (tid == 0) {
-    if (a.lse) a.lse[t] = lse;
-    if (a.entropy) a.entropy[t] = empty ? 0.f : kLn2 * (log2f(s) - u / s);
+  for (int o = 16; o; o >>= 1) x.m = fmaxf(x.m, __shfl_xor_sync(~0u, x.m, o));
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5].m = x.m;
+  __syncthreads();
+  for (int w = 0; w < kWarps; ++w) x.m = fmaxf(x.m, scratch[w].m);
+  for (unsigned j = j0 + threadIdx.x; j < j1; j += kThreads) {
+    const float v = to_f32(row[j]);
+    if (v == -INFINITY) continue;
+    const float d = (v - x.m) * c, e = exp2f(d);
+    x.s += e;
+    if (e != 0.f) x.u += e * d;
+  }
+  return block_join(x, c, scratch);
+}
+// The k largest keys of [j0, j1), in descending order in list[0 .. k): k walks.
+template <typename T>
+__device__ __noinline__ void careful_top(const T* row, unsigned j0, unsigned j1, int k, unsigned long long* list,
+                                         unsigned long long* scratch) {
+  unsigned long long last = ~0ull;
+  for (int i = 0; i < k; ++i) {
+    unsigned long long best = 0;
+    for (unsigned j = j0 + threadIdx.x; j < j1; j += kThreads) {
+      const unsigned long long q = key_of(to_f32(row[j]), j);
+      if (q < last && q > best) best = q;
+    }
+    best = warp_max(best);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = best;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) best = scratch[w] > best ? scratch[w] : best;
+    last = best;
+    if (threadIdx.x == 0) list[i] = best;
+  }
+  __syncthreads();
+}
+
+// One warp: the k largest of keys[0 .. n), descending, to list[0 .. k) (0 where there are no more).
+__device__ __forceinline__ void warp_top(const unsigned long long* keys, int n, int k, unsigned long long* list) {
+  const int lane = threadIdx.x & 31;
+  unsigned long long last = ~0ull;
+  for (int i = 0; i < k; ++i) {
+    unsigned long long best = 0;
+    for (int j = lane; j < n; j += 32)
+      if (keys[j] < last && keys[j] > best) best = keys[j];
+    last = best = warp_max(best);
+    if (lane == 0) list[i] = best;
+  }
+  __syncwarp();
+}
+
+constexpr int kUnroll = 4;           // 16-byte loads in flight per thread
+constexpr int kCandidates = 1024;
+constexpr int kMaxTop = COCODC_LM_MAX_TOP;
+
+struct RowShared {
+  Stats scratch[kWarps];
+  Stats part;                                       // this CTA's part of the row, read by the cluster's first CTA
+  unsigned long long warp_keys[kWarps];
+  unsigned long long lists[kWarps * kMaxTop];
+  unsigned long long top[kMaxTop];                  // this CTA's part's largest keys
+  unsigned long long candidates[kCandidates];
+  unsigned long long gathered[8 * kMaxTop];         // first CTA: the parts' lists
+  int flagged[kMaxTop], n_flagged, n_candidates;
+};
+
+// A row is read once.  Each thread keeps (m, s, u) of its own elements, rescaled when its largest logit grows, in
+// batches of kUnroll 16-byte words; the parts are joined through shuffles and shared memory, and between the CTAs of a cluster (a row is
+// split over 1 to 8 CTAs, so that few rows still fill the GPU) through distributed shared memory.
+//
+// The alternatives cost the walk nothing but a note of the batch in which the thread's largest logit came.  Keys (value,
+// position) are distinct, so the k largest keys of the CTA lie with the k threads whose own largest keys are the k
+// largest among the threads' (tau is the smallest of these k): only what those threads saw is read again (from L2), and
+// of it only keys >= tau are sorted.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int parts) {
+  using W = Words<T>;
+  __shared__ RowShared sh;
+  const long long t = blockIdx.x / parts;
+  const int part = blockIdx.x - (int)(t * parts);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const T* row = static_cast<const T*>(a.logits) + t * a.stride;
+  const float c = a.scale * kLog2e;
+
+  // [j0, j1): this CTA's part; whole 16-byte words from `base` on, what is left at the row's ends goes element by element
+  const unsigned lead = min(a.V, (unsigned)((16 - ((uintptr_t)row & 15)) & 15) / (unsigned)sizeof(T));
+  const unsigned words = (a.V - lead) / W::n, per = (words + parts - 1) / parts;
+  const unsigned w0 = min(words, part * per), w1 = min(words, w0 + per), n = w1 - w0;
+  const unsigned j0 = part == 0 ? 0 : lead + w0 * W::n, j1 = part == parts - 1 ? a.V : lead + w1 * W::n;
+  const unsigned base = lead + w0 * W::n, tail = lead + w1 * W::n;
+  const uint4* src = reinterpret_cast<const uint4*>(row + base);
+
+  Stats x{-W::kFar, 0.f, 0.f};
+  float mc = x.m * c;
+  unsigned at = 0;                                  // TOP: batch (from 2 on) or end (0, 1) that holds the thread's largest logit
+  const auto raise = [&](float m) {
+    const float d = fmaxf((x.m - m) * c, -1e4f), f = exp2f(d);
+    x.u = (x.u + d * x.s) * f;
+    x.s *= f;
+    x.m = m;
+    mc = m * c;
+  };
+  const auto add = [&](float v) {
+    const float d = fmaf(v, c, -mc), e = fast_exp2(d);
+    x.s += e;
+    x.u = fmaf(e, d, x.u);
+  };
+  const auto single = [&](unsigned j, unsigned where) {
+    float v;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(to_f32(row[j])), "f"(-W::kFar));
+    if (v > x.m) { raise(v); at = where; }
+    add(v);
+  };
+  if (j0 + tid < base) single(j0 + tid, 0);
+  unsigned batch = 2;
+  for (unsigned i = tid; i < n; i += kThreads * kUnroll, ++batch) {
+    W w[kUnroll];
+    uint4 raw[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) raw[k] = i + k * kThreads < n ? __ldg(src + i + k * kThreads) : W::far();
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) w[k].set(raw[k]);
+    float m = w[0].largest();
+#pragma unroll
+    for (int k = 1; k < kUnroll; ++k) m = fmaxf(m, w[k].largest());
+    if (m > x.m) { raise(m); at = batch; }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+      for (int q = 0; q < W::n; ++q) add(w[k].at(q));
+  }
+  if (tail + tid < j1) single(tail + tid, 1);
+  const Stats mine = x;
+  x = block_join(x, c, sh.scratch);
+  // a NaN or +Inf, nothing but very low logits, a very small scale: once more, with care (also the alternatives)
+  const bool careful = !(x.m > -W::kFar / 2) || !(x.s < INFINITY) || !(c * (W::kFar / 2) > 200.f);
+  if (careful) x = careful_stats(row, j0, j1, c, sh.scratch);
+
+  if (TOP) {
+    if (tid == 0) sh.n_flagged = sh.n_candidates = 0;
+    __syncthreads();
+    bool done = false;
+    if (!careful) {
+      // the thread's largest key: its value is known, the lowest position holding it is in the noted batch
+      unsigned long long key = 0;
+      if (mine.s > 0.f && mine.m > -W::kFar) {
+        unsigned j = 0;
+        if (at < 2) {
+          j = at ? tail + tid : j0 + tid;
+        } else {
+          const unsigned i = tid + (at - 2) * kThreads * kUnroll;
+          bool found = false;
+#pragma unroll
+          for (int k = 0; k < kUnroll; ++k)
+            if (!found && i + k * kThreads < n) {
+              W w;
+              w.set(src[i + k * kThreads]);
+#pragma unroll
+              for (int q = 0; q < W::n; ++q)
+                if (!found && w.at(q) == mine.m) { found = true; j = base + (i + k * kThreads) * W::n + q; }
+            }
+        }
+        key = key_of(mine.m, j);
+      }
+      // the k largest of the threads' keys: per warp, then over the warps
+      unsigned long long rest = key;
+      for (int r = 0; r < a.top_k; ++r) {
+        const unsigned long long best = warp_max(rest);
+        if (lane == 0) sh.lists[warp * a.top_k + r] = best;
+        if (rest == best) rest = 0;
+      }
+      __syncthreads();
+      if (warp == 0) warp_top(sh.lists, kWarps * a.top_k, a.top_k, sh.top);
+      __syncthreads();
+      const unsigned long long tau = sh.top[a.top_k - 1];
+      // tau 0: fewer threads than alternatives hold anything; leave it to the careful way
+      if (tau != 0) {
+        if (key >= tau) sh.flagged[atomicAdd(&sh.n_flagged, 1)] = tid;
+        __syncthreads();
+        const auto offer = [&](float v, unsigned j) {
+          const unsigned long long q = key_of(v, j);
+          if (q < tau) return;
+          const int slot = atomicAdd(&sh.n_candidates, 1);
+          if (slot < kCandidates) sh.candidates[slot] = q;
+        };
+        for (int f = warp; f < a.top_k; f += kWarps) {
+          const unsigned who = sh.flagged[f];
+          if (lane == 0 && j0 + who < base) offer(to_f32(row[j0 + who]), j0 + who);
+          if (lane == 1 && tail + who < j1) offer(to_f32(row[tail + who]), tail + who);
+          for (unsigned i = who + lane * kThreads; i < n; i += 32 * kThreads) {
+            W w;
+            w.set(src[i]);
+            if (ordered(w.largest()) < (unsigned)(tau >> 32)) continue;
+#pragma unroll
+            for (int q = 0; q < W::n; ++q) offer(w.at(q), base + i * W::n + q);
+          }
+        }
+        __syncthreads();
+        done = sh.n_candidates <= kCandidates;
+        if (done && warp == 0) warp_top(sh.candidates, sh.n_candidates, a.top_k, sh.top);
+        __syncthreads();
+      }
+    }
+    if (!done) careful_top(row, j0, j1, a.top_k, sh.top, sh.warp_keys);
+  }
+
+  // the parts of the row come together in the cluster's first CTA
+  const unsigned long long* top = sh.top;
+  if (parts > 1) {
+    if (tid == 0) sh.part = x;
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (part == 0) {
+      if (tid == 0) {
+        const unsigned here = (unsigned)__cvta_generic_to_shared(&sh.part);
+        for (int p = 1; p < parts; ++p) {
+          unsigned there;
+          Stats y;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(p));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y.m) : "r"(there));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y.s) : "r"(there + 4));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y.u) : "r"(there + 8));
+          x = join(x, y, c);
+        }
+      }
+      if (TOP) {
+        const unsigned here = (unsigned)__cvta_generic_to_shared(sh.top);
+        for (int i = tid; i < parts * a.top_k; i += kThreads) {
+          unsigned there;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here + i % a.top_k * 8), "r"(i / a.top_k));
+          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(sh.gathered[i]) : "r"(there));
+        }
+        __syncthreads();
+        if (warp == 0) warp_top(sh.gathered, parts * a.top_k, a.top_k, sh.lists);
+        top = sh.lists;
+      }
+    }
+    // the others' shared memory stays until it has been read
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (part != 0) return;
+  }
+
+  if (warp != 0) return;
+  const bool empty = x.m == -INFINITY && x.s == 0.f;
+  float log2s = empty ? -INFINITY : log2f(x.s);
+  const float top_mc = x.m * c;
+  log2s = __shfl_sync(~0u, log2s, 0);
+  const float mc0 = __shfl_sync(~0u, top_mc, 0);
+  const bool none = __shfl_sync(~0u, (int)empty, 0);
+  const float m0 = __shfl_sync(~0u, x.m, 0);
+  // log probability of a logit: ln 2 (c x - c m - log2 s), in which the rounding of c m cancels against the sum's; logits so
+  // low that c x (or c m) overflows are taken in the natural base
+  const auto logp_of = [&](float v) {
+    const float r = fmaf(v, c, -mc0) - log2s;
+    return none ? -INFINITY : fabsf(r) < INFINITY ? kLn2 * r : (v - m0) * a.scale - kLn2 * log2s;
+  };
+  if (lane == 0) {
+    if (a.lse) a.lse[t] = none ? -INFINITY : fabsf(mc0) < INFINITY ? kLn2 * (mc0 + log2s) : m0 * a.scale + kLn2 * log2s;
+    if (a.entropy) a.entropy[t] = none ? 0.f : kLn2 * (log2s - x.u / x.s);
     if (a.logp) {
       const long long y = token_at(a.targets, a.targets64, t, a.V, a.status);
-      a.logp[t] = y < 0 ? 0.f : empty ? -INFINITY : to_f32(row[y]) * a.scale - lse;
+      a.logp[t] = y < 0 ? 0.f : logp_of(to_f32(row[y]));
     }
   }
-  unsigned long long last = ~0ull;
-  for (int i = 0; i < a.top_k; ++i) {
-    unsigned long long k = 0;
-    for (unsigned j = tid; j < a.V; j += kThreads) {
-      const unsigned long long q = key_of(to_f32(row[j]), j);
-      if (q < last && q > k) k = q;
-    }
-    k = warp_max(k);
-    __syncthreads();
-    if (lane == 0) best[warp] = k;
-    __syncthreads();
-    for (int w = 0; w < kWarps; ++w) k = best[w] > k ? best[w] : k;
-    last = k;
-    if (tid == 0 && k != 0) {
-      const unsigned j = position_of(k);
-      a.top_ids[t * a.top_k + i] = (int)j;
-      a.top_logp[t * a.top_k + i] = empty ? -INFINITY : to_f32(row[j]) * a.scale - lse;
-    }
+  if (TOP && lane < a.top_k) {
+    const unsigned j = position_of(top[lane]);
+    a.top_ids[t * a.top_k + lane] = (int)j;
+    a.top_logp[t * a.top_k + lane] = logp_of(to_f32(row[j]));
   }
 }
 
@@ -121,27 +415,86 @@ struct GradArgs {
   int* status;
 };
 
-constexpr int kGradElems = 2048;   // elements of a row that one CTA takes
+// One read and one write of every logit: bound by memory.  A CTA takes kThreads * kUnroll 16-byte words of one row.
+template <typename T> struct Out;   // packs results the way Words unpacks logits
+template <> struct Out<float> {
+  static __device__ __forceinline__ uint4 of(const float (&d)[4]) {
+    return make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
+  }
+};
+template <typename T2, typename F> __device__ __forceinline__ uint4 pack8(const float (&d)[8], F&& pair) {
+  unsigned u[4];
+  for (int i = 0; i < 4; ++i) {
+    const T2 v = pair(d[2 * i], d[2 * i + 1]);
+    u[i] = *reinterpret_cast<const unsigned*>(&v);
+  }
+  return make_uint4(u[0], u[1], u[2], u[3]);
+}
+template <> struct Out<__nv_bfloat16> {
+  static __device__ __forceinline__ uint4 of(const float (&d)[8]) {
+    return pack8<__nv_bfloat162>(d, [](float x, float y) { return __floats2bfloat162_rn(x, y); });
+  }
+};
+template <> struct Out<__half> {
+  static __device__ __forceinline__ uint4 of(const float (&d)[8]) {
+    return pack8<__half2>(d, [](float x, float y) { return __floats2half2_rn(x, y); });
+  }
+};
+template <typename T> constexpr unsigned kGradElems = kThreads * kUnroll * (16 / sizeof(T));
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_logprobs_grad(const GradArgs a) {
-  const long long chunks = (a.V + kGradElems - 1LL) / kGradElems;
+__global__ void __launch_bounds__(kThreads) k_logprobs_grad(const GradArgs a, unsigned chunks) {
+  constexpr int n = 16 / sizeof(T);
   const long long t = blockIdx.x / chunks;
-  const unsigned j0 = (unsigned)(blockIdx.x - t * chunks) * kGradElems;
+  const unsigned chunk = blockIdx.x - (unsigned)(t * chunks);
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
   T* out = static_cast<T*>(a.dlogits) + t * a.dstride;
   const long long y = a.dlogp ? token_at(a.targets, a.targets64, t, a.V, a.status) : -1;
   const float lse = a.lse[t];
-  const float g = y >= 0 ? a.dlogp[t] : 0.f;
+  float g = y >= 0 ? a.dlogp[t] : 0.f;
   const float h = a.dentropy ? a.dentropy[t] : 0.f, H = a.dentropy ? a.entropy[t] : 0.f;
-  for (unsigned j = j0 + threadIdx.x; j < a.V && j < j0 + kGradElems; j += kThreads) {
-    float d = 0.f;
-    if (lse != -INFINITY) {
-      const float lp = to_f32(row[j]) * a.scale - lse, p = expf(lp);
-      if (lp != -INFINITY) d = -p * (g + h * (lp + H));
-      if (j == y) d += g;
+  const bool none = lse == -INFINITY;
+  if (lse != lse) g = lse;                              // a row without valid probabilities: NaN everywhere
+  // -p (g + h (log p + H)); log p is kept above -1e4, where p is 0, so that a masked logit's -Inf does not meet that 0
+  const auto slope = [&](float x) {
+    const float lp = fmaxf(fmaf(x, a.scale, -lse), -1e4f);
+    return -fast_exp2(lp * kLog2e) * fmaf(h, lp + H, g);
+  };
+  const auto single = [&](unsigned j) {
+    out[j] = from_f32<T>(none ? 0.f : a.scale * (slope(to_f32(row[j])) + (j == y ? g : 0.f)));
+  };
+  if (((uintptr_t)row ^ (uintptr_t)out) & 15) {         // no common 16-byte boundaries
+    const unsigned j0 = chunk * kGradElems<T>, j1 = min(a.V, j0 + kGradElems<T>);
+    for (unsigned j = j0 + threadIdx.x; j < j1; j += kThreads) single(j);
+    return;
+  }
+  const unsigned lead = min(a.V, (unsigned)((16 - ((uintptr_t)row & 15)) & 15) / (unsigned)sizeof(T));
+  const unsigned words = (a.V - lead) / n, tail = lead + words * n;
+  if (chunk == 0 && threadIdx.x < lead) single(threadIdx.x);
+  if (chunk == chunks - 1 && tail + threadIdx.x < a.V) single(tail + threadIdx.x);
+  const uint4* src = reinterpret_cast<const uint4*>(row + lead);
+  uint4* dst = reinterpret_cast<uint4*>(out + lead);
+  const unsigned i0 = chunk * (kThreads * kUnroll) + threadIdx.x;
+  uint4 raw[kUnroll];
+#pragma unroll
+  for (int k = 0; k < kUnroll; ++k)
+    if (i0 + k * kThreads < words) raw[k] = src[i0 + k * kThreads];
+#pragma unroll
+  for (int k = 0; k < kUnroll; ++k) {
+    const unsigned i = i0 + k * kThreads;
+    if (i >= words) continue;
+    float d[n];
+    const T* e = reinterpret_cast<const T*>(&raw[k]);
+#pragma unroll
+    for (int q = 0; q < n; ++q) d[q] = slope(to_f32(e[q]));
+    const long long hit = y - (long long)(lead + i * n);
+    if (hit >= 0 && hit < n) {
+#pragma unroll
+      for (int q = 0; q < n; ++q) d[q] += q == hit ? g : 0.f;
     }
-    out[j] = from_f32<T>(a.scale * d);
+#pragma unroll
+    for (int q = 0; q < n; ++q) d[q] = none ? 0.f : d[q] * a.scale;
+    dst[i] = Out<T>::of(d);
   }
 }
 
@@ -180,11 +533,27 @@ cocodc_status cocodc_lm_logprobs(cocodc_lm* lm, const void* logits, int32_t type
   if (!scope.ok) return COCODC_ERR_CUDA;
   const RowArgs a{logits, stride, T, (unsigned)V, targets, targets_type == COCODC_I64, scale, logp, entropy, lse,
                   top_k, top_ids, top_logp, lm->d_status};
-  with_type(type, [&](auto x) {
-    k_logprobs<decltype(x)><<<(unsigned)T, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    return true;
+  // few rows: each over as many CTAs (a cluster) as it takes to give every SM one, but at least 4 KB of the row to each
+  int parts = 1;
+  while (parts < 8 && T * parts < lm->sm_count && V * es >= 8192 * parts) parts *= 2;
+  if (T > INT32_MAX / parts) return COCODC_ERR_INVALID_ARG;
+  cudaLaunchAttribute cluster{};
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = (unsigned)parts;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3((unsigned)(T * parts));
+  config.blockDim = dim3(kThreads);
+  config.stream = static_cast<cudaStream_t>(stream);
+  config.attrs = &cluster;
+  config.numAttrs = 1;
+  const bool ok = with_type(type, [&](auto x) {
+    using E = decltype(x);
+    return (top_k ? cudaLaunchKernelEx(&config, k_logprobs<E, true>, a, parts)
+                  : cudaLaunchKernelEx(&config, k_logprobs<E, false>, a, parts)) == cudaSuccess;
   });
-  return launched(lm);
+  const cocodc_status s = launched(lm);
+  return ok ? s : COCODC_ERR_CUDA;
 }
 
 cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t type, int64_t stride, int64_t T,
@@ -208,14 +577,15 @@ cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t
       meet(out, span(targets, 1, T, T, targets ? index_bytes(targets_type) : 1)) || meet(out, span(lse, 1, T, T, 4)) ||
       meet(out, span(entropy, 1, T, T, 4)) || meet(out, span(dlogp, 1, T, T, 4)) || meet(out, span(dentropy, 1, T, T, 4)))
     return COCODC_ERR_ALIAS;
-  const long long blocks = T * ((V + kGradElems - 1) / kGradElems);
+  const long long elems = type == COCODC_F32 ? kGradElems<float> : kGradElems<__half>;
+  const long long chunks = (V + elems - 1) / elems, blocks = T * chunks;
   if (blocks > INT32_MAX) return COCODC_ERR_INVALID_ARG;
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   const GradArgs a{logits, stride, T, (unsigned)V, targets, targets_type == COCODC_I64, scale, lse, entropy, dlogp,
                    dentropy, dlogits, dlogits_stride, lm->d_status};
   with_type(type, [&](auto x) {
-    k_logprobs_grad<decltype(x)><<<(unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    k_logprobs_grad<decltype(x)><<<(unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, (unsigned)chunks);
     return true;
   });
   return launched(lm);
