@@ -33,6 +33,16 @@ template <typename T, int W> struct Pack {
   }
 };
 
+// the same as it came from memory, converted when it is used
+template <typename T, int W> struct Raw {
+  alignas(16) T e[W];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (W == 1) e[0] = *p;
+    else *reinterpret_cast<uint4*>(e) = __ldg(reinterpret_cast<const uint4*>(p));
+  }
+  __device__ __forceinline__ float at(int i) const { return to_f32(e[i]); }
+};
+
 // ---- lookup ------------------------------------------------------------------------------------
 // A gather: bound by memory.  A thread moves U packs of W elements, 256 apart, so that U loads are in flight; T * D / W packs
 // are numbered row by row.
@@ -64,24 +74,27 @@ __global__ void __launch_bounds__(256) k_embed(const TIn* __restrict__ table, lo
   }
 }
 
-// ---- gradient, step 1: the tokens sorted by id --------------------------------------------------
-// One CTA owns the kBinRows (or fewer) consecutive table rows from lo on and finds their tokens itself by walking over all T ids
-// twice; no CTA waits for another.  Walk 1 counts, per row and warp, how often the row occurs in the warp's contiguous
-// part of the ids, and how many ids lie below lo (where this CTA's rows start in the sorted order).  A prefix sum
-// over (row, warp) turns the counts into positions, and walk 2 places every token: equal ids stay in the order of
-// their positions because a warp's part precedes the next warp's and ballots rank the lanes of a warp.
-// All T ids are read by every CTA, from L2 after the first: at 65536 tokens of 4 bytes and 148 CTAs 39 MB a walk.
+// ---- gradient, step 1: the tokens in order of their rows ------------------------------------------
+// The table's rows are dealt to B bins (a power of two), row v to bin v mod B, so that the frequent tokens, whose ids
+// tend to lie together, end up in different bins; the sorted order is by (bin, row, token position).  One CTA per bin finds its
+// tokens itself by walking over all T ids; no CTA waits for another.  A warp walks over its contiguous part of the
+// ids and appends the hits, in order, to a list in shared memory; ids in lower bins are counted: their number is where this
+// bin begins.  The hits counted per (row, warp), a prefix sum over the counts gives every row's and warp's first
+// position, and a second run over the lists (over the ids, where a list was too short) places the tokens: equal ids
+// stay in the order of their positions because a warp's part precedes the next warp's.
+// Every CTA reads all ids, from L2 after the first: 256 CTAs and 65536 tokens of 4 bytes make 67 MB.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kMaxBinRows = 768;                       // (rows * 33 + 64) * 4 bytes of shared memory: 99 KB
+constexpr int kMaxBinRows = 768;
 constexpr int kBinPitch = kSortWarps + 1;              // counters of a warp's lanes fall into different banks
+constexpr int kListLength = 256;                       // hits that a warp keeps, at most 128 of them new per step
 
 struct GradArgs {
   const void* ids;
   int is64;
   int T;
   long long V, D;
-  int bin_rows;
+  int bins_log2, bin_rows;
   int accumulate;
   float scale;
   const void* dy;
@@ -90,7 +103,7 @@ struct GradArgs {
   long long dtable_stride;
   int dtable_esize;
   int dtable_wide;    // rows start on 16-byte boundaries
-  int* row_start;     // [V + 1] first sorted position of every row
+  int* row_start;     // [bins * bin_rows + 1] first sorted position of every row, in sorted order
   int2* sorted;       // [T] (token position, row) in sorted order
   float* partial;     // [tiles][2][padded D]: sums of the rows that a tile shares with its neighbours
   int* arrived;       // [tiles][column blocks]: tiles that have left their part of the row that begins in the tile
@@ -99,87 +112,139 @@ struct GradArgs {
   long long pitch;    // padded D
   int* status;
 };
-
-__device__ __forceinline__ int block_sum(int v, int* scratch) {   // scratch: 32 ints
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-  __syncthreads();
-  int s = 0;
-  for (int w = 0; w < kSortWarps; ++w) s += scratch[w];
-  __syncthreads();
-  return s;
+// where a row comes in the sorted order
+__device__ __forceinline__ int order_of(const GradArgs& a, int row) {
+  return (row & ((1 << a.bins_log2) - 1)) * a.bin_rows + (row >> a.bins_log2);
 }
 
-__global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
-  extern __shared__ int smem[];
-  int* cnt = smem;                                   // [bin_rows][kBinPitch]
-  int* scratch = smem + a.bin_rows * kBinPitch;      // [32]
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long lo = (long long)blockIdx.x * a.bin_rows;
-  const int rows = (int)min((long long)a.bin_rows, a.V - lo);
-  const long long part = ((a.T + kSortWarps - 1LL) / kSortWarps + 31) / 32 * 32;
-  const long long t0 = warp * part, t1 = min((long long)a.T, t0 + part);
+struct SortShared {
+  int2 list[kSortWarps][kListLength];                  // (token position, row of the bin)
+  int scratch[kSortWarps];
+  int again;                                           // a list was too short
+  int cnt[];                                           // [bin_rows][kBinPitch]
+};
 
-  for (int i = tid; i < rows * kBinPitch; i += kSortThreads) cnt[i] = 0;
-  for (long long i = (long long)blockIdx.x * kSortThreads + tid; i < a.n_arrived; i += (long long)gridDim.x * kSortThreads)
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
+  extern __shared__ __align__(16) unsigned char dyn[];
+  SortShared& sh = *reinterpret_cast<SortShared*>(dyn);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int bin = blockIdx.x, mask = (1 << a.bins_log2) - 1;
+  const long long part = ((a.T + kSortWarps - 1LL) / kSortWarps + 127) / 128 * 128;
+  const long long t0 = warp * part, t1 = min((long long)a.T, t0 + part);
+  const I* ids = static_cast<const I*>(a.ids);
+  const bool wide = ((uintptr_t)ids & 15) == 0;
+
+  for (int i = tid; i < a.bin_rows * kBinPitch; i += kSortThreads) sh.cnt[i] = 0;
+  for (long long i = (long long)bin * kSortThreads + tid; i < a.n_arrived; i += (long long)gridDim.x * kSortThreads)
     a.arrived[i] = 0;
+  if (tid == 0) sh.again = 0;
   __syncthreads();
-  // calls f(position, row of this bin or -1) for the ids of the warp's part in order, four loads ahead
-  int below = 0;
-  const auto walk = [&](auto&& f) {
-    for (long long t = t0; t < t1; t += 128) {
-      int r[4];
-      for (int i = 0; i < 4; ++i) {
-        const long long at = t + i * 32 + lane, v = at < t1 ? token_at(a.ids, a.is64, at, a.V, a.status) : -1;
-        below += v >= 0 && v < lo;
-        r[i] = v >= lo && v < lo + rows ? (int)(v - lo) : -1;
-      }
-      for (int i = 0; i < 4; ++i)
-        if (__ballot_sync(~0u, r[i] >= 0)) {
-          f(t + i * 32 + lane, r[i], __match_any_sync(~0u, r[i]));
-          __syncwarp();
-        }
+
+  // f on hits [0, n) of the warp's list, 32 at a time: the hit (row -1: none) and the lanes with the same row
+  const auto each = [&](int n, auto&& f) {
+    __syncwarp();
+    for (int i = 0; i < n; i += 32) {
+      const int2 e = i + lane < n ? sh.list[warp][i + lane] : make_int2(0, -1);
+      f(e, __match_any_sync(~0u, e.y));
+      __syncwarp();
     }
   };
-  walk([&](long long, int r, unsigned same) {
-    if (r >= 0 && lane == __ffs(same) - 1) cnt[r * kBinPitch + warp] += __popc(same);
-  });
-  const int first = block_sum(below, scratch);
-  __syncthreads();
+  int below = 0, hits = 0;
+  bool flushed = false;
+  const auto walk = [&](auto&& f) {
+    hits = 0;
+    for (long long t = t0; t < t1; t += 128) {         // lane l takes ids t + 4 l .. t + 4 l + 3
+      const long long first = t + lane * 4;
+      I v[4];
+      if (wide && first + 4 <= t1) {
+        constexpr int words = 4 * sizeof(I) / 16;
+        for (int i = 0; i < words; ++i) reinterpret_cast<uint4*>(v)[i] = __ldg(reinterpret_cast<const uint4*>(ids + first) + i);
+      } else {
+        for (int i = 0; i < 4; ++i) v[i] = first + i < t1 ? ids[first + i] : I(-1);
+      }
+      unsigned mine = 0;
+      for (int i = 0; i < 4; ++i) {
+        if (v[i] >= a.V) { record(a.status, COCODC_ERR_INVALID_ARG); v[i] = -1; }
+        const int b = (int)v[i] & mask;
+        below += v[i] >= 0 && b < bin;
+        mine |= (unsigned)(v[i] >= 0 && b == bin) << i;
+      }
+      if (!__any_sync(~0u, mine)) continue;
+      int before = 0, all = 0;
+      for (int i = 0; i < 4; ++i) {
+        const unsigned m = __ballot_sync(~0u, mine >> i & 1);
+        before += __popc(m & ((1u << lane) - 1));
+        all += __popc(m);
+      }
+      for (int i = 0; i < 4; ++i)
+        if (mine >> i & 1) sh.list[warp][hits + before++] = make_int2((int)(first + i), (int)(v[i] >> a.bins_log2));
+      hits += all;
+      if (hits > kListLength - 128) {
+        each(hits, f);
+        hits = 0;
+        flushed = true;
+      }
+    }
+  };
+  const auto count = [&](int2 e, unsigned same) {
+    if (e.y >= 0 && lane == __ffs(same) - 1) sh.cnt[e.y * kBinPitch + warp] += __popc(same);
+  };
+  walk(count);
+  each(hits, count);
+  if (flushed && lane == 0) sh.again = 1;
 
-  // positions: exclusive prefix over the rows of the bin, then over the warps inside a row
+  for (int o = 16; o; o >>= 1) below += __shfl_xor_sync(~0u, below, o);
+  if (lane == 0) sh.scratch[warp] = below;
+  __syncthreads();
+  int at = 0;                                          // of the bin, then of the thread's row
+  for (int w = 0; w < kSortWarps; ++w) at += sh.scratch[w];
+  __syncthreads();
   int total = 0;
-  if (tid < rows)
-    for (int w = 0; w < kSortWarps; ++w) total += cnt[tid * kBinPitch + w];
+  if (tid < a.bin_rows)
+    for (int w = 0; w < kSortWarps; ++w) total += sh.cnt[tid * kBinPitch + w];
   int incl = total;
   for (int o = 1; o < 32; o <<= 1) {
     const int up = __shfl_up_sync(~0u, incl, o);
     if (lane >= o) incl += up;
   }
-  if (lane == 31) scratch[warp] = incl;
+  if (lane == 31) sh.scratch[warp] = incl;
   __syncthreads();
-  int at = first + incl - total;
-  for (int w = 0; w < warp; ++w) at += scratch[w];
-  if (tid < rows) {
-    a.row_start[lo + tid] = at;
-    if (lo + tid == a.V - 1) a.row_start[a.V] = at + total;
+  at += incl - total;
+  for (int w = 0; w < warp; ++w) at += sh.scratch[w];
+  if (tid < a.bin_rows) {
+    a.row_start[bin * a.bin_rows + tid] = at;
+    if (bin == mask && tid == a.bin_rows - 1) a.row_start[(bin + 1) * a.bin_rows] = at + total;
     int run = at;
     for (int w = 0; w < kSortWarps; ++w) {
-      const int c = cnt[tid * kBinPitch + w];
-      cnt[tid * kBinPitch + w] = run;
+      const int c = sh.cnt[tid * kBinPitch + w];
+      sh.cnt[tid * kBinPitch + w] = run;
       run += c;
     }
-    cnt[tid * kBinPitch + kSortWarps] = total;       // the padding word keeps the row's count
+    sh.cnt[tid * kBinPitch + kSortWarps] = total;      // the padding word keeps the row's count
   }
   __syncthreads();
 
-  // rows that no token names: zeros, on their way while the second walk runs
+  const auto place = [&](int2 e, unsigned same) {
+    const int leader = __ffs(same) - 1;
+    int base = 0;
+    if (e.y >= 0 && lane == leader) {
+      base = sh.cnt[e.y * kBinPitch + warp];
+      sh.cnt[e.y * kBinPitch + warp] = base + __popc(same);
+    }
+    base = __shfl_sync(~0u, base, leader);
+    if (e.y >= 0) a.sorted[base + __popc(same & ((1u << lane) - 1))] = make_int2(e.x, (e.y << a.bins_log2) + bin);
+  };
+  if (sh.again) walk(place);
+  each(hits, place);
+
+  // rows that no token names: zeros
   if (!a.accumulate) {
-    const bool wide = a.dtable_wide;
-    const long long bytes = a.D * a.dtable_esize, n16 = wide ? bytes / 16 : 0;
-    for (int r = warp; r < rows; r += kSortWarps) {
-      if (cnt[r * kBinPitch + kSortWarps]) continue;
-      char* p = static_cast<char*>(a.dtable) + (lo + r) * a.dtable_stride * a.dtable_esize;
+    const long long bytes = a.D * a.dtable_esize, n16 = a.dtable_wide ? bytes / 16 : 0;
+    for (int r = warp; r < a.bin_rows; r += kSortWarps) {
+      const long long v = ((long long)r << a.bins_log2) + bin;
+      if (v >= a.V || sh.cnt[r * kBinPitch + kSortWarps]) continue;
+      char* p = static_cast<char*>(a.dtable) + v * a.dtable_stride * a.dtable_esize;
       for (long long i = lane; i < n16; i += 32) reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
       for (long long i = n16 * 16 + lane * a.dtable_esize; i < bytes; i += 32 * a.dtable_esize) {
         if (a.dtable_esize == 4) *reinterpret_cast<float*>(p + i) = 0.f;
@@ -187,17 +252,6 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
       }
     }
   }
-
-  walk([&](long long t, int r, unsigned same) {
-    const int leader = __ffs(same) - 1;
-    int base = 0;
-    if (r >= 0 && lane == leader) {
-      base = cnt[r * kBinPitch + warp];
-      cnt[r * kBinPitch + warp] = base + __popc(same);
-    }
-    base = __shfl_sync(~0u, base, leader);
-    if (r >= 0) a.sorted[base + __popc(same & ((1u << lane) - 1))] = make_int2((int)t, (int)(lo + r));
-  });
 }
 
 // ---- gradient, step 2: the sums -----------------------------------------------------------------
@@ -215,7 +269,7 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
   const int width = blockDim.x / kGroups, group = threadIdx.x / width, c = threadIdx.x % width;
   const long long col = ((long long)blockIdx.y * width + c) * W;
   const bool active = col < a.D;
-  const int n = a.row_start[a.V];
+  const int n = a.row_start[a.bin_rows << a.bins_log2];
   const int tile = blockIdx.x, span = kGroups * a.positions, begin = tile * span;
   if (begin >= n) return;
   const TIn* dy = static_cast<const TIn*>(a.dy) + (active ? col : 0);
@@ -248,12 +302,14 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
     int row = row_at(p0);
     clear();
     for (int p = p0; p < p1; p += 8) {
-      Pack<TIn, W> x[8];
+      Raw<TIn, W> x[8];
       int2 e[8];
-      for (int i = 0; i < 8; ++i) {
-        e[i] = p + i < p1 ? a.sorted[p + i] : make_int2(-1, row);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = p + i < p1 ? a.sorted[p + i] : make_int2(-1, row);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
         if (e[i].x >= 0) x[i].load(dy + (long long)e[i].x * a.dy_stride);
-      }
+#pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (e[i].x < 0) continue;
         if (e[i].y != row) {
@@ -263,7 +319,7 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
           row = e[i].y;
           clear();
         }
-        for (int k = 0; k < W; ++k) acc[k] += x[i].v[k];
+        for (int k = 0; k < W; ++k) acc[k] += x[i].at(k);
       }
     }
     float* to = open ? head : goes_on ? tail : nullptr;
@@ -317,7 +373,7 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
     const int row = pending_row[threadIdx.x];
     int last = 0;
     if (row >= 0) {
-      const int first = a.row_start[row] / span, end = (a.row_start[row + 1] - 1) / span;
+      const int g = order_of(a, row), first = a.row_start[g] / span, end = (a.row_start[g + 1] - 1) / span;
       __threadfence();
       last = atomicAdd(&a.arrived[(long long)first * gridDim.y + blockIdx.y], 1) == end - first;
       __threadfence();
@@ -327,7 +383,8 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
   __syncthreads();
   for (int s = 0; s < 2; ++s) {
     if (!is_last[s]) continue;
-    const int row = pending_row[s], first = a.row_start[row] / span, parts = (a.row_start[row + 1] - 1) / span - first + 1;
+    const int row = pending_row[s], g = order_of(a, row);
+    const int first = a.row_start[g] / span, parts = (a.row_start[g + 1] - 1) / span - first + 1;
     clear();
     const int j1 = (int)((long long)parts * (group + 1) / kGroups);
     if (active)
@@ -360,6 +417,15 @@ int positions_for(int64_t T) {
 }
 
 uint64_t up16(uint64_t n) { return (n + 15) / 16 * 16; }
+// 256 bins (all resident at two CTAs per SM), fewer for a smaller table, more where a bin's rows would not fit shared memory
+int bins_log2_for(int64_t V) {
+  int l = 0;
+  while (l < 8 && (int64_t(1) << l) < V) ++l;
+  while ((V + (int64_t(1) << l) - 1) >> l > kMaxBinRows) ++l;
+  return l;
+}
+int64_t bin_rows_for(int64_t V) { return (V + (int64_t(1) << bins_log2_for(V)) - 1) >> bins_log2_for(V); }
+int64_t starts_for(int64_t V) { return (bin_rows_for(V) << bins_log2_for(V)) + 1; }
 int64_t padded(int64_t D) { return (D + 7) / 8 * 8; }
 int64_t tiles_for(int64_t T) { return (T + kGroups * positions_for(T) - 1) / (kGroups * positions_for(T)); }
 
@@ -367,8 +433,9 @@ int64_t tiles_for(int64_t T) { return (T + kGroups * positions_for(T) - 1) / (kG
 
 namespace cocodc_lm_impl {
 bool embed_prepare() {
-  return cudaFuncSetAttribute(k_embed_sort, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (kMaxBinRows * kBinPitch + 32) * 4) == cudaSuccess;
+  const int most = (int)sizeof(SortShared) + kMaxBinRows * kBinPitch * 4;
+  return cudaFuncSetAttribute(k_embed_sort<int>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
+         cudaFuncSetAttribute(k_embed_sort<long long>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
 }
 }  // namespace cocodc_lm_impl
 
@@ -415,7 +482,7 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
 uint64_t cocodc_lm_embed_grad_workspace(int64_t V, int64_t D, int64_t T) {
   if (!sane(V) || !sane(D) || !sane(T)) return 0;
   const uint64_t tiles = (uint64_t)tiles_for(T);
-  return up16((uint64_t)(V + 1) * sizeof(int)) + up16((uint64_t)T * sizeof(int2)) + tiles * 2 * padded(D) * sizeof(float) +
+  return up16((uint64_t)starts_for(V) * sizeof(int)) + up16((uint64_t)T * sizeof(int2)) + tiles * 2 * padded(D) * sizeof(float) +
          up16(tiles * (uint64_t)((D + 31) / 32) * sizeof(int));
 }
 
@@ -423,7 +490,7 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
                                    int32_t ids_type, int64_t T, int64_t V, int64_t D, float scale, int32_t accumulate,
                                    void* dtable, int32_t dtable_type, int64_t dtable_stride, void* workspace,
                                    uint64_t workspace_bytes, void* stream) {
-  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || T > INT32_MAX || V >= INT32_MAX || !dtable ||
+  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || T > INT32_MAX || V > (int64_t(1) << 30) || !dtable ||
       !known_type(dy_type) || !known_type(dtable_type) || (ids_type != COCODC_I32 && ids_type != COCODC_I64) ||
       dy_stride < D || dtable_stride < D || !sane(dy_stride) || !sane(dtable_stride))
     return COCODC_ERR_INVALID_ARG;
@@ -456,7 +523,7 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
   const int64_t tiles = tiles_for(T);
   char* at = static_cast<char*>(workspace);
   const auto take = [&](uint64_t bytes) { char* p = at; at += up16(bytes); return p; };
-  a.row_start = reinterpret_cast<int*>(take((uint64_t)(V + 1) * sizeof(int)));
+  a.row_start = reinterpret_cast<int*>(take((uint64_t)starts_for(V) * sizeof(int)));
   a.sorted = reinterpret_cast<int2*>(take((uint64_t)T * sizeof(int2)));
   a.partial = reinterpret_cast<float*>(take((uint64_t)tiles * 2 * padded(D) * sizeof(float)));
   a.arrived = reinterpret_cast<int*>(at);
@@ -471,10 +538,11 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
   const long long columns = (packs + width - 1) / width;
   if (columns > 65535) return COCODC_ERR_INVALID_ARG;
   a.n_arrived = tiles * columns;
-  const long long per_sm = (V + lm->sm_count - 1) / lm->sm_count;
-  a.bin_rows = (int)(per_sm < kMaxBinRows ? per_sm : kMaxBinRows);
-  const unsigned bins = (unsigned)((V + a.bin_rows - 1) / a.bin_rows);
-  k_embed_sort<<<bins, kSortThreads, (a.bin_rows * kBinPitch + 32) * 4, st>>>(a);
+  a.bins_log2 = bins_log2_for(V);
+  a.bin_rows = (int)bin_rows_for(V);
+  const unsigned bins = 1u << a.bins_log2, smem_sort = (unsigned)sizeof(SortShared) + a.bin_rows * kBinPitch * 4;
+  if (a.is64) k_embed_sort<long long><<<bins, kSortThreads, smem_sort, st>>>(a);
+  else k_embed_sort<int><<<bins, kSortThreads, smem_sort, st>>>(a);
   if (T > 0)
     with_type(dy_type, [&](auto in) {
       return with_type(dtable_type, [&](auto out) {

@@ -108,17 +108,48 @@ __global__ void __launch_bounds__(256) k_product_plain(const PlainArgs<T> p) {
 
 // ---- the element-wise part of the gradient ------------------------------------------------------
 // dg and du go to scratch of pitch F rounded up to 8 elements, so that its rows start on 16-byte boundaries.
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) k_glu_slope(const T* dh, long long dh_stride, const T* gate, const T* up,
-                                                   long long gu_stride, long long rows, long long F, T* dg, T* du,
-                                                   long long pitch) {
-  const long long n = rows * F;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-    const long long t = i / F, f = i - t * F;
-    const float d = to_f32(dh[t * dh_stride + f]), u = to_f32(up[t * gu_stride + f]);
-    const Activation x = activate<ACT>(to_f32(gate[t * gu_stride + f]));
-    dg[t * pitch + f] = from_f32<T>(d * u * x.slope);
-    du[t * pitch + f] = from_f32<T>(d * x.value);
+// One read of dh, gate and up, one write of dg and du: bound by memory.  WIDE: the inputs' rows start on 16-byte
+// boundaries; a thread takes 8 columns (the last ones of a row one by one), otherwise one.
+template <typename T, int ACT, bool WIDE>
+__global__ void __launch_bounds__(256) k_glu_slope(const T* __restrict__ dh, long long dh_stride, const T* __restrict__ gate,
+                                                   const T* __restrict__ up, long long gu_stride, long long rows, unsigned F,
+                                                   T* __restrict__ dg, T* __restrict__ du, long long pitch) {
+  constexpr unsigned W = WIDE ? 8 : 1;
+  const unsigned packs = (F + W - 1) / W;
+  const long long blocks = (rows * packs + 255) / 256;
+  const auto one = [&](float d, float g, float u, float& out_g, float& out_u) {
+    const Activation x = activate<ACT>(g);
+    out_g = d * u * x.slope;
+    out_u = d * x.value;
+  };
+  for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const long long first = b * 256, row0 = first / packs;
+    const unsigned rest = (unsigned)(first - row0 * packs) + threadIdx.x, down = rest / packs, f = (rest - down * packs) * W;
+    const long long t = row0 + down;
+    if (t >= rows) return;
+    const T *pd = dh + t * dh_stride + f, *pg = gate + t * gu_stride + f, *pu = up + t * gu_stride + f;
+    if (WIDE && f + 8 <= F) {
+      const uint4 rd = __ldg(reinterpret_cast<const uint4*>(pd)), rg = __ldg(reinterpret_cast<const uint4*>(pg)),
+                  ru = __ldg(reinterpret_cast<const uint4*>(pu));
+      const T *d = reinterpret_cast<const T*>(&rd), *g = reinterpret_cast<const T*>(&rg), *u = reinterpret_cast<const T*>(&ru);
+      unsigned og[4], ou[4];
+      for (int i = 0; i < 4; ++i) {
+        float g0, g1, u0, u1;
+        one(to_f32(d[2 * i]), to_f32(g[2 * i]), to_f32(u[2 * i]), g0, u0);
+        one(to_f32(d[2 * i + 1]), to_f32(g[2 * i + 1]), to_f32(u[2 * i + 1]), g1, u1);
+        og[i] = pack2<T>(g0, g1);
+        ou[i] = pack2<T>(u0, u1);
+      }
+      *reinterpret_cast<uint4*>(dg + t * pitch + f) = make_uint4(og[0], og[1], og[2], og[3]);
+      *reinterpret_cast<uint4*>(du + t * pitch + f) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+    } else {
+      for (unsigned i = 0; i < W && f + i < F; ++i) {
+        float og, ou;
+        one(to_f32(pd[i]), to_f32(pg[i]), to_f32(pu[i]), og, ou);
+        dg[t * pitch + f + i] = from_f32<T>(og);
+        du[t * pitch + f + i] = from_f32<T>(ou);
+      }
+    }
   }
 }
 
@@ -293,10 +324,15 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
     E* du = dg + T * pitch;
     const auto took = [&](cocodc_status s) { if (result == COCODC_OK) result = s; };
     if (T > 0) {
-      const long long blocks = (T * F + 255) / 256;
-      k_glu_slope<E, decltype(a)::value><<<(unsigned)(blocks < (1 << 16) ? blocks : (1 << 16)), 256, 0, st>>>(
-          static_cast<const E*>(dh), dh_stride, static_cast<const E*>(gate), static_cast<const E*>(up), gu_stride, T, F,
-          dg, du, pitch);
+      const bool wide = rows_aligned(dh, dh_stride, 2) && rows_aligned(gate, gu_stride, 2) && rows_aligned(up, gu_stride, 2);
+      const auto slope = [&](auto kernel, int W) {
+        const long long blocks = (T * ((F + W - 1) / W) + 255) / 256;
+        kernel<<<(unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st>>>(
+            static_cast<const E*>(dh), dh_stride, static_cast<const E*>(gate), static_cast<const E*>(up), gu_stride, T,
+            (unsigned)F, dg, du, pitch);
+      };
+      if (wide) slope(k_glu_slope<E, decltype(a)::value, true>, 8);
+      else slope(k_glu_slope<E, decltype(a)::value, false>, 1);
       took(launched(lm));
     }
     TcArgs c{};
