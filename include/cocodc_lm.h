@@ -69,7 +69,7 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
  * dtable[v][:] = scale * sum over t with ids[t] == v of dy[t][:]  (accumulate: added to what dtable holds).
  * Every row is written (zeros for tokens that do not occur); with accumulate only the rows of tokens that occur
  * are touched.  The tokens are sorted by id, equal ids by position, and each row is summed in fp32 in an order
- * that depends on the ids alone.  T < 2^31.
+ * that depends on the ids alone.  T <= 2^27, V <= 2^30.
  *   dy [T][D]; dtable [V][D]; types independent of each other
  */
 uint64_t cocodc_lm_embed_grad_workspace(int64_t V, int64_t D, int64_t T);

@@ -2,6 +2,8 @@
 
 #include "lm_common.cuh"
 
+#include <type_traits>
+
 using namespace cocodc_lm_impl;
 
 namespace {
@@ -43,6 +45,23 @@ template <typename T, int W> struct Raw {
   __device__ __forceinline__ float at(int i) const { return to_f32(e[i]); }
 };
 
+// W sums of one thread, in shared or global scratch
+template <int W> __device__ __forceinline__ void put(float* to, const float (&v)[W]) {
+  if constexpr (W % 4 == 0)
+    for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+  else
+    for (int i = 0; i < W; ++i) to[i] = v[i];
+}
+template <int W, bool GLOBAL> __device__ __forceinline__ void get(float (&v)[W], const float* from) {
+  if constexpr (W % 4 == 0)
+    for (int i = 0; i < W; i += 4) {
+      const float4 x = GLOBAL ? __ldcg(reinterpret_cast<const float4*>(from + i)) : *reinterpret_cast<const float4*>(from + i);
+      v[i] = x.x; v[i + 1] = x.y; v[i + 2] = x.z; v[i + 3] = x.w;
+    }
+  else
+    for (int i = 0; i < W; ++i) v[i] = GLOBAL ? __ldcg(from + i) : from[i];
+}
+
 // ---- lookup ------------------------------------------------------------------------------------
 // A gather: bound by memory.  A thread moves U packs of W elements, 256 apart, so that U loads are in flight; T * D / W packs
 // are numbered row by row.
@@ -82,12 +101,15 @@ __global__ void __launch_bounds__(256) k_embed(const TIn* __restrict__ table, lo
 // bin begins.  The hits counted per (row, warp), a prefix sum over the counts gives every row's and warp's first
 // position, and a second run over the lists (over the ids, where a list was too short) places the tokens: equal ids
 // stay in the order of their positions because a warp's part precedes the next warp's.
-// Every CTA reads all ids, from L2 after the first: 256 CTAs and 65536 tokens of 4 bytes make 67 MB.
+// Every CTA reads all ids, from L2 after the first: 128 CTAs and 65536 tokens of 4 bytes make 34 MB.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kMaxBinRows = 768;
 constexpr int kBinPitch = kSortWarps + 1;              // counters of a warp's lanes fall into different banks
-constexpr int kListLength = 256;                       // hits that a warp keeps, at most 128 of them new per step
+constexpr int kListLength = 512;                       // hits that a warp keeps, at most 128 of them new per step
+constexpr int kRowBits = 10;                           // of a list entry; the others hold the position in the warp's part
+constexpr long long kMostTokens = 1ll << (32 - kRowBits + 5);
+static_assert(kMaxBinRows <= 1 << kRowBits, "a bin's rows do not fit a list entry");
 
 struct GradArgs {
   const void* ids;
@@ -118,7 +140,7 @@ __device__ __forceinline__ int order_of(const GradArgs& a, int row) {
 }
 
 struct SortShared {
-  int2 list[kSortWarps][kListLength];                  // (token position, row of the bin)
+  unsigned list[kSortWarps][kListLength];              // position in the warp's part << kRowBits | row of the bin
   int scratch[kSortWarps];
   int again;                                           // a list was too short
   int cnt[];                                           // [bin_rows][kBinPitch]
@@ -141,12 +163,13 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
   if (tid == 0) sh.again = 0;
   __syncthreads();
 
-  // f on hits [0, n) of the warp's list, 32 at a time: the hit (row -1: none) and the lanes with the same row
+  // f on hits [0, n) of the warp's list, 32 at a time: token position, row (-1: none), the lanes with the same row
   const auto each = [&](int n, auto&& f) {
     __syncwarp();
     for (int i = 0; i < n; i += 32) {
-      const int2 e = i + lane < n ? sh.list[warp][i + lane] : make_int2(0, -1);
-      f(e, __match_any_sync(~0u, e.y));
+      const unsigned e = sh.list[warp][min(i + lane, n - 1)];
+      const int row = i + lane < n ? (int)(e & ((1u << kRowBits) - 1)) : -1;
+      f((int)(t0 + (e >> kRowBits)), row, __match_any_sync(~0u, row));
       __syncwarp();
     }
   };
@@ -165,10 +188,12 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
       }
       unsigned mine = 0;
       for (int i = 0; i < 4; ++i) {
-        if (v[i] >= a.V) { record(a.status, COCODC_ERR_INVALID_ARG); v[i] = -1; }
-        const int b = (int)v[i] & mask;
-        below += v[i] >= 0 && b < bin;
-        mine |= (unsigned)(v[i] >= 0 && b == bin) << i;
+        using U = typename std::make_unsigned<I>::type;
+        const bool there = (U)v[i] < (U)a.V;           // false for negative ids too
+        if (!there && v[i] >= 0) record(a.status, COCODC_ERR_INVALID_ARG);
+        const int b = there ? (int)v[i] & mask : mask + 1;
+        below += b < bin;
+        mine |= (unsigned)(b == bin) << i;
       }
       if (!__any_sync(~0u, mine)) continue;
       int before = 0, all = 0;
@@ -178,7 +203,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
         all += __popc(m);
       }
       for (int i = 0; i < 4; ++i)
-        if (mine >> i & 1) sh.list[warp][hits + before++] = make_int2((int)(first + i), (int)(v[i] >> a.bins_log2));
+        if (mine >> i & 1) sh.list[warp][hits + before++] = (unsigned)(first + i - t0) << kRowBits | (unsigned)(v[i] >> a.bins_log2);
       hits += all;
       if (hits > kListLength - 128) {
         each(hits, f);
@@ -187,8 +212,8 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
       }
     }
   };
-  const auto count = [&](int2 e, unsigned same) {
-    if (e.y >= 0 && lane == __ffs(same) - 1) sh.cnt[e.y * kBinPitch + warp] += __popc(same);
+  const auto count = [&](int, int row, unsigned same) {
+    if (row >= 0 && lane == __ffs(same) - 1) sh.cnt[row * kBinPitch + warp] += __popc(same);
   };
   walk(count);
   each(hits, count);
@@ -225,20 +250,21 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
   }
   __syncthreads();
 
-  const auto place = [&](int2 e, unsigned same) {
+  const auto place = [&](int t, int row, unsigned same) {
     const int leader = __ffs(same) - 1;
     int base = 0;
-    if (e.y >= 0 && lane == leader) {
-      base = sh.cnt[e.y * kBinPitch + warp];
-      sh.cnt[e.y * kBinPitch + warp] = base + __popc(same);
+    if (row >= 0 && lane == leader) {
+      base = sh.cnt[row * kBinPitch + warp];
+      sh.cnt[row * kBinPitch + warp] = base + __popc(same);
     }
     base = __shfl_sync(~0u, base, leader);
-    if (e.y >= 0) a.sorted[base + __popc(same & ((1u << lane) - 1))] = make_int2(e.x, (e.y << a.bins_log2) + bin);
+    if (row >= 0) a.sorted[base + __popc(same & ((1u << lane) - 1))] = make_int2(t, (row << a.bins_log2) + bin);
   };
   if (sh.again) walk(place);
   each(hits, place);
 
-  // rows that no token names: zeros
+  // Rows that no token names: zeros.  (Written by CTAs of the next launch, beside the sums, they took 4 us longer at
+  // 50257 x 768 and 2 us longer at 32000 x 1024.)
   if (!a.accumulate) {
     const long long bytes = a.D * a.dtable_esize, n16 = a.dtable_wide ? bytes / 16 : 0;
     for (int r = warp; r < a.bin_rows; r += kSortWarps) {
@@ -261,11 +287,13 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
 // boundaries are joined in shared memory in order; those that cross tile boundaries leave their parts in the
 // workspace, and the tile that arrives last at the row's counter adds all parts in tile order (nobody waits).
 constexpr int kGroups = 4;
+constexpr int kAhead = 4;      // loads in flight per thread
 
 template <typename TIn, typename TOut, int W>
-__global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
-  extern __shared__ float part[];                       // [kGroups][2][threads of a group][W]: head, tail
-  __shared__ int pending_row[2], is_last[2];
+__global__ void __launch_bounds__(kGroups * 128, 2) k_embed_sum(const GradArgs a) {
+  extern __shared__ __align__(16) float part[];                       // [kGroups][2][threads of a group][W]: head, tail
+  __shared__ int pending_row[2], is_last[2], pending_first[2], pending_parts[2];
+  __shared__ int edge[2 * kGroups + 2];                 // rows of: the entry before the tile, each group's first and last, the entry after
   const int width = blockDim.x / kGroups, group = threadIdx.x / width, c = threadIdx.x % width;
   const long long col = ((long long)blockIdx.y * width + c) * W;
   const bool active = col < a.D;
@@ -289,42 +317,61 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
     }
     o.store(p);
   };
-  const auto row_at = [&](int p) { return a.sorted[p].y; };
-  // entries p - 1 and p belong to one row
-  const auto joined = [&](int p) { return p > 0 && p < n && row_at(p - 1) == row_at(p); };
   float* head = part + ((group * 2) * width + c) * W;
   float* tail = part + ((group * 2 + 1) * width + c) * W;
 
   const int p0 = min(n, begin + group * a.positions), p1 = min(n, p0 + a.positions);
   if (p0 < p1) {
-    bool open = joined(p0);                              // the current sum continues a row of the group before
-    const bool goes_on = joined(p1);
-    int row = row_at(p0);
+    // lane i holds entry i of the group: its row, where its gradient starts, and whether a row begins there
+    const int lane = threadIdx.x & 31, entries = p1 - p0;
+    const int2 mine = lane < entries ? a.sorted[p0 + lane] : make_int2(0, -1);
+    const int left = p0 > 0 ? a.sorted[p0 - 1].y : -1, right = p1 < n ? a.sorted[p1].y : -1;
+    const long long offset = mine.x * a.dy_stride;
+    const int before = __shfl_up_sync(~0u, mine.y, 1);
+    const unsigned starts = __ballot_sync(~0u, lane > 0 && mine.y != before);
+    const int row_in = __shfl_sync(~0u, mine.y, 0), row_out = __shfl_sync(~0u, mine.y, entries - 1);
+    bool open = left == row_in;                          // the current sum continues a row of the group before
+    const bool goes_on = right == row_out;
+    if (c == 0) {
+      edge[1 + 2 * group] = row_in;
+      edge[2 + 2 * group] = row_out;
+      if (group == 0) edge[0] = left;
+      if (p1 == min(n, begin + span)) {
+        edge[1 + 2 * kGroups] = right;
+        for (int g = group + 1; g < kGroups; ++g) edge[1 + 2 * g] = edge[2 + 2 * g] = -1;   // groups without entries
+      }
+      // the rows that cross the tile's ends: where they begin and how many tiles share them
+      for (int s = 0; s < 2; ++s) {
+        const int row = s == 0 ? (group == 0 && open ? row_in : -1) : (p1 == min(n, begin + span) && goes_on ? row_out : -1);
+        if (row < 0) continue;
+        const int g = order_of(a, row);
+        pending_first[s] = a.row_start[g] / span;
+        pending_parts[s] = (a.row_start[g + 1] - 1) / span - pending_first[s] + 1;
+      }
+    }
     clear();
-    for (int p = p0; p < p1; p += 8) {
-      Raw<TIn, W> x[8];
-      int2 e[8];
+    for (int p = 0; p < entries; p += kAhead) {
+      Raw<TIn, W> x[kAhead];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = p + i < p1 ? a.sorted[p + i] : make_int2(-1, row);
+      for (int i = 0; i < kAhead; ++i) {
+        const long long at = __shfl_sync(~0u, offset, (p + i) & 31);
+        if (p + i < entries) x[i].load(dy + at);
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (e[i].x >= 0) x[i].load(dy + (long long)e[i].x * a.dy_stride);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (e[i].x < 0) continue;
-        if (e[i].y != row) {
-          if (open) for (int k = 0; k < W; ++k) head[k] = acc[k];
-          else write_row(row);
+      for (int i = 0; i < kAhead; ++i) {
+        if (p + i >= entries) break;
+        if (starts >> (p + i) & 1) {
+          if (open) put<W>(head, acc);
+          else write_row(__shfl_sync(~0u, mine.y, p + i - 1));
           open = false;
-          row = e[i].y;
           clear();
         }
         for (int k = 0; k < W; ++k) acc[k] += x[i].at(k);
       }
     }
     float* to = open ? head : goes_on ? tail : nullptr;
-    if (to) for (int k = 0; k < W; ++k) to[k] = acc[k];
-    else write_row(row);
+    if (to) put<W>(to, acc);
+    else write_row(row_out);
   }
   if (threadIdx.x < 2) pending_row[threadIdx.x] = -1;
   __syncthreads();
@@ -334,21 +381,18 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
     bool running = false, outside = false;               // a sum is open; it began in an earlier tile
     int row = -1;
     const auto leave = [&](int slot) {                   // slot 0: begun in an earlier tile, 1: begun here
-      if (active) {
-        float* w = a.partial + ((long long)tile * 2 + slot) * a.pitch + col;
-        for (int k = 0; k < W; ++k) w[k] = acc[k];
-      }
+      if (active) put<W>(a.partial + ((long long)tile * 2 + slot) * a.pitch + col, acc);
       if (c == 0) pending_row[slot] = row;
       __threadfence();
     };
-    for (int g = 0; g < kGroups; ++g) {
-      const int q0 = begin + g * a.positions, q1 = min(n, q0 + a.positions);
-      if (q0 >= n) break;
-      const bool left = joined(q0), right = joined(q1);
-      const bool through = left && right && row_at(q0) == row_at(q1 - 1);
+    for (int g = 0; g < kGroups && edge[1 + 2 * g] >= 0; ++g) {
+      const int row_in = edge[1 + 2 * g], row_out = edge[2 + 2 * g];
+      const int follower = g + 1 < kGroups && edge[3 + 2 * g] >= 0 ? edge[3 + 2 * g] : edge[1 + 2 * kGroups];
+      const bool left = edge[2 * g] == row_in, right = follower == row_out, through = left && right && row_in == row_out;
       if (left) {
-        if (!running) { clear(); running = true; outside = true; row = row_at(q0); }
-        const float* h = part + ((g * 2) * width + c) * W;
+        if (!running) { clear(); running = true; outside = true; row = row_in; }
+        float h[W];
+        get<W, false>(h, part + ((g * 2) * width + c) * W);
         for (int k = 0; k < W; ++k) acc[k] += h[k];
         if (!through) {
           if (outside) leave(0);
@@ -357,11 +401,10 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
         }
       }
       if (right && !running) {
-        const float* h = part + ((g * 2 + 1) * width + c) * W;
-        for (int k = 0; k < W; ++k) acc[k] = h[k];
+        get<W, false>(acc, part + ((g * 2 + 1) * width + c) * W);
         running = true;
         outside = false;
-        row = row_at(q1 - 1);
+        row = row_out;
       }
     }
     if (running) leave(outside ? 0 : 1);
@@ -373,9 +416,9 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
     const int row = pending_row[threadIdx.x];
     int last = 0;
     if (row >= 0) {
-      const int g = order_of(a, row), first = a.row_start[g] / span, end = (a.row_start[g + 1] - 1) / span;
       __threadfence();
-      last = atomicAdd(&a.arrived[(long long)first * gridDim.y + blockIdx.y], 1) == end - first;
+      last = atomicAdd(&a.arrived[(long long)pending_first[threadIdx.x] * gridDim.y + blockIdx.y], 1) ==
+             pending_parts[threadIdx.x] - 1;
       __threadfence();
     }
     is_last[threadIdx.x] = last;
@@ -383,33 +426,32 @@ __global__ void __launch_bounds__(kGroups * 128) k_embed_sum(const GradArgs a) {
   __syncthreads();
   for (int s = 0; s < 2; ++s) {
     if (!is_last[s]) continue;
-    const int row = pending_row[s], g = order_of(a, row);
-    const int first = a.row_start[g] / span, parts = (a.row_start[g + 1] - 1) / span - first + 1;
+    const int row = pending_row[s], first = pending_first[s], parts = pending_parts[s];
     clear();
     const int j1 = (int)((long long)parts * (group + 1) / kGroups);
     if (active)
       for (int j = (int)((long long)parts * group / kGroups); j < j1; j += 4) {
         float x[4][W];
         for (int i = 0; i < 4; ++i)
-          if (j + i < j1) {
-            const float* w = a.partial + ((long long)(first + j + i) * 2 + (j + i == 0 ? 1 : 0)) * a.pitch + col;
-            for (int k = 0; k < W; ++k) x[i][k] = __ldcg(w + k);
-          }
+          if (j + i < j1) get<W, true>(x[i], a.partial + ((long long)(first + j + i) * 2 + (j + i == 0 ? 1 : 0)) * a.pitch + col);
         for (int i = 0; i < 4; ++i)
           if (j + i < j1) for (int k = 0; k < W; ++k) acc[k] += x[i][k];
       }
-    for (int k = 0; k < W; ++k) head[k] = acc[k];
+    put<W>(head, acc);
     __syncthreads();
     if (group == 0) {
-      for (int g = 1; g < kGroups; ++g)
-        for (int k = 0; k < W; ++k) acc[k] += part[((g * 2) * width + c) * W + k];
+      for (int g = 1; g < kGroups; ++g) {
+        float h[W];
+        get<W, false>(h, part + ((g * 2) * width + c) * W);
+        for (int k = 0; k < W; ++k) acc[k] += h[k];
+      }
       write_row(row);
     }
     __syncthreads();
   }
 }
 
-// Sorted entries per group: 32 amortise the boundaries; with few tokens fewer, so that there are tiles for all SMs.
+// Sorted entries per group (a lane each): 32 amortise the boundaries; with few tokens fewer, so that there are tiles for all SMs.
 int positions_for(int64_t T) {
   int p = 32;
   while (p > 4 && T < (int64_t)148 * 2 * kGroups * p) p /= 2;
@@ -417,10 +459,11 @@ int positions_for(int64_t T) {
 }
 
 uint64_t up16(uint64_t n) { return (n + 15) / 16 * 16; }
-// 256 bins (all resident at two CTAs per SM), fewer for a smaller table, more where a bin's rows would not fit shared memory
+// 128 bins (one CTA per SM: every CTA reads all ids, so twice as many took 7 us longer at 65536 tokens), fewer for a smaller
+// table, more where a bin's rows would not fit shared memory
 int bins_log2_for(int64_t V) {
   int l = 0;
-  while (l < 8 && (int64_t(1) << l) < V) ++l;
+  while (l < 7 && (int64_t(1) << l) < V) ++l;
   while ((V + (int64_t(1) << l) - 1) >> l > kMaxBinRows) ++l;
   return l;
 }
@@ -490,7 +533,7 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
                                    int32_t ids_type, int64_t T, int64_t V, int64_t D, float scale, int32_t accumulate,
                                    void* dtable, int32_t dtable_type, int64_t dtable_stride, void* workspace,
                                    uint64_t workspace_bytes, void* stream) {
-  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || T > INT32_MAX || V > (int64_t(1) << 30) || !dtable ||
+  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || T > kMostTokens || V > (int64_t(1) << 30) || !dtable ||
       !known_type(dy_type) || !known_type(dtable_type) || (ids_type != COCODC_I32 && ids_type != COCODC_I64) ||
       dy_stride < D || dtable_stride < D || !sane(dy_stride) || !sane(dtable_stride))
     return COCODC_ERR_INVALID_ARG;
