@@ -2,6 +2,8 @@
 
 #include "lm_common.cuh"
 
+#include <type_traits>
+
 using namespace cocodc_lm_impl;
 
 namespace {
@@ -18,6 +20,7 @@ __device__ __forceinline__ unsigned ordered(float x) {
   const unsigned b = __float_as_uint(x + 0.f);
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
+__device__ __forceinline__ float value_of(unsigned o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
 __device__ __forceinline__ unsigned long long key_of(float x, unsigned j) {
   return ((unsigned long long)ordered(x) << 32) | (0xfffffffeu - j);
 }
@@ -43,6 +46,30 @@ struct RowArgs {
   int* status;
 };
 
+// ---- pairs of fp32 numbers: one instruction for two ----------------------------------------------
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
+  f32x2 v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ void split(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 v;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+
 // ---- sixteen bytes of a row ---------------------------------------------------------------------
 // Logits below -kFar take part in the sums as -kFar (-Inf would turn 0 * d into NaN in the entropy's sum).  That is exact
 // where their exponentials are 0 either way: where the largest logit is above -kFar / 2 and c kFar / 2 is above 200;
@@ -58,6 +85,7 @@ template <> struct Words<float> {
   }
   static __device__ __forceinline__ uint4 far() { const unsigned v = __float_as_uint(-kFar); return make_uint4(v, v, v, v); }
   __device__ __forceinline__ float at(int i) const { return e[i]; }
+  __device__ __forceinline__ f32x2 two(int i) const { return pair_of(e[2 * i], e[2 * i + 1]); }
   __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])); }
 };
 template <> struct Words<__nv_bfloat16> {
@@ -75,6 +103,10 @@ template <> struct Words<__nv_bfloat16> {
     return make_uint4(v, v, v, v);
   }
   __device__ __forceinline__ float at(int i) const { return i & 1 ? __high2float(e[i / 2]) : __low2float(e[i / 2]); }
+  __device__ __forceinline__ f32x2 two(int i) const {   // a bfloat16 is the upper half of the same fp32 number
+    const unsigned u = *reinterpret_cast<const unsigned*>(&e[i]);
+    return pair_of(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  }
   __device__ __forceinline__ float largest() const {
     const __nv_bfloat162 m = __hmax2(__hmax2(e[0], e[1]), __hmax2(e[2], e[3]));
     return fmaxf(__low2float(m), __high2float(m));
@@ -95,6 +127,10 @@ template <> struct Words<__half> {
     return make_uint4(v, v, v, v);
   }
   __device__ __forceinline__ float at(int i) const { return i & 1 ? __high2float(e[i / 2]) : __low2float(e[i / 2]); }
+  __device__ __forceinline__ f32x2 two(int i) const {
+    const float2 f = __half22float2(e[i]);
+    return pair_of(f.x, f.y);
+  }
   __device__ __forceinline__ float largest() const {
     const __half2 m = __hmax2(__hmax2(e[0], e[1]), __hmax2(e[2], e[3]));
     return fmaxf(__low2float(m), __high2float(m));
@@ -109,18 +145,29 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
   const float m = fmaxf(a.m, b.m);
   // the offsets are bounded so that 0 * offset stays 0; a part without sum keeps its zeros
   const float da = fmaxf((a.m == m ? 0.f : (a.m - m) * c), -1e4f), db = fmaxf((b.m == m ? 0.f : (b.m - m) * c), -1e4f);
-  const float fa = exp2f(da), fb = exp2f(db);
+  const float fa = fast_exp2(da), fb = fast_exp2(db);
   return Stats{m, a.s * fa + b.s * fb, (a.u + da * a.s) * fa + (b.u + db * b.s) * fb};
 }
+// All lanes' parts at once: scaled to the warp's largest logit, then summed; lanes without a part hold m = -Inf, s = u = 0.
+__device__ __forceinline__ Stats warp_join(Stats x, float c) {
+  const unsigned top = __reduce_max_sync(~0u, ordered(x.m));
+  const float m = value_of(top);
+  const float d = fmaxf(x.m == m ? 0.f : (x.m - m) * c, -1e4f), f = fast_exp2(d);
+  x.u = (x.u + d * x.s) * f;
+  x.s *= f;
+  for (int o = 16; o; o >>= 1) {
+    x.s += __shfl_xor_sync(~0u, x.s, o);
+    x.u += __shfl_xor_sync(~0u, x.u, o);
+  }
+  return Stats{m, x.s, x.u};
+}
 __device__ __forceinline__ Stats block_join(Stats x, float c, Stats* scratch) {
-  for (int o = 16; o; o >>= 1)
-    x = join(x, Stats{__shfl_xor_sync(~0u, x.m, o), __shfl_xor_sync(~0u, x.s, o), __shfl_xor_sync(~0u, x.u, o)}, c);
+  x = warp_join(x, c);
   __syncthreads();
   if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
   __syncthreads();
-  x = scratch[0];
-  for (int w = 1; w < kWarps; ++w) x = join(x, scratch[w], c);
-  return x;
+  const int lane = threadIdx.x & 31;
+  return warp_join(lane < kWarps ? scratch[lane] : Stats{-INFINITY, 0.f, 0.f}, c);
 }
 
 // The careful way: any values, any number of them, element by element.  [j0, j1) of the row.
@@ -170,7 +217,27 @@ __device__ __noinline__ void careful_top(const T* row, unsigned j0, unsigned j1,
 }
 
 // One warp: the k largest of keys[0 .. n), descending, to list[0 .. k) (0 where there are no more).
+template <int PER> __device__ __forceinline__ void warp_top_held(const unsigned long long* keys, int n, int k, unsigned long long* list) {
+  const int lane = threadIdx.x & 31;
+  unsigned long long held[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) held[j] = lane + 32 * j < n ? keys[lane + 32 * j] : 0;
+  __syncwarp();
+  for (int i = 0; i < k; ++i) {
+    unsigned long long best = held[0];
+#pragma unroll
+    for (int j = 1; j < PER; ++j) best = held[j] > best ? held[j] : best;
+    best = warp_max(best);
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (held[j] == best) held[j] = 0;
+    if (lane == 0) list[i] = best;
+  }
+  __syncwarp();
+}
 __device__ __forceinline__ void warp_top(const unsigned long long* keys, int n, int k, unsigned long long* list) {
+  if (n <= 64) return warp_top_held<2>(keys, n, k, list);
+  if (n <= 256) return warp_top_held<8>(keys, n, k, list);
   const int lane = threadIdx.x & 31;
   unsigned long long last = ~0ull;
   for (int i = 0; i < k; ++i) {
@@ -224,46 +291,69 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
   const unsigned base = lead + w0 * W::n, tail = lead + w1 * W::n;
   const uint4* src = reinterpret_cast<const uint4*>(row + base);
 
+  // the target's logit is on its way before the walk
+  long long y = -1;
+  float target = 0.f;
+  if (a.logp && part == 0 && tid == 0) {
+    y = token_at(a.targets, a.targets64, t, a.V, a.status);
+    if (y >= 0) target = to_f32(row[y]);
+  }
   Stats x{-W::kFar, 0.f, 0.f};
-  float mc = x.m * c;
-  unsigned at = 0;                                  // TOP: batch (from 2 on) or end (0, 1) that holds the thread's largest logit
+  f32x2 s2 = 0, u2 = 0, mc2 = pair_of(-x.m * c, -x.m * c);   // sums of the even and the odd elements; -c m twice
+  const f32x2 c2 = pair_of(c, c);
+  unsigned at = 0;                                  // TOP: where the thread's largest logit came: 2 + first word of the batch, or an end (0, 1)
   const auto raise = [&](float m) {
     const float d = fmaxf((x.m - m) * c, -1e4f), f = exp2f(d);
-    x.u = (x.u + d * x.s) * f;
-    x.s *= f;
+    u2 = mul2(fma2(pair_of(d, d), s2, u2), pair_of(f, f));
+    s2 = mul2(s2, pair_of(f, f));
     x.m = m;
-    mc = m * c;
+    mc2 = pair_of(-m * c, -m * c);
   };
-  const auto add = [&](float v) {
-    const float d = fmaf(v, c, -mc), e = fast_exp2(d);
-    x.s += e;
-    x.u = fmaf(e, d, x.u);
+  const auto add = [&](f32x2 v) {
+    const f32x2 d = fma2(v, c2, mc2);
+    float lo, hi;
+    split(d, lo, hi);
+    const f32x2 e = pair_of(fast_exp2(lo), fast_exp2(hi));
+    s2 = add2(s2, e);
+    u2 = fma2(e, d, u2);
   };
   const auto single = [&](unsigned j, unsigned where) {
     float v;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(to_f32(row[j])), "f"(-W::kFar));
     if (v > x.m) { raise(v); at = where; }
-    add(v);
+    const float d = fmaf(v, c, -x.m * c), e = fast_exp2(d);
+    s2 = add2(s2, pair_of(e, 0.f));
+    u2 = add2(u2, pair_of(e * d, 0.f));
   };
   if (j0 + tid < base) single(j0 + tid, 0);
-  unsigned batch = 2;
-  for (unsigned i = tid; i < n; i += kThreads * kUnroll, ++batch) {
-    W w[kUnroll];
-    uint4 raw[kUnroll];
+  const auto words_at = [&](unsigned i, auto count) {
+    constexpr int N = decltype(count)::value;
+    uint4 raw[N];
+    W w[N];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) raw[k] = i + k * kThreads < n ? __ldg(src + i + k * kThreads) : W::far();
+    for (int k = 0; k < N; ++k) raw[k] = __ldg(src + i + k * kThreads);
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) w[k].set(raw[k]);
+    for (int k = 0; k < N; ++k) w[k].set(raw[k]);
     float m = w[0].largest();
 #pragma unroll
-    for (int k = 1; k < kUnroll; ++k) m = fmaxf(m, w[k].largest());
-    if (m > x.m) { raise(m); at = batch; }
+    for (int k = 1; k < N; ++k) m = fmaxf(m, w[k].largest());
+    if (m > x.m) { raise(m); at = 2 + i; }
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
+    for (int k = 0; k < N; ++k)
 #pragma unroll
-      for (int q = 0; q < W::n; ++q) add(w[k].at(q));
-  }
+      for (int q = 0; q < W::n / 2; ++q) add(w[k].two(q));
+  };
+  unsigned i = tid;
+  for (; i + (kUnroll - 1) * kThreads < n; i += kThreads * kUnroll) words_at(i, std::integral_constant<int, kUnroll>());
+  for (; i < n; i += kThreads) words_at(i, std::integral_constant<int, 1>());
   if (tail + tid < j1) single(tail + tid, 1);
+  {
+    float lo, hi;
+    split(s2, lo, hi);
+    x.s = lo + hi;
+    split(u2, lo, hi);
+    x.u = lo + hi;
+  }
   const Stats mine = x;
   x = block_join(x, c, sh.scratch);
   // a NaN or +Inf, nothing but very low logits, a very small scale: once more, with care (also the alternatives)
@@ -282,7 +372,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
         if (at < 2) {
           j = at ? tail + tid : j0 + tid;
         } else {
-          const unsigned i = tid + (at - 2) * kThreads * kUnroll;
+          const unsigned i = at - 2;
           bool found = false;
 #pragma unroll
           for (int k = 0; k < kUnroll; ++k)
@@ -390,15 +480,11 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
   if (lane == 0) {
     if (a.lse) a.lse[t] = none ? -INFINITY : fabsf(mc0) < INFINITY ? kLn2 * (mc0 + log2s) : m0 * a.scale + kLn2 * log2s;
     if (a.entropy) a.entropy[t] = none ? 0.f : kLn2 * (log2s - x.u / x.s);
-    if (a.logp) {
-      const long long y = token_at(a.targets, a.targets64, t, a.V, a.status);
-      a.logp[t] = y < 0 ? 0.f : logp_of(to_f32(row[y]));
-    }
+    if (a.logp) a.logp[t] = y < 0 ? 0.f : logp_of(target);
   }
   if (TOP && lane < a.top_k) {
-    const unsigned j = position_of(top[lane]);
-    a.top_ids[t * a.top_k + lane] = (int)j;
-    a.top_logp[t * a.top_k + lane] = logp_of(to_f32(row[j]));
+    a.top_ids[t * a.top_k + lane] = (int)position_of(top[lane]);
+    a.top_logp[t * a.top_k + lane] = logp_of(value_of((unsigned)(top[lane] >> 32)));
   }
 }
 
