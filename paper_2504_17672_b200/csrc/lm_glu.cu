@@ -106,6 +106,116 @@ __global__ void __launch_bounds__(256) k_product_plain(const PlainArgs<T> p) {
     }
 }
 
+// ---- few tokens -----------------------------------------------------------------------------------
+// Bound by reading the weights once.  A CTA takes 16 rows of Wg and of Wu; its warps share the contraction in blocks of 32
+// k and every lane loads 16 consecutive bytes of a row, straight into the fragments of mma.sync: the k's of a lane's
+// fragment places are permuted, the same way for weights and tokens, which a contraction does not notice.  The warps' sums meet
+// in shared memory in fixed order.  TILES: groups of eight tokens.
+constexpr int kFewWarps = 8;
+constexpr int kFewTokens = 16;
+
+template <typename E> __device__ __forceinline__ void mma16816(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3,
+                                                               unsigned b0, unsigned b1);
+template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], unsigned a0, unsigned a1, unsigned a2,
+                                                                    unsigned a3, unsigned b0, unsigned b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3,
+                                                             unsigned b0, unsigned b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <typename E> struct FewArgs {
+  const E *x, *wg, *wu;
+  long long x_stride, w_stride;
+  int T, D, F;
+  E *h, *gate, *up;
+  long long h_stride, gu_stride;
+};
+
+// 8 elements of a row from k on; zeros from D on
+template <typename E> __device__ __forceinline__ uint4 load_end(const E* row, int k, int D) {
+  alignas(16) E v[8];
+  for (int i = 0; i < 8; ++i) v[i] = k + i < D ? row[k + i] : from_f32<E>(0.f);
+  return *reinterpret_cast<const uint4*>(v);
+}
+
+template <typename E, int ACT, int TILES>
+__global__ void __launch_bounds__(kFewWarps * 32) k_glu_few(const FewArgs<E> p) {
+  constexpr int kBlocks = 4;                                      // k blocks in flight per warp
+  constexpr int kSums = 16 * 8 * TILES;                           // of one matrix
+  extern __shared__ float sums[];                                 // [warp][gate, up][token][row]
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, q = lane % 4;
+  const int f0 = blockIdx.x * 16;
+  // rows and tokens outside are taken from the last one inside; what they give is not written
+  const long long r0 = min(f0 + r, p.F - 1) * p.w_stride + q * 8, r1 = min(f0 + r + 8, p.F - 1) * p.w_stride + q * 8;
+  const E* rows[4] = {p.wg + r0, p.wg + r1, p.wu + r0, p.wu + r1};
+  const E* tokens[TILES];
+#pragma unroll
+  for (int n = 0; n < TILES; ++n) tokens[n] = p.x + min(n * 8 + r, p.T - 1) * p.x_stride + q * 8;
+  float g[TILES][4] = {}, u[TILES][4] = {};
+  const auto multiply = [&](const uint4 (&w)[4], const uint4& x, int n) {
+    mma16816<E>(g[n], w[0].x, w[1].x, w[0].y, w[1].y, x.x, x.y);
+    mma16816<E>(u[n], w[2].x, w[3].x, w[2].y, w[3].y, x.x, x.y);
+    mma16816<E>(g[n], w[0].z, w[1].z, w[0].w, w[1].w, x.z, x.w);
+    mma16816<E>(u[n], w[2].z, w[3].z, w[2].w, w[3].w, x.z, x.w);
+  };
+  const auto blocks_at = [&](int b, auto count) {
+    constexpr int N = decltype(count)::value;
+    uint4 w[N][4], x[N][TILES];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) w[i][m] = __ldg(reinterpret_cast<const uint4*>(rows[m] + (b + i * kFewWarps) * 32));
+#pragma unroll
+      for (int n = 0; n < TILES; ++n) x[i][n] = __ldg(reinterpret_cast<const uint4*>(tokens[n] + (b + i * kFewWarps) * 32));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int n = 0; n < TILES; ++n) multiply(w[i], x[i][n], n);
+  };
+  const int whole = p.D / 32;
+  int b = warp;
+  for (; b + (kBlocks - 1) * kFewWarps < whole; b += kFewWarps * kBlocks) blocks_at(b, std::integral_constant<int, kBlocks>());
+  for (; b < whole; b += kFewWarps) blocks_at(b, std::integral_constant<int, 1>());
+  if (b == whole && p.D % 32) {                                   // the last, partial block
+    uint4 w[4];
+    const int k = whole * 32;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) w[m] = load_end(rows[m] + k, 0, p.D - k - q * 8);
+#pragma unroll
+    for (int n = 0; n < TILES; ++n) multiply(w, load_end(tokens[n] + k, 0, p.D - k - q * 8), n);
+  }
+  float* mine = sums + warp * 2 * kSums;
+#pragma unroll
+  for (int n = 0; n < TILES; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = (n * 8 + q * 2 + (i & 1)) * 16 + r + (i >> 1) * 8;
+      mine[at] = g[n][i];
+      mine[kSums + at] = u[n][i];
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kSums; i += kFewWarps * 32) {
+    const int t = i / 16, f = f0 + i % 16;
+    if (t >= p.T || f >= p.F) continue;
+    float gs = 0.f, us = 0.f;
+    for (int w = 0; w < kFewWarps; ++w) {
+      gs += sums[w * 2 * kSums + i];
+      us += sums[w * 2 * kSums + kSums + i];
+    }
+    p.h[t * p.h_stride + f] = from_f32<E>(act_value<ACT>(gs) * us);
+    if (p.gate) {
+      p.gate[t * p.gu_stride + f] = from_f32<E>(gs);
+      p.up[t * p.gu_stride + f] = from_f32<E>(us);
+    }
+  }
+}
+template <int TILES> constexpr unsigned kFewSmem = kFewWarps * 2 * 16 * 8 * TILES * sizeof(float);
+
 // ---- the element-wise part of the gradient ------------------------------------------------------
 // dg and du go to scratch of pitch F rounded up to 8 elements, so that its rows start on 16-byte boundaries.
 // One read of dh, gate and up, one write of dg and du: bound by memory.  WIDE: the inputs' rows start on 16-byte
@@ -179,11 +289,19 @@ template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t strid
 
 int tiles_of(int64_t n, int tile) { return (int)((n + tile - 1) / tile); }
 
-template <typename E, int MODE, int ACT> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
-  const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices;
+template <typename E, int MODE, int ACT, int BN> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
+  const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices, most = (long long)TcShape<BN>::kPerSm * lm->sm_count;
   if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;
-  k_glu_tc<E, MODE, ACT><<<(unsigned)(tiles < lm->sm_count ? tiles : lm->sm_count), kTcThreads, kTcSmem, st>>>(a);
+  k_glu_tc<E, MODE, ACT, BN><<<(unsigned)(tiles < most ? tiles : most), kTcThreads, TcShape<BN>::kSmem, st>>>(a);
   return launched(lm);
+}
+
+int a_rows_for(int64_t T) { return T >= kBM ? kBM : (int)((T + 7) / 8 * 8); }
+// Width of the tiles in columns of an output: the widest that gives every SM a tile.
+int width_for(const cocodc_lm* lm, int64_t M, int64_t N, int widest, int narrowest) {
+  int w = widest;
+  while (w > narrowest && (long long)tiles_of(M, kBM) * tiles_of(N, w) < lm->sm_count) w /= 2;
+  return w;
 }
 
 bool tiles_fit(int64_t rows, int64_t cols) { return (rows + kTile - 1) / kTile <= INT32_MAX && (cols + kTile - 1) / kTile <= 65535; }
@@ -199,17 +317,27 @@ bool glu_prepare() {
     g_encode.store(reinterpret_cast<EncodeTiled>(fn));
   }
   bool ok = true;
-  const auto allow = [&](auto kernel) {
-    ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) == cudaSuccess;
+  const auto allow = [&](auto kernel, unsigned smem) {
+    ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess;
   };
-  allow(k_glu_tc<__nv_bfloat16, GLU_FWD, COCODC_ACT_SILU>);
-  allow(k_glu_tc<__nv_bfloat16, GLU_FWD, COCODC_ACT_GELU>);
-  allow(k_glu_tc<__half, GLU_FWD, COCODC_ACT_SILU>);
-  allow(k_glu_tc<__half, GLU_FWD, COCODC_ACT_GELU>);
-  allow(k_glu_tc<__nv_bfloat16, GLU_DX, 0>);
-  allow(k_glu_tc<__half, GLU_DX, 0>);
-  allow(k_glu_tc<__nv_bfloat16, GLU_DW, 0>);
-  allow(k_glu_tc<__half, GLU_DW, 0>);
+  const auto allow_tc = [&](auto e, auto width) {
+    using E = decltype(e);
+    constexpr int BN = decltype(width)::value;
+    allow(k_glu_tc<E, GLU_FWD, COCODC_ACT_SILU, BN>, TcShape<BN>::kSmem);
+    allow(k_glu_tc<E, GLU_FWD, COCODC_ACT_GELU, BN>, TcShape<BN>::kSmem);
+    if constexpr (BN >= 64) {
+      allow(k_glu_tc<E, GLU_DX, 0, BN>, TcShape<BN>::kSmem);
+      allow(k_glu_tc<E, GLU_DW, 0, BN>, TcShape<BN>::kSmem);
+    }
+  };
+  const auto allow_type = [&](auto e) {
+    allow_tc(e, std::integral_constant<int, 256>());
+    allow_tc(e, std::integral_constant<int, 128>());
+    allow_tc(e, std::integral_constant<int, 64>());
+    allow_tc(e, std::integral_constant<int, 32>());
+  };
+  allow_type(__nv_bfloat16());
+  allow_type(__half());
   return ok;
 }
 }  // namespace cocodc_lm_impl
@@ -242,15 +370,28 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
   const bool tensor = rows_aligned(x, x_stride, 2) && rows_aligned(wg, w_stride, 2) && rows_aligned(wu, w_stride, 2) &&
                       rows_aligned(h, h_stride, 2) && (!gate || (rows_aligned(gate, gu_stride, 2) && rows_aligned(up, gu_stride, 2)));
   cocodc_status result = COCODC_OK;
+  const bool few = T <= kFewTokens && rows_aligned(x, x_stride, 2) && rows_aligned(wg, w_stride, 2) && rows_aligned(wu, w_stride, 2);
   with_glu(type, act, [&](auto e, auto a) {
     using E = decltype(e);
+    if (few) {
+      constexpr int A = decltype(a)::value;
+      const FewArgs<E> p{static_cast<const E*>(x), static_cast<const E*>(wg), static_cast<const E*>(wu), x_stride, w_stride,
+                         (int)T, (int)D, (int)F, static_cast<E*>(h), static_cast<E*>(gate), static_cast<E*>(up), h_stride, gu_stride};
+      const unsigned grid = (unsigned)((F + 15) / 16);
+      if (T <= 8) k_glu_few<E, A, 1><<<grid, kFewWarps * 32, kFewSmem<1>, st>>>(p);
+      else k_glu_few<E, A, 2><<<grid, kFewWarps * 32, kFewSmem<2>, st>>>(p);
+      result = launched(lm);
+      return;
+    }
     if (tensor) {
       TcArgs c{};
-      bool ok = map_of<E>(&c.a[0], x, x_stride, T, D, kBM) && map_of<E>(&c.b[0], wg, w_stride, F, D, kBN / 2) &&
-                map_of<E>(&c.b[1], wu, w_stride, F, D, kBN / 2) && map_of<E>(&c.c[0], h, h_stride, T, F, 32);
+      const int width = width_for(lm, T, F, 128, 16);
+      bool ok = map_of<E>(&c.a[0], x, x_stride, T, D, a_rows_for(T)) && map_of<E>(&c.b[0], wg, w_stride, F, D, width) &&
+                map_of<E>(&c.b[1], wu, w_stride, F, D, width) && map_of<E>(&c.c[0], h, h_stride, T, F, 32);
+      c.a_bytes = a_rows_for(T) * kBK * 2;
       if (gate) ok = ok && map_of<E>(&c.c[1], gate, gu_stride, T, F, 32) && map_of<E>(&c.c[2], up, gu_stride, T, F, 32);
       c.m_tiles = tiles_of(T, kBM);
-      c.n_tiles = tiles_of(F, kBN / 2);
+      c.n_tiles = tiles_of(F, width);
       c.matrices = c.sources = 1;
       c.k_blocks = tiles_of(D, kBK);
       c.M = (int)T;
@@ -259,7 +400,12 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
       c.out[0] = h; c.out[1] = gate; c.out[2] = up;
       c.ld[0] = h_stride; c.ld[1] = c.ld[2] = gu_stride;
       c.status = lm->d_status;
-      result = ok ? run_tc<E, GLU_FWD, decltype(a)::value>(lm, c, st) : COCODC_ERR_CUDA;
+      constexpr int A = decltype(a)::value;
+      result = !ok            ? COCODC_ERR_CUDA
+               : width == 128 ? run_tc<E, GLU_FWD, A, 256>(lm, c, st)
+               : width == 64  ? run_tc<E, GLU_FWD, A, 128>(lm, c, st)
+               : width == 32  ? run_tc<E, GLU_FWD, A, 64>(lm, c, st)
+                              : run_tc<E, GLU_FWD, A, 32>(lm, c, st);
       return;
     }
     PlainArgs<E> p{};
@@ -338,9 +484,17 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
     TcArgs c{};
     c.status = lm->d_status;
     c.N = (int)D;
-    c.n_tiles = tiles_of(D, kBN);
+    const auto run = [&](auto mode, int width) {
+      constexpr int MODE = decltype(mode)::value;
+      return width == 256 ? run_tc<E, MODE, 0, 256>(lm, c, st)
+             : width == 128 ? run_tc<E, MODE, 0, 128>(lm, c, st)
+                            : run_tc<E, MODE, 0, 64>(lm, c, st);
+    };
     if (dx && T > 0 && tensor_dx) {
-      const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, kBM) && map_of<E>(&c.a[1], du, pitch, T, F, kBM) &&
+      const int width = width_for(lm, T, D, 256, 64);
+      c.n_tiles = tiles_of(D, width);
+      c.a_bytes = a_rows_for(T) * kBK * 2;
+      const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, a_rows_for(T)) && map_of<E>(&c.a[1], du, pitch, T, F, a_rows_for(T)) &&
                       map_of<E>(&c.b[0], wg, w_stride, F, D, kBK) && map_of<E>(&c.b[1], wu, w_stride, F, D, kBK) &&
                       map_of<E>(&c.c[0], dx, dx_stride, T, D, 32);
       c.m_tiles = tiles_of(T, kBM);
@@ -350,7 +504,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       c.ld[0] = dx_stride;
       c.k_blocks = tiles_of(F, kBK);
       c.M = (int)T;
-      took(ok ? run_tc<E, GLU_DX, 0>(lm, c, st) : COCODC_ERR_CUDA);
+      took(ok ? run(std::integral_constant<int, GLU_DX>(), width) : COCODC_ERR_CUDA);
     } else if (dx && T > 0) {
       PlainArgs<E> p{};
       p.a[0] = {dg, pitch, 1};
@@ -365,6 +519,9 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       took(launched(lm));
     }
     if (dwg && tensor_dw && T > 0) {
+      const int width = width_for(lm, 2 * F, D, 256, 64);
+      c.n_tiles = tiles_of(D, width);
+      c.a_bytes = kABytes;
       const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, kBK) && map_of<E>(&c.a[1], du, pitch, T, F, kBK) &&
                       map_of<E>(&c.b[0], x, x_stride, T, D, kBK) && map_of<E>(&c.c[0], dwg, dw_stride, F, D, 32) &&
                       map_of<E>(&c.c[1], dwu, dw_stride, F, D, 32);
@@ -375,7 +532,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       c.ld[0] = c.ld[1] = dw_stride;
       c.k_blocks = tiles_of(T, kBK);
       c.M = (int)F;
-      took(ok ? run_tc<E, GLU_DW, 0>(lm, c, st) : COCODC_ERR_CUDA);
+      took(ok ? run(std::integral_constant<int, GLU_DW>(), width) : COCODC_ERR_CUDA);
     } else if (dwg) {
       PlainArgs<E> p{};
       p.a[0] = {dg, 1, pitch};

@@ -1,10 +1,12 @@
 // Tensor-core kernel of the gated block: its forward pass and the two products of its gradient.
 //
-// Persistent, one CTA per SM, 128 x 256 output tiles (M x N), k-blocks of 64:
+// Persistent, 128 x BN output tiles (M x N), k-blocks of 64:
 //   warp 0   producer: TMA copies of the operands' tiles into a ring of shared-memory stages
-//   warp 1   issuer: tcgen05.mma of each stage into one of two TMEM accumulators of 256 columns
+//   warp 1   issuer: tcgen05.mma of each stage into one of two TMEM accumulators of BN columns
 //   warps 2-5 epilogue: TMEM -> registers -> activation -> shared memory -> TMA store, while the other accumulator fills
-// Forward: N = 128 columns of F, the tile's B rows are the gate's 128 weight rows followed by the up projection's, so a
+// BN = 256 feeds the tensor cores best (one CTA per SM); narrower tiles are for few tokens, where there would be fewer
+// tiles than SMs and the time goes into reading the weights.
+// Forward: BN / 2 columns of F, the tile's B rows are the gate's weight rows followed by the up projection's, so a
 // thread of the epilogue finds gate and up of one element in its own TMEM lane and the product needs no exchange.
 // dx = dg Wg + du Wu: one accumulator, the k loop runs through both sources.  dw = d^T x: the tile index picks dg or du.
 // The operands of the gradient whose contraction runs along rows are taken MN-major as they lie in memory.
@@ -25,6 +27,7 @@ struct TcArgs {
   int k_blocks;              // of one source
   int sources;               // GLU_DX: 2
   int M, N;                  // rows and columns of the outputs
+  int a_bytes;               // of A's part of a stage: fewer than 128 tokens are loaded as they are
   int save;                  // GLU_FWD: also write gate and up (c[1], c[2])
   void* out[3];              // what c[] describes, for columns that a copy cannot write alone
   long long ld[3];
@@ -32,16 +35,22 @@ struct TcArgs {
 };
 
 constexpr int kTcThreads = 192;
-constexpr int kBM = 128, kBN = 256, kBK = 64;
-constexpr int kStages = 4;
-constexpr unsigned kABytes = kBM * kBK * 2, kBBytes = kBN * kBK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int kBM = 128, kBK = 64;
+constexpr unsigned kABytes = kBM * kBK * 2;
 constexpr unsigned kSlab = 64 * kBK * 2;            // an MN-major operand's 64 columns of m or n: 64 k rows of 128 bytes
 constexpr unsigned kOutBytes = 32 * 128;            // one warp's staged output: 32 rows of 64 columns
-constexpr unsigned kTcSmem = 1024 + kStages * kStageBytes + 4 * 2 * kOutBytes;
+template <int BN> struct TcShape {
+  static constexpr unsigned kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
+  // wide tiles: all shared memory in one CTA, outputs staged for TMA stores; narrow ones: two CTAs per SM, outputs from registers
+  static constexpr bool kStaged = BN >= 128;
+  static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 4 : 5;
+  static constexpr unsigned kSmem = 1024 + kStages * kStageBytes + (kStaged ? 4 * 2 * kOutBytes : 0);
+  static constexpr int kPerSm = kStaged ? 1 : 2;
+};
 constexpr int kGroupM = 16;                         // tiles of consecutive rows that go through one column in turn
 
 struct TcShared {
-  unsigned long long full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+  unsigned long long full[6], empty[6], acc_full[2], acc_empty[2], drain;
   unsigned tmem;
   int stop;
 };
@@ -79,6 +88,20 @@ __device__ __forceinline__ void send(const TcArgs& a, int what, int x, int y, un
   }
   if (lane == 0) store_commit();
 }
+// N columns (packed in pairs) of a row straight to global memory; rows start on 16-byte boundaries
+template <int N> __device__ __forceinline__ void store_row(const TcArgs& a, int what, int x, int y, const unsigned* v) {
+  unsigned short* row = static_cast<unsigned short*>(a.out[what]) + y * a.ld[what] + x;
+#pragma unroll
+  for (int q = 0; q < N / 8; ++q) {
+    if (x + q * 8 + 8 <= a.N) {
+      reinterpret_cast<uint4*>(row)[q] = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (x + q * 8 + i < a.N) row[q * 8 + i] = (unsigned short)(v[4 * q + i / 2] >> (i % 2 * 16));
+    }
+  }
+}
 // 32 columns (packed in pairs) of the thread's row into columns half*32.. of the staged tile, swizzled as the copy expects
 __device__ __forceinline__ void stage32(unsigned buf, int row, int half, const unsigned (&v)[16]) {
   for (int q = 0; q < 4; ++q)
@@ -86,10 +109,13 @@ __device__ __forceinline__ void stage32(unsigned buf, int row, int half, const u
                  "r"(v[4 * q]), "r"(v[4 * q + 1]), "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
 }
 
-template <typename E, int MODE, int ACT>
-__global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant__ TcArgs a) {
+template <typename E, int MODE, int ACT, int BN>
+__global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(const __grid_constant__ TcArgs a) {
   extern __shared__ unsigned char dyn[];
   __shared__ TcShared sh;
+  using S = TcShape<BN>;
+  constexpr int kStages = S::kStages, kColumns = MODE == GLU_FWD ? BN / 2 : BN;   // of an output
+  constexpr unsigned kStageBytes = S::kStageBytes, kBBytes = S::kBBytes;
   const unsigned base = (smem_addr(dyn) + 1023u) & ~1023u;
   const unsigned staging = base + kStages * kStageBytes;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -110,7 +136,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant_
     sh.stop = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc(smem_addr(&sh.tmem), 512);
+  if (warp == 1) tmem_alloc(smem_addr(&sh.tmem), 2 * BN);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -123,14 +149,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant_
       bool ok = true;
       for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
         const TileAt t = tile_at(a, tile);
-        const int m0 = t.m * kBM, n0 = t.n * (MODE == GLU_FWD ? kBN / 2 : kBN);
+        const int m0 = t.m * kBM, n0 = t.n * kColumns;
         for (int kb = 0; kb < blocks; ++kb, ++it) {
           const int s = (int)(it % kStages);
           ok = bar_wait(smem_addr(&sh.empty[s]), (unsigned)((it / kStages) & 1) ^ 1, stop);
           if (!ok) break;
           const unsigned full = smem_addr(&sh.full[s]), sa = base + s * kStageBytes, sb = sa + kABytes;
           const int src = kb >= a.k_blocks, k0 = (kb - src * a.k_blocks) * kBK;
-          bar_expect(full, kStageBytes);
+          bar_expect(full, a.a_bytes + kBBytes);
           if (MODE == GLU_FWD) {
             tma_load(sa, &a.a[0], k0, m0, full);
             tma_load(sb, &a.b[0], k0, n0, full);
@@ -141,7 +167,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant_
             } else {
               for (int i = 0; i < kBM / 64; ++i) tma_load(sa + i * kSlab, &a.a[t.z], m0 + i * 64, k0, full);
             }
-            for (int i = 0; i < kBN / 64; ++i)
+            for (int i = 0; i < BN / 64; ++i)
               tma_load(sb + i * kSlab, &a.b[MODE == GLU_DX ? src : 0], n0 + i * 64, k0, full);
           }
         }
@@ -153,7 +179,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant_
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      constexpr unsigned idesc = instr_desc<E>(kBM, kBN, a_mn, b_mn);
+      constexpr unsigned idesc = instr_desc<E>(kBM, BN, a_mn, b_mn);
       long long it = 0;
       int turn = 0;
       bool ok = true;
@@ -169,7 +195,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant_
           const unsigned sa = base + s * kStageBytes, sb = sa + kABytes;
           const unsigned long long da = tile_desc(sa, a_mn ? kSlab : 16), db = tile_desc(sb, b_mn ? kSlab : 16);
           for (int k = 0; k < kBK / 16; ++k)   // 16 k: 32 bytes along a K-major row, 16 rows of an MN-major tile
-            tc_mma(tmem + acc * kBN, da + (unsigned)(k * (a_mn ? 2048 : 32) >> 4), db + (unsigned)(k * (b_mn ? 2048 : 32) >> 4),
+            tc_mma(tmem + acc * BN, da + (unsigned)(k * (a_mn ? 2048 : 32) >> 4), db + (unsigned)(k * (b_mn ? 2048 : 32) >> 4),
                    idesc, kb > 0 || k > 0);
           tc_commit(smem_addr(&sh.empty[s]));
         }
@@ -187,39 +213,77 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant_
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
       const int acc = turn & 1;
       const TileAt t = tile_at(a, tile);
-      const int row0 = t.m * kBM + quarter * 32, n0 = t.n * (MODE == GLU_FWD ? kBN / 2 : kBN);
+      const int row0 = t.m * kBM + quarter * 32, n0 = t.n * kColumns;
       if (!__all_sync(~0u, bar_wait(smem_addr(&sh.acc_full[acc]), (unsigned)((turn >> 1) & 1), stop))) break;
       tc_fence_after();
-      const unsigned src = tmem + acc * kBN + ((unsigned)(quarter * 32) << 16);
-      // one staged tile of 64 columns after the other, two buffers in turn
-      const int pieces = MODE == GLU_FWD ? (a.save ? 6 : 2) : 4;
-      for (int p = 0; p < pieces; ++p) {
-        const int chunk = MODE == GLU_FWD ? (a.save ? p / 3 : p) : p, what = MODE == GLU_FWD && a.save ? p % 3 : 0;
-        const unsigned buf = out + (sent & 1) * kOutBytes;
-        const int x = n0 + chunk * 64;
-        if (x >= a.N || row0 >= a.M) continue;
-        if (lane == 0) store_wait_read<1>();
-        __syncwarp();
-        for (int half = 0; half < 2; ++half) {
-          float v[32];
-          unsigned packed[16];
-          const int col = chunk * 64 + half * 32;
-          if (MODE == GLU_FWD && what == 0) {
-            float u[32];
-            tmem_load32(v, src + col);
-            tmem_load32(u, src + kBN / 2 + col);
+      const unsigned src = tmem + acc * BN + ((unsigned)(quarter * 32) << 16);
+      if constexpr (S::kStaged) {
+        // one staged tile of 64 columns after the other, two buffers in turn
+        const int pieces = kColumns / 64 * (MODE == GLU_FWD && a.save ? 3 : 1);
+        for (int p = 0; p < pieces; ++p) {
+          const int chunk = MODE == GLU_FWD && a.save ? p / 3 : p, what = MODE == GLU_FWD && a.save ? p % 3 : 0;
+          const unsigned buf = out + (sent & 1) * kOutBytes;
+          const int x = n0 + chunk * 64;
+          if (x >= a.N || row0 >= a.M) continue;
+          if (lane == 0) store_wait_read<1>();
+          __syncwarp();
+          for (int half = 0; half < 2; ++half) {
+            float v[32];
+            unsigned packed[16];
+            const int col = chunk * 64 + half * 32;
+            if (MODE == GLU_FWD && what == 0) {
+              float u[32];
+              tmem_load32(v, src + col);
+              tmem_load32(u, src + BN / 2 + col);
+              tmem_wait_loads();
+              for (int i = 0; i < 16; ++i)
+                packed[i] = pack2<E>(act_value<ACT>(v[2 * i]) * u[2 * i], act_value<ACT>(v[2 * i + 1]) * u[2 * i + 1]);
+            } else {
+              tmem_load32(v, src + col + (what == 2 ? BN / 2 : 0));
+              tmem_wait_loads();
+              for (int i = 0; i < 16; ++i) packed[i] = pack2<E>(v[2 * i], v[2 * i + 1]);
+            }
+            stage32(buf, lane, half, packed);
+          }
+          send(a, MODE == GLU_DW ? t.z : what, x, row0, buf, lane);
+          ++sent;
+        }
+      } else if (row0 < a.M) {
+        const bool mine = row0 + lane < a.M;
+        if constexpr (MODE == GLU_FWD) {
+          constexpr int kPart = kColumns < 32 ? kColumns : 32;   // columns of gate and of up at a time
+          for (int col = 0; col < kColumns; col += kPart) {
+            float v[32], u[32];
+            unsigned packed[16];
+            if constexpr (kPart == 32) {
+              tmem_load32(v, src + col);
+              tmem_load32(u, src + BN / 2 + col);
+            } else {
+              tmem_load32(v, src);                                // 16 columns of gate, then 16 of up
+            }
             tmem_wait_loads();
-            for (int i = 0; i < 16; ++i)
+            if constexpr (kPart < 32)
+              for (int i = 0; i < kPart; ++i) u[i] = v[kPart + i];
+            for (int i = 0; i < kPart / 2; ++i)
               packed[i] = pack2<E>(act_value<ACT>(v[2 * i]) * u[2 * i], act_value<ACT>(v[2 * i + 1]) * u[2 * i + 1]);
-          } else {
-            tmem_load32(v, src + col + (what == 2 ? kBN / 2 : 0));
+            if (mine) store_row<kPart>(a, 0, n0 + col, row0 + lane, packed);
+            if (a.save) {
+              for (int i = 0; i < kPart / 2; ++i) packed[i] = pack2<E>(v[2 * i], v[2 * i + 1]);
+              if (mine) store_row<kPart>(a, 1, n0 + col, row0 + lane, packed);
+              for (int i = 0; i < kPart / 2; ++i) packed[i] = pack2<E>(u[2 * i], u[2 * i + 1]);
+              if (mine) store_row<kPart>(a, 2, n0 + col, row0 + lane, packed);
+            }
+          }
+        } else {
+          for (int col = 0; col < kColumns; col += 32) {
+            float v[32];
+            unsigned packed[16];
+            tmem_load32(v, src + col);
             tmem_wait_loads();
             for (int i = 0; i < 16; ++i) packed[i] = pack2<E>(v[2 * i], v[2 * i + 1]);
+            if (mine) store_row<32>(a, MODE == GLU_DW ? t.z : 0, n0 + col, row0 + lane, packed);
           }
-          stage32(buf, lane, half, packed);
         }
-        send(a, MODE == GLU_DW ? t.z : what, x, row0, buf, lane);
-        ++sent;
       }
       tc_fence_before();
       __syncwarp();
@@ -232,7 +296,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant_
   if (threadIdx.x == 0 && sh.stop) record(a.status, COCODC_ERR_TIMEOUT);
   if (warp == 1) {
     tc_fence_after();
-    tmem_free(tmem, 512);
+    tmem_free(tmem, 2 * BN);
   }
 }
 
