@@ -107,10 +107,11 @@ __global__ void __launch_bounds__(256) k_product_plain(const PlainArgs<T> p) {
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------
-// Bound by reading the weights once.  A CTA takes 16 rows of Wg and of Wu; its warps share the contraction in blocks of 32
-// k and every lane loads 16 consecutive bytes of a row, straight into the fragments of mma.sync: the k's of a lane's
-// fragment places are permuted, the same way for weights and tokens, which a contraction does not notice.  The warps' sums meet
-// in shared memory in fixed order.  TILES: groups of eight tokens.
+// Bound by reading the weights once.  A CTA takes 8 columns of the output: the 16 rows of an mma.sync tile are 8 rows of
+// Wg and the same 8 of Wu, so that a thread's accumulators hold gate and up of the same elements.  The warps share the
+// contraction in blocks of 64 k, and every lane loads 32 consecutive bytes of a row of each matrix per block, straight
+// into fragments: the k's of a lane's fragment places are permuted, the same way for weights and tokens, which a
+// contraction does not notice.  The warps' sums meet in shared memory in fixed order.  TILES: groups of eight tokens.
 constexpr int kFewWarps = 8;
 constexpr int kFewTokens = 16;
 
@@ -126,6 +127,19 @@ template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], unsi
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// weights: read once, not kept in L1
+__device__ __forceinline__ uint4 load_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+// 8 elements of a row, zeros from the n-th on
+template <typename E> __device__ __forceinline__ uint4 load_end(const E* p, int n) {
+  alignas(16) E v[8];
+  for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : from_f32<E>(0.f);
+  return *reinterpret_cast<const uint4*>(v);
+}
 
 template <typename E> struct FewArgs {
   const E *x, *wg, *wu;
@@ -135,86 +149,79 @@ template <typename E> struct FewArgs {
   long long h_stride, gu_stride;
 };
 
-// 8 elements of a row from k on; zeros from D on
-template <typename E> __device__ __forceinline__ uint4 load_end(const E* row, int k, int D) {
-  alignas(16) E v[8];
-  for (int i = 0; i < 8; ++i) v[i] = k + i < D ? row[k + i] : from_f32<E>(0.f);
-  return *reinterpret_cast<const uint4*>(v);
-}
-
 template <typename E, int ACT, int TILES>
 __global__ void __launch_bounds__(kFewWarps * 32) k_glu_few(const FewArgs<E> p) {
   constexpr int kBlocks = 4;                                      // k blocks in flight per warp
-  constexpr int kSums = 16 * 8 * TILES;                           // of one matrix
-  extern __shared__ float sums[];                                 // [warp][gate, up][token][row]
+  __shared__ float sums[kFewWarps][2][TILES * 8 * 8];             // [warp][gate, up][token, column]
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, q = lane % 4;
-  const int f0 = blockIdx.x * 16;
-  // rows and tokens outside are taken from the last one inside; what they give is not written
-  const long long r0 = min(f0 + r, p.F - 1) * p.w_stride + q * 8, r1 = min(f0 + r + 8, p.F - 1) * p.w_stride + q * 8;
-  const E* rows[4] = {p.wg + r0, p.wg + r1, p.wu + r0, p.wu + r1};
-  const E* tokens[TILES];
+  const int f0 = blockIdx.x * 8;
+  // columns and tokens outside are taken from the last one inside; what they give is not written
+  const long long row = min(f0 + r, p.F - 1) * p.w_stride + q * 16;
+  const E *wg = p.wg + row, *wu = p.wu + row, *tokens[TILES];
 #pragma unroll
-  for (int n = 0; n < TILES; ++n) tokens[n] = p.x + min(n * 8 + r, p.T - 1) * p.x_stride + q * 8;
-  float g[TILES][4] = {}, u[TILES][4] = {};
-  const auto multiply = [&](const uint4 (&w)[4], const uint4& x, int n) {
-    mma16816<E>(g[n], w[0].x, w[1].x, w[0].y, w[1].y, x.x, x.y);
-    mma16816<E>(u[n], w[2].x, w[3].x, w[2].y, w[3].y, x.x, x.y);
-    mma16816<E>(g[n], w[0].z, w[1].z, w[0].w, w[1].w, x.z, x.w);
-    mma16816<E>(u[n], w[2].z, w[3].z, w[2].w, w[3].w, x.z, x.w);
+  for (int n = 0; n < TILES; ++n) tokens[n] = p.x + min(n * 8 + r, p.T - 1) * p.x_stride + q * 16;
+  float c[TILES][4] = {};
+  const auto multiply = [&](const uint4& g, const uint4& u, const uint4& x, int n) {
+    mma16816<E>(c[n], g.x, u.x, g.y, u.y, x.x, x.y);
+    mma16816<E>(c[n], g.z, u.z, g.w, u.w, x.z, x.w);
   };
   const auto blocks_at = [&](int b, auto count) {
     constexpr int N = decltype(count)::value;
-    uint4 w[N][4], x[N][TILES];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-#pragma unroll
-      for (int m = 0; m < 4; ++m) w[i][m] = __ldg(reinterpret_cast<const uint4*>(rows[m] + (b + i * kFewWarps) * 32));
-#pragma unroll
-      for (int n = 0; n < TILES; ++n) x[i][n] = __ldg(reinterpret_cast<const uint4*>(tokens[n] + (b + i * kFewWarps) * 32));
-    }
+    uint4 g[N][2], u[N][2], x[N][TILES][2];
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (int n = 0; n < TILES; ++n) multiply(w[i], x[i][n], n);
+      for (int k = 0; k < 2; ++k) {
+        const int at = (b + i * kFewWarps) * 64 + k * 8;
+        g[i][k] = load_once(wg + at);
+        u[i][k] = load_once(wu + at);
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) x[i][n][k] = __ldg(reinterpret_cast<const uint4*>(tokens[n] + at));
+      }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) multiply(g[i][k], u[i][k], x[i][n][k], n);
   };
-  const int whole = p.D / 32;
+  const int whole = p.D / 64;
   int b = warp;
   for (; b + (kBlocks - 1) * kFewWarps < whole; b += kFewWarps * kBlocks) blocks_at(b, std::integral_constant<int, kBlocks>());
-  for (; b < whole; b += kFewWarps) blocks_at(b, std::integral_constant<int, 1>());
-  if (b == whole && p.D % 32) {                                   // the last, partial block
-    uint4 w[4];
-    const int k = whole * 32;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) w[m] = load_end(rows[m] + k, 0, p.D - k - q * 8);
-#pragma unroll
-    for (int n = 0; n < TILES; ++n) multiply(w, load_end(tokens[n] + k, 0, p.D - k - q * 8), n);
+  if (b + kFewWarps < whole) {
+    blocks_at(b, std::integral_constant<int, 2>());
+    b += 2 * kFewWarps;
   }
-  float* mine = sums + warp * 2 * kSums;
+  for (; b < whole; b += kFewWarps) blocks_at(b, std::integral_constant<int, 1>());
+  if (b == whole && p.D % 64) {                                   // the last, partial block
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int at = whole * 64 + k * 8, left = p.D - at - q * 16;
+      const uint4 g = load_end(wg + at, left), u = load_end(wu + at, left);
+#pragma unroll
+      for (int n = 0; n < TILES; ++n) multiply(g, u, load_end(tokens[n] + at, left), n);
+    }
+  }
 #pragma unroll
   for (int n = 0; n < TILES; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int at = (n * 8 + q * 2 + (i & 1)) * 16 + r + (i >> 1) * 8;
-      mine[at] = g[n][i];
-      mine[kSums + at] = u[n][i];
-    }
+    for (int i = 0; i < 4; ++i) sums[warp][i >> 1][(n * 8 + q * 2 + (i & 1)) * 8 + r] = c[n][i];
   __syncthreads();
-  for (int i = threadIdx.x; i < kSums; i += kFewWarps * 32) {
-    const int t = i / 16, f = f0 + i % 16;
-    if (t >= p.T || f >= p.F) continue;
-    float gs = 0.f, us = 0.f;
-    for (int w = 0; w < kFewWarps; ++w) {
-      gs += sums[w * 2 * kSums + i];
-      us += sums[w * 2 * kSums + kSums + i];
-    }
-    p.h[t * p.h_stride + f] = from_f32<E>(act_value<ACT>(gs) * us);
-    if (p.gate) {
-      p.gate[t * p.gu_stride + f] = from_f32<E>(gs);
-      p.up[t * p.gu_stride + f] = from_f32<E>(us);
-    }
+  if (threadIdx.x >= TILES * 64) return;
+  const int t = threadIdx.x / 8, f = f0 + threadIdx.x % 8;
+  if (t >= p.T || f >= p.F) return;
+  float gs = 0.f, us = 0.f;
+#pragma unroll
+  for (int w = 0; w < kFewWarps; ++w) {
+    gs += sums[w][0][threadIdx.x];
+    us += sums[w][1][threadIdx.x];
+  }
+  p.h[t * p.h_stride + f] = from_f32<E>(act_value<ACT>(gs) * us);
+  if (p.gate) {
+    p.gate[t * p.gu_stride + f] = from_f32<E>(gs);
+    p.up[t * p.gu_stride + f] = from_f32<E>(us);
   }
 }
-template <int TILES> constexpr unsigned kFewSmem = kFewWarps * 2 * 16 * 8 * TILES * sizeof(float);
 
 // ---- the element-wise part of the gradient ------------------------------------------------------
 // dg and du go to scratch of pitch F rounded up to 8 elements, so that its rows start on 16-byte boundaries.
@@ -297,11 +304,14 @@ template <typename E, int MODE, int ACT, int BN> cocodc_status run_tc(cocodc_lm*
 }
 
 int a_rows_for(int64_t T) { return T >= kBM ? kBM : (int)((T + 7) / 8 * 8); }
-// Width of the tiles in columns of an output: the widest that gives every SM a tile.
-int width_for(const cocodc_lm* lm, int64_t M, int64_t N, int widest, int narrowest) {
-  int w = widest;
-  while (w > narrowest && (long long)tiles_of(M, kBM) * tiles_of(N, w) < lm->sm_count) w /= 2;
-  return w;
+// Width of the tiles in columns of an output: the narrowest that still gives every tile an SM of its own (few tokens:
+// more SMs read weights), and the widest once there are more tiles than SMs (fewer bytes per product).  Forward, us at widths
+// 128 / 64 / 32: 128 tokens, 2048 x 5632: 19.0 / 15.4 / 16.1 (88 tiles of 64); 256 tokens: 19.5 / 25.1 / 24.4 (88 tiles of
+// 128); 128 tokens, 1024 x 2816: 12.2 / 10.0 / 9.5 (88 tiles of 32).
+int width_for(const cocodc_lm* lm, int64_t M, int64_t N, int widest) {
+  for (int w = widest / 4; w < widest; w *= 2)
+    if ((long long)tiles_of(M, kBM) * tiles_of(N, w) <= lm->sm_count) return w;
+  return widest;
 }
 
 bool tiles_fit(int64_t rows, int64_t cols) { return (rows + kTile - 1) / kTile <= INT32_MAX && (cols + kTile - 1) / kTile <= 65535; }
@@ -325,16 +335,13 @@ bool glu_prepare() {
     constexpr int BN = decltype(width)::value;
     allow(k_glu_tc<E, GLU_FWD, COCODC_ACT_SILU, BN>, TcShape<BN>::kSmem);
     allow(k_glu_tc<E, GLU_FWD, COCODC_ACT_GELU, BN>, TcShape<BN>::kSmem);
-    if constexpr (BN >= 64) {
-      allow(k_glu_tc<E, GLU_DX, 0, BN>, TcShape<BN>::kSmem);
-      allow(k_glu_tc<E, GLU_DW, 0, BN>, TcShape<BN>::kSmem);
-    }
+    allow(k_glu_tc<E, GLU_DX, 0, BN>, TcShape<BN>::kSmem);
+    allow(k_glu_tc<E, GLU_DW, 0, BN>, TcShape<BN>::kSmem);
   };
   const auto allow_type = [&](auto e) {
     allow_tc(e, std::integral_constant<int, 256>());
     allow_tc(e, std::integral_constant<int, 128>());
     allow_tc(e, std::integral_constant<int, 64>());
-    allow_tc(e, std::integral_constant<int, 32>());
   };
   allow_type(__nv_bfloat16());
   allow_type(__half());
@@ -377,15 +384,15 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
       constexpr int A = decltype(a)::value;
       const FewArgs<E> p{static_cast<const E*>(x), static_cast<const E*>(wg), static_cast<const E*>(wu), x_stride, w_stride,
                          (int)T, (int)D, (int)F, static_cast<E*>(h), static_cast<E*>(gate), static_cast<E*>(up), h_stride, gu_stride};
-      const unsigned grid = (unsigned)((F + 15) / 16);
-      if (T <= 8) k_glu_few<E, A, 1><<<grid, kFewWarps * 32, kFewSmem<1>, st>>>(p);
-      else k_glu_few<E, A, 2><<<grid, kFewWarps * 32, kFewSmem<2>, st>>>(p);
+      const unsigned grid = (unsigned)((F + 7) / 8);
+      if (T <= 8) k_glu_few<E, A, 1><<<grid, kFewWarps * 32, 0, st>>>(p);
+      else k_glu_few<E, A, 2><<<grid, kFewWarps * 32, 0, st>>>(p);
       result = launched(lm);
       return;
     }
     if (tensor) {
       TcArgs c{};
-      const int width = width_for(lm, T, F, 128, 16);
+      const int width = width_for(lm, T, F, 128);
       bool ok = map_of<E>(&c.a[0], x, x_stride, T, D, a_rows_for(T)) && map_of<E>(&c.b[0], wg, w_stride, F, D, width) &&
                 map_of<E>(&c.b[1], wu, w_stride, F, D, width) && map_of<E>(&c.c[0], h, h_stride, T, F, 32);
       c.a_bytes = a_rows_for(T) * kBK * 2;
@@ -404,8 +411,7 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
       result = !ok            ? COCODC_ERR_CUDA
                : width == 128 ? run_tc<E, GLU_FWD, A, 256>(lm, c, st)
                : width == 64  ? run_tc<E, GLU_FWD, A, 128>(lm, c, st)
-               : width == 32  ? run_tc<E, GLU_FWD, A, 64>(lm, c, st)
-                              : run_tc<E, GLU_FWD, A, 32>(lm, c, st);
+                              : run_tc<E, GLU_FWD, A, 64>(lm, c, st);
       return;
     }
     PlainArgs<E> p{};
@@ -491,7 +497,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
                             : run_tc<E, MODE, 0, 64>(lm, c, st);
     };
     if (dx && T > 0 && tensor_dx) {
-      const int width = width_for(lm, T, D, 256, 64);
+      const int width = width_for(lm, T, D, 256);
       c.n_tiles = tiles_of(D, width);
       c.a_bytes = a_rows_for(T) * kBK * 2;
       const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, a_rows_for(T)) && map_of<E>(&c.a[1], du, pitch, T, F, a_rows_for(T)) &&
@@ -519,7 +525,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       took(launched(lm));
     }
     if (dwg && tensor_dw && T > 0) {
-      const int width = width_for(lm, 2 * F, D, 256, 64);
+      const int width = width_for(lm, 2 * F, D, 256);
       c.n_tiles = tiles_of(D, width);
       c.a_bytes = kABytes;
       const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, kBK) && map_of<E>(&c.a[1], du, pitch, T, F, kBK) &&

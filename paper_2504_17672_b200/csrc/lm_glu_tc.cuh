@@ -43,7 +43,7 @@ template <int BN> struct TcShape {
   static constexpr unsigned kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
   // wide tiles: all shared memory in one CTA, outputs staged for TMA stores; narrow ones: two CTAs per SM, outputs from registers
   static constexpr bool kStaged = BN >= 128;
-  static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 4 : 5;
+  static constexpr int kStages = BN == 128 ? 6 : 4;
   static constexpr unsigned kSmem = 1024 + kStages * kStageBytes + (kStaged ? 4 * 2 * kOutBytes : 0);
   static constexpr int kPerSm = kStaged ? 1 : 2;
 };
@@ -88,11 +88,11 @@ __device__ __forceinline__ void send(const TcArgs& a, int what, int x, int y, un
   }
   if (lane == 0) store_commit();
 }
-// N columns (packed in pairs) of a row straight to global memory; rows start on 16-byte boundaries
-template <int N> __device__ __forceinline__ void store_row(const TcArgs& a, int what, int x, int y, const unsigned* v) {
+// 32 columns (packed in pairs) of a row straight to global memory; rows start on 16-byte boundaries
+__device__ __forceinline__ void store_row(const TcArgs& a, int what, int x, int y, const unsigned (&v)[16]) {
   unsigned short* row = static_cast<unsigned short*>(a.out[what]) + y * a.ld[what] + x;
 #pragma unroll
-  for (int q = 0; q < N / 8; ++q) {
+  for (int q = 0; q < 4; ++q) {
     if (x + q * 8 + 8 <= a.N) {
       reinterpret_cast<uint4*>(row)[q] = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
     } else {
@@ -251,27 +251,20 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
       } else if (row0 < a.M) {
         const bool mine = row0 + lane < a.M;
         if constexpr (MODE == GLU_FWD) {
-          constexpr int kPart = kColumns < 32 ? kColumns : 32;   // columns of gate and of up at a time
-          for (int col = 0; col < kColumns; col += kPart) {
+          for (int col = 0; col < kColumns; col += 32) {
             float v[32], u[32];
             unsigned packed[16];
-            if constexpr (kPart == 32) {
-              tmem_load32(v, src + col);
-              tmem_load32(u, src + BN / 2 + col);
-            } else {
-              tmem_load32(v, src);                                // 16 columns of gate, then 16 of up
-            }
+            tmem_load32(v, src + col);
+            tmem_load32(u, src + BN / 2 + col);
             tmem_wait_loads();
-            if constexpr (kPart < 32)
-              for (int i = 0; i < kPart; ++i) u[i] = v[kPart + i];
-            for (int i = 0; i < kPart / 2; ++i)
+            for (int i = 0; i < 16; ++i)
               packed[i] = pack2<E>(act_value<ACT>(v[2 * i]) * u[2 * i], act_value<ACT>(v[2 * i + 1]) * u[2 * i + 1]);
-            if (mine) store_row<kPart>(a, 0, n0 + col, row0 + lane, packed);
+            if (mine) store_row(a, 0, n0 + col, row0 + lane, packed);
             if (a.save) {
-              for (int i = 0; i < kPart / 2; ++i) packed[i] = pack2<E>(v[2 * i], v[2 * i + 1]);
-              if (mine) store_row<kPart>(a, 1, n0 + col, row0 + lane, packed);
-              for (int i = 0; i < kPart / 2; ++i) packed[i] = pack2<E>(u[2 * i], u[2 * i + 1]);
-              if (mine) store_row<kPart>(a, 2, n0 + col, row0 + lane, packed);
+              for (int i = 0; i < 16; ++i) packed[i] = pack2<E>(v[2 * i], v[2 * i + 1]);
+              if (mine) store_row(a, 1, n0 + col, row0 + lane, packed);
+              for (int i = 0; i < 16; ++i) packed[i] = pack2<E>(u[2 * i], u[2 * i + 1]);
+              if (mine) store_row(a, 2, n0 + col, row0 + lane, packed);
             }
           }
         } else {
@@ -281,7 +274,7 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
             tmem_load32(v, src + col);
             tmem_wait_loads();
             for (int i = 0; i < 16; ++i) packed[i] = pack2<E>(v[2 * i], v[2 * i + 1]);
-            if (mine) store_row<32>(a, MODE == GLU_DW ? t.z : 0, n0 + col, row0 + lane, packed);
+            if (mine) store_row(a, MODE == GLU_DW ? t.z : 0, n0 + col, row0 + lane, packed);
           }
         }
       }
