@@ -375,30 +375,39 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
 
 
+def _raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):      # the same number without a Stream object (2 us a call)
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _matrix(t: torch.Tensor, name: str):
     """(address, row stride) of a row-major matrix; a single row (or column) may have any stride."""
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions, not {t.dim()}")
-    rows, cols = t.shape
     s0, s1 = t.stride()
+    rows, cols = t.shape
     if s1 != 1 and cols > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return t.data_ptr(), (s0 if rows > 1 else max(cols, s0))
+    return t.data_ptr(), (s0 if rows > 1 or s0 > cols else cols)
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype) -> Optional[int]:
     """Address of a packed vector (or matrix) of n elements; None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a packed {dtype} tensor of {n} elements")
     return t.data_ptr()
 
 
 def _ids(t: torch.Tensor, name: str, n: int):
-    if t.dtype not in _INDEX_TYPES or t.numel() != n or not t.is_contiguous():
+    kind = _INDEX_TYPES.get(t.dtype)
+    if kind is None or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a packed int32 or int64 tensor of {n} elements")
-    return t.data_ptr(), _INDEX_TYPES[t.dtype]
+    return t.data_ptr(), kind
 
 
 class LmOps:
@@ -412,6 +421,7 @@ class LmOps:
         self._h = ctypes.c_void_p()
         device = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
         self.device = torch.device("cuda", device.index or 0)
+        self._index = self.device.index
         _check(_lib.cocodc_lm_create(ctypes.byref(self._h), self.device.index), "cocodc_lm_create")
 
     def close(self) -> None:
@@ -434,11 +444,12 @@ class LmOps:
         return int(_lib.cocodc_lm_poll_status(self._h, self._stream(stream)))
 
     def _stream(self, stream) -> int:
-        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+        return _raw_stream(self._index) if stream is None else stream.cuda_stream
 
     def _on_device(self, *tensors) -> None:
+        index = self._index
         for t in tensors:
-            if t is not None and t.device != self.device:
+            if t is not None and t.get_device() != index:      # -1 for a CPU tensor
                 raise ValueError(f"a tensor is on {t.device}, the handle on {self.device}")
 
     def _scratch(self, workspace, need: int, stream):
@@ -568,14 +579,15 @@ class LmOps:
 
 
 def _type(t: torch.Tensor) -> int:
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise ValueError(f"type {t.dtype} is not supported (float32, bfloat16, float16)")
-    return _TYPES[t.dtype]
+    return kind
 
 
 def _one_type(*tensors) -> int:
-    first = tensors[0]
+    first = tensors[0].dtype
     for t in tensors:
-        if t is not None and t.dtype != first.dtype:
+        if t is not None and t.dtype is not first:
             raise ValueError("the tensors must have one type")
-    return _type(first)
+    return _type(tensors[0])
