@@ -115,7 +115,13 @@ __global__ void __launch_bounds__(256) k_product_plain(const PlainArgs<T> p) {
 // Four CTAs per SM (64 registers) for one group: 11.2 -> 9.6 us at 2048 x 5632, 36.9 -> 32.6 us at 4096 x 11008; two groups
 // then spill, and run three.
 constexpr int kFewWarps = 8;
-constexpr int kFewTokens = 16;
+// Up to 8 tokens always; up to 32 where tokens (in eights) x D x F stay below kFewProduct, us here / on tcgen05 tiles: 16 tokens,
+// 2048 x 5632: 11.7 / 14.5, 3200 x 8640: 26.6 / 23.1; 32 tokens, 1024 x 2816: 6.6 / 9.1, 2048 x 5632: 16.3 / 14.9.
+constexpr long long kFewProduct = 190 * 1000 * 1000;
+bool few_tokens(int64_t T, int64_t D, int64_t F) {
+  const int64_t rows = T <= 8 ? 8 : T <= 16 ? 16 : 32;
+  return T <= 8 || (T <= 32 && D * F <= kFewProduct / rows);
+}
 
 template <typename E> __device__ __forceinline__ void mma16816(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3,
                                                                unsigned b0, unsigned b1);
@@ -152,8 +158,8 @@ template <typename E> struct FewArgs {
 };
 
 template <typename E, int ACT, int TILES>
-__global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : 3) k_glu_few(const FewArgs<E> p) {
-  constexpr int kBlocks = 4;                                      // k blocks in flight per warp
+__global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : TILES == 2 ? 3 : 2) k_glu_few(const FewArgs<E> p) {
+  constexpr int kBlocks = TILES <= 2 ? 4 : 2;                     // k blocks in flight per warp
   __shared__ float sums[kFewWarps][2][TILES * 8 * 8];             // [warp][gate, up][token, column]
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, q = lane % 4;
   const int f0 = blockIdx.x * 8;
@@ -190,7 +196,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : 3) k_glu_few(
   const int whole = p.D / 64;
   int b = warp;
   for (; b + (kBlocks - 1) * kFewWarps < whole; b += kFewWarps * kBlocks) blocks_at(b, std::integral_constant<int, kBlocks>());
-  if (b + kFewWarps < whole) {
+  if (kBlocks > 2 && b + kFewWarps < whole) {
     blocks_at(b, std::integral_constant<int, 2>());
     b += 2 * kFewWarps;
   }
@@ -209,6 +215,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : 3) k_glu_few(
 #pragma unroll
     for (int i = 0; i < 4; ++i) sums[warp][i >> 1][(n * 8 + q * 2 + (i & 1)) * 8 + r] = c[n][i];
   __syncthreads();
+  static_assert(TILES * 64 <= kFewWarps * 32, "one output per thread");
   if (threadIdx.x >= TILES * 64) return;
   const int t = threadIdx.x / 8, f = f0 + threadIdx.x % 8;
   if (t >= p.T || f >= p.F) return;
@@ -379,7 +386,7 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
   const bool tensor = rows_aligned(x, x_stride, 2) && rows_aligned(wg, w_stride, 2) && rows_aligned(wu, w_stride, 2) &&
                       rows_aligned(h, h_stride, 2) && (!gate || (rows_aligned(gate, gu_stride, 2) && rows_aligned(up, gu_stride, 2)));
   cocodc_status result = COCODC_OK;
-  const bool few = T <= kFewTokens && rows_aligned(x, x_stride, 2) && rows_aligned(wg, w_stride, 2) && rows_aligned(wu, w_stride, 2);
+  const bool few = few_tokens(T, D, F) && rows_aligned(x, x_stride, 2) && rows_aligned(wg, w_stride, 2) && rows_aligned(wu, w_stride, 2);
   with_glu(type, act, [&](auto e, auto a) {
     using E = decltype(e);
     if (few) {
@@ -388,7 +395,8 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
                          (int)T, (int)D, (int)F, static_cast<E*>(h), static_cast<E*>(gate), static_cast<E*>(up), h_stride, gu_stride};
       const unsigned grid = (unsigned)((F + 7) / 8);
       if (T <= 8) k_glu_few<E, A, 1><<<grid, kFewWarps * 32, 0, st>>>(p);
-      else k_glu_few<E, A, 2><<<grid, kFewWarps * 32, 0, st>>>(p);
+      else if (T <= 16) k_glu_few<E, A, 2><<<grid, kFewWarps * 32, 0, st>>>(p);
+      else k_glu_few<E, A, 4><<<grid, kFewWarps * 32, 0, st>>>(p);
       result = launched(lm);
       return;
     }

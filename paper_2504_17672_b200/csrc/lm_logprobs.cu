@@ -263,6 +263,11 @@ constexpr int kUnroll = 4;           // 16-byte loads in flight per thread
 constexpr int kCandidates = 1024;
 constexpr int kMaxTop = COCODC_LM_MAX_TOP;
 
+template <int N, bool PARTIAL> struct Batch {     // words of a step; PARTIAL: some may lie beyond the end
+  static constexpr int value = N;
+  static constexpr bool partial = PARTIAL;
+};
+
 struct RowShared {
   Stats scratch[kWarps];
   Stats part;                                       // this CTA's part of the row, read by the cluster's first CTA
@@ -340,7 +345,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     uint4 raw[N];
     W w[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) raw[k] = __ldg(src + i + k * kThreads);
+    for (int k = 0; k < N; ++k) raw[k] = !count.partial || i + k * kThreads < n ? __ldg(src + i + k * kThreads) : W::far();
 #pragma unroll
     for (int k = 0; k < N; ++k) w[k].set(raw[k]);
     float m = w[0].largest();
@@ -353,8 +358,9 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
       for (int q = 0; q < W::n / 2; ++q) add(w[k].two(q));
   };
   unsigned i = tid;
-  for (; i + (kUnroll - 1) * kThreads < n; i += kThreads * kUnroll) words_at(i, std::integral_constant<int, kUnroll>());
-  for (; i < n; i += kThreads) words_at(i, std::integral_constant<int, 1>());
+  for (; i + (kUnroll - 1) * kThreads < n; i += kThreads * kUnroll) words_at(i, Batch<kUnroll, false>());
+  if (i + kThreads < n) words_at(i, Batch<kUnroll, true>());   // two or three words left: one round trip
+  else if (i < n) words_at(i, Batch<1, false>());
   if (tail + tid < j1) single(tail + tid, 1);
   {
     float lo, hi;
