@@ -225,6 +225,38 @@ __device__ __noinline__ void careful_top(const T* row, unsigned j0, unsigned j1,
   __syncthreads();
 }
 
+// One warp, one value per lane (0: none): the k largest, descending, to list[0 .. k) (0 where there are no more).
+__device__ __forceinline__ void warp_largest(unsigned v, int k, unsigned* list) {
+  const int lane = threadIdx.x & 31;
+  for (int i = 0; i < k; ++i) {
+    const unsigned best = __reduce_max_sync(~0u, v), holders = __ballot_sync(~0u, v == best);
+    if (lane == __ffs(holders) - 1) v = 0;
+    if (lane == 0) list[i] = best;
+  }
+}
+// One warp: the k-th largest of list[0 .. n), n <= 256, counting equal ones separately.
+__device__ __forceinline__ unsigned warp_kth(const unsigned* list, int n, int k) {
+  const int lane = threadIdx.x & 31;
+  unsigned held[8], best = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) held[j] = lane + 32 * j < n ? list[lane + 32 * j] : 0;
+  for (int i = 0; i < k; ++i) {
+    unsigned mine = held[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) mine = max(mine, held[j]);
+    best = __reduce_max_sync(~0u, mine);
+    const unsigned holders = __ballot_sync(~0u, mine == best);
+    if (lane == __ffs(holders) - 1) {
+      bool gone = false;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (!gone && held[j] == best) { held[j] = 0; gone = true; }
+      }
+    }
+  }
+  return best;
+}
+
 // One warp: the k largest of keys[0 .. n), descending, to list[0 .. k) (0 where there are no more).
 template <int PER> __device__ __forceinline__ void warp_top_held(const unsigned long long* keys, int n, int k, unsigned long long* list) {
   const int lane = threadIdx.x & 31;
@@ -272,21 +304,21 @@ struct RowShared {
   Stats scratch[kWarps];
   Stats part;                                       // this CTA's part of the row, read by the cluster's first CTA
   unsigned long long warp_keys[kWarps];
-  unsigned long long lists[kWarps * kMaxTop];
+  unsigned lists[kWarps * kMaxTop];                 // the warps' largest thread maxima
   unsigned long long top[kMaxTop];                  // this CTA's part's largest keys
   unsigned long long candidates[kCandidates];
-  unsigned long long gathered[8 * kMaxTop];         // first CTA: the parts' lists
-  int flagged[kMaxTop], n_flagged, n_candidates;
+  unsigned long long gathered[8 * kMaxTop], merged[kMaxTop];   // first CTA: the parts' lists, the row's
+  int flagged[kThreads], n_flagged, n_candidates;
+  unsigned tau;
 };
 
 // A row is read once.  Each thread keeps (m, s, u) of its own elements, rescaled when its largest logit grows, in
 // batches of kUnroll 16-byte words; the parts are joined through shuffles and shared memory, and between the CTAs of a cluster (a row is
 // split over 1 to 8 CTAs, so that few rows still fill the GPU) through distributed shared memory.
 //
-// The alternatives cost the walk nothing but a note of the batch in which the thread's largest logit came.  Keys (value,
-// position) are distinct, so the k largest keys of the CTA lie with the k threads whose own largest keys are the k
-// largest among the threads' (tau is the smallest of these k): only what those threads saw is read again (from L2), and
-// of it only keys >= tau are sorted.
+// The alternatives cost the walk nothing: tau, the k-th largest of the threads' largest logits, is not above the k-th
+// largest logit, so every alternative lies with a thread whose largest logit is at least tau.  Only what those threads saw
+// is read again (from L2), and of it only logits >= tau are sorted, by value and position.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int parts) {
   using W = Words<T>;
@@ -315,7 +347,6 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
   Stats x{-W::kFar, 0.f, 0.f};
   f32x2 s2 = 0, u2 = 0, mc2 = pair_of(-x.m * c, -x.m * c);   // sums of the even and the odd elements; -c m twice
   const f32x2 c2 = pair_of(c, c);
-  unsigned at = 0;                                  // TOP: where the thread's largest logit came: 2 + first word of the batch, or an end (0, 1)
   const auto raise = [&](float m) {
     const float d = fmaxf((x.m - m) * c, -1e4f), f = exp2f(d);
     u2 = mul2(fma2(pair_of(d, d), s2, u2), pair_of(f, f));
@@ -331,15 +362,15 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     s2 = add2(s2, e);
     u2 = fma2(e, d, u2);
   };
-  const auto single = [&](unsigned j, unsigned where) {
+  const auto single = [&](unsigned j) {
     float v;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(to_f32(row[j])), "f"(-W::kFar));
-    if (v > x.m) { raise(v); at = where; }
+    if (v > x.m) raise(v);
     const float d = fmaf(v, c, -x.m * c), e = fast_exp2(d);
     s2 = add2(s2, pair_of(e, 0.f));
     u2 = add2(u2, pair_of(e * d, 0.f));
   };
-  if (j0 + tid < base) single(j0 + tid, 0);
+  if (j0 + tid < base) single(j0 + tid);
   const auto words_at = [&](unsigned i, auto count) {
     constexpr int N = decltype(count)::value;
     uint4 raw[N];
@@ -351,7 +382,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     float m = w[0].largest();
 #pragma unroll
     for (int k = 1; k < N; ++k) m = fmaxf(m, w[k].largest());
-    if (m > x.m) { raise(m); at = 2 + i; }
+    if (m > x.m) raise(m);
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
@@ -361,7 +392,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
   for (; i + (kUnroll - 1) * kThreads < n; i += kThreads * kUnroll) words_at(i, Batch<kUnroll, false>());
   if (i + kThreads < n) words_at(i, Batch<kUnroll, true>());   // two or three words left: one round trip
   else if (i < n) words_at(i, Batch<1, false>());
-  if (tail + tid < j1) single(tail + tid, 1);
+  if (tail + tid < j1) single(tail + tid);
   {
     float lo, hi;
     split(s2, lo, hi);
@@ -369,75 +400,51 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     split(u2, lo, hi);
     x.u = lo + hi;
   }
-  const Stats mine = x;
+  // the thread's largest logit; 0: nothing above -kFar
+  const unsigned largest = TOP && x.m > -W::kFar ? ordered(x.m) : 0;
+  if (TOP) {
+    warp_largest(largest, a.top_k, sh.lists + warp * a.top_k);
+    if (tid == 0) sh.n_flagged = sh.n_candidates = 0;
+  }
   x = block_join(x, c, sh.scratch);
   // a NaN or +Inf, nothing but very low logits, a very small scale: once more, with care (also the alternatives)
   const bool careful = !(x.m > -W::kFar / 2) || !(x.s < INFINITY) || !(c * (W::kFar / 2) > 200.f);
   if (careful) x = careful_stats(row, j0, j1, c, sh.scratch);
 
   if (TOP) {
-    if (tid == 0) sh.n_flagged = sh.n_candidates = 0;
-    __syncthreads();
     bool done = false;
     if (!careful) {
-      // the thread's largest key: its value is known, the lowest position holding it is in the noted batch
-      unsigned long long key = 0;
-      if (mine.s > 0.f && mine.m > -W::kFar) {
-        unsigned j = 0;
-        if (at < 2) {
-          j = at ? tail + tid : j0 + tid;
-        } else {
-          const unsigned i = at - 2;
-          bool found = false;
-#pragma unroll
-          for (int k = 0; k < kUnroll; ++k)
-            if (!found && i + k * kThreads < n) {
-              W w;
-              w.set(src[i + k * kThreads]);
-#pragma unroll
-              for (int q = 0; q < W::n; ++q)
-                if (!found && w.at(q) == mine.m) { found = true; j = base + (i + k * kThreads) * W::n + q; }
-            }
-        }
-        key = key_of(mine.m, j);
-      }
-      // the k largest of the threads' keys: per warp, then over the warps
-      unsigned long long rest = key;
-      for (int r = 0; r < a.top_k; ++r) {
-        const unsigned long long best = warp_max(rest);
-        if (lane == 0) sh.lists[warp * a.top_k + r] = best;
-        if (rest == best) rest = 0;
+      if (warp == 0) {
+        const unsigned t0 = warp_kth(sh.lists, kWarps * a.top_k, a.top_k);
+        if (lane == 0) sh.tau = t0;
       }
       __syncthreads();
-      if (warp == 0) warp_top(sh.lists, kWarps * a.top_k, a.top_k, sh.top);
-      __syncthreads();
-      const unsigned long long tau = sh.top[a.top_k - 1];
+      const unsigned tau = sh.tau;
       // tau 0: fewer threads than alternatives hold anything; leave it to the careful way
       if (tau != 0) {
-        if (key >= tau) sh.flagged[atomicAdd(&sh.n_flagged, 1)] = tid;
+        if (largest >= tau) sh.flagged[atomicAdd(&sh.n_flagged, 1)] = tid;
         __syncthreads();
         const auto offer = [&](float v, unsigned j) {
-          const unsigned long long q = key_of(v, j);
-          if (q < tau) return;
+          if (ordered(v) < tau) return;
           const int slot = atomicAdd(&sh.n_candidates, 1);
-          if (slot < kCandidates) sh.candidates[slot] = q;
+          if (slot < kCandidates) sh.candidates[slot] = key_of(v, j);
         };
-        for (int f = warp; f < a.top_k; f += kWarps) {
+        for (int f = warp; f < sh.n_flagged; f += kWarps) {
           const unsigned who = sh.flagged[f];
           if (lane == 0 && j0 + who < base) offer(to_f32(row[j0 + who]), j0 + who);
           if (lane == 1 && tail + who < j1) offer(to_f32(row[tail + who]), tail + who);
           for (unsigned i = who + lane * kThreads; i < n; i += 32 * kThreads) {
             W w;
-            w.set(src[i]);
-            if (ordered(w.largest()) < (unsigned)(tau >> 32)) continue;
+            w.set(__ldg(src + i));
+            if (ordered(w.largest()) < tau) continue;
 #pragma unroll
             for (int q = 0; q < W::n; ++q) offer(w.at(q), base + i * W::n + q);
           }
         }
         __syncthreads();
+        // many equal logits at the border may not fit the list
         done = sh.n_candidates <= kCandidates;
         if (done && warp == 0) warp_top(sh.candidates, sh.n_candidates, a.top_k, sh.top);
-        __syncthreads();
       }
     }
     if (!done) careful_top(row, j0, j1, a.top_k, sh.top, sh.warp_keys);
@@ -469,8 +476,8 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
           asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(sh.gathered[i]) : "r"(there));
         }
         __syncthreads();
-        if (warp == 0) warp_top(sh.gathered, parts * a.top_k, a.top_k, sh.lists);
-        top = sh.lists;
+        if (warp == 0) warp_top(sh.gathered, parts * a.top_k, a.top_k, sh.merged);
+        top = sh.merged;
       }
     }
     // the others' shared memory stays until it has been read
