@@ -384,14 +384,14 @@ if hasattr(torch._C, "_cuda_getCurrentRawStream"):      # the same number withou
 
 
 def _matrix(t: torch.Tensor, name: str):
-    """(address, row stride) of a row-major matrix; a single row (or column) may have any stride."""
-    if t.dim() != 2:
-        raise ValueError(f"{name} must have two dimensions, not {t.dim()}")
-    s0, s1 = t.stride()
-    rows, cols = t.shape
+    """(address, row stride, rows, columns) of a row-major matrix; a single row (or column) may have any stride."""
+    try:
+        (rows, cols), (s0, s1) = t.shape, t.stride()
+    except ValueError:
+        raise ValueError(f"{name} must have two dimensions, not {t.dim()}") from None
     if s1 != 1 and cols > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return t.data_ptr(), (s0 if rows > 1 or s0 > cols else cols)
+    return t.data_ptr(), (s0 if rows > 1 or s0 > cols else cols), rows, cols
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype) -> Optional[int]:
@@ -408,6 +408,26 @@ def _ids(t: torch.Tensor, name: str, n: int):
     if kind is None or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a packed int32 or int64 tensor of {n} elements")
     return t.data_ptr(), kind
+
+
+def _type(t: torch.Tensor) -> int:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"type {t.dtype} is not supported (float32, bfloat16, float16)")
+    return kind
+
+
+def _one_type(*tensors) -> int:
+    first = tensors[0].dtype
+    for t in tensors:
+        if t is not None and t.dtype is not first:
+            raise ValueError("the tensors must have one type")
+    return _type(tensors[0])
+
+
+def _sized(name: str, rows: int, cols: int, want_rows: int, want_cols: int) -> None:
+    if rows != want_rows or cols != want_cols:
+        raise ValueError(f"{name} must be {want_rows} x {want_cols}, not {rows} x {cols}")
 
 
 class LmOps:
@@ -466,128 +486,128 @@ class LmOps:
     def cocodc_lm_embed(self, table, ids, y, scale: float = 1.0, stream=None) -> None:
         """y[t] = scale * table[ids[t]]; zeros where ids[t] < 0."""
         self._on_device(table, ids, y)
-        (V, D), T = table.shape, ids.numel()
-        if y.shape != (T, D):
-            raise ValueError(f"y must be {T} x {D}")
-        tp, ts = _matrix(table, "table")
-        yp, ys = _matrix(y, "y")
+        tp, ts, V, D = _matrix(table, "table")
+        yp, ys, T, cols = _matrix(y, "y")
+        if cols != D:
+            _sized("y", T, cols, T, D)
         ip, it = _ids(ids, "ids", T)
-        _check(_lib.cocodc_lm_embed(self._h, tp, _type(table), ts, V, D, ip, it, T, scale, yp, _type(y), ys,
-                                    self._stream(stream)), "cocodc_lm_embed")
+        code = _lib.cocodc_lm_embed(self._h, tp, _type(table), ts, V, D, ip, it, T, scale, yp, _type(y), ys,
+                                    self._stream(stream))
+        if code:
+            raise CocodcError(code, "cocodc_lm_embed")
 
     def cocodc_lm_embed_grad(self, dy, ids, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None,
                              stream=None) -> None:
         """dtable[v] (+)= scale * sum of dy[t] over the t with ids[t] == v."""
         self._on_device(dy, ids, dtable)
-        (V, D), T = dtable.shape, ids.numel()
-        if dy.shape != (T, D):
-            raise ValueError(f"dy must be {T} x {D}")
-        dp, ds = _matrix(dy, "dy")
-        gp, gs = _matrix(dtable, "dtable")
+        dp, ds, T, cols = _matrix(dy, "dy")
+        gp, gs, V, D = _matrix(dtable, "dtable")
+        if cols != D:
+            _sized("dy", T, cols, T, D)
         ip, it = _ids(ids, "ids", T)
         w = self._scratch(workspace, _lib.cocodc_lm_embed_grad_workspace(V, D, T), stream)
-        _check(_lib.cocodc_lm_embed_grad(self._h, dp, _type(dy), ds, ip, it, T, V, D, scale, int(accumulate), gp,
-                                         _type(dtable), gs, w.data_ptr(), w.numel() * w.element_size(),
-                                         self._stream(stream)), "cocodc_lm_embed_grad")
+        code = _lib.cocodc_lm_embed_grad(self._h, dp, _type(dy), ds, ip, it, T, V, D, scale, int(accumulate), gp,
+                                         _type(dtable), gs, w.data_ptr(), w.numel() * w.element_size(), self._stream(stream))
+        if code:
+            raise CocodcError(code, "cocodc_lm_embed_grad")
 
     def cocodc_lm_glu(self, x, wg, wu, h, gate=None, up=None, act="silu", stream=None) -> None:
         """h = act(x wg^T) * (x wu^T); gate and up receive the two products (both or neither)."""
-        self._on_device(x, wg, wu, h, gate, up)
-        (T, D), F = x.shape, wg.shape[0]
-        if wg.shape != (F, D) or wu.shape != (F, D) or h.shape != (T, F) or (gate is not None and gate.shape != (T, F)) or \
-                (up is not None and up.shape != (T, F)):
-            raise ValueError(f"shapes do not fit x {T} x {D} and wg {F} x {D}")
-        kind = _one_type(x, wg, wu, h, gate, up)
-        xp, xs = _matrix(x, "x")
-        (gp, ws), (up_, us) = _matrix(wg, "wg"), _matrix(wu, "wu")
-        if ws != us and F > 1:
+        self._on_device(x, wg, wu, h)
+        xp, xs, T, D = _matrix(x, "x")
+        gp, gs, F, cols = _matrix(wg, "wg")
+        up_, us, rows, cols2 = _matrix(wu, "wu")
+        hp, hs, T2, F2 = _matrix(h, "h")
+        if not (cols == cols2 == D and rows == F2 == F and T2 == T):
+            _sized("wg", F, cols, F, D)
+            _sized("wu", rows, cols2, F, D)
+            _sized("h", T2, F2, T, F)
+        if gs != us and F > 1:
             raise ValueError("wg and wu must have the same row stride")
-        hp, hs = _matrix(h, "h")
-        gt = ut = None
-        gs = gs2 = F
-        if gate is not None:
-            gt, gs = _matrix(gate, "gate")
-        if up is not None:
-            ut, gs2 = _matrix(up, "up")
-        if gate is not None and up is not None and gs != gs2 and T > 1:
-            raise ValueError("gate and up must have the same row stride")
-        _check(_lib.cocodc_lm_glu(self._h, _ACTS[act], kind, xp, xs, gp, up_, ws, T, D, F, hp, hs, gt, ut, gs,
-                                  self._stream(stream)), "cocodc_lm_glu")
+        kind = _one_type(x, wg, wu, h, gate, up)
+        gtp = utp = None
+        gus = F
+        if gate is not None or up is not None:
+            self._on_device(gate, up)
+            strides = []
+            for name, t in (("gate", gate), ("up", up)):
+                if t is not None:
+                    p, st, r, c = _matrix(t, name)
+                    _sized(name, r, c, T, F)
+                    strides.append(st)
+                    gtp, utp = (p, utp) if name == "gate" else (gtp, p)
+            gus = strides[0]
+            if strides[-1] != gus and T > 1:
+                raise ValueError("gate and up must have the same row stride")
+        code = _lib.cocodc_lm_glu(self._h, _ACTS[act], kind, xp, xs, gp, up_, gs, T, D, F, hp, hs, gtp, utp, gus,
+                                  self._stream(stream))
+        if code:
+            raise CocodcError(code, "cocodc_lm_glu")
 
     def cocodc_lm_glu_grad(self, dh, gate, up, x, wg, wu, dx=None, dwg=None, dwu=None, act="silu", workspace=None,
                            stream=None) -> None:
         """dx, dwg, dwu of cocodc_lm_glu from dh and the gate and up that it wrote; dx, or dwg and dwu, may be None."""
         self._on_device(dh, gate, up, x, wg, wu, dx, dwg, dwu)
-        (T, D), F = x.shape, wg.shape[0]
-        for name, t, shape in (("dh", dh, (T, F)), ("gate", gate, (T, F)), ("up", up, (T, F)), ("wg", wg, (F, D)), ("wu", wu, (F, D)),
-                               ("dx", dx, (T, D)), ("dwg", dwg, (F, D)), ("dwu", dwu, (F, D))):
-            if t is not None and t.shape != shape:
-                raise ValueError(f"{name} must be {shape[0]} x {shape[1]}")
+        xp, xs, T, D = _matrix(x, "x")
+        gp, ws, F, cols = _matrix(wg, "wg")
+        _sized("wg", F, cols, F, D)
         kind = _one_type(x, wg, wu, dh, gate, up, dx, dwg, dwu)
-        hp, hs = _matrix(dh, "dh")
-        (gt, gs), (ut, us) = _matrix(gate, "gate"), _matrix(up, "up")
-        xp, xs = _matrix(x, "x")
-        (gp, ws), (up_, ws2) = _matrix(wg, "wg"), _matrix(wu, "wu")
+
+        def take(t, name, rows, cols):
+            if t is None:
+                return None, cols
+            p, stride, r, c = _matrix(t, name)
+            _sized(name, r, c, rows, cols)
+            return p, stride
+
+        wup, ws2 = take(wu, "wu", F, D)
+        hp, hs = take(dh, "dh", T, F)
+        (gtp, gs), (utp, us) = take(gate, "gate", T, F), take(up, "up", T, F)
+        dxp, dxs = take(dx, "dx", T, D)
+        (dgp, dws), (dup, dws2) = take(dwg, "dwg", F, D), take(dwu, "dwu", F, D)
         if (gs != us and T > 1) or (ws != ws2 and F > 1):
             raise ValueError("gate and up, and wg and wu, must have the same row stride")
-        dxp, dxs = _matrix(dx, "dx") if dx is not None else (None, D)
-        dgp, dws = _matrix(dwg, "dwg") if dwg is not None else (None, D)
-        dup, dws2 = _matrix(dwu, "dwu") if dwu is not None else (None, dws)
-        if dwg is not None and dws != dws2 and F > 1:
+        if dwg is not None and dwu is not None and dws != dws2 and F > 1:
             raise ValueError("dwg and dwu must have the same row stride")
         w = self._scratch(workspace, _lib.cocodc_lm_glu_grad_workspace(T, D, F), stream)
-        _check(_lib.cocodc_lm_glu_grad(self._h, _ACTS[act], kind, hp, hs, gt, ut, gs, xp, xs, gp, up_, ws, T, D, F, dxp, dxs,
-                                       dgp, dup, dws, w.data_ptr(), w.numel() * w.element_size(), self._stream(stream)),
-               "cocodc_lm_glu_grad")
+        code = _lib.cocodc_lm_glu_grad(self._h, _ACTS[act], kind, hp, hs, gtp, utp, gs, xp, xs, gp, wup, ws, T, D, F, dxp, dxs,
+                                       dgp, dup, dws, w.data_ptr(), w.numel() * w.element_size(), self._stream(stream))
+        if code:
+            raise CocodcError(code, "cocodc_lm_glu_grad")
 
     def cocodc_lm_logprobs(self, logits, targets, logp, entropy=None, lse=None, top_ids=None, top_logp=None,
                            scale: float = 1.0, stream=None) -> None:
         """Per row of scale * logits: log probability of targets[t] (0 where it is negative), entropy, log-sum-exp, and the
         largest logits' ids and log probabilities (top_ids, top_logp: T x k).  targets and logp may both be None."""
         self._on_device(logits, targets, logp, entropy, lse, top_ids, top_logp)
-        T, V = logits.shape
-        lp, ls = _matrix(logits, "logits")
+        lp, ls, T, V = _matrix(logits, "logits")
         tp, tt = _ids(targets, "targets", T) if targets is not None else (None, 0)
         f32 = torch.float32
-        k = 0
+        k, kp, kl = 0, None, None
         if top_ids is not None:
             if top_ids.dim() != 2 or top_ids.shape[0] != T:
                 raise ValueError("top_ids must be T x k")
             k = top_ids.shape[1]
-        _check(_lib.cocodc_lm_logprobs(self._h, lp, _type(logits), ls, T, V, tp, tt, scale, _vector(logp, "logp", T, f32),
-                                       _vector(entropy, "entropy", T, f32), _vector(lse, "lse", T, f32), k,
-                                       _vector(top_ids, "top_ids", T * k, torch.int32) if k else None,
-                                       _vector(top_logp, "top_logp", T * k, f32) if k else None, self._stream(stream)),
-               "cocodc_lm_logprobs")
+        if k:
+            kp, kl = _vector(top_ids, "top_ids", T * k, torch.int32), _vector(top_logp, "top_logp", T * k, f32)
+        code = _lib.cocodc_lm_logprobs(self._h, lp, _type(logits), ls, T, V, tp, tt, scale, _vector(logp, "logp", T, f32),
+                                       _vector(entropy, "entropy", T, f32), _vector(lse, "lse", T, f32), k, kp, kl,
+                                       self._stream(stream))
+        if code:
+            raise CocodcError(code, "cocodc_lm_logprobs")
 
     def cocodc_lm_logprobs_grad(self, logits, targets, lse, entropy, dlogp, dentropy, dlogits, scale: float = 1.0,
                                 stream=None) -> None:
         """dlogits of cocodc_lm_logprobs given d/dlogp and d/dentropy (None for zero); dlogits may be logits itself."""
         self._on_device(logits, targets, lse, entropy, dlogp, dentropy, dlogits)
-        T, V = logits.shape
-        if dlogits.shape != (T, V):
-            raise ValueError(f"dlogits must be {T} x {V}")
+        lp, ls, T, V = _matrix(logits, "logits")
+        dp, ds, T2, V2 = _matrix(dlogits, "dlogits")
+        _sized("dlogits", T2, V2, T, V)
         kind = _one_type(logits, dlogits)
-        lp, ls = _matrix(logits, "logits")
-        dp, ds = _matrix(dlogits, "dlogits")
         tp, tt = _ids(targets, "targets", T) if targets is not None else (None, 0)
         f32 = torch.float32
-        _check(_lib.cocodc_lm_logprobs_grad(self._h, lp, kind, ls, T, V, tp, tt, scale, _vector(lse, "lse", T, f32),
+        code = _lib.cocodc_lm_logprobs_grad(self._h, lp, kind, ls, T, V, tp, tt, scale, _vector(lse, "lse", T, f32),
                                             _vector(entropy, "entropy", T, f32), _vector(dlogp, "dlogp", T, f32),
-                                            _vector(dentropy, "dentropy", T, f32), dp, ds, self._stream(stream)),
-               "cocodc_lm_logprobs_grad")
-
-
-def _type(t: torch.Tensor) -> int:
-    kind = _TYPES.get(t.dtype)
-    if kind is None:
-        raise ValueError(f"type {t.dtype} is not supported (float32, bfloat16, float16)")
-    return kind
-
-
-def _one_type(*tensors) -> int:
-    first = tensors[0].dtype
-    for t in tensors:
-        if t is not None and t.dtype is not first:
-            raise ValueError("the tensors must have one type")
-    return _type(tensors[0])
+                                            _vector(dentropy, "dentropy", T, f32), dp, ds, self._stream(stream))
+        if code:
+            raise CocodcError(code, "cocodc_lm_logprobs_grad")

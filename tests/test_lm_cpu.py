@@ -40,7 +40,7 @@ def test_matrices_are_described_by_their_strides(B):
     import torch
     t = torch.zeros(6, 10)
     assert B._matrix(t, "t")[1] == 10
-    assert B._matrix(t[::2, 2:7], "t") == (t.data_ptr() + 8, 20)
+    assert B._matrix(t[::2, 2:7], "t") == (t.data_ptr() + 8, 20, 3, 5)
     assert B._matrix(t[:1, :4], "t")[1] >= 4
     with pytest.raises(ValueError):
         B._matrix(t.t(), "t")
