@@ -47,7 +47,10 @@ template <int BN> struct TcShape {
   static constexpr unsigned kSmem = 1024 + kStages * kStageBytes + (kStaged ? 4 * 2 * kOutBytes : 0);
   static constexpr int kPerSm = kStaged ? 1 : 2;
 };
-constexpr int kGroupM = 16;                         // tiles of consecutive rows that go through one column in turn
+// Tiles of consecutive rows that go through one column of tiles in turn.  Under the power cap, where fewer bytes from L2 mean
+// a higher clock, 8 / 16 / 32 / 64 of them took 740 / 706 / 687 / 697 us forward (8192 x 3200 x 8640) and 8 / 16 / 32 took
+// 708 / 724 / 717 us for the gradient (8192 x 2048 x 5632, all three launches).
+template <int MODE> constexpr int kGroupM = MODE == GLU_FWD ? 32 : 8;
 
 struct TcShared {
   unsigned long long full[6], empty[6], acc_full[2], acc_empty[2], drain;
@@ -56,15 +59,15 @@ struct TcShared {
 };
 
 struct TileAt { int z, m, n; };
-// Tiles in groups of kGroupM row tiles, inside a group column after column: CTAs that run together share operands in L2.
-__device__ __forceinline__ TileAt tile_at(const TcArgs& a, int tile) {
+// Tiles in groups of row tiles, inside a group column after column: CTAs that run together share operands in L2.
+template <int MODE> __device__ __forceinline__ TileAt tile_at(const TcArgs& a, int tile) {
   TileAt t;
   const int per = a.m_tiles * a.n_tiles;
   t.z = tile / per;
   tile -= t.z * per;
-  const int group = tile / (kGroupM * a.n_tiles), first = group * kGroupM;
-  const int height = min(kGroupM, a.m_tiles - first);
-  tile -= group * kGroupM * a.n_tiles;
+  const int group = tile / (kGroupM<MODE> * a.n_tiles), first = group * kGroupM<MODE>;
+  const int height = min(kGroupM<MODE>, a.m_tiles - first);
+  tile -= group * kGroupM<MODE> * a.n_tiles;
   t.m = first + tile % height;
   t.n = tile / height;
   return t;
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
       long long it = 0;
       bool ok = true;
       for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
-        const TileAt t = tile_at(a, tile);
+        const TileAt t = tile_at<MODE>(a, tile);
         const int m0 = t.m * kBM, n0 = t.n * kColumns;
         for (int kb = 0; kb < blocks; ++kb, ++it) {
           const int s = (int)(it % kStages);
@@ -172,6 +175,9 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
           }
         }
       }
+      // the issuer's last arrivals come before the CTA leaves
+      for (long long i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
+        ok = bar_wait(smem_addr(&sh.empty[i % kStages]), (unsigned)((i / kStages) & 1), stop);
       // given up: the copies in flight land before the CTA leaves its shared memory
       if (!ok)
         for (long long i = it > kStages ? it - kStages : 0; i < it; ++i)
@@ -212,7 +218,7 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
     int turn = 0, sent = 0;
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
       const int acc = turn & 1;
-      const TileAt t = tile_at(a, tile);
+      const TileAt t = tile_at<MODE>(a, tile);
       const int row0 = t.m * kBM + quarter * 32, n0 = t.n * kColumns;
       if (!__all_sync(~0u, bar_wait(smem_addr(&sh.acc_full[acc]), (unsigned)((turn >> 1) & 1), stop))) break;
       tc_fence_after();
@@ -284,6 +290,7 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
     }
     if (lane == 0) store_wait_all();
   }
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && sh.stop) record(a.status, COCODC_ERR_TIMEOUT);

@@ -7,7 +7,7 @@
 
 namespace cocodc_lm_impl {
 
-constexpr int kBarrierPolls = 1 << 22;   // polls of an mbarrier before a wait gives up
+constexpr unsigned long long kWaitNs = 4000000000ull;   // how long a wait on an mbarrier may last before it gives up
 
 __device__ __forceinline__ unsigned smem_addr(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
 
@@ -26,19 +26,24 @@ __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// false when the wait gave up: `stop` (shared, raised by the first role that gave up) or the poll limit
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+// false when the wait gave up: `stop` (shared, raised by the first role that gave up) or the time limit
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile int* stop) {
   if (bar_try(bar, parity)) return true;
-  for (int i = 0; i < kBarrierPolls; ++i) {
+  const unsigned long long t0 = now_ns();
+  while (!*stop && now_ns() - t0 < kWaitNs)
     if (bar_try(bar, parity)) return true;
-    if (*stop) return false;
-  }
   *stop = 1;
   return false;
 }
 // the same without the shared flag, for draining
 __device__ __forceinline__ void bar_drain(unsigned bar, unsigned parity) {
-  for (int i = 0; i < kBarrierPolls && !bar_try(bar, parity); ++i) {}
+  const unsigned long long t0 = now_ns();
+  while (!bar_try(bar, parity) && now_ns() - t0 < kWaitNs) {}
 }
 
 __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {

@@ -210,7 +210,10 @@ GLU_SHAPES = [(1, 1, 1), (1, 64, 128), (1, 2048, 5632), (2, 40, 24), (3, 72, 200
               (129, 192, 384), (200, 33, 65), (257, 1024, 136), (300, 264, 520), (1000, 512, 776)]
 
 
-@pytest.mark.parametrize("T,D,F", GLU_SHAPES)
+GLU_WIDE = [(2100, 2600, 1000), (4000, 1288, 1411), (1290, 77, 5003)]      # more tiles than SMs
+
+
+@pytest.mark.parametrize("T,D,F", GLU_SHAPES + GLU_WIDE)
 @pytest.mark.parametrize("dtype,act", [(BF16, "silu"), (F16, "gelu"), (BF16, "gelu"), (F16, "silu")])
 def test_glu(ops, T, D, F, dtype, act):
     g = gen(T + D + F)
@@ -238,7 +241,7 @@ def test_glu(ops, T, D, F, dtype, act):
             untouched(o[0], o[1], float("nan"))
 
 
-@pytest.mark.parametrize("T,D,F", GLU_SHAPES)
+@pytest.mark.parametrize("T,D,F", GLU_SHAPES + GLU_WIDE)
 @pytest.mark.parametrize("dtype,act", [(BF16, "silu"), (F16, "gelu"), (BF16, "gelu")])
 def test_glu_grad(ops, T, D, F, dtype, act):
     g = gen(T + D + F + 1)
