@@ -289,6 +289,25 @@ template <typename F> void with_glu(int32_t type, int32_t act, F&& f) {
   }
 }
 
+int tiles_of(int64_t n, int tile) { return (int)((n + tile - 1) / tile); }
+
+// Parts of dx's contraction where its tiles leave at least half of the SMs without one: as many as there are SMs for each
+// tile, with at least 16 k-blocks to a part.  One row of tiles takes narrow ones (more SMs read weights), more rows the
+// widest (the tokens are read once per tile); 2048 x 5632 without parts, with parts of 64 and of 256 columns, us for the
+// whole of dx: 128 tokens 57 / 28 / 35, 512 tokens 59 / 61 (no parts) / 41.
+constexpr int kPartTiles = 148;                       // tiles x parts at most; bounds the scratch
+int part_width(int64_t T) { return T <= kBM ? 64 : 256; }
+int parts_for(int64_t T, int64_t D, int64_t F) {
+  const long long tiles = (long long)tiles_of(T, kBM) * tiles_of(D, part_width(T)), blocks = 2ll * tiles_of(F, kBK);
+  const long long parts = tiles > 0 ? kPartTiles / tiles : 1, most = blocks / 16;
+  const long long p = parts < most ? parts : most;
+  return p < 2 ? 1 : (int)p;
+}
+uint64_t part_bytes(int64_t T, int64_t D, int64_t F) {
+  const int p = parts_for(T, D, F), w = part_width(T);
+  return p < 2 ? 0 : (uint64_t)p * tiles_of(T, kBM) * tiles_of(D, w) * kBM * w * sizeof(float);
+}
+
 int64_t scratch_pitch(int64_t F) { return (F + 7) / 8 * 8; }
 
 // ---- tensor-core path: host side ----------------------------------------------------------------
@@ -303,7 +322,6 @@ template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t strid
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int tiles_of(int64_t n, int tile) { return (int)((n + tile - 1) / tile); }
 
 template <typename E, int MODE, int ACT, int BN> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
   const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices, most = (long long)TcShape<BN>::kPerSm * lm->sm_count;
@@ -346,6 +364,7 @@ bool glu_prepare() {
     allow(k_glu_tc<E, GLU_FWD, COCODC_ACT_GELU, BN>, TcShape<BN>::kSmem);
     allow(k_glu_tc<E, GLU_DX, 0, BN>, TcShape<BN>::kSmem);
     allow(k_glu_tc<E, GLU_DW, 0, BN>, TcShape<BN>::kSmem);
+    if constexpr (BN != 128) allow(k_glu_tc<E, GLU_DX_PARTS, 0, BN>, TcShape<BN>::kSmem);
   };
   const auto allow_type = [&](auto e) {
     allow_tc(e, std::integral_constant<int, 256>());
@@ -443,7 +462,7 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
 
 uint64_t cocodc_lm_glu_grad_workspace(int64_t T, int64_t D, int64_t F) {
   if (!sane(T) || !sane(D) || !sane(F)) return 0;
-  return 16 + 2 * (uint64_t)T * (uint64_t)scratch_pitch(F) * 2;
+  return 16 + 2 * (uint64_t)T * (uint64_t)scratch_pitch(F) * 2 + part_bytes(T, D, F);
 }
 
 cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const void* dh, int64_t dh_stride,
@@ -499,6 +518,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
     }
     TcArgs c{};
     c.status = lm->d_status;
+    c.splits = 1;
     c.N = (int)D;
     const auto run = [&](auto mode, int width) {
       constexpr int MODE = decltype(mode)::value;
@@ -507,20 +527,35 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
                             : run_tc<E, MODE, 0, 64>(lm, c, st);
     };
     if (dx && T > 0 && tensor_dx) {
-      const int width = width_for(lm, T, D, 256);
+      const int splits = parts_for(T, D, F), width = splits > 1 ? part_width(T) : width_for(lm, T, D, 256);
       c.n_tiles = tiles_of(D, width);
       c.a_bytes = a_rows_for(T) * kBK * 2;
+      c.splits = splits;
+      c.parts = reinterpret_cast<float*>(du + T * pitch);
       const bool ok = map_of<E>(&c.a[0], dg, pitch, T, F, a_rows_for(T)) && map_of<E>(&c.a[1], du, pitch, T, F, a_rows_for(T)) &&
                       map_of<E>(&c.b[0], wg, w_stride, F, D, kBK) && map_of<E>(&c.b[1], wu, w_stride, F, D, kBK) &&
                       map_of<E>(&c.c[0], dx, dx_stride, T, D, 32);
       c.m_tiles = tiles_of(T, kBM);
-      c.matrices = 1;
+      c.matrices = splits;
       c.sources = 2;
       c.out[0] = dx;
       c.ld[0] = dx_stride;
       c.k_blocks = tiles_of(F, kBK);
       c.M = (int)T;
-      took(ok ? run(std::integral_constant<int, GLU_DX>(), width) : COCODC_ERR_CUDA);
+      if (!ok) {
+        took(COCODC_ERR_CUDA);
+      } else if (splits == 1) {
+        took(run(std::integral_constant<int, GLU_DX>(), width));
+      } else {
+        const auto in_parts = [&](auto w) {
+          constexpr int BN = decltype(w)::value;
+          took(run_tc<E, GLU_DX_PARTS, 0, BN>(lm, c, st));
+          k_add_parts<E, BN><<<(unsigned)(c.m_tiles * c.n_tiles * (kBM / 8)), 256, 0, st>>>(c);
+          took(launched(lm));
+        };
+        if (width == 64) in_parts(std::integral_constant<int, 64>());
+        else in_parts(std::integral_constant<int, 256>());
+      }
     } else if (dx && T > 0) {
       PlainArgs<E> p{};
       p.a[0] = {dg, pitch, 1};

@@ -10,6 +10,8 @@
 // thread of the epilogue finds gate and up of one element in its own TMEM lane and the product needs no exchange.
 // dx = dg Wg + du Wu: one accumulator, the k loop runs through both sources.  dw = d^T x: the tile index picks dg or du.
 // The operands of the gradient whose contraction runs along rows are taken MN-major as they lie in memory.
+// With few tokens dx has few tiles and a long contraction: it is cut into parts (GLU_DX_PARTS, the slowest tile index),
+// whose fp32 sums k_add_parts adds in order.
 // Ragged sizes: TMA fills what lies outside a matrix with zeros, and clips rows and whole 16-byte groups of columns
 // when it writes; the last N mod 8 columns of an output leave by ordinary stores (a copy rounds them up to 16 bytes).
 #pragma once
@@ -18,14 +20,16 @@
 
 namespace cocodc_lm_impl {
 
-enum { GLU_FWD = 0, GLU_DX = 1, GLU_DW = 2 };
+enum { GLU_FWD = 0, GLU_DX = 1, GLU_DW = 2, GLU_DX_PARTS = 3 };
 
 struct TcArgs {
   CUtensorMap a[2], b[2], c[3];
   int m_tiles, n_tiles;      // of one matrix
-  int matrices;              // GLU_DW: 2
+  int matrices;              // GLU_DW: 2; GLU_DX_PARTS: splits
   int k_blocks;              // of one source
   int sources;               // GLU_DX: 2
+  int splits;                // GLU_DX_PARTS: parts of the contraction, whose sums go to `parts` in fp32
+  float* parts;              // [splits][tile][128][BN]
   int M, N;                  // rows and columns of the outputs
   int a_bytes;               // of A's part of a stage: fewer than 128 tokens are loaded as they are
   int save;                  // GLU_FWD: also write gate and up (c[1], c[2])
@@ -125,6 +129,8 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
   constexpr bool a_mn = MODE == GLU_DW, b_mn = MODE != GLU_FWD;
   const int tiles = a.m_tiles * a.n_tiles * a.matrices;
   const int blocks = a.k_blocks * a.sources;
+  const auto first_block = [&](int z) { return MODE == GLU_DX_PARTS ? (int)((long long)blocks * z / a.splits) : 0; };
+  constexpr bool kDx = MODE == GLU_DX || MODE == GLU_DX_PARTS;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -153,7 +159,8 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
       for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
         const TileAt t = tile_at<MODE>(a, tile);
         const int m0 = t.m * kBM, n0 = t.n * kColumns;
-        for (int kb = 0; kb < blocks; ++kb, ++it) {
+        const int kb0 = first_block(t.z), kb1 = MODE == GLU_DX_PARTS ? first_block(t.z + 1) : blocks;
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
           const int s = (int)(it % kStages);
           ok = bar_wait(smem_addr(&sh.empty[s]), (unsigned)((it / kStages) & 1) ^ 1, stop);
           if (!ok) break;
@@ -165,13 +172,13 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
             tma_load(sb, &a.b[0], k0, n0, full);
             tma_load(sb + kBBytes / 2, &a.b[1], k0, n0, full);
           } else {
-            if (MODE == GLU_DX) {
+            if (kDx) {
               tma_load(sa, &a.a[src], k0, m0, full);
             } else {
               for (int i = 0; i < kBM / 64; ++i) tma_load(sa + i * kSlab, &a.a[t.z], m0 + i * 64, k0, full);
             }
             for (int i = 0; i < BN / 64; ++i)
-              tma_load(sb + i * kSlab, &a.b[MODE == GLU_DX ? src : 0], n0 + i * 64, k0, full);
+              tma_load(sb + i * kSlab, &a.b[kDx ? src : 0], n0 + i * 64, k0, full);
           }
         }
       }
@@ -190,10 +197,11 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
       int turn = 0;
       bool ok = true;
       for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++turn) {
-        const int acc = turn & 1;
+        const int acc = turn & 1, z = MODE == GLU_DX_PARTS ? tile / (a.m_tiles * a.n_tiles) : 0;
+        const int kb0 = first_block(z), kb1 = MODE == GLU_DX_PARTS ? first_block(z + 1) : blocks;
         ok = bar_wait(smem_addr(&sh.acc_empty[acc]), (unsigned)((turn >> 1) & 1) ^ 1, stop);
         tc_fence_after();
-        for (int kb = 0; ok && kb < blocks; ++kb, ++it) {
+        for (int kb = kb0; ok && kb < kb1; ++kb, ++it) {
           const int s = (int)(it % kStages);
           ok = bar_wait(smem_addr(&sh.full[s]), (unsigned)((it / kStages) & 1), stop);
           if (!ok) break;
@@ -202,7 +210,7 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
           const unsigned long long da = tile_desc(sa, a_mn ? kSlab : 16), db = tile_desc(sb, b_mn ? kSlab : 16);
           for (int k = 0; k < kBK / 16; ++k)   // 16 k: 32 bytes along a K-major row, 16 rows of an MN-major tile
             tc_mma(tmem + acc * BN, da + (unsigned)(k * (a_mn ? 2048 : 32) >> 4), db + (unsigned)(k * (b_mn ? 2048 : 32) >> 4),
-                   idesc, kb > 0 || k > 0);
+                   idesc, kb > kb0 || k > 0);
           tc_commit(smem_addr(&sh.empty[s]));
         }
         if (ok) tc_commit(smem_addr(&sh.acc_full[acc]));
@@ -223,7 +231,16 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
       if (!__all_sync(~0u, bar_wait(smem_addr(&sh.acc_full[acc]), (unsigned)((turn >> 1) & 1), stop))) break;
       tc_fence_after();
       const unsigned src = tmem + acc * BN + ((unsigned)(quarter * 32) << 16);
-      if constexpr (S::kStaged) {
+      if constexpr (MODE == GLU_DX_PARTS) {
+        if (row0 < a.M)
+          for (int col = 0; col < kColumns; col += 32) {
+            float v[32];
+            tmem_load32(v, src + col);
+            tmem_wait_loads();
+            float4* to = reinterpret_cast<float4*>(a.parts + ((long long)tile * kBM + quarter * 32 + lane) * BN + col);
+            for (int i = 0; i < 8; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          }
+      } else if constexpr (S::kStaged) {
         // one staged tile of 64 columns after the other, two buffers in turn
         const int pieces = kColumns / 64 * (MODE == GLU_FWD && a.save ? 3 : 1);
         for (int p = 0; p < pieces; ++p) {
@@ -297,6 +314,28 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
   if (warp == 1) {
     tc_fence_after();
     tmem_free(tmem, 2 * BN);
+  }
+}
+
+// The parts of dx added in order.  Tiles are numbered as in the kernel above.
+template <typename E, int BN> __global__ void __launch_bounds__(256) k_add_parts(const __grid_constant__ TcArgs a) {
+  const int per = a.m_tiles * a.n_tiles;
+  const int tile = blockIdx.x / (kBM / 8), row = blockIdx.x % (kBM / 8) * 8 + threadIdx.x / 32;
+  const TileAt t = tile_at<GLU_DX_PARTS>(a, tile);
+  const int y = t.m * kBM + row;
+  if (y >= a.M) return;
+  for (int col = threadIdx.x % 32 * 2; col < BN; col += 64) {
+    const int x = t.n * BN + col;
+    if (x >= a.N) continue;
+    float2 sum = make_float2(0.f, 0.f);
+    for (int z = 0; z < a.splits; ++z) {
+      const float2 v = *reinterpret_cast<const float2*>(a.parts + (((long long)z * per + tile) * kBM + row) * BN + col);
+      sum.x += v.x;
+      sum.y += v.y;
+    }
+    E* out = static_cast<E*>(a.out[0]) + y * a.ld[0] + x;
+    out[0] = from_f32<E>(sum.x);
+    if (x + 1 < a.N) out[1] = from_f32<E>(sum.y);
   }
 }
 
