@@ -181,15 +181,21 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
   bool flushed = false;
   const auto walk = [&](auto&& f) {
     hits = 0;
-    for (long long t = t0; t < t1; t += 128) {         // lane l takes ids t + 4 l .. t + 4 l + 3
+    I v[4], next[4];
+    const auto fetch = [&](long long t) {              // lane l takes ids t + 4 l .. t + 4 l + 3
       const long long first = t + lane * 4;
-      I v[4];
       if (wide && first + 4 <= t1) {
         constexpr int words = 4 * sizeof(I) / 16;
-        for (int i = 0; i < words; ++i) reinterpret_cast<uint4*>(v)[i] = __ldg(reinterpret_cast<const uint4*>(ids + first) + i);
+        for (int i = 0; i < words; ++i) reinterpret_cast<uint4*>(next)[i] = __ldg(reinterpret_cast<const uint4*>(ids + first) + i);
       } else {
-        for (int i = 0; i < 4; ++i) v[i] = first + i < t1 ? ids[first + i] : I(-1);
+        for (int i = 0; i < 4; ++i) next[i] = first + i < t1 ? ids[first + i] : I(-1);
       }
+    };
+    fetch(t0);
+    for (long long t = t0; t < t1; t += 128) {
+      const long long first = t + lane * 4;
+      for (int i = 0; i < 4; ++i) v[i] = next[i];
+      if (t + 128 < t1) fetch(t + 128);                // on its way while this step is worked on
       unsigned mine = 0;
       for (int i = 0; i < 4; ++i) {
         using U = typename std::make_unsigned<I>::type;
