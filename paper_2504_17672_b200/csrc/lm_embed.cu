@@ -197,23 +197,30 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
       for (int i = 0; i < 4; ++i) v[i] = next[i];
       if (t + 128 < t1) fetch(t + 128);                // on its way while this step is worked on
       unsigned mine = 0;
+      bool bad = false;
       for (int i = 0; i < 4; ++i) {
         using U = typename std::make_unsigned<I>::type;
         const bool there = (U)v[i] < (U)a.V;           // false for negative ids too
-        if (!there && v[i] >= 0) record(a.status, COCODC_ERR_INVALID_ARG);
+        bad |= v[i] >= (I)a.V;
         const int b = there ? (int)v[i] & mask : mask + 1;
         below += b < bin;
         mine |= (unsigned)(b == bin) << i;
       }
-      if (!__any_sync(~0u, mine)) continue;
-      int before = 0, all = 0;
-      for (int i = 0; i < 4; ++i) {
-        const unsigned m = __ballot_sync(~0u, mine >> i & 1);
-        before += __popc(m & ((1u << lane) - 1));
-        all += __popc(m);
-      }
-      for (int i = 0; i < 4; ++i)
-        if (mine >> i & 1) sh.list[warp][hits + before++] = (unsigned)(first + i - t0) << kRowBits | (unsigned)(v[i] >> a.bins_log2);
+      if (bad) record(a.status, COCODC_ERR_INVALID_ARG);
+      const unsigned with = __ballot_sync(~0u, mine != 0);
+      if (!with) continue;
+      const int n = __popc(mine);
+      const unsigned under = (1u << lane) - 1;
+      int before = __popc(with & under), all = __popc(with);
+      if (__any_sync(~0u, n > 1))
+        for (int i = 2; i <= 4; ++i) {
+          const unsigned m = __ballot_sync(~0u, n >= i);
+          before += __popc(m & under);
+          all += __popc(m);
+        }
+      if (mine)
+        for (int i = 0; i < 4; ++i)
+          if (mine >> i & 1) sh.list[warp][hits + before++] = (unsigned)(first + i - t0) << kRowBits | (unsigned)(v[i] >> a.bins_log2);
       hits += all;
       if (hits > kListLength - 128) {
         each(hits, f);
