@@ -291,7 +291,7 @@ __device__ __forceinline__ void warp_top(const unsigned long long* keys, int n, 
   __syncwarp();
 }
 
-constexpr int kUnroll = 4;           // 16-byte loads in flight per thread
+constexpr int kUnroll = 4;           // 16-byte loads in flight per thread (fp32 rows without alternatives: 6, see k_logprobs)
 constexpr int kCandidates = 1024;
 constexpr int kMaxTop = COCODC_LM_MAX_TOP;
 
@@ -322,6 +322,9 @@ struct RowShared {
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int parts) {
   using W = Words<T>;
+  // loads in flight per thread: six at fp32 (4000 x 50257: 130 -> 120 us); with alternatives, or twice the logits per word, the
+  // registers that takes cost more CTAs than it gives (bf16: 70 -> 81 us)
+  constexpr int kAhead = sizeof(T) == 4 && !TOP ? 6 : kUnroll;
   __shared__ RowShared sh;
   const long long t = blockIdx.x / parts;
   const int part = blockIdx.x - (int)(t * parts);
@@ -389,8 +392,8 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
       for (int q = 0; q < W::n / 2; ++q) add(w[k].two(q));
   };
   unsigned i = tid;
-  for (; i + (kUnroll - 1) * kThreads < n; i += kThreads * kUnroll) words_at(i, Batch<kUnroll, false>());
-  if (i + kThreads < n) words_at(i, Batch<kUnroll, true>());   // two or three words left: one round trip
+  for (; i + (kAhead - 1) * kThreads < n; i += kThreads * kAhead) words_at(i, Batch<kAhead, false>());
+  if (i + kThreads < n) words_at(i, Batch<kAhead, true>());   // the last words in one round trip
   else if (i < n) words_at(i, Batch<1, false>());
   if (tail + tid < j1) single(tail + tid);
   {
@@ -656,9 +659,12 @@ cocodc_status cocodc_lm_logprobs(cocodc_lm* lm, const void* logits, int32_t type
   if (!scope.ok) return COCODC_ERR_CUDA;
   const RowArgs a{logits, stride, T, (unsigned)V, targets, targets_type == COCODC_I64, scale, logp, entropy, lse,
                   top_k, top_ids, top_logp, lm->d_status};
-  // few rows: each over as many CTAs (a cluster) as it takes to give every SM one, but at least 4 KB of the row to each
+  // few rows: each over as many CTAs (a cluster) as it takes to give every SM one, but at least 4 KB of the row to each; to
+  // give every SM two where 48 KB remain to each (200 rows of 50257 fp32: 20 -> 14.5 us; with shorter parts the joining costs
+  // more: 64 rows of 50257 bf16 5.5 -> 6.5 us)
   int parts = 1;
   while (parts < 8 && T * parts < lm->sm_count && V * es >= 8192 * parts) parts *= 2;
+  while (parts < 8 && T * parts < 2 * lm->sm_count && V * es >= 2 * 49152 * parts) parts *= 2;
   if (T > INT32_MAX / parts) return COCODC_ERR_INVALID_ARG;
   cudaLaunchAttribute cluster{};
   cluster.id = cudaLaunchAttributeClusterDimension;
