@@ -64,7 +64,9 @@ template <int W, bool GLOBAL> __device__ __forceinline__ void get(float (&v)[W],
 }
 
 // ---- lookup ------------------------------------------------------------------------------------
-// A gather: bound by memory.  `lanes` neighbouring lanes (a power of two, up to a warp) take up to U packs of W elements each
+// A gather: bound by memory, and at fp32 tables by what L2 gives the SMs beside the writes: 65536 rows of 1024 in 39 us fp32 to
+// bfloat16 (134 MB written, 268 MB gathered, 64 MB of them from DRAM), 29 us bfloat16 to
+// bfloat16; 8 rows of 768 in 1.9 us.  `lanes` neighbouring lanes (a power of two, up to a warp) take up to U packs of W elements each
 // of one token's row, all loads before the first store; a longer row is several items.
 template <typename TIn, typename TOut, int W, int U>
 __global__ void __launch_bounds__(256) k_embed(const TIn* __restrict__ table, long long table_stride, long long V,
@@ -105,7 +107,9 @@ __global__ void __launch_bounds__(256) k_embed(const TIn* __restrict__ table, lo
 // bin begins.  The hits counted per (row, warp), a prefix sum over the counts gives every row's and warp's first
 // position, and a second run over the lists (over the ids, where a list was too short) places the tokens: equal ids
 // stay in the order of their positions because a warp's part precedes the next warp's.
-// Every CTA reads all ids, from L2 after the first: 128 CTAs and 65536 tokens of 4 bytes make 34 MB.
+// Every CTA reads all ids, from L2 after the first: 128 CTAs and 65536 tokens of 4 bytes make 34 MB.  Measured, zero rows
+// included: 28 us for 4099 tokens and 50257 rows of 768 (of which 22 us are the zeros, 144 MB), 29 us for 65536 tokens
+// and 32000 rows of 1024 (20 us the walk: issue slots and shared memory, not bytes).
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kMaxBinRows = 768;
@@ -303,6 +307,9 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
 // starts a new sum where the row changes.  A row that lies inside one group is written at once.  Rows that cross group
 // boundaries are joined in shared memory in order; those that cross tile boundaries leave their parts in the
 // workspace, and the tile that arrives last at the row's counter adds all parts in tile order (nobody waits).
+// Measured: 45 us for 65536 gradients of 1024 bfloat16 (134 MB read, 79 MB written: 4.7 TB/s), 11 us for 4099 of 768.  The
+// time not spent on bytes goes into the joins, most tiles begin and end inside a frequent token's row.  Eight loads
+// ahead instead of four spilled (62 us).
 constexpr int kGroups = 4;
 constexpr int kAhead = 4;      // loads in flight per thread
 

@@ -312,7 +312,9 @@ struct RowShared {
   unsigned tau;
 };
 
-// A row is read once.  Each thread keeps (m, s, u) of its own elements, rescaled when its largest logit grows, in
+// A row is read once: bound by memory, closely followed by the issue slots (7 instructions a logit: unpacking, fma, exponential,
+// two sums, maximum).  8192 x 50257 bfloat16 in 146-154 us (5.4-5.6 TB/s), 1333 x 32000 fp32 with five alternatives in
+// 37 us, one row of 50257 with eight in 9 us.  Each thread keeps (m, s, u) of its own elements, rescaled when its largest logit grows, in
 // batches of kUnroll 16-byte words; the parts are joined through shuffles and shared memory, and between the CTAs of a cluster (a row is
 // split over 1 to 8 CTAs, so that few rows still fill the GPU) through distributed shared memory.
 //
@@ -526,7 +528,8 @@ struct GradArgs {
   int* status;
 };
 
-// One read and one write of every logit: bound by memory.  A CTA takes a row or an even part of it.
+// One read and one write of every logit: bound by memory (8192 x 50257 bfloat16 in 288 us, 5.7 TB/s).  A CTA takes a row or
+// an even part of it: seven CTAs to a row, each with its own set-up, took 303 us.
 template <typename T> struct Out;   // packs results the way Words unpacks logits
 template <> struct Out<float> {
   static __device__ __forceinline__ uint4 of(const float (&d)[4]) {
