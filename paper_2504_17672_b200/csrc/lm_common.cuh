@@ -35,6 +35,27 @@ struct DeviceScope {
   ~DeviceScope() { if (switched) cudaSetDevice(prev); }
 };
 
+// Launches with programmatic dependence on the stream's previous kernel: the next kernel's blocks may become resident once
+// all blocks of this one have called may_follow(), and touch global memory only after wait_for_previous() (which
+// returns when the previous kernel is done and its writes are visible), so that launch and set-up hide behind its end.
+template <typename... P, typename... A>
+inline void start(void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, cudaStream_t st, unsigned cluster, const A&... args) {
+  cudaLaunchAttribute attrs[2] = {};
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = cluster;
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = grid;
+  config.blockDim = dim3(threads);
+  config.dynamicSmemBytes = smem;
+  config.stream = st;
+  config.attrs = attrs;
+  config.numAttrs = cluster > 1 ? 2 : 1;
+  cudaLaunchKernelEx(&config, kernel, P(args)...);     // a failure is found by launched()
+}
+
 inline cocodc_status launched(cocodc_lm* lm, int kernels = 1) {
   lm->launches.fetch_add(kernels, std::memory_order_relaxed);
   return cudaGetLastError() == cudaSuccess ? COCODC_OK : COCODC_ERR_CUDA;
@@ -61,6 +82,10 @@ inline Span span(const void* p, int64_t rows, int64_t stride, int64_t width, int
 inline bool meet(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
 
 // ---- device side -------------------------------------------------------------------------------
+// see start()
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void may_follow() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }

@@ -73,6 +73,8 @@ __global__ void __launch_bounds__(256) k_embed(const TIn* __restrict__ table, lo
                                                unsigned packs, int lanes_log2, unsigned items_per_row, const void* ids,
                                                int is64, long long T, float scale, TOut* __restrict__ y, long long y_stride,
                                                int* status) {
+  wait_for_previous();
+  may_follow();
   const int lanes = 1 << lanes_log2, sub = threadIdx.x & (lanes - 1);
   const long long items = T * items_per_row, step = (long long)gridDim.x * 256 >> lanes_log2;
   for (long long item = ((long long)blockIdx.x * 256 + threadIdx.x) >> lanes_log2; item < items; item += step) {
@@ -156,6 +158,8 @@ struct SortShared {
 
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
+  wait_for_previous();
+  may_follow();
   extern __shared__ __align__(16) unsigned char dyn[];
   SortShared& sh = *reinterpret_cast<SortShared*>(dyn);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -315,6 +319,8 @@ constexpr int kAhead = 4;      // loads in flight per thread
 
 template <typename TIn, typename TOut, int W>
 __global__ void __launch_bounds__(kGroups * 128, 2) k_embed_sum(const GradArgs a) {
+  wait_for_previous();
+  may_follow();
   extern __shared__ __align__(16) float part[];                       // [kGroups][2][threads of a group][W]: head, tail
   __shared__ int pending_row[2], is_last[2], pending_first[2], pending_parts[2];
   __shared__ int edge[2 * kGroups + 2];                 // rows of: the entry before the tile, each group's first and last, the entry after
@@ -536,7 +542,7 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
         while (lanes_log2 < 5 && (1u << lanes_log2) < packs) ++lanes_log2;
         const unsigned per_row = (packs + (U << lanes_log2) - 1) / (U << lanes_log2);
         const long long blocks = (((T * per_row) << lanes_log2) + 255) / 256;
-        kernel<<<(unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st>>>(
+        start(kernel, (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st, 1,
             static_cast<const TIn*>(table), table_stride, V, packs, lanes_log2, per_row, ids, ids_type == COCODC_I64, T, scale,
             static_cast<TOut*>(y), y_stride, lm->d_status);
       };
@@ -614,8 +620,8 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
   a.bins_log2 = bins_log2_for(V);
   a.bin_rows = (int)bin_rows_for(V);
   const unsigned bins = 1u << a.bins_log2, smem_sort = (unsigned)sizeof(SortShared) + a.bin_rows * kBinPitch * 4;
-  if (a.is64) k_embed_sort<long long><<<bins, kSortThreads, smem_sort, st>>>(a);
-  else k_embed_sort<int><<<bins, kSortThreads, smem_sort, st>>>(a);
+  if (a.is64) start(k_embed_sort<long long>, bins, kSortThreads, smem_sort, st, 1, a);
+  else start(k_embed_sort<int>, bins, kSortThreads, smem_sort, st, 1, a);
   if (T > 0)
     with_type(dy_type, [&](auto in) {
       return with_type(dtable_type, [&](auto out) {
@@ -623,8 +629,8 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
         using TOut = decltype(out);
         const dim3 grid((unsigned)tiles, (unsigned)columns);
         const unsigned smem = kGroups * 2 * width * W * sizeof(float);
-        if (W > 1) k_embed_sum<TIn, TOut, 16 / (int)sizeof(TIn)><<<grid, kGroups * width, smem, st>>>(a);
-        else k_embed_sum<TIn, TOut, 1><<<grid, kGroups * width, smem, st>>>(a);
+        if (W > 1) start(k_embed_sum<TIn, TOut, 16 / (int)sizeof(TIn)>, grid, kGroups * width, smem, st, 1, a);
+        else start(k_embed_sum<TIn, TOut, 1>, grid, kGroups * width, smem, st, 1, a);
         return true;
       });
     });

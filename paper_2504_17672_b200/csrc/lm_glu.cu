@@ -74,6 +74,8 @@ template <typename T> struct PlainArgs {
 
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) k_glu_plain(const PlainArgs<T> p) {
+  wait_for_previous();
+  may_follow();
   __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
   const long long m0 = (long long)blockIdx.x * kTile, n0 = (long long)blockIdx.y * kTile;
   float g[4][4] = {}, u[4][4] = {};
@@ -94,6 +96,8 @@ __global__ void __launch_bounds__(256) k_glu_plain(const PlainArgs<T> p) {
 // SUM: one output, both sources added (dx); otherwise source and output z (dwg, dwu)
 template <typename T, bool SUM>
 __global__ void __launch_bounds__(256) k_product_plain(const PlainArgs<T> p) {
+  wait_for_previous();
+  may_follow();
   __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
   const long long m0 = (long long)blockIdx.x * kTile, n0 = (long long)blockIdx.y * kTile;
   const int z = blockIdx.z;
@@ -160,6 +164,8 @@ template <typename E> struct FewArgs {
 
 template <typename E, int ACT, int TILES>
 __global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : TILES == 2 ? 3 : 2) k_glu_few(const FewArgs<E> p) {
+  wait_for_previous();
+  may_follow();
   constexpr int kBlocks = TILES <= 2 ? 4 : 2;                     // k blocks in flight per warp
   __shared__ float sums[kFewWarps][2][TILES * 8 * 8];             // [warp][gate, up][token, column]
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, q = lane % 4;
@@ -242,6 +248,8 @@ template <typename T, int ACT, bool WIDE>
 __global__ void __launch_bounds__(256) k_glu_slope(const T* __restrict__ dh, long long dh_stride, const T* __restrict__ gate,
                                                    const T* __restrict__ up, long long gu_stride, long long rows, unsigned F,
                                                    T* __restrict__ dg, T* __restrict__ du, long long pitch) {
+  wait_for_previous();
+  may_follow();
   constexpr unsigned W = WIDE ? 8 : 1;
   const unsigned packs = (F + W - 1) / W;
   const long long blocks = (rows * packs + 255) / 256;
@@ -328,7 +336,7 @@ template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t strid
 template <typename E, int MODE, int ACT, int BN> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
   const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices, most = (long long)TcShape<BN>::kPerSm * lm->sm_count;
   if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;
-  k_glu_tc<E, MODE, ACT, BN><<<(unsigned)(tiles < most ? tiles : most), kTcThreads, TcShape<BN>::kSmem, st>>>(a);
+  start(k_glu_tc<E, MODE, ACT, BN>, (unsigned)(tiles < most ? tiles : most), kTcThreads, TcShape<BN>::kSmem, st, 1, a);
   return launched(lm);
 }
 
@@ -415,9 +423,9 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
       const FewArgs<E> p{static_cast<const E*>(x), static_cast<const E*>(wg), static_cast<const E*>(wu), x_stride, w_stride,
                          (int)T, (int)D, (int)F, static_cast<E*>(h), static_cast<E*>(gate), static_cast<E*>(up), h_stride, gu_stride};
       const unsigned grid = (unsigned)((F + 7) / 8);
-      if (T <= 8) k_glu_few<E, A, 1><<<grid, kFewWarps * 32, 0, st>>>(p);
-      else if (T <= 16) k_glu_few<E, A, 2><<<grid, kFewWarps * 32, 0, st>>>(p);
-      else k_glu_few<E, A, 4><<<grid, kFewWarps * 32, 0, st>>>(p);
+      if (T <= 8) start(k_glu_few<E, A, 1>, grid, kFewWarps * 32, 0, st, 1, p);
+      else if (T <= 16) start(k_glu_few<E, A, 2>, grid, kFewWarps * 32, 0, st, 1, p);
+      else start(k_glu_few<E, A, 4>, grid, kFewWarps * 32, 0, st, 1, p);
       result = launched(lm);
       return;
     }
@@ -456,7 +464,7 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
     p.ld = h_stride;
     p.ld_gu = gu_stride;
     const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((F + kTile - 1) / kTile));
-    k_glu_plain<E, decltype(a)::value><<<grid, 256, 0, st>>>(p);
+    start(k_glu_plain<E, decltype(a)::value>, grid, 256, 0, st, 1, p);
     result = launched(lm);
   });
   return result;
@@ -510,7 +518,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       const bool wide = rows_aligned(dh, dh_stride, 2) && rows_aligned(gate, gu_stride, 2) && rows_aligned(up, gu_stride, 2);
       const auto slope = [&](auto kernel, int W) {
         const long long blocks = (T * ((F + W - 1) / W) + 255) / 256;
-        kernel<<<(unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st>>>(
+        start(kernel, (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st, 1,
             static_cast<const E*>(dh), dh_stride, static_cast<const E*>(gate), static_cast<const E*>(up), gu_stride, T,
             (unsigned)F, dg, du, pitch);
       };
@@ -552,7 +560,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
         const auto in_parts = [&](auto w) {
           constexpr int BN = decltype(w)::value;
           took(run_tc<E, GLU_DX_PARTS, 0, BN>(lm, c, st));
-          k_add_parts<E, BN><<<(unsigned)(c.m_tiles * c.n_tiles * (kBM / 8)), 256, 0, st>>>(c);
+          start(k_add_parts<E, BN>, (unsigned)(c.m_tiles * c.n_tiles * (kBM / 8)), 256, 0, st, 1, c);
           took(launched(lm));
         };
         if (width == 64) in_parts(std::integral_constant<int, 64>());
@@ -568,7 +576,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       p.out[0] = static_cast<E*>(dx);
       p.ld = dx_stride;
       const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile));
-      k_product_plain<E, true><<<grid, 256, 0, st>>>(p);
+      start(k_product_plain<E, true>, grid, 256, 0, st, 1, p);
       took(launched(lm));
     }
     if (dwg && tensor_dw && T > 0) {
@@ -596,7 +604,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       p.out[1] = static_cast<E*>(dwu);
       p.ld = dw_stride;
       const dim3 grid((unsigned)((F + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile), 2);
-      k_product_plain<E, false><<<grid, 256, 0, st>>>(p);
+      start(k_product_plain<E, false>, grid, 256, 0, st, 1, p);
       took(launched(lm));
     }
   });

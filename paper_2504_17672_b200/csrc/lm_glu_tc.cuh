@@ -149,10 +149,14 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
     sh.stop = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // Before TMEM is taken: a block that held it while it waited could starve a block of the kernel it waits for; and only
+  // then may the next kernel's blocks come.
+  wait_for_previous();
   if (warp == 1) tmem_alloc(smem_addr(&sh.tmem), 2 * BN);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  may_follow();
   const unsigned tmem = sh.tmem;
   volatile int* stop = &sh.stop;
 
@@ -323,6 +327,8 @@ __global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(cons
 
 // The parts of dx added in order.  Tiles are numbered as in the kernel above.
 template <typename E, int BN> __global__ void __launch_bounds__(256) k_add_parts(const __grid_constant__ TcArgs a) {
+  wait_for_previous();
+  may_follow();
   const int per = a.m_tiles * a.n_tiles;
   const int tile = blockIdx.x / (kBM / 8), row = blockIdx.x % (kBM / 8) * 8 + threadIdx.x / 32;
   const TileAt t = tile_at<GLU_DX_PARTS>(a, tile);

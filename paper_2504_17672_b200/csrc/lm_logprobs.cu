@@ -323,6 +323,8 @@ struct RowShared {
 // is read again (from L2), and of it only logits >= tau are sorted, by value and position.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int parts) {
+  wait_for_previous();
+  may_follow();
   using W = Words<T>;
   // loads in flight per thread: six at fp32 (4000 x 50257: 130 -> 120 us); with alternatives, or twice the logits per word, the
   // registers that takes cost more CTAs than it gives (bf16: 70 -> 81 us)
@@ -557,6 +559,8 @@ template <> struct Out<__half> {
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 8) k_logprobs_grad(const GradArgs a, unsigned chunks) {
+  wait_for_previous();
+  may_follow();
   constexpr int n = 16 / sizeof(T);
   const long long t = blockIdx.x / chunks;
   const unsigned chunk = blockIdx.x - (unsigned)(t * chunks);
@@ -669,23 +673,13 @@ cocodc_status cocodc_lm_logprobs(cocodc_lm* lm, const void* logits, int32_t type
   while (parts < 8 && T * parts < lm->sm_count && V * es >= 8192 * parts) parts *= 2;
   while (parts < 8 && T * parts < 2 * lm->sm_count && V * es >= 2 * 49152 * parts) parts *= 2;
   if (T > INT32_MAX / parts) return COCODC_ERR_INVALID_ARG;
-  cudaLaunchAttribute cluster{};
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = (unsigned)parts;
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-  cudaLaunchConfig_t config{};
-  config.gridDim = dim3((unsigned)(T * parts));
-  config.blockDim = dim3(kThreads);
-  config.stream = static_cast<cudaStream_t>(stream);
-  config.attrs = &cluster;
-  config.numAttrs = 1;
-  const bool ok = with_type(type, [&](auto x) {
+  with_type(type, [&](auto x) {
     using E = decltype(x);
-    return (top_k ? cudaLaunchKernelEx(&config, k_logprobs<E, true>, a, parts)
-                  : cudaLaunchKernelEx(&config, k_logprobs<E, false>, a, parts)) == cudaSuccess;
+    start(top_k ? k_logprobs<E, true> : k_logprobs<E, false>, (unsigned)(T * parts), kThreads, 0,
+          static_cast<cudaStream_t>(stream), (unsigned)parts, a, parts);
+    return true;
   });
-  const cocodc_status s = launched(lm);
-  return ok ? s : COCODC_ERR_CUDA;
+  return launched(lm);
 }
 
 cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t type, int64_t stride, int64_t T,
@@ -720,7 +714,7 @@ cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t
   const GradArgs a{logits, stride, T, (unsigned)V, targets, targets_type == COCODC_I64, scale, lse, entropy, dlogp,
                    dentropy, dlogits, dlogits_stride, lm->d_status};
   with_type(type, [&](auto x) {
-    k_logprobs_grad<decltype(x)><<<(unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, (unsigned)chunks);
+    start(k_logprobs_grad<decltype(x)>, (unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream), 1, a, (unsigned)chunks);
     return true;
   });
   return launched(lm);
