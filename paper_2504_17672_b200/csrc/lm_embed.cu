@@ -164,8 +164,8 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
   SortShared& sh = *reinterpret_cast<SortShared*>(dyn);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int bin = blockIdx.x, mask = (1 << a.bins_log2) - 1;
-  const long long part = ((a.T + kSortWarps - 1LL) / kSortWarps + 127) / 128 * 128;
-  const long long t0 = warp * part, t1 = min((long long)a.T, t0 + part);
+  const int part = ((a.T + kSortWarps - 1) / kSortWarps + 127) / 128 * 128;       // T <= kMostTokens: no overflow
+  const int t0 = warp * part, t1 = min(a.T, t0 + part);
   const I* ids = static_cast<const I*>(a.ids);
   const bool wide = ((uintptr_t)ids & 15) == 0;
 
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
     for (int i = 0; i < n; i += 32) {
       const unsigned e = sh.list[warp][min(i + lane, n - 1)];
       const int row = i + lane < n ? (int)(e & ((1u << kRowBits) - 1)) : -1;
-      f((int)(t0 + (e >> kRowBits)), row, __match_any_sync(~0u, row));
+      f(t0 + (int)(e >> kRowBits), row, __match_any_sync(~0u, row));
       __syncwarp();
     }
   };
@@ -190,8 +190,8 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
   const auto walk = [&](auto&& f) {
     hits = 0;
     I v[4], next[4];
-    const auto fetch = [&](long long t) {              // lane l takes ids t + 4 l .. t + 4 l + 3
-      const long long first = t + lane * 4;
+    const auto fetch = [&](int t) {                    // lane l takes ids t + 4 l .. t + 4 l + 3
+      const int first = t + lane * 4;
       if (wide && first + 4 <= t1) {
         constexpr int words = 4 * sizeof(I) / 16;
         for (int i = 0; i < words; ++i) reinterpret_cast<uint4*>(next)[i] = __ldg(reinterpret_cast<const uint4*>(ids + first) + i);
@@ -200,8 +200,8 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
       }
     };
     fetch(t0);
-    for (long long t = t0; t < t1; t += 128) {
-      const long long first = t + lane * 4;
+    for (int t = t0; t < t1; t += 128) {
+      const int first = t + lane * 4;
       for (int i = 0; i < 4; ++i) v[i] = next[i];
       if (t + 128 < t1) fetch(t + 128);                // on its way while this step is worked on
       unsigned mine = 0;
@@ -497,6 +497,12 @@ int bins_log2_for(int64_t V) {
   while ((V + (int64_t(1) << l) - 1) >> l > kMaxBinRows) ++l;
   return l;
 }
+// At least more than half of an SM's shared memory: a block that starts while the previous kernel ends must not join
+// another one on an SM that happens to be free first (65536 tokens: 77 -> 96 us for the whole gradient)
+unsigned sort_smem(int bin_rows) {
+  const unsigned need = (unsigned)sizeof(SortShared) + bin_rows * kBinPitch * 4, alone = 120 * 1024;
+  return need > alone ? need : alone;
+}
 int64_t bin_rows_for(int64_t V) { return (V + (int64_t(1) << bins_log2_for(V)) - 1) >> bins_log2_for(V); }
 int64_t starts_for(int64_t V) { return (bin_rows_for(V) << bins_log2_for(V)) + 1; }
 int64_t padded(int64_t D) { return (D + 7) / 8 * 8; }
@@ -506,7 +512,7 @@ int64_t tiles_for(int64_t T) { return (T + kGroups * positions_for(T) - 1) / (kG
 
 namespace cocodc_lm_impl {
 bool embed_prepare() {
-  const int most = (int)sizeof(SortShared) + kMaxBinRows * kBinPitch * 4;
+  const int most = (int)sort_smem(kMaxBinRows);
   return cudaFuncSetAttribute(k_embed_sort<int>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
          cudaFuncSetAttribute(k_embed_sort<long long>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
 }
@@ -619,7 +625,7 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
   a.n_arrived = tiles * columns;
   a.bins_log2 = bins_log2_for(V);
   a.bin_rows = (int)bin_rows_for(V);
-  const unsigned bins = 1u << a.bins_log2, smem_sort = (unsigned)sizeof(SortShared) + a.bin_rows * kBinPitch * 4;
+  const unsigned bins = 1u << a.bins_log2, smem_sort = sort_smem(a.bin_rows);
   if (a.is64) start(k_embed_sort<long long>, bins, kSortThreads, smem_sort, st, 1, a);
   else start(k_embed_sort<int>, bins, kSortThreads, smem_sort, st, 1, a);
   if (T > 0)

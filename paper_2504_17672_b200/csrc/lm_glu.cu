@@ -334,7 +334,7 @@ template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t strid
 
 
 template <typename E, int MODE, int ACT, int BN> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
-  const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices, most = (long long)TcShape<BN>::kPerSm * lm->sm_count;
+  const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices, most = lm->sm_count;
   if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;
   start(k_glu_tc<E, MODE, ACT, BN>, (unsigned)(tiles < most ? tiles : most), kTcThreads, TcShape<BN>::kSmem, st, 1, a);
   return launched(lm);

@@ -49,11 +49,10 @@ constexpr unsigned kSlab = 64 * kBK * 2;            // an MN-major operand's 64 
 constexpr unsigned kOutBytes = 32 * 128;            // one warp's staged output: 32 rows of 64 columns
 template <int BN> struct TcShape {
   static constexpr unsigned kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
-  // wide tiles: all shared memory in one CTA, outputs staged for TMA stores; narrow ones: two CTAs per SM, outputs from registers
+  // one CTA per SM; wide tiles stage their outputs for TMA stores, narrow ones write them from registers
   static constexpr bool kStaged = BN >= 128;
-  static constexpr int kStages = BN == 128 ? 6 : 4;
+  static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
   static constexpr unsigned kSmem = 1024 + kStages * kStageBytes + (kStaged ? 4 * 2 * kOutBytes : 0);
-  static constexpr int kPerSm = kStaged ? 1 : 2;
 };
 // Tiles of consecutive rows that go through one column of tiles in turn.  Under the power cap, where fewer bytes from L2 mean
 // a higher clock, 8 / 16 / 32 / 64 of them took 740 / 706 / 687 / 697 us forward (8192 x 3200 x 8640) and 8 / 16 / 32 took
@@ -61,7 +60,7 @@ template <int BN> struct TcShape {
 template <int MODE> constexpr int kGroupM = MODE == GLU_FWD ? 32 : 8;
 
 struct TcShared {
-  unsigned long long full[6], empty[6], acc_full[2], acc_empty[2], drain;
+  unsigned long long full[8], empty[8], acc_full[2], acc_empty[2], drain;
   unsigned tmem;
   int stop;
 };
@@ -121,7 +120,7 @@ __device__ __forceinline__ void stage32(unsigned buf, int row, int half, const u
 }
 
 template <typename E, int MODE, int ACT, int BN>
-__global__ void __launch_bounds__(kTcThreads, TcShape<BN>::kPerSm) k_glu_tc(const __grid_constant__ TcArgs a) {
+__global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant__ TcArgs a) {
   extern __shared__ unsigned char dyn[];
   __shared__ TcShared sh;
   using S = TcShape<BN>;
