@@ -20,8 +20,9 @@
  *   - Calls are asynchronous on the given stream and allocate nothing.  Calls that need scratch take it as a
  *     workspace (16-byte aligned, at least cocodc_lm_*_workspace bytes, contents arbitrary and undefined
  *     afterwards).  Nothing is kept from one call for the next, so one handle may be used on several streams
- *     and from several threads at the same time as long as the calls' workspaces differ.
- *   - T = 0 (no tokens) is legal everywhere.
+ *     and from several threads at the same time as long as the calls' workspaces differ.  Kernels are launched with
+ *     programmatic dependence on the stream's previous kernel; they touch no memory before it has finished.
+ *   - T = 0 (no tokens) is legal everywhere; pointers to nothing may then be NULL or not.
  *   - Token ids: a negative id means "no token here" (padding, ignored target).  An id >= V is an error that
  *     the kernel finds: it is treated as a negative one and COCODC_ERR_INVALID_ARG is recorded in the status
  *     word (cocodc_lm_poll_status).  It never leads to an access outside a buffer.
@@ -102,7 +103,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
                                  void* workspace, uint64_t workspace_bytes, void* stream);
 
 /*
- * Row t of logits [T][V] (any type) gives z = scale * logits[t] (scale > 0: one over the temperature) and
+ * Row t of logits [T][V] (any type) gives z = scale * logits[t] (0 < scale <= 1e30: one over the temperature) and
  *   lse[t]     = log sum_j exp(z_j)
  *   logp[t]    = z_y - lse, y = targets[t]; 0 where y < 0
  *   entropy[t] = lse - sum_j p_j z_j,  p_j = exp(z_j - lse)

@@ -396,8 +396,8 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
       !sane(T) || !sane(D) || !sane(F) || T > INT32_MAX || D < 1 || D > INT32_MAX || F < 1 || F > INT32_MAX ||
       x_stride < D || w_stride < D || h_stride < F || !sane(x_stride) || !sane(w_stride) || !sane(h_stride))
     return COCODC_ERR_INVALID_ARG;
-  if ((gate == nullptr) != (up == nullptr) || (gate && (gu_stride < F || !sane(gu_stride)))) return COCODC_ERR_INVALID_ARG;
   if (T == 0) return COCODC_OK;
+  if ((gate == nullptr) != (up == nullptr) || (gate && (gu_stride < F || !sane(gu_stride)))) return COCODC_ERR_INVALID_ARG;
   if (!x || !wg || !wu || !h || !tiles_fit(T, F)) return COCODC_ERR_INVALID_ARG;
   for (const void* p : {x, wg, wu, (const void*)h, (const void*)gate, (const void*)up})
     if (!on_boundary(p, 2)) return COCODC_ERR_ALIGNMENT;
@@ -484,8 +484,9 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       !sane(T) || !sane(D) || !sane(F) || T > INT32_MAX || D < 1 || D > INT32_MAX || F < 1 || F > INT32_MAX ||
       x_stride < D || w_stride < D || dh_stride < F || gu_stride < F || !sane(x_stride) || !sane(w_stride) ||
       !sane(dh_stride) || !sane(gu_stride) || (dx && (dx_stride < D || !sane(dx_stride))) ||
-      (dwg == nullptr) != (dwu == nullptr) || (dwg && (dw_stride < D || !sane(dw_stride))) || (!dx && !dwg))
+      (dwg == nullptr) != (dwu == nullptr) || (dwg && (dw_stride < D || !sane(dw_stride))))
     return COCODC_ERR_INVALID_ARG;
+  if (!dx && !dwg) return T == 0 ? COCODC_OK : COCODC_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < cocodc_lm_glu_grad_workspace(T, D, F)) return COCODC_ERR_INVALID_ARG;
   if (T > 0 && (!dh || !gate || !up || (dwg && !x) || (dx && (!wg || !wu)))) return COCODC_ERR_INVALID_ARG;
   if (!tiles_fit(T, D) || !tiles_fit(F, D)) return COCODC_ERR_INVALID_ARG;

@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr float kMostScale = 1e30f;   // times log2 e still finite
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // A logit as a 32-bit number with the same order (NaN above +Inf, -0 equal to +0), and with the position behind it
@@ -643,12 +644,12 @@ cocodc_status cocodc_lm_logprobs(cocodc_lm* lm, const void* logits, int32_t type
                                  const void* targets, int32_t targets_type, float scale, float* logp, float* entropy,
                                  float* lse, int32_t top_k, int32_t* top_ids, float* top_logp, void* stream) {
   if (!lm || !known_type(type) || !sane(T) || T > INT32_MAX || V < 1 || V > INT32_MAX || stride < V || !sane(stride) ||
-      !(scale > 0.f) || scale > 3.4e38f || top_k < 0 || top_k > COCODC_LM_MAX_TOP || top_k > V)
-    return COCODC_ERR_INVALID_ARG;
-  if ((targets == nullptr) != (logp == nullptr) || (top_k > 0 && T > 0) != (top_ids != nullptr && top_logp != nullptr) ||
-      (targets && targets_type != COCODC_I32 && targets_type != COCODC_I64))
+      !(scale > 0.f && scale <= kMostScale) || top_k < 0 || top_k > COCODC_LM_MAX_TOP || top_k > V)
     return COCODC_ERR_INVALID_ARG;
   if (T == 0) return COCODC_OK;
+  if ((targets == nullptr) != (logp == nullptr) || (top_k > 0) != (top_ids != nullptr) || (top_k > 0) != (top_logp != nullptr) ||
+      (targets && targets_type != COCODC_I32 && targets_type != COCODC_I64))
+    return COCODC_ERR_INVALID_ARG;
   if (!logits || (!logp && !entropy && !lse && top_k == 0)) return COCODC_ERR_INVALID_ARG;
   const int es = type_bytes(type);
   if (!on_boundary(logits, es) || (targets && !on_boundary(targets, index_bytes(targets_type))) || !on_boundary(logp, 4) ||
@@ -687,7 +688,7 @@ cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t
                                       const float* lse, const float* entropy, const float* dlogp,
                                       const float* dentropy, void* dlogits, int64_t dlogits_stride, void* stream) {
   if (!lm || !known_type(type) || !sane(T) || T > INT32_MAX || V < 1 || V > INT32_MAX || stride < V || !sane(stride) ||
-      dlogits_stride < V || !sane(dlogits_stride) || !(scale > 0.f) || scale > 3.4e38f)
+      dlogits_stride < V || !sane(dlogits_stride) || !(scale > 0.f && scale <= kMostScale))
     return COCODC_ERR_INVALID_ARG;
   if (T == 0) return COCODC_OK;
   if (!logits || !lse || !dlogits || (!dlogp && !dentropy) || (targets == nullptr) != (dlogp == nullptr) ||

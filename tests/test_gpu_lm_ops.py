@@ -613,6 +613,36 @@ def test_offsets_beyond_32_bits(ops):
     assert torch.equal(d, far)
 
 
+def test_no_rows_of_something(ops):
+    """T = 0 as a slice of a longer buffer (its address is not NULL) and as an empty tensor (its address is)."""
+    before = ops.launch_count
+    for cut in (lambda t: t[:0], lambda t: torch.empty(0, *t.shape[1:], dtype=t.dtype, device="cuda")):
+        x, h, w = cut(torch.ones(4, 16, dtype=BF16, device="cuda")), cut(torch.ones(4, 24, dtype=BF16, device="cuda")), torch.ones(24, 16, dtype=BF16, device="cuda")
+        ids, f = cut(torch.zeros(4, dtype=torch.int64, device="cuda")), cut(torch.zeros(4, device="cuda"))
+        ti, tl = cut(torch.zeros(4, 3, dtype=torch.int32, device="cuda")), cut(torch.zeros(4, 3, device="cuda"))
+        empty = torch.empty(0, device="cuda")
+        ops.cocodc_lm_embed(w, ids, x)
+        ops.cocodc_lm_glu(x, w, w, h, gate=h, up=torch.empty(0, 24, dtype=BF16, device="cuda"))
+        ops.cocodc_lm_logprobs(x, ids, empty, entropy=f, lse=empty, top_ids=ti, top_logp=tl)
+        ops.cocodc_lm_logprobs_grad(x, ids, f, empty, f, empty, x)
+        ops.cocodc_lm_glu_grad(h, h, h, x, w, w, dx=torch.empty(0, 16, dtype=BF16, device="cuda"))
+    assert ops.launch_count == before
+
+
+def test_long_masked_stretches_over_several_blocks(ops):
+    """Few rows are split over blocks; whole parts masked, a part with the only NaN, alternatives from one part alone."""
+    V = 40000
+    g = gen(12)
+    base = randn(g, 4, V, dtype=BF16)
+    targets = torch.tensor([5, V - 1, V // 2, 0], device="cuda")
+    for lo, hi in ((0, V - 3000), (3000, V), (1000, V - 1000)):
+        x = base.clone()
+        x[:, lo:hi] = -math.inf
+        check_logprobs(ops, x, targets, 1.0, 20)
+        x[2, hi - 1 if hi == V else lo] = math.nan
+        check_logprobs(ops, x, targets, 1.0, 20)
+
+
 # ------------------------------------------------------------------------------------------------------------- refusals
 
 def test_refusals(B, ops):
@@ -644,6 +674,8 @@ def test_refusals(B, ops):
     refused(inv, ops.cocodc_lm_logprobs, x, ids, f, scale=0.0)
     refused(inv, ops.cocodc_lm_logprobs, x, ids, f, scale=float("nan"))
     refused(inv, ops.cocodc_lm_logprobs, x, ids, f, scale=float("inf"))
+    refused(inv, ops.cocodc_lm_logprobs, x, ids, f, scale=1e31)
+    refused(inv, ops.cocodc_lm_logprobs, x, None, None, lse=f, top_ids=torch.empty(4, 2, dtype=torch.int32, device="cuda"))   # no top_logp
     refused(alias, ops.cocodc_lm_logprobs, x, ids, f, lse=f)
     for k in (17, 33):                                                               # more than V, more than the limit
         refused(inv, ops.cocodc_lm_logprobs, x if k == 17 else w.view(4, 96), None, None,
