@@ -133,6 +133,18 @@ cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t
                                       const float* lse, const float* entropy, const float* dlogp,
                                       const float* dentropy, void* dlogits, int64_t dlogits_stride, void* stream);
 
+/*
+ * The calls above with their arguments in one record of 64-bit words, for bindings that pay for every argument of a
+ * foreign call (sixteen of them cost a microsecond more than one): record[0] is the operator, then come its
+ * arguments in the order of its declaration, without the handle: pointers and integers as int64_t, scale as a
+ * double.  Returns what the call returns; INVALID_ARG for an unknown operator.
+ */
+typedef enum {
+  COCODC_LM_EMBED = 0, COCODC_LM_EMBED_GRAD = 1, COCODC_LM_GLU = 2, COCODC_LM_GLU_GRAD = 3, COCODC_LM_LOGPROBS = 4,
+  COCODC_LM_LOGPROBS_GRAD = 5
+} cocodc_lm_operator;
+cocodc_status cocodc_lm_submit(cocodc_lm* lm, const void* record);
+
 #ifdef __cplusplus
 }
 #endif

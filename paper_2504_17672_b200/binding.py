@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -33,7 +34,7 @@ EXPORTS = (
     "cocodc_lm_create", "cocodc_lm_destroy", "cocodc_lm_poll_status", "cocodc_lm_launch_count",
     "cocodc_lm_embed", "cocodc_lm_embed_grad", "cocodc_lm_embed_grad_workspace",
     "cocodc_lm_glu", "cocodc_lm_glu_grad", "cocodc_lm_glu_grad_workspace",
-    "cocodc_lm_logprobs", "cocodc_lm_logprobs_grad",
+    "cocodc_lm_logprobs", "cocodc_lm_logprobs_grad", "cocodc_lm_submit",
 )
 NOALLOC_MAX_K, NOALLOC_MAX_SEGMENTS = 64, 64
 
@@ -128,6 +129,7 @@ def _load() -> ctypes.CDLL:
     lib.cocodc_lm_glu_grad_workspace.argtypes = [i64, i64, i64]
     lib.cocodc_lm_logprobs.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, i32, vp, vp, vp]
     lib.cocodc_lm_logprobs_grad.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, i64, vp]
+    lib.cocodc_lm_submit.argtypes = [vp, ctypes.c_char_p]
     other = {"cocodc_launch_count": i64, "cocodc_status_string": ctypes.c_char_p, "cocodc_lm_launch_count": i64,
              "cocodc_lm_embed_grad_workspace": u64, "cocodc_lm_glu_grad_workspace": u64}
     for name, restype in other.items():
@@ -373,6 +375,10 @@ LM_MAX_TOP = 32
 _ACTS = {"silu": ACT_SILU, "gelu": ACT_GELU, ACT_SILU: ACT_SILU, ACT_GELU: ACT_GELU}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
+# records of cocodc_lm_submit: the operator's number, then its arguments (q: pointer or integer, d: scale)
+_EMBED, _EMBED_GRAD, _GLU, _GLU_GRAD, _LOGPROBS, _LOGPROBS_GRAD = (
+    struct.Struct("=" + f).pack for f in ("9qd4q", "9qd7q", "17q", "24q", "8qd7q", "8qd7q"))
+_submit = _lib.cocodc_lm_submit
 
 
 def _raw_stream(index: int) -> int:
@@ -394,10 +400,10 @@ def _matrix(t: torch.Tensor, name: str):
     return t.data_ptr(), (s0 if rows > 1 or s0 > cols else cols), rows, cols
 
 
-def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype) -> Optional[int]:
-    """Address of a packed vector (or matrix) of n elements; None for None."""
+def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype) -> int:
+    """Address of a packed vector (or matrix) of n elements; 0 for None."""
     if t is None:
-        return None
+        return 0
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a packed {dtype} tensor of {n} elements")
     return t.data_ptr()
@@ -491,8 +497,7 @@ class LmOps:
         if cols != D:
             _sized("y", T, cols, T, D)
         ip, it = _ids(ids, "ids", T)
-        code = _lib.cocodc_lm_embed(self._h, tp, _type(table), ts, V, D, ip, it, T, scale, yp, _type(y), ys,
-                                    self._stream(stream))
+        code = _submit(self._h, _EMBED(0, tp, _type(table), ts, V, D, ip, it, T, scale, yp, _type(y), ys, self._stream(stream)))
         if code:
             raise CocodcError(code, "cocodc_lm_embed")
 
@@ -506,8 +511,8 @@ class LmOps:
             _sized("dy", T, cols, T, D)
         ip, it = _ids(ids, "ids", T)
         w = self._scratch(workspace, _lib.cocodc_lm_embed_grad_workspace(V, D, T), stream)
-        code = _lib.cocodc_lm_embed_grad(self._h, dp, _type(dy), ds, ip, it, T, V, D, scale, int(accumulate), gp,
-                                         _type(dtable), gs, w.data_ptr(), w.numel() * w.element_size(), self._stream(stream))
+        code = _submit(self._h, _EMBED_GRAD(1, dp, _type(dy), ds, ip, it, T, V, D, scale, bool(accumulate), gp, _type(dtable), gs,
+                                            w.data_ptr(), w.numel() * w.element_size(), self._stream(stream)))
         if code:
             raise CocodcError(code, "cocodc_lm_embed_grad")
 
@@ -525,7 +530,7 @@ class LmOps:
         if gs != us and F > 1:
             raise ValueError("wg and wu must have the same row stride")
         kind = _one_type(x, wg, wu, h, gate, up)
-        gtp = utp = None
+        gtp = utp = 0
         gus = F
         if gate is not None or up is not None:
             self._on_device(gate, up)
@@ -539,8 +544,7 @@ class LmOps:
             gus = strides[0]
             if strides[-1] != gus and T > 1:
                 raise ValueError("gate and up must have the same row stride")
-        code = _lib.cocodc_lm_glu(self._h, _ACTS[act], kind, xp, xs, gp, up_, gs, T, D, F, hp, hs, gtp, utp, gus,
-                                  self._stream(stream))
+        code = _submit(self._h, _GLU(2, _ACTS[act], kind, xp, xs, gp, up_, gs, T, D, F, hp, hs, gtp, utp, gus, self._stream(stream)))
         if code:
             raise CocodcError(code, "cocodc_lm_glu")
 
@@ -555,7 +559,7 @@ class LmOps:
 
         def take(t, name, rows, cols):
             if t is None:
-                return None, cols
+                return 0, cols
             p, stride, r, c = _matrix(t, name)
             _sized(name, r, c, rows, cols)
             return p, stride
@@ -570,8 +574,8 @@ class LmOps:
         if dwg is not None and dwu is not None and dws != dws2 and F > 1:
             raise ValueError("dwg and dwu must have the same row stride")
         w = self._scratch(workspace, _lib.cocodc_lm_glu_grad_workspace(T, D, F), stream)
-        code = _lib.cocodc_lm_glu_grad(self._h, _ACTS[act], kind, hp, hs, gtp, utp, gs, xp, xs, gp, wup, ws, T, D, F, dxp, dxs,
-                                       dgp, dup, dws, w.data_ptr(), w.numel() * w.element_size(), self._stream(stream))
+        code = _submit(self._h, _GLU_GRAD(3, _ACTS[act], kind, hp, hs, gtp, utp, gs, xp, xs, gp, wup, ws, T, D, F, dxp, dxs, dgp, dup,
+                                          dws, w.data_ptr(), w.numel() * w.element_size(), self._stream(stream)))
         if code:
             raise CocodcError(code, "cocodc_lm_glu_grad")
 
@@ -581,18 +585,18 @@ class LmOps:
         largest logits' ids and log probabilities (top_ids, top_logp: T x k).  targets and logp may both be None."""
         self._on_device(logits, targets, logp, entropy, lse, top_ids, top_logp)
         lp, ls, T, V = _matrix(logits, "logits")
-        tp, tt = _ids(targets, "targets", T) if targets is not None else (None, 0)
+        tp, tt = _ids(targets, "targets", T) if targets is not None else (0, 0)
         f32 = torch.float32
-        k, kp, kl = 0, None, None
+        k = kp = kl = 0
         if top_ids is not None:
             if top_ids.dim() != 2 or top_ids.shape[0] != T:
                 raise ValueError("top_ids must be T x k")
             k = top_ids.shape[1]
         if k:
             kp, kl = _vector(top_ids, "top_ids", T * k, torch.int32), _vector(top_logp, "top_logp", T * k, f32)
-        code = _lib.cocodc_lm_logprobs(self._h, lp, _type(logits), ls, T, V, tp, tt, scale, _vector(logp, "logp", T, f32),
-                                       _vector(entropy, "entropy", T, f32), _vector(lse, "lse", T, f32), k, kp, kl,
-                                       self._stream(stream))
+        code = _submit(self._h, _LOGPROBS(4, lp, _type(logits), ls, T, V, tp, tt, scale, _vector(logp, "logp", T, f32),
+                                          _vector(entropy, "entropy", T, f32), _vector(lse, "lse", T, f32), k, kp, kl,
+                                          self._stream(stream)))
         if code:
             raise CocodcError(code, "cocodc_lm_logprobs")
 
@@ -604,10 +608,10 @@ class LmOps:
         dp, ds, T2, V2 = _matrix(dlogits, "dlogits")
         _sized("dlogits", T2, V2, T, V)
         kind = _one_type(logits, dlogits)
-        tp, tt = _ids(targets, "targets", T) if targets is not None else (None, 0)
+        tp, tt = _ids(targets, "targets", T) if targets is not None else (0, 0)
         f32 = torch.float32
-        code = _lib.cocodc_lm_logprobs_grad(self._h, lp, kind, ls, T, V, tp, tt, scale, _vector(lse, "lse", T, f32),
-                                            _vector(entropy, "entropy", T, f32), _vector(dlogp, "dlogp", T, f32),
-                                            _vector(dentropy, "dentropy", T, f32), dp, ds, self._stream(stream))
+        code = _submit(self._h, _LOGPROBS_GRAD(5, lp, kind, ls, T, V, tp, tt, scale, _vector(lse, "lse", T, f32),
+                                               _vector(entropy, "entropy", T, f32), _vector(dlogp, "dlogp", T, f32),
+                                               _vector(dentropy, "dentropy", T, f32), dp, ds, self._stream(stream)))
         if code:
             raise CocodcError(code, "cocodc_lm_logprobs_grad")

@@ -2,9 +2,41 @@
 
 #include "lm_common.cuh"
 
+#include <cstring>
 #include <new>
+#include <tuple>
+#include <type_traits>
 
 using namespace cocodc_lm_impl;
+
+namespace {
+// The next word of a record, as what the parameter asks for.
+struct Reader {
+  const char* at;
+  int64_t word() {
+    int64_t w;
+    std::memcpy(&w, at, 8);
+    at += 8;
+    return w;
+  }
+  template <typename T> T next() {
+    if constexpr (std::is_pointer_v<T>) {
+      return reinterpret_cast<T>(static_cast<uintptr_t>(word()));
+    } else if constexpr (std::is_floating_point_v<T>) {
+      const int64_t w = word();
+      double d;
+      std::memcpy(&d, &w, 8);
+      return static_cast<T>(d);
+    } else {
+      return static_cast<T>(word());
+    }
+  }
+};
+template <typename... P> cocodc_status call(cocodc_status (*f)(cocodc_lm*, P...), cocodc_lm* lm, Reader r) {
+  std::tuple<P...> args{r.next<P>()...};     // braces: read from left to right
+  return std::apply([&](const P&... p) { return f(lm, p...); }, args);
+}
+}  // namespace
 
 extern "C" {
 
@@ -54,6 +86,20 @@ cocodc_status cocodc_lm_poll_status(cocodc_lm* lm, void* stream) {
                     cudaStreamSynchronize(st) != cudaSuccess))
     return COCODC_ERR_CUDA;
   return static_cast<cocodc_status>(word);
+}
+
+cocodc_status cocodc_lm_submit(cocodc_lm* lm, const void* record) {
+  if (!lm || !record) return COCODC_ERR_INVALID_ARG;
+  Reader r{static_cast<const char*>(record)};
+  switch (r.word()) {
+    case COCODC_LM_EMBED: return call(cocodc_lm_embed, lm, r);
+    case COCODC_LM_EMBED_GRAD: return call(cocodc_lm_embed_grad, lm, r);
+    case COCODC_LM_GLU: return call(cocodc_lm_glu, lm, r);
+    case COCODC_LM_GLU_GRAD: return call(cocodc_lm_glu_grad, lm, r);
+    case COCODC_LM_LOGPROBS: return call(cocodc_lm_logprobs, lm, r);
+    case COCODC_LM_LOGPROBS_GRAD: return call(cocodc_lm_logprobs_grad, lm, r);
+  }
+  return COCODC_ERR_INVALID_ARG;
 }
 
 int64_t cocodc_lm_launch_count(const cocodc_lm* lm) { return lm ? (int64_t)lm->launches.load() : 0; }

@@ -26,6 +26,23 @@ def test_null_handle_is_rejected(B):
     assert lib.cocodc_lm_logprobs_grad(None, None, 0, 1, 1, 1, None, 0, 1.0, None, None, None, None, None, 1, None) == B.ERR_INVALID_ARG
 
 
+def test_records_hold_what_the_calls_take(B):
+    """A record is the operator's number and the call's arguments without the handle; scale is its only floating word."""
+    import ctypes
+    lib = B.library()
+    for name in ("embed", "embed_grad", "glu", "glu_grad", "logprobs", "logprobs_grad"):
+        types = getattr(lib, "cocodc_lm_" + name).argtypes[1:]
+        pack = getattr(B, "_" + name.upper())
+        args = [0.5 if t is ctypes.c_float else 7 for t in types]
+        assert len(pack(0, *args)) == 8 * (1 + len(types)), name
+        with pytest.raises(Exception):
+            pack(0, *args, 7)
+    assert lib.cocodc_lm_submit(None, b"\0" * 256) == B.ERR_INVALID_ARG
+    handle = ctypes.create_string_buffer(256)
+    assert lib.cocodc_lm_submit(ctypes.addressof(handle), None) == B.ERR_INVALID_ARG
+    assert lib.cocodc_lm_submit(ctypes.addressof(handle), b"\x63" + b"\0" * 255) == B.ERR_INVALID_ARG
+
+
 def test_workspace_sizes(B):
     lib = B.library()
     for V, D, T in ((1, 1, 0), (50257, 768, 4099), (32000, 1024, 65536)):
