@@ -148,9 +148,19 @@ template <> struct Words<__half> {
 };
 
 // What a part of a row comes to, in base 2: m the largest logit, s = sum 2^(c (x - m)), u = sum c (x - m) 2^(c (x - m)).
+// The walk measures every logit against c m as it is rounded (one fma a logit), which is off by up to half a unit in the last place of
+// c m, another amount for every thread's m.  So parts of a walk are joined by the distance of these shifts, and only the CTA's sums are
+// taken to c m itself (to_largest): everything after that is measured against the largest logit, and logits that share a
+// large offset lose no digits to it.
 struct Stats {
   float m, s, u;
 };
+__device__ __forceinline__ float shift_of(float m, float c) { return __fmul_rn(m, c); }   // never contracted into an fma
+__device__ __forceinline__ Stats to_largest(const Stats& x, float c) {
+  const float off = fmaf(x.m, c, -shift_of(x.m, c)), f = exp2f(-off);
+  return Stats{x.m, x.s * f, (x.u - off * x.s) * f};
+}
+// Two parts measured against their largest logits.
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
   const float m = fmaxf(a.m, b.m);
   // the offsets are bounded so that 0 * offset stays 0; a part without sum keeps its zeros
@@ -158,11 +168,12 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
   const float fa = fast_exp2(da), fb = fast_exp2(db);
   return Stats{m, a.s * fa + b.s * fb, (a.u + da * a.s) * fa + (b.u + db * b.s) * fb};
 }
-// All lanes' parts at once: scaled to the warp's largest logit, then summed; lanes without a part hold m = -Inf, s = u = 0.
+// All lanes' parts at once, measured against their shifts: scaled to the warp's largest, then summed; lanes without a part hold
+// m = -Inf, s = u = 0.  (Lanes with one m in common are only summed, whatever they are measured against.)
 __device__ __forceinline__ Stats warp_join(Stats x, float c) {
   const unsigned top = __reduce_max_sync(~0u, ordered(x.m));
   const float m = value_of(top);
-  const float d = fmaxf(x.m == m ? 0.f : (x.m - m) * c, -1e4f), f = fast_exp2(d);
+  const float d = fmaxf(x.m == m ? 0.f : shift_of(x.m, c) - shift_of(m, c), -1e4f), f = fast_exp2(d);
   x.u = (x.u + d * x.s) * f;
   x.s *= f;
   for (int o = 16; o; o >>= 1) {
@@ -353,17 +364,23 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     if (y >= 0) target = to_f32(row[y]);
   }
   Stats x{-W::kFar, 0.f, 0.f};
-  f32x2 s2 = 0, u2 = 0, mc2 = pair_of(-x.m * c, -x.m * c);   // sums of the even and the odd elements; -c m twice
+  f32x2 s2 = 0, u2 = 0;                                      // sums of the even and the odd elements
+  f32x2 less2 = pair_of(-shift_of(x.m, c), -shift_of(x.m, c));   // minus the shift, twice
+  const auto less = [&] {
+    float lo, hi;
+    split(less2, lo, hi);
+    return lo;
+  };
   const f32x2 c2 = pair_of(c, c);
   const auto raise = [&](float m) {
-    const float d = fmaxf((x.m - m) * c, -1e4f), f = exp2f(d);
+    const float to = shift_of(m, c), d = fmaxf(-(less() + to), -1e4f), f = exp2f(d);
     u2 = mul2(fma2(pair_of(d, d), s2, u2), pair_of(f, f));
     s2 = mul2(s2, pair_of(f, f));
     x.m = m;
-    mc2 = pair_of(-m * c, -m * c);
+    less2 = pair_of(-to, -to);
   };
   const auto add = [&](f32x2 v) {
-    const f32x2 d = fma2(v, c2, mc2);
+    const f32x2 d = fma2(v, c2, less2);
     float lo, hi;
     split(d, lo, hi);
     const f32x2 e = pair_of(fast_exp2(lo), fast_exp2(hi));
@@ -374,7 +391,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     float v;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(to_f32(row[j])), "f"(-W::kFar));
     if (v > x.m) raise(v);
-    const float d = fmaf(v, c, -x.m * c), e = fast_exp2(d);
+    const float d = fmaf(v, c, less()), e = fast_exp2(d);
     s2 = add2(s2, pair_of(e, 0.f));
     u2 = add2(u2, pair_of(e * d, 0.f));
   };
@@ -417,7 +434,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
   x = block_join(x, c, sh.scratch);
   // a NaN or +Inf, nothing but very low logits, a very small scale: once more, with care (also the alternatives)
   const bool careful = !(x.m > -W::kFar / 2) || !(x.s < INFINITY) || !(c * (W::kFar / 2) > 200.f);
-  if (careful) x = careful_stats(row, j0, j1, c, sh.scratch);
+  x = careful ? careful_stats(row, j0, j1, c, sh.scratch) : to_largest(x, c);
 
   if (TOP) {
     bool done = false;
@@ -495,21 +512,13 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
 
   if (warp != 0) return;
   const bool empty = x.m == -INFINITY && x.s == 0.f;
-  float log2s = empty ? -INFINITY : log2f(x.s);
-  const float top_mc = x.m * c;
-  log2s = __shfl_sync(~0u, log2s, 0);
-  const float mc0 = __shfl_sync(~0u, top_mc, 0);
+  const float log_s = __shfl_sync(~0u, empty ? -INFINITY : kLn2 * log2f(x.s), 0), m = __shfl_sync(~0u, x.m, 0);
   const bool none = __shfl_sync(~0u, (int)empty, 0);
-  const float m0 = __shfl_sync(~0u, x.m, 0);
-  // log probability of a logit: ln 2 (c x - c m - log2 s), in which the rounding of c m cancels against the sum's; logits so
-  // low that c x (or c m) overflows are taken in the natural base
-  const auto logp_of = [&](float v) {
-    const float r = fmaf(v, c, -mc0) - log2s;
-    return none ? -INFINITY : fabsf(r) < INFINITY ? kLn2 * r : (v - m0) * a.scale - kLn2 * log2s;
-  };
+  // the distance of two logits is formed of their halves, which cannot overflow
+  const auto logp_of = [&](float v) { return none ? -INFINITY : (0.5f * v - 0.5f * m) * (2.f * a.scale) - log_s; };
   if (lane == 0) {
-    if (a.lse) a.lse[t] = none ? -INFINITY : fabsf(mc0) < INFINITY ? kLn2 * (mc0 + log2s) : m0 * a.scale + kLn2 * log2s;
-    if (a.entropy) a.entropy[t] = none ? 0.f : kLn2 * (log2s - x.u / x.s);
+    if (a.lse) a.lse[t] = none ? -INFINITY : __fmul_rn(m, a.scale) + log_s;
+    if (a.entropy) a.entropy[t] = none ? 0.f : log_s - kLn2 * (x.u / x.s);
     if (a.logp) a.logp[t] = y < 0 ? 0.f : logp_of(target);
   }
   if (TOP && lane < a.top_k) {

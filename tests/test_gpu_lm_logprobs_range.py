@@ -1,0 +1,78 @@
+"""Token log probabilities over the range of their arguments: logits that share a large offset, large and small products of scale
+and logit, against the definition in 64 bits measured from the row's largest logit.
+
+Bounds, derived before any run (e = 2^-24, z = scale * x, r_j = z_j - max z, S = sum exp(r_j), p_j = exp(r_j) / S):
+  S               each exponent is off by 2.5 e |r_j| (the constant log2 e * scale, one fma), relatively to p_j that is 2.5 e sum p |r| <=
+                  2.5 e log V; the exponential 4 e; V / 512 + 20 rounded sums of positive terms; some 5 rescalings of a thread's sums and 2 joins
+                  at 6 e each; the logarithm, of a value up to log V, 4 e log V:  E = e (V / 512 + 180) for log V <= 11
+  log probability E + 3 e |r|: the distance of two logits is rounded once and multiplied once
+  entropy         E for log S, 3 E for each unit of sum p |r| = entropy - log S: E (1 + 3 (entropy - log S))
+  log-sum-exp     E + 2 e |max z|
+None of these but the last grows with an offset of the logits.
+"""
+
+import math
+
+import pytest
+import torch
+
+from test_gpu_lm_ops import E24, F32, gen, put, randn, within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2504_17672_b200 import binding as B
+    o = B.LmOps(0)
+    yield o
+    assert o.cocodc_lm_poll_status() == B.OK
+    o.close()
+
+
+def reference(x, targets, scale):
+    """(logp, entropy, lse, log probabilities of the whole row, log S, max z) in 64 bits; rows need a finite logit."""
+    scale = float(torch.tensor(scale, dtype=F32))
+    z = x.double()
+    m = z.amax(1, keepdim=True)
+    r = (z - m) * scale
+    logS = torch.log(torch.exp(r).sum(1, keepdim=True))
+    lp = r - logS
+    p = torch.exp(lp)
+    H = logS.squeeze(1) - torch.where(p > 0, p * r, torch.zeros_like(p)).sum(1)
+    top = m.squeeze(1) * scale
+    return lp.gather(1, targets.unsqueeze(1)).squeeze(1), H, top + logS.squeeze(1), lp, logS.squeeze(1), top
+
+
+def check(ops, x, targets, scale, k):
+    T, V = x.shape
+    out = {n: torch.full((T,), 77.0, device="cuda") for n in ("logp", "entropy", "lse")}
+    out["top_ids"] = torch.full((T, k), -5, dtype=torch.int32, device="cuda")
+    out["top_logp"] = torch.full((T, k), 77.0, device="cuda")
+    ops.cocodc_lm_logprobs(x, targets, scale=scale, **out)
+    logp, H, lse, lp, logS, top = reference(x, targets, scale)
+    E = E24 * (V / 512 + 180)
+    far = lambda v: 3 * E24 * torch.nan_to_num(v, 0, 0, 0).abs()  # noqa: E731
+    # what leaves fp32's range is infinite there
+    as_f32 = lambda v: torch.where(v.abs() < 3.4028e38, v, torch.sign(v) * math.inf)  # noqa: E731
+    within(out["logp"], as_f32(logp), E + far(logp), "logp")
+    within(out["entropy"], H, E * (1 + 3 * (H - logS).abs()), "entropy")
+    within(out["lse"], as_f32(lse), E + 2 * E24 * top.abs(), "lse")
+    order = torch.sort(x.double(), dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(out["top_ids"].long(), order)
+    want = lp.gather(1, order)
+    within(out["top_logp"], as_f32(want), E + far(want), "top")
+    alone = torch.full((T,), 77.0, device="cuda")            # without alternatives: another kernel
+    ops.cocodc_lm_logprobs(x, targets, alone, scale=scale)
+    within(alone, as_f32(logp), E + far(logp), "logp alone")
+
+
+# few rows are split over several blocks, many are not
+@pytest.mark.parametrize("T,V", [(1, 1000), (1, 32000), (3, 40001), (200, 32000), (150, 77)])
+@pytest.mark.parametrize("offset", [0.0, 1e3, -1e3, 1e4, -1e4, 1e5, -1e5, 1e6, -1e6])
+def test_an_offset_costs_no_digits(ops, T, V, offset):
+    g = gen(T + V)
+    x = randn(g, T, V, std=2.0) + offset
+    targets = torch.randint(0, V, (T,), generator=g, device="cuda")
+    check(ops, put(x, V + 1, 1), targets, 1.0, 4)
+    check(ops, x, targets, 0.8, 4)
