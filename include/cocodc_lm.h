@@ -114,6 +114,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
  * Masked logits (-Inf) have p = 0 and add nothing to the entropy.  A row of nothing but -Inf has lse = -Inf,
  * entropy 0 and log probabilities -Inf.  A row with a NaN or +Inf has NaN in lse, entropy, logp (where y >= 0)
  * and top_logp; among its alternatives NaN ranks above +Inf.
+ * All finite logits and all legal scales are good; lse is +-Inf where it leaves fp32's range, the other outputs do not suffer from it.
  */
 #define COCODC_LM_MAX_TOP 32
 cocodc_status cocodc_lm_logprobs(cocodc_lm* lm, const void* logits, int32_t type, int64_t stride, int64_t T, int64_t V,

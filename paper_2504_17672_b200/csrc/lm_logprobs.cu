@@ -74,11 +74,12 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
 // ---- sixteen bytes of a row ---------------------------------------------------------------------
 // Logits below -kFar take part in the sums as -kFar (-Inf would turn 0 * d into NaN in the entropy's sum).  That is exact
 // where their exponentials are 0 either way: where the largest logit is above -kFar / 2 and c kFar / 2 is above 200;
-// anything else goes the careful way.  kFar is a power of two, so that c * kFar is c's bits and -kFar's distance to itself is 0.
+// anything else goes the careful way.  kFar is a power of two, so that c * kFar is c's bits and -kFar's distance to itself is 0; it
+// is finite times the largest c, and masks of -1e9 and lower lie beyond it.
 template <typename T> struct Words;
 template <> struct Words<float> {
   static constexpr int n = 4;
-  static constexpr float kFar = 0x1p100f;
+  static constexpr float kFar = 0x1p27f;
   float e[4];
   __device__ __forceinline__ void set(uint4 w) {
     const float f[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
@@ -94,7 +95,7 @@ template <> struct Words<float> {
 };
 template <> struct Words<__nv_bfloat16> {
   static constexpr int n = 8;
-  static constexpr float kFar = 0x1p100f;
+  static constexpr float kFar = 0x1p27f;
   __nv_bfloat162 e[4];
   static __device__ __forceinline__ __nv_bfloat162 low() { return __float2bfloat162_rn(-kFar); }
   __device__ __forceinline__ void set(uint4 w) {
@@ -155,16 +156,20 @@ template <> struct Words<__half> {
 struct Stats {
   float m, s, u;
 };
+// Below this a shift's rounding changes the exponents by at most 32; from about 2^31 on it could take a sum to 0 or Inf.
+constexpr float kMostShift = 0x1p30f;
 __device__ __forceinline__ float shift_of(float m, float c) { return __fmul_rn(m, c); }   // never contracted into an fma
 __device__ __forceinline__ Stats to_largest(const Stats& x, float c) {
   const float off = fmaf(x.m, c, -shift_of(x.m, c)), f = exp2f(-off);
   return Stats{x.m, x.s * f, (x.u - off * x.s) * f};
 }
+// c (x - m), of two logits' halves, whose distance cannot overflow
+__device__ __forceinline__ float distance(float x, float m, float c) { return (0.5f * x - 0.5f * m) * (c + c); }
 // Two parts measured against their largest logits.
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
   const float m = fmaxf(a.m, b.m);
   // the offsets are bounded so that 0 * offset stays 0; a part without sum keeps its zeros
-  const float da = fmaxf((a.m == m ? 0.f : (a.m - m) * c), -1e4f), db = fmaxf((b.m == m ? 0.f : (b.m - m) * c), -1e4f);
+  const float da = fmaxf(a.m == m ? 0.f : distance(a.m, m, c), -1e4f), db = fmaxf(b.m == m ? 0.f : distance(b.m, m, c), -1e4f);
   const float fa = fast_exp2(da), fb = fast_exp2(db);
   return Stats{m, a.s * fa + b.s * fb, (a.u + da * a.s) * fa + (b.u + db * b.s) * fb};
 }
@@ -209,7 +214,7 @@ __device__ __noinline__ Stats careful_stats(const T* row, unsigned j0, unsigned 
   for (unsigned j = j0 + threadIdx.x; j < j1; j += kThreads) {
     const float v = to_f32(row[j]);
     if (v == -INFINITY) continue;
-    const float d = (v - x.m) * c, e = exp2f(d);
+    const float d = distance(v, x.m, c), e = exp2f(d);
     x.s += e;
     if (e != 0.f) x.u += e * d;
   }
@@ -432,8 +437,10 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     if (tid == 0) sh.n_flagged = sh.n_candidates = 0;
   }
   x = block_join(x, c, sh.scratch);
-  // a NaN or +Inf, nothing but very low logits, a very small scale: once more, with care (also the alternatives)
-  const bool careful = !(x.m > -W::kFar / 2) || !(x.s < INFINITY) || !(c * (W::kFar / 2) > 200.f);
+  // a NaN or +Inf, nothing but very low logits, a very small scale, a very large product of scale and largest logit: once more, with
+  // care (also the alternatives)
+  const bool careful = !(x.m > -W::kFar / 2) || !(x.s + fabsf(x.u) < INFINITY) || !(c * (W::kFar / 2) > 200.f) ||
+                       !(fabsf(shift_of(x.m, c)) < kMostShift);
   x = careful ? careful_stats(row, j0, j1, c, sh.scratch) : to_largest(x, c);
 
   if (TOP) {
@@ -514,8 +521,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
   const bool empty = x.m == -INFINITY && x.s == 0.f;
   const float log_s = __shfl_sync(~0u, empty ? -INFINITY : kLn2 * log2f(x.s), 0), m = __shfl_sync(~0u, x.m, 0);
   const bool none = __shfl_sync(~0u, (int)empty, 0);
-  // the distance of two logits is formed of their halves, which cannot overflow
-  const auto logp_of = [&](float v) { return none ? -INFINITY : (0.5f * v - 0.5f * m) * (2.f * a.scale) - log_s; };
+  const auto logp_of = [&](float v) { return none ? -INFINITY : distance(v, m, a.scale) - log_s; };
   if (lane == 0) {
     if (a.lse) a.lse[t] = none ? -INFINITY : __fmul_rn(m, a.scale) + log_s;
     if (a.entropy) a.entropy[t] = none ? 0.f : log_s - kLn2 * (x.u / x.s);

@@ -16,7 +16,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_lm_ops import E24, F32, gen, put, randn, within
+from test_gpu_lm_ops import BF16, E24, F16, F32, gen, put, randn, within
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +76,42 @@ def test_an_offset_costs_no_digits(ops, T, V, offset):
     targets = torch.randint(0, V, (T,), generator=g, device="cuda")
     check(ops, put(x, V + 1, 1), targets, 1.0, 4)
     check(ops, x, targets, 0.8, 4)
+
+
+@pytest.mark.parametrize("T,V", [(1, 1), (2, 64), (1, 40001), (3, 40001), (200, 3000)])
+@pytest.mark.parametrize("scale", [1e-38, 1e-6, 1e-3, 30.0, 1e4, 1e6, 1e8, 3e8, 1e9, 1e10, 1e20, 1e30])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_scales(ops, T, V, scale, dtype):
+    """Up to the largest scale: a temperature near zero, with and without masked logits."""
+    g = gen(V)
+    x = randn(g, T, V, std=3.0, dtype=dtype)
+    targets = torch.randint(0, V, (T,), generator=g, device="cuda")
+    targets[0] = x[0].float().argmax()
+    check(ops, x, targets, scale, min(V, 3))
+    if V > 1:
+        x[:, 1::3] = -math.inf
+        targets[-1] = V // 2 // 3 * 3
+        check(ops, x, targets, scale, min(V, 3))
+        x[:, V // 4:] = -math.inf                            # some blocks of a row have nothing left
+        check(ops, x, targets, scale, 3)
+
+
+@pytest.mark.parametrize("T,V", [(1, 1), (2, 64), (1, 40001), (3, 40001), (200, 3000)])
+@pytest.mark.parametrize("value", [-1e4, -1e6, -1e8, -1e9, -1e10, -1e12, -1e15, -1e30, -3e38, 1e9, 1e12, 1e30, 3e38])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_logits(ops, T, V, value, dtype):
+    """Rows of one value throughout, rows with that value in some or most places, rows of random multiples of it."""
+    g = gen(V + 1)
+    k = min(V, 3)
+    targets = torch.randint(0, V, (T,), generator=g, device="cuda")
+    same = torch.full((T, V), value, device="cuda").to(dtype)
+    for scale in (1.0, 0.7, 1e-3):
+        check(ops, same, targets, scale, k)
+    x = randn(g, T, V, std=2.0, dtype=dtype)
+    for keep in (torch.rand(T, V, generator=g, device="cuda") < 0.7, torch.arange(V, device="cuda").expand(T, V) < V // 5 + 1):
+        for scale in (1.0, 1.3):
+            check(ops, torch.where(keep, x, same), targets, scale, k)
+    check(ops, (torch.rand(T, V, generator=g, device="cuda") * value).to(dtype), targets, 1.0, k)
+    spread = (torch.rand(T, V, generator=g, device="cuda") * 2 - 1) * value      # distances beyond fp32's range at 3e38
+    check(ops, spread.to(dtype), targets, 1.0, k)
+    check(ops, spread.to(dtype), targets, 4.0 / abs(value), k)
