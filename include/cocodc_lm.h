@@ -125,8 +125,9 @@ cocodc_status cocodc_lm_logprobs(cocodc_lm* lm, const void* logits, int32_t type
  * Gradient of logp and entropy with respect to the logits, given d/dlogp [T] and d/dentropy [T] of a scalar:
  *   dlogits[t][j] = scale * ( dlogp[t] * (1[j = y] - p_j) - dentropy[t] * p_j * (log p_j + entropy[t]) )
  * with lse and entropy as the forward call wrote them.  dlogp is NULL (with targets NULL) or dentropy is NULL
- * (entropy is not read then) for "zero".  dlogp[t] is not used where y < 0.  A row of nothing but -Inf gets
- * zeros, a row whose lse is NaN gets NaN.  dlogits has the logits' type; dlogits == logits with the same stride
+ * (entropy is not read then) for "zero".  dlogp[t] is not used where y < 0.  p_j = exp(z_j - lse) with z_j rounded
+ * to fp32, as lse is: good to |lse| 2^-23 relatively.  A row of nothing but -Inf (or whose lse is -Inf) gets zeros, a row whose lse
+ * is NaN or +Inf gets NaN.  dlogits has the logits' type; dlogits == logits with the same stride
  * is legal (in place).
  */
 cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t type, int64_t stride, int64_t T,

@@ -115,3 +115,46 @@ def test_large_logits(ops, T, V, value, dtype):
     spread = (torch.rand(T, V, generator=g, device="cuda") * 2 - 1) * value      # distances beyond fp32's range at 3e38
     check(ops, spread.to(dtype), targets, 1.0, k)
     check(ops, spread.to(dtype), targets, 4.0 / abs(value), k)
+
+
+@pytest.mark.parametrize("T,V", [(2, 64), (3, 40001), (150, 3000)])
+@pytest.mark.parametrize("scale", [3e3, 1e4, 1e6, 1e8, 1e9, 1e10, 1e20, 1e30])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_gradient_at_a_temperature_near_zero(ops, T, V, scale, dtype):
+    """The largest logit is a half above the others: at these scales it has all of the probability, exp(-1500) and less are 0.
+
+    z and lse are the same fp32 number there, p is exactly 0 or 1; dlogp times scale is rounded twice, the entropy that the forward
+    call gives is 0 up to 8 e, and so is what it is multiplied with."""
+    g = gen(V)
+    x = randn(g, T, V, std=0.5).clamp_(-2.5, 2.5)
+    at = torch.randint(0, V, (T,), generator=g, device="cuda")
+    x.scatter_(1, at.unsqueeze(1), 3.0 + torch.rand(T, 1, generator=g, device="cuda"))
+    x = x.to(dtype)
+    targets = torch.randint(0, V, (T,), generator=g, device="cuda")
+    targets[0] = at[0]
+    logp, H, lse = (torch.empty(T, device="cuda") for _ in range(3))
+    ops.cocodc_lm_logprobs(x, targets, logp, entropy=H, lse=lse, scale=scale)
+    dlogp, dH = randn(g, T), randn(g, T)
+    got = torch.empty_like(x)
+    want = torch.zeros(T, V, dtype=torch.float64, device="cuda")
+    size = float(torch.tensor(scale, dtype=F32)) * dlogp.double()
+    want.scatter_(1, targets.unsqueeze(1), size.unsqueeze(1))
+    want.scatter_add_(1, at.unsqueeze(1), -size.unsqueeze(1))
+    most = torch.finfo(dtype).max
+    fits = lambda v: torch.where(v.abs() <= most, v, torch.sign(v) * math.inf)  # noqa: E731
+    bound = torch.zeros_like(want).scatter_(1, at.unsqueeze(1), 16 * E24 * scale * dH.double().abs().unsqueeze(1)) + 2 * E24 * size.abs().unsqueeze(1)
+    for a, b in ((dlogp, dH), (dlogp, None)):
+        ops.cocodc_lm_logprobs_grad(x, targets, lse, H if b is not None else None, a, b, got, scale=scale)
+        within(got, fits(want), bound, "gradient")
+
+
+def test_gradient_without_a_finite_log_sum_exp(ops):
+    """Beyond fp32's range no probabilities can be formed: NaN above it, zeros below it (as for rows of -Inf)."""
+    x = torch.tensor([[1e20, 2e20, 0.0], [-1e20, -2e20, -1e20], [0.5, 0.25, 0.0]], device="cuda")
+    lse, got = torch.empty(3, device="cuda"), torch.empty(3, 3, device="cuda")
+    t = torch.tensor([0, 0, 0], device="cuda")
+    logp = torch.empty(3, device="cuda")
+    ops.cocodc_lm_logprobs(x, t, logp, lse=lse, scale=1e25)
+    assert lse[0] == math.inf and lse[1] == -math.inf and abs(float(lse[2]) - 5e24) < 1e18
+    ops.cocodc_lm_logprobs_grad(x, t, lse, None, torch.ones(3, device="cuda"), None, got, scale=1e25)
+    assert bool(torch.isnan(got[0]).all()) and bool((got[1] == 0).all()) and bool((got[2] == 0).all())
