@@ -16,7 +16,8 @@
  *   - Base pointers need the alignment of their element type.  Buffers whose base and row stride are multiples
  *     of 16 bytes take the vector / tensor-core paths; others run on slower kernels with the same results up
  *     to the order of fp32 sums.
- *   - Outputs must not overlap inputs or each other (COCODC_ERR_ALIAS), except where a call says so.
+ *   - Outputs must not overlap inputs or each other (COCODC_ERR_ALIAS), except where a call says so.  Different columns of one
+ *     buffer (rows equally far apart) do not overlap; matrices with different distances of their rows must not lie within each other.
  *   - Calls are asynchronous on the given stream and allocate nothing.  Calls that need scratch take it as a
  *     workspace (16-byte aligned, at least cocodc_lm_*_workspace bytes, contents arbitrary and undefined
  *     afterwards).  Nothing is kept from one call for the next, so one handle may be used on several streams

@@ -72,14 +72,26 @@ inline bool rows_aligned(const void* p, int64_t stride, int esize) {
 // Sizes whose products with an element size stay far inside 64 bits.
 inline bool sane(int64_t n) { return n >= 0 && n <= (int64_t(1) << 40); }
 
-// The bytes [lo, hi) that a matrix spans; empty for no rows.
-struct Span { uintptr_t lo, hi; };
+// The bytes [lo, hi) that a matrix spans, from its first element to its last; empty for no rows.
+struct Span {
+  uintptr_t lo, hi;
+  uintptr_t pitch, width;    // bytes from row to row (0: one row) and of a row
+};
 inline Span span(const void* p, int64_t rows, int64_t stride, int64_t width, int esize) {
   const uintptr_t b = reinterpret_cast<uintptr_t>(p);
-  if (!p || rows < 1 || width < 1) return Span{b, b};
-  return Span{b, b + ((uintptr_t)(rows - 1) * (uintptr_t)stride + (uintptr_t)width) * (uintptr_t)esize};
+  if (!p || rows < 1 || width < 1) return Span{b, b, 0, 0};
+  const uintptr_t pitch = (uintptr_t)stride * (uintptr_t)esize, w = (uintptr_t)width * (uintptr_t)esize;
+  return Span{b, b + (uintptr_t)(rows - 1) * pitch + w, rows > 1 ? pitch : 0, w};
 }
-inline bool meet(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
+// Whether two matrices have a byte in common.  Those with rows equally far apart (one row: as far as the other's) may be different
+// columns of one buffer; where rows are not equally far apart, spans that meet count as matrices that do.
+inline bool meet(const Span& a, const Span& b) {
+  if (a.lo >= a.hi || b.lo >= b.hi || a.lo >= b.hi || b.lo >= a.hi) return false;
+  const uintptr_t pitch = a.pitch ? a.pitch : b.pitch;
+  if (pitch == 0 || (b.pitch && b.pitch != pitch) || a.width > pitch || b.width > pitch) return true;
+  const uintptr_t d = b.lo >= a.lo ? (b.lo - a.lo) % pitch : (pitch - (a.lo - b.lo) % pitch) % pitch;   // b's first column from a's
+  return d < a.width || d + b.width > pitch;
+}
 
 // ---- device side -------------------------------------------------------------------------------
 // see start()
