@@ -78,13 +78,17 @@ cocodc_status cocodc_lm_poll_status(cocodc_lm* lm, void* stream) {
   DeviceScope scope(lm->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int word = 0;
+  const auto failed = [] {
+    cudaGetLastError();                                // reported here, nobody else is to find it
+    return COCODC_ERR_CUDA;
+  };
   if (!scope.ok || cudaMemcpyAsync(&word, lm->d_status, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
       cudaStreamSynchronize(st) != cudaSuccess)
-    return COCODC_ERR_CUDA;
+    return failed();
   // cleared only when something was read: an error that a call on another stream records meanwhile is not lost
   if (word != 0 && (cudaMemsetAsync(lm->d_status, 0, sizeof(int), st) != cudaSuccess ||
                     cudaStreamSynchronize(st) != cudaSuccess))
-    return COCODC_ERR_CUDA;
+    return failed();
   return static_cast<cocodc_status>(word);
 }
 

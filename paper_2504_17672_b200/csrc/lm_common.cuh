@@ -38,8 +38,10 @@ struct DeviceScope {
 // Launches with programmatic dependence on the stream's previous kernel: the next kernel's blocks may become resident once
 // all blocks of this one have called may_follow(), and touch global memory only after wait_for_previous() (which
 // returns when the previous kernel is done and its writes are visible), so that launch and set-up hide behind its end.
+// The status is this launch's own, whatever the thread has left of older errors; what would read its results is not launched after a failure.
 template <typename... P, typename... A>
-inline void start(void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, cudaStream_t st, unsigned cluster, const A&... args) {
+inline cocodc_status start(cocodc_lm* lm, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, cudaStream_t st,
+                           unsigned cluster, const A&... args) {
   cudaLaunchAttribute attrs[2] = {};
   attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attrs[0].val.programmaticStreamSerializationAllowed = 1;
@@ -53,12 +55,12 @@ inline void start(void (*kernel)(P...), dim3 grid, unsigned threads, unsigned sm
   config.stream = st;
   config.attrs = attrs;
   config.numAttrs = cluster > 1 ? 2 : 1;
-  cudaLaunchKernelEx(&config, kernel, P(args)...);     // a failure is found by launched()
-}
-
-inline cocodc_status launched(cocodc_lm* lm, int kernels = 1) {
-  lm->launches.fetch_add(kernels, std::memory_order_relaxed);
-  return cudaGetLastError() == cudaSuccess ? COCODC_OK : COCODC_ERR_CUDA;
+  if (cudaLaunchKernelEx(&config, kernel, P(args)...) != cudaSuccess) {
+    cudaGetLastError();                                // reported here, nobody else is to find it
+    return COCODC_ERR_CUDA;
+  }
+  lm->launches.fetch_add(1, std::memory_order_relaxed);
+  return COCODC_OK;
 }
 
 inline bool known_type(int32_t t) { return t == COCODC_F32 || t == COCODC_BF16 || t == COCODC_F16; }
@@ -123,7 +125,7 @@ __device__ __forceinline__ float fast_exp2(float x) {
 }
 
 // Calls f with a value of the C++ type that a type code stands for.
-template <typename F> bool with_type(int32_t t, F&& f) {
+template <typename F> cocodc_status with_type(int32_t t, F&& f) {
   if (t == COCODC_F32) return f(float());
   if (t == COCODC_BF16) return f(__nv_bfloat16());
   return f(__half());

@@ -538,7 +538,7 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = rows_aligned(table, table_stride, es) && rows_aligned(y, y_stride, ys) && D % 8 == 0;
-  with_type(table_type, [&](auto in) {
+  return with_type(table_type, [&](auto in) {
     return with_type(y_type, [&](auto out) {
       using TIn = decltype(in);
       using TOut = decltype(out);
@@ -548,20 +548,18 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
         while (lanes_log2 < 5 && (1u << lanes_log2) < packs) ++lanes_log2;
         const unsigned per_row = (packs + (U << lanes_log2) - 1) / (U << lanes_log2);
         const long long blocks = (((T * per_row) << lanes_log2) + 255) / 256;
-        start(kernel, (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st, 1,
-            static_cast<const TIn*>(table), table_stride, V, packs, lanes_log2, per_row, ids, ids_type == COCODC_I64, T, scale,
-            static_cast<TOut*>(y), y_stride, lm->d_status);
+        return start(lm, kernel, (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st, 1,
+                     static_cast<const TIn*>(table), table_stride, V, packs, lanes_log2, per_row, ids, ids_type == COCODC_I64, T,
+                     scale, static_cast<TOut*>(y), y_stride, lm->d_status);
       };
       // few packs: one per thread, so that they spread over the SMs.  65536 x 1024 in us at U = 2 / 4: fp32 to bf16 40.9 / 36.6,
       // bf16 to bf16 33.3 / 28.6, fp32 to fp32 66.0 / 71.8
       constexpr int U = sizeof(TIn) + sizeof(TOut) == 8 ? 2 : 4;
-      if (!wide) run(k_embed<TIn, TOut, 1, 4>, 1, 4);
-      else if (T * (D / 8) < (long long)lm->sm_count * 2048) run(k_embed<TIn, TOut, 8, 1>, 8, 1);
-      else run(k_embed<TIn, TOut, 8, U>, 8, U);
-      return true;
+      if (!wide) return run(k_embed<TIn, TOut, 1, 4>, 1, 4);
+      if (T * (D / 8) < (long long)lm->sm_count * 2048) return run(k_embed<TIn, TOut, 8, 1>, 8, 1);
+      return run(k_embed<TIn, TOut, 8, U>, 8, U);
     });
   });
-  return launched(lm);
 }
 
 uint64_t cocodc_lm_embed_grad_workspace(int64_t V, int64_t D, int64_t T) {
@@ -626,21 +624,19 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
   a.bins_log2 = bins_log2_for(V);
   a.bin_rows = (int)bin_rows_for(V);
   const unsigned bins = 1u << a.bins_log2, smem_sort = sort_smem(a.bin_rows);
-  if (a.is64) start(k_embed_sort<long long>, bins, kSortThreads, smem_sort, st, 1, a);
-  else start(k_embed_sort<int>, bins, kSortThreads, smem_sort, st, 1, a);
-  if (T > 0)
-    with_type(dy_type, [&](auto in) {
-      return with_type(dtable_type, [&](auto out) {
-        using TIn = decltype(in);
-        using TOut = decltype(out);
-        const dim3 grid((unsigned)tiles, (unsigned)columns);
-        const unsigned smem = kGroups * 2 * width * W * sizeof(float);
-        if (W > 1) start(k_embed_sum<TIn, TOut, 16 / (int)sizeof(TIn)>, grid, kGroups * width, smem, st, 1, a);
-        else start(k_embed_sum<TIn, TOut, 1>, grid, kGroups * width, smem, st, 1, a);
-        return true;
-      });
+  const cocodc_status sorted = a.is64 ? start(lm, k_embed_sort<long long>, bins, kSortThreads, smem_sort, st, 1, a)
+                                      : start(lm, k_embed_sort<int>, bins, kSortThreads, smem_sort, st, 1, a);
+  if (sorted != COCODC_OK || T == 0) return sorted;
+  return with_type(dy_type, [&](auto in) {
+    return with_type(dtable_type, [&](auto out) {
+      using TIn = decltype(in);
+      using TOut = decltype(out);
+      const dim3 grid((unsigned)tiles, (unsigned)columns);
+      const unsigned smem = kGroups * 2 * width * W * sizeof(float);
+      return W > 1 ? start(lm, k_embed_sum<TIn, TOut, 16 / (int)sizeof(TIn)>, grid, kGroups * width, smem, st, 1, a)
+                   : start(lm, k_embed_sum<TIn, TOut, 1>, grid, kGroups * width, smem, st, 1, a);
     });
-  return launched(lm, T > 0 ? 2 : 1);
+  });
 }
 
 }  // extern "C"

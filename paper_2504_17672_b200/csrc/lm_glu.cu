@@ -336,8 +336,7 @@ template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t strid
 template <typename E, int MODE, int ACT, int BN> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
   const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices, most = lm->sm_count;
   if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;
-  start(k_glu_tc<E, MODE, ACT, BN>, (unsigned)(tiles < most ? tiles : most), kTcThreads, TcShape<BN>::kSmem, st, 1, a);
-  return launched(lm);
+  return start(lm, k_glu_tc<E, MODE, ACT, BN>, (unsigned)(tiles < most ? tiles : most), kTcThreads, TcShape<BN>::kSmem, st, 1, a);
 }
 
 int a_rows_for(int64_t T) { return T >= kBM ? kBM : (int)((T + 7) / 8 * 8); }
@@ -423,10 +422,9 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
       const FewArgs<E> p{static_cast<const E*>(x), static_cast<const E*>(wg), static_cast<const E*>(wu), x_stride, w_stride,
                          (int)T, (int)D, (int)F, static_cast<E*>(h), static_cast<E*>(gate), static_cast<E*>(up), h_stride, gu_stride};
       const unsigned grid = (unsigned)((F + 7) / 8);
-      if (T <= 8) start(k_glu_few<E, A, 1>, grid, kFewWarps * 32, 0, st, 1, p);
-      else if (T <= 16) start(k_glu_few<E, A, 2>, grid, kFewWarps * 32, 0, st, 1, p);
-      else start(k_glu_few<E, A, 4>, grid, kFewWarps * 32, 0, st, 1, p);
-      result = launched(lm);
+      result = T <= 8    ? start(lm, k_glu_few<E, A, 1>, grid, kFewWarps * 32, 0, st, 1, p)
+               : T <= 16 ? start(lm, k_glu_few<E, A, 2>, grid, kFewWarps * 32, 0, st, 1, p)
+                         : start(lm, k_glu_few<E, A, 4>, grid, kFewWarps * 32, 0, st, 1, p);
       return;
     }
     if (tensor) {
@@ -464,8 +462,7 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
     p.ld = h_stride;
     p.ld_gu = gu_stride;
     const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((F + kTile - 1) / kTile));
-    start(k_glu_plain<E, decltype(a)::value>, grid, 256, 0, st, 1, p);
-    result = launched(lm);
+    result = start(lm, k_glu_plain<E, decltype(a)::value>, grid, 256, 0, st, 1, p);
   });
   return result;
 }
@@ -514,18 +511,16 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
     const int64_t pitch = scratch_pitch(F);
     E* dg = static_cast<E*>(workspace);
     E* du = dg + T * pitch;
-    const auto took = [&](cocodc_status s) { if (result == COCODC_OK) result = s; };
     if (T > 0) {
       const bool wide = rows_aligned(dh, dh_stride, 2) && rows_aligned(gate, gu_stride, 2) && rows_aligned(up, gu_stride, 2);
       const auto slope = [&](auto kernel, int W) {
         const long long blocks = (T * ((F + W - 1) / W) + 255) / 256;
-        start(kernel, (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st, 1,
-            static_cast<const E*>(dh), dh_stride, static_cast<const E*>(gate), static_cast<const E*>(up), gu_stride, T,
-            (unsigned)F, dg, du, pitch);
+        return start(lm, kernel, (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), 256, 0, st, 1,
+                     static_cast<const E*>(dh), dh_stride, static_cast<const E*>(gate), static_cast<const E*>(up), gu_stride, T,
+                     (unsigned)F, dg, du, pitch);
       };
-      if (wide) slope(k_glu_slope<E, decltype(a)::value, true>, 8);
-      else slope(k_glu_slope<E, decltype(a)::value, false>, 1);
-      took(launched(lm));
+      result = wide ? slope(k_glu_slope<E, decltype(a)::value, true>, 8) : slope(k_glu_slope<E, decltype(a)::value, false>, 1);
+      if (result != COCODC_OK) return;                 // dg and du were not written
     }
     TcArgs c{};
     c.status = lm->d_status;
@@ -553,20 +548,15 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       c.ld[0] = dx_stride;
       c.k_blocks = tiles_of(F, kBK);
       c.M = (int)T;
-      if (!ok) {
-        took(COCODC_ERR_CUDA);
-      } else if (splits == 1) {
-        took(run(std::integral_constant<int, GLU_DX>(), width));
-      } else {
-        const auto in_parts = [&](auto w) {
-          constexpr int BN = decltype(w)::value;
-          took(run_tc<E, GLU_DX_PARTS, 0, BN>(lm, c, st));
-          start(k_add_parts<E, BN>, (unsigned)(c.m_tiles * c.n_tiles * (kBM / 8)), 256, 0, st, 1, c);
-          took(launched(lm));
-        };
-        if (width == 64) in_parts(std::integral_constant<int, 64>());
-        else in_parts(std::integral_constant<int, 256>());
-      }
+      const auto in_parts = [&](auto w) {
+        constexpr int BN = decltype(w)::value;
+        const cocodc_status s = run_tc<E, GLU_DX_PARTS, 0, BN>(lm, c, st);
+        return s != COCODC_OK ? s : start(lm, k_add_parts<E, BN>, (unsigned)(c.m_tiles * c.n_tiles * (kBM / 8)), 256, 0, st, 1, c);
+      };
+      result = !ok           ? COCODC_ERR_CUDA
+               : splits == 1 ? run(std::integral_constant<int, GLU_DX>(), width)
+               : width == 64 ? in_parts(std::integral_constant<int, 64>())
+                             : in_parts(std::integral_constant<int, 256>());
     } else if (dx && T > 0) {
       PlainArgs<E> p{};
       p.a[0] = {dg, pitch, 1};
@@ -577,9 +567,9 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       p.out[0] = static_cast<E*>(dx);
       p.ld = dx_stride;
       const dim3 grid((unsigned)((T + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile));
-      start(k_product_plain<E, true>, grid, 256, 0, st, 1, p);
-      took(launched(lm));
+      result = start(lm, k_product_plain<E, true>, grid, 256, 0, st, 1, p);
     }
+    if (result != COCODC_OK) return;
     if (dwg && tensor_dw && T > 0) {
       const int width = width_for(lm, 2 * F, D, 256);
       c.n_tiles = tiles_of(D, width);
@@ -594,7 +584,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       c.ld[0] = c.ld[1] = dw_stride;
       c.k_blocks = tiles_of(T, kBK);
       c.M = (int)F;
-      took(ok ? run(std::integral_constant<int, GLU_DW>(), width) : COCODC_ERR_CUDA);
+      result = ok ? run(std::integral_constant<int, GLU_DW>(), width) : COCODC_ERR_CUDA;
     } else if (dwg) {
       PlainArgs<E> p{};
       p.a[0] = {dg, 1, pitch};
@@ -605,8 +595,7 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
       p.out[1] = static_cast<E*>(dwu);
       p.ld = dw_stride;
       const dim3 grid((unsigned)((F + kTile - 1) / kTile), (unsigned)((D + kTile - 1) / kTile), 2);
-      start(k_product_plain<E, false>, grid, 256, 0, st, 1, p);
-      took(launched(lm));
+      result = start(lm, k_product_plain<E, false>, grid, 256, 0, st, 1, p);
     }
   });
   return result;

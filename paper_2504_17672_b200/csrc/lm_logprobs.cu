@@ -589,10 +589,10 @@ __global__ void __launch_bounds__(kThreads, 8) k_logprobs_grad(const GradArgs a,
   const float h = a.dentropy ? a.scale * a.dentropy[t] : 0.f, H = a.dentropy ? a.entropy[t] : 0.f;
   if (!(lse < INFINITY)) g = NAN;
   const bool none = lse == -INFINITY;
-  // -p (g + h (log p + H)), the bracket as one fma of log p; log p is kept above -1e4, where p is 0, so that a masked logit's -Inf does not meet that 0.  The product
-  // with the scale is rounded before lse is taken off, as it was in lse: the largest logit's log p is then never above 0, while in one
-  // fma the product's rounding would stay and be exponentiated.  (As single products: of a product
-  // of pairs and a sum of pairs that fma is made all the same.)
+  // -p (g + h (log p + H)), the bracket as one fma of log p; log p is kept above -1e4, where p is 0, so that a masked logit's -Inf
+  // does not meet that 0.  The product with the scale is rounded before lse is taken off, as it was in lse: the largest logit's
+  // log p is then never above 0, while in one fma the product's rounding would stay and be exponentiated.  (As single products: of a
+  // product of pairs and a sum of pairs that fma is made all the same.)
   const f32x2 lse2 = pair_of(-lse, -lse), log2e2 = pair_of(kLog2e, kLog2e),
               slope = pair_of(-h, -h), level = pair_of(-fmaf(h, H, g), -fmaf(h, H, g));
   const auto slope2 = [&](f32x2 x) {
@@ -693,13 +693,11 @@ cocodc_status cocodc_lm_logprobs(cocodc_lm* lm, const void* logits, int32_t type
   while (parts < 8 && T * parts < lm->sm_count && V * es >= 8192 * parts) parts *= 2;
   while (parts < 8 && T * parts < 2 * lm->sm_count && V * es >= 2 * 49152 * parts) parts *= 2;
   if (T > INT32_MAX / parts) return COCODC_ERR_INVALID_ARG;
-  with_type(type, [&](auto x) {
+  return with_type(type, [&](auto x) {
     using E = decltype(x);
-    start(top_k ? k_logprobs<E, true> : k_logprobs<E, false>, (unsigned)(T * parts), kThreads, 0,
-          static_cast<cudaStream_t>(stream), (unsigned)parts, a, parts);
-    return true;
+    return start(lm, top_k ? k_logprobs<E, true> : k_logprobs<E, false>, (unsigned)(T * parts), kThreads, 0,
+                 static_cast<cudaStream_t>(stream), (unsigned)parts, a, parts);
   });
-  return launched(lm);
 }
 
 cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t type, int64_t stride, int64_t T,
@@ -733,11 +731,10 @@ cocodc_status cocodc_lm_logprobs_grad(cocodc_lm* lm, const void* logits, int32_t
   if (!scope.ok) return COCODC_ERR_CUDA;
   const GradArgs a{logits, stride, T, (unsigned)V, targets, targets_type == COCODC_I64, scale, lse, entropy, dlogp,
                    dentropy, dlogits, dlogits_stride, lm->d_status};
-  with_type(type, [&](auto x) {
-    start(k_logprobs_grad<decltype(x)>, (unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream), 1, a, (unsigned)chunks);
-    return true;
+  return with_type(type, [&](auto x) {
+    return start(lm, k_logprobs_grad<decltype(x)>, (unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream), 1, a,
+                 (unsigned)chunks);
   });
-  return launched(lm);
 }
 
 }  // extern "C"
