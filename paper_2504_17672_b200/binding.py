@@ -588,11 +588,11 @@ class LmOps:
         tp, tt = _ids(targets, "targets", T) if targets is not None else (0, 0)
         f32 = torch.float32
         k = kp = kl = 0
-        if top_ids is not None:
-            if top_ids.dim() != 2 or top_ids.shape[0] != T:
-                raise ValueError("top_ids must be T x k")
-            k = top_ids.shape[1]
-        if k:
+        if top_ids is not None or top_logp is not None:      # one without the other is refused by the call
+            shape = (top_logp if top_ids is None else top_ids).shape
+            if len(shape) != 2 or shape[0] != T:
+                raise ValueError("top_ids and top_logp must be T x k")
+            k = shape[1]
             kp, kl = _vector(top_ids, "top_ids", T * k, torch.int32), _vector(top_logp, "top_logp", T * k, f32)
         code = _submit(self._h, _LOGPROBS(4, lp, _type(logits), ls, T, V, tp, tt, scale, _vector(logp, "logp", T, f32),
                                           _vector(entropy, "entropy", T, f32), _vector(lse, "lse", T, f32), k, kp, kl,
