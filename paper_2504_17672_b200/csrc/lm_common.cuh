@@ -38,6 +38,8 @@ struct DeviceScope {
 // Launches with programmatic dependence on the stream's previous kernel: the next kernel's blocks may become resident once
 // all blocks of this one have called may_follow(), and touch global memory only after wait_for_previous() (which
 // returns when the previous kernel is done and its writes are visible), so that launch and set-up hide behind its end.
+// What they read may thus have been written during their own lifetime: ordinary loads only, none through the read-only path (__ldg,
+// ld.global.nc, const __restrict__ pointers), which is for data that no one writes while the kernel exists.
 // The status is this launch's own, whatever the thread has left of older errors; what would read its results is not launched after a failure.
 template <typename... P, typename... A>
 inline cocodc_status start(cocodc_lm* lm, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, cudaStream_t st,
@@ -100,6 +102,13 @@ inline bool meet(const Span& a, const Span& b) {
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void may_follow() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// 16 bytes by an ordinary load.  As volatile assembly it stays behind wait_for_previous(), and where it was written: plain C++
+// loads took more registers in k_logprobs (4000 x 50257 bf16 with eight alternatives: 92 -> 96 us).
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }

@@ -41,7 +41,7 @@ template <typename T, int W> struct Raw {
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (W == 1) e[0] = *p;
     else
-      for (int i = 0; i < W * (int)sizeof(T) / 16; ++i) reinterpret_cast<uint4*>(e)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+      for (int i = 0; i < W * (int)sizeof(T) / 16; ++i) reinterpret_cast<uint4*>(e)[i] = load16(reinterpret_cast<const uint4*>(p) + i);
   }
   __device__ __forceinline__ float at(int i) const { return to_f32(e[i]); }
 };
@@ -69,9 +69,9 @@ template <int W, bool GLOBAL> __device__ __forceinline__ void get(float (&v)[W],
 // bfloat16; 8 rows of 768 in 1.9 us.  `lanes` neighbouring lanes (a power of two, up to a warp) take up to U packs of W elements each
 // of one token's row, all loads before the first store; a longer row is several items.
 template <typename TIn, typename TOut, int W, int U>
-__global__ void __launch_bounds__(256) k_embed(const TIn* __restrict__ table, long long table_stride, long long V,
+__global__ void __launch_bounds__(256) k_embed(const TIn* table, long long table_stride, long long V,
                                                unsigned packs, int lanes_log2, unsigned items_per_row, const void* ids,
-                                               int is64, long long T, float scale, TOut* __restrict__ y, long long y_stride,
+                                               int is64, long long T, float scale, TOut* y, long long y_stride,
                                                int* status) {
   wait_for_previous();
   may_follow();
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
       const int first = t + lane * 4;
       if (wide && first + 4 <= t1) {
         constexpr int words = 4 * sizeof(I) / 16;
-        for (int i = 0; i < words; ++i) reinterpret_cast<uint4*>(next)[i] = __ldg(reinterpret_cast<const uint4*>(ids + first) + i);
+        for (int i = 0; i < words; ++i) reinterpret_cast<uint4*>(next)[i] = load16(reinterpret_cast<const uint4*>(ids + first) + i);
       } else {
         for (int i = 0; i < 4; ++i) next[i] = first + i < t1 ? ids[first + i] : I(-1);
       }

@@ -143,7 +143,7 @@ template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], unsi
 // weights: read once, not kept in L1
 __device__ __forceinline__ uint4 load_once(const void* p) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];"
+  asm volatile("ld.global.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : TILES == 2 ? 
         g[i][k] = load_once(wg + at);
         u[i][k] = load_once(wu + at);
 #pragma unroll
-        for (int n = 0; n < TILES; ++n) x[i][n][k] = __ldg(reinterpret_cast<const uint4*>(tokens[n] + at));
+        for (int n = 0; n < TILES; ++n) x[i][n][k] = load16(tokens[n] + at);
       }
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -245,9 +245,9 @@ __global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : TILES == 2 ? 
 // the writes still in L2).  WIDE: the inputs' rows start on 16-byte
 // boundaries; a thread takes 8 columns (the last ones of a row one by one), otherwise one.
 template <typename T, int ACT, bool WIDE>
-__global__ void __launch_bounds__(256) k_glu_slope(const T* __restrict__ dh, long long dh_stride, const T* __restrict__ gate,
-                                                   const T* __restrict__ up, long long gu_stride, long long rows, unsigned F,
-                                                   T* __restrict__ dg, T* __restrict__ du, long long pitch) {
+__global__ void __launch_bounds__(256) k_glu_slope(const T* dh, long long dh_stride, const T* gate, const T* up,
+                                                   long long gu_stride, long long rows, unsigned F, T* dg, T* du,
+                                                   long long pitch) {
   wait_for_previous();
   may_follow();
   constexpr unsigned W = WIDE ? 8 : 1;
@@ -265,8 +265,7 @@ __global__ void __launch_bounds__(256) k_glu_slope(const T* __restrict__ dh, lon
     if (t >= rows) return;
     const T *pd = dh + t * dh_stride + f, *pg = gate + t * gu_stride + f, *pu = up + t * gu_stride + f;
     if (WIDE && f + 8 <= F) {
-      const uint4 rd = __ldg(reinterpret_cast<const uint4*>(pd)), rg = __ldg(reinterpret_cast<const uint4*>(pg)),
-                  ru = __ldg(reinterpret_cast<const uint4*>(pu));
+      const uint4 rd = load16(pd), rg = load16(pg), ru = load16(pu);
       const T *d = reinterpret_cast<const T*>(&rd), *g = reinterpret_cast<const T*>(&rg), *u = reinterpret_cast<const T*>(&ru);
       unsigned og[4], ou[4];
       for (int i = 0; i < 4; ++i) {

@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
     uint4 raw[N];
     W w[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) raw[k] = !count.partial || i + k * kThreads < n ? __ldg(src + i + k * kThreads) : W::far();
+    for (int k = 0; k < N; ++k) raw[k] = !count.partial || i + k * kThreads < n ? load16(src + i + k * kThreads) : W::far();
 #pragma unroll
     for (int k = 0; k < N; ++k) w[k].set(raw[k]);
     float m = w[0].largest();
@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
           if (lane == 1 && tail + who < j1) offer(to_f32(row[tail + who]), tail + who);
           for (unsigned i = who + lane * kThreads; i < n; i += 32 * kThreads) {
             W w;
-            w.set(__ldg(src + i));
+            w.set(load16(src + i));
             if (ordered(w.largest()) < tau) continue;
 #pragma unroll
             for (int q = 0; q < W::n; ++q) offer(w.at(q), base + i * W::n + q);
