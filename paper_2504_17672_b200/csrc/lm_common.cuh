@@ -102,6 +102,12 @@ inline bool meet(const Span& a, const Span& b) {
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void may_follow() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// All threads of the cluster have come here, and what they wrote to shared memory before is visible to all after.  (The lanes of a warp
+// come to an .aligned instruction together, which after a branch only __syncwarp() promises.)
+__device__ __forceinline__ void cluster_barrier() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // 16 bytes by an ordinary load.  As volatile assembly it stays behind wait_for_previous(), and where it was written: plain C++
 // loads took more registers in k_logprobs (4000 x 50257 bf16 with eight alternatives: 92 -> 96 us).
 __device__ __forceinline__ uint4 load16(const void* p) {

@@ -214,7 +214,11 @@ __global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : TILES == 2 ? 
       const int at = whole * 64 + k * 8, left = p.D - at - q * 16;
       const uint4 g = load_end(wg + at, left), u = load_end(wu + at, left);
 #pragma unroll
-      for (int n = 0; n < TILES; ++n) multiply(g, u, load_end(tokens[n] + at, left), n);
+      for (int n = 0; n < TILES; ++n) {
+        const uint4 x = load_end(tokens[n] + at, left);
+        __syncwarp();                                             // lanes load different numbers of elements; mma.sync takes them together
+        multiply(g, u, x, n);
+      }
     }
   }
 #pragma unroll

@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
   const unsigned long long* top = sh.top;
   if (parts > 1) {
     if (tid == 0) sh.part = x;
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_barrier();
     if (part == 0) {
       if (tid == 0) {
         const unsigned here = (unsigned)__cvta_generic_to_shared(&sh.part);
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int part
       }
     }
     // the others' shared memory stays until it has been read
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_barrier();
     if (part != 0) return;
   }
 

@@ -60,11 +60,15 @@ __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.w
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ---- tcgen05 ------------------------------------------------------------------------------------
+// An .aligned instruction is for warps whose lanes are together, which after a branch that lanes took differently nothing but
+// __syncwarp() promises; the wrappers of those that follow such branches begin with it.
 __device__ __forceinline__ void tmem_alloc(unsigned dst_smem, int columns) {
+  __syncwarp();
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(columns) : "memory");
   asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
 }
 __device__ __forceinline__ void tmem_free(unsigned addr, int columns) {
+  __syncwarp();
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -80,6 +84,7 @@ __device__ __forceinline__ void tc_commit(unsigned bar) {
 // 32 columns of this warp's 32 TMEM lanes: v[i] is column i of the thread's lane
 __device__ __forceinline__ void tmem_load32(float (&v)[32], unsigned addr) {
   unsigned r[32];
+  __syncwarp();
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
       "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
