@@ -20,7 +20,7 @@
  *     buffer (rows equally far apart) do not overlap; matrices with different distances of their rows must not lie within each other.
  *   - Calls are asynchronous on the given stream and allocate nothing.  Calls that need scratch take it as a
  *     workspace (16-byte aligned, at least cocodc_lm_*_workspace bytes, contents arbitrary and undefined
- *     afterwards).  Nothing is kept from one call for the next, so one handle may be used on several streams
+ *     afterwards; the size is 0 where the call refuses the sizes).  Nothing is kept from one call for the next, so one handle may be used on several streams
  *     and from several threads at the same time as long as the calls' workspaces differ.  Kernels are launched with
  *     programmatic dependence on the stream's previous kernel; they touch no memory before it has finished.
  *   - T = 0 (no tokens) is legal everywhere; pointers to nothing may then be NULL or not.

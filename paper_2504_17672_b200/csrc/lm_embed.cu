@@ -119,6 +119,7 @@ constexpr int kBinPitch = kSortWarps + 1;              // counters of a warp's l
 constexpr int kListLength = 512;                       // hits that a warp keeps, at most 128 of them new per step
 constexpr int kRowBits = 10;                           // of a list entry; the others hold the position in the warp's part
 constexpr long long kMostTokens = 1ll << (32 - kRowBits + 5);
+constexpr long long kMostRows = 1ll << 30;
 static_assert(kMaxBinRows <= 1 << kRowBits, "a bin's rows do not fit a list entry");
 
 struct GradArgs {
@@ -563,7 +564,7 @@ cocodc_status cocodc_lm_embed(cocodc_lm* lm, const void* table, int32_t table_ty
 }
 
 uint64_t cocodc_lm_embed_grad_workspace(int64_t V, int64_t D, int64_t T) {
-  if (!sane(V) || !sane(D) || !sane(T)) return 0;
+  if (V < 0 || D < 0 || T < 0 || V > kMostRows || D > INT32_MAX || T > kMostTokens) return 0;
   const uint64_t tiles = (uint64_t)tiles_for(T);
   return up16((uint64_t)starts_for(V) * sizeof(int)) + up16((uint64_t)T * sizeof(int2)) + tiles * 2 * padded(D) * sizeof(float) +
          up16(tiles * (uint64_t)((D + 31) / 32) * sizeof(int));
@@ -573,7 +574,7 @@ cocodc_status cocodc_lm_embed_grad(cocodc_lm* lm, const void* dy, int32_t dy_typ
                                    int32_t ids_type, int64_t T, int64_t V, int64_t D, float scale, int32_t accumulate,
                                    void* dtable, int32_t dtable_type, int64_t dtable_stride, void* workspace,
                                    uint64_t workspace_bytes, void* stream) {
-  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || T > kMostTokens || V > (int64_t(1) << 30) || !dtable ||
+  if (!lm || !sane(V) || !sane(D) || !sane(T) || V < 1 || D < 1 || D > INT32_MAX || T > kMostTokens || V > kMostRows || !dtable ||
       !known_type(dy_type) || !known_type(dtable_type) || (ids_type != COCODC_I32 && ids_type != COCODC_I64) ||
       dy_stride < D || dtable_stride < D || !sane(dy_stride) || !sane(dtable_stride))
     return COCODC_ERR_INVALID_ARG;

@@ -471,7 +471,7 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
 }
 
 uint64_t cocodc_lm_glu_grad_workspace(int64_t T, int64_t D, int64_t F) {
-  if (!sane(T) || !sane(D) || !sane(F)) return 0;
+  if (T < 0 || D < 0 || F < 0 || T > INT32_MAX || D > INT32_MAX || F > INT32_MAX) return 0;
   return 16 + 2 * (uint64_t)T * (uint64_t)scratch_pitch(F) * 2 + part_bytes(T, D, F);
 }
 
