@@ -94,7 +94,7 @@ cocodc_status cocodc_lm_glu(cocodc_lm* lm, int32_t act, int32_t type, const void
  * Its gradient.  With dg = dh * up * act'(gate) and du = dh * act(gate):
  *   dx = dg Wg + du Wu   [T][D]        dwg = dg^T x, dwu = du^T x   [F][D] (one stride)
  * dx may be NULL; dwg and dwu may both be NULL.  dg and du are rounded to the type between the element-wise part
- * and the products, as tensor cores take them; the products accumulate in fp32.  T = 0 sets dwg and dwu to zero.
+ * and the products, as tensor cores take them (F16: Inf beyond 65504); the products accumulate in fp32.  T = 0 sets dwg and dwu to zero.
  */
 uint64_t cocodc_lm_glu_grad_workspace(int64_t T, int64_t D, int64_t F);
 cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const void* dh, int64_t dh_stride,
@@ -115,6 +115,9 @@ cocodc_status cocodc_lm_glu_grad(cocodc_lm* lm, int32_t act, int32_t type, const
  * Masked logits (-Inf) have p = 0 and add nothing to the entropy.  A row of nothing but -Inf has lse = -Inf,
  * entropy 0 and log probabilities -Inf.  A row with a NaN or +Inf has NaN in lse, entropy, logp (where y >= 0)
  * and top_logp; among its alternatives NaN ranks above +Inf.
+ * Rows (where T is small, parts of a row) with such a value, with nothing left above a mask of -1e9 or lower or less than top_k, with
+ * more than 1024 equal logits among the largest, or with |scale * logit| above 7e8 are read again element by element: once or twice for the
+ * sums, top_k times for the alternatives (ten times the time for top_k = 8 where all of many rows are so).
  * All finite logits and all legal scales are good; lse is +-Inf where it leaves fp32's range, the other outputs do not suffer from it.
  */
 #define COCODC_LM_MAX_TOP 32

@@ -54,7 +54,7 @@ cocodc_status cocodc_lm_create(cocodc_lm** lm_out, int32_t device) {
   bool ok = cudaDeviceGetAttribute(&lm->sm_count, cudaDevAttrMultiProcessorCount, device) == cudaSuccess;
   ok = ok && cudaMalloc(&lm->d_status, sizeof(int)) == cudaSuccess;
   ok = ok && cudaMemset(lm->d_status, 0, sizeof(int)) == cudaSuccess;
-  ok = ok && embed_prepare() && glu_prepare() && logprobs_prepare();
+  ok = ok && embed_prepare() && glu_prepare();
   if (!ok) {
     cudaGetLastError();
     cudaFree(lm->d_status);

@@ -19,11 +19,10 @@ struct cocodc_lm {
 
 namespace cocodc_lm_impl {
 
-// Each source file opts its kernels in to the shared memory they need, once, at creation of a handle (the
+// The source files whose kernels need more shared memory than any kernel may have opt them in, at creation of a handle (the
 // attribute is per device and outlives the handle).
 bool embed_prepare();
 bool glu_prepare();
-bool logprobs_prepare();
 
 struct DeviceScope {
   int prev = -1;

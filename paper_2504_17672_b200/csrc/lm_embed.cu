@@ -482,7 +482,8 @@ __global__ void __launch_bounds__(kGroups * 128, 2) k_embed_sum(const GradArgs a
   }
 }
 
-// Sorted entries per group (a lane each): 32 amortise the boundaries; with few tokens fewer, so that there are tiles for all SMs.
+// Sorted entries per group (a lane each): 32 amortise the boundaries; with few tokens fewer, so that there are tiles for all SMs.  (148, a
+// B200's: the size of a workspace is asked for without a handle.)
 int positions_for(int64_t T) {
   int p = 32;
   while (p > 4 && T < (int64_t)148 * 2 * kGroups * p) p /= 2;

@@ -308,7 +308,7 @@ int tiles_of(int64_t n, int tile) { return (int)((n + tile - 1) / tile); }
 // tile, with at least 16 k-blocks to a part.  One row of tiles takes narrow ones (more SMs read weights), more rows the
 // widest (the tokens are read once per tile); 2048 x 5632 without parts, with parts of 64 and of 256 columns, us for the
 // whole of dx: 128 tokens 57 / 28 / 35, 512 tokens 59 / 61 (no parts) / 41.
-constexpr int kPartTiles = 148;                       // tiles x parts at most; bounds the scratch
+constexpr int kPartTiles = 148;                       // tiles x parts at most: a B200's SMs (the workspace's size is asked for without a handle)
 int part_width(int64_t T) { return T <= kBM ? 64 : 256; }
 int parts_for(int64_t T, int64_t D, int64_t F) {
   const long long tiles = (long long)tiles_of(T, kBM) * tiles_of(D, part_width(T)), blocks = 2ll * tiles_of(F, kBK);

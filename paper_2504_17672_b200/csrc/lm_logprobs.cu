@@ -200,11 +200,8 @@ __device__ __forceinline__ Stats block_join(Stats x, float c, Stats* scratch) {
 template <typename T>
 __device__ __noinline__ Stats careful_stats(const T* row, unsigned j0, unsigned j1, float c, Stats* scratch) {
   Stats x{-INFINITY, 0.f, 0.f};
-  bool nan = false;
   for (unsigned j = j0 + threadIdx.x; j < j1; j += kThreads) {
-    const float v = to_f32(row[j]);
-    nan |= v != v;
-    x.m = fmaxf(x.m, v);
+    x.m = fmaxf(x.m, to_f32(row[j]));
   }
   for (int o = 16; o; o >>= 1) x.m = fmaxf(x.m, __shfl_xor_sync(~0u, x.m, o));
   __syncthreads();
@@ -220,7 +217,8 @@ __device__ __noinline__ Stats careful_stats(const T* row, unsigned j0, unsigned 
   }
   return block_join(x, c, scratch);
 }
-// The k largest keys of [j0, j1), in descending order in list[0 .. k): k walks.
+// The k largest keys of [j0, j1), in descending order in list[0 .. k): k walks, element by element.  1333 x 32000 fp32 with eight, where a
+// row takes this way: 49 -> 370-450 us; one row of 50257 bfloat16, some of whose eight parts do: 13 -> 25 us.
 template <typename T>
 __device__ __noinline__ void careful_top(const T* row, unsigned j0, unsigned j1, int k, unsigned long long* list,
                                          unsigned long long* scratch) {
@@ -335,9 +333,11 @@ struct RowShared {
 // batches of kUnroll 16-byte words; the parts are joined through shuffles and shared memory, and between the CTAs of a cluster (a row is
 // split over 1 to 8 CTAs, so that few rows still fill the GPU) through distributed shared memory.
 //
-// The alternatives cost the walk nothing: tau, the k-th largest of the threads' largest logits, is not above the k-th
+// Where nothing stands in the way, the alternatives cost the walk nothing: tau, the k-th largest of the threads' largest logits, is not above the k-th
 // largest logit, so every alternative lies with a thread whose largest logit is at least tau.  Only what those threads saw
-// is read again (from L2), and of it only logits >= tau are sorted, by value and position.
+// is read again (from L2), and of it only logits >= tau are sorted, by value and position.  The careful way instead: rows (of a few
+// rows, parts of a row) with a NaN or +Inf, with fewer threads that hold a logit above -kFar than alternatives, with more than
+// kCandidates equal logits at the border, and those whose sums have to be taken with care.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) k_logprobs(const RowArgs a, int parts) {
   wait_for_previous();
@@ -652,10 +652,6 @@ __global__ void __launch_bounds__(kThreads, 8) k_logprobs_grad(const GradArgs a,
 }
 
 }  // namespace
-
-namespace cocodc_lm_impl {
-bool logprobs_prepare() { return true; }
-}  // namespace cocodc_lm_impl
 
 extern "C" {
 
