@@ -64,9 +64,9 @@ template <int W, bool GLOBAL> __device__ __forceinline__ void get(float (&v)[W],
 }
 
 // ---- lookup ------------------------------------------------------------------------------------
-// A gather: bound by memory, and at fp32 tables by what L2 gives the SMs beside the writes: 65536 rows of 1024 in 39 us fp32 to
-// bfloat16 (134 MB written, 268 MB gathered, 64 MB of them from DRAM), 29 us bfloat16 to
-// bfloat16; 8 rows of 768 in 1.9 us.  `lanes` neighbouring lanes (a power of two, up to a warp) take up to U packs of W elements each
+// A gather: bound by memory, and at fp32 tables by what L2 gives the SMs beside the writes: 65536 rows of 1024 in 36 us fp32 to
+// bfloat16 (134 MB written, 268 MB gathered, 64 MB of them from DRAM), 28 us bfloat16 to
+// bfloat16; 65536 rows of 777, element by element, in 104 us; 8 rows of 768 in 1.4 us (in a graph).  `lanes` neighbouring lanes (a power of two, up to a warp) take up to U packs of W elements each
 // of one token's row, all loads before the first store; a longer row is several items.
 template <typename TIn, typename TOut, int W, int U>
 __global__ void __launch_bounds__(256) k_embed(const TIn* table, long long table_stride, long long V,
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const GradArgs a) {
 // starts a new sum where the row changes.  A row that lies inside one group is written at once.  Rows that cross group
 // boundaries are joined in shared memory in order; those that cross tile boundaries leave their parts in the
 // workspace, and the tile that arrives last at the row's counter adds all parts in tile order (nobody waits).
-// Measured: 45 us for 65536 gradients of 1024 bfloat16 (134 MB read, 79 MB written: 4.7 TB/s), 11 us for 4099 of 768.  The
+// Measured: 45 us for 65536 gradients of 1024 bfloat16 (134 MB read, 79 MB written: 4.7 TB/s), 13 us for 4099 of 768.  The
 // time not spent on bytes goes into the joins, most tiles begin and end inside a frequent token's row.  Eight loads
 // ahead instead of four spilled (62 us).
 constexpr int kGroups = 4;

@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(256) k_product_plain(const PlainArgs<T> p) {
 // contraction in blocks of 64 k, and every lane loads 32 consecutive bytes of a row of each matrix per block, straight
 // into fragments: the k's of a lane's fragment places are permuted, the same way for weights and tokens, which a
 // contraction does not notice.  The warps' sums meet in shared memory in fixed order.  TILES: groups of eight tokens.
-// Four CTAs per SM (64 registers) for one group: 11.2 -> 9.6 us at 2048 x 5632, 36.9 -> 32.6 us at 4096 x 11008; two groups
+// Four CTAs per SM (64 registers) for one group: 11.2 -> 9.6 us at 2048 x 5632, 36.9 -> 32.6 us at 4096 x 11008 (9.1 and 32 now, with early starts); two groups
 // then spill, and run three.
 constexpr int kFewWarps = 8;
 // Up to 8 tokens always; up to 32 where tokens (in eights) x D x F stay below kFewProduct, us here / on tcgen05 tiles: 16 tokens,
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, TILES == 1 ? 4 : TILES == 2 ? 
 
 // ---- the element-wise part of the gradient ------------------------------------------------------
 // dg and du go to scratch of pitch F rounded up to 8 elements, so that its rows start on 16-byte boundaries.
-// One read of dh, gate and up, one write of dg and du: bound by memory (8192 x 5632: 461 MB in 63 us, 7.3 TB/s with part of
+// One read of dh, gate and up, one write of dg and du: bound by memory (8192 x 5632: 461 MB in 65 us, 7.1 TB/s with part of
 // the writes still in L2).  WIDE: the inputs' rows start on 16-byte
 // boundaries; a thread takes 8 columns (the last ones of a row one by one), otherwise one.
 template <typename T, int ACT, bool WIDE>

@@ -10,9 +10,9 @@
 // thread of the epilogue finds gate and up of one element in its own TMEM lane and the product needs no exchange.
 // dx = dg Wg + du Wu: one accumulator, the k loop runs through both sources.  dw = d^T x: the tile index picks dg or du.
 // The operands of the gradient whose contraction runs along rows are taken MN-major as they lie in memory.
-// Measured: forward 8192 x 3200 x 8640 with gate and up kept 612 us alone (1.48 PFLOP/s, tensor pipe 80 % active) and 745 us
+// Measured: forward 8192 x 3200 x 8640 with gate and up kept 612-621 us alone (1.46-1.48 PFLOP/s, tensor pipe 81 % active) and 747-756 us
 // back to back, where the power cap lowers the clock (without keeping them 687 us; a library product of the same size
-// 645-685 us in the same loop); dx 270 us and dw 263 us alone at 8192 x 2048 x 5632 (1.40, 1.44 PFLOP/s).  Pairs of CTAs with
+// 645-685 us in the same loop); dx 270-276 us and dw 263-267 us alone at 8192 x 2048 x 5632 (1.40, 1.44 PFLOP/s).  Pairs of CTAs with
 // 256 x 256 tiles (cta_group::2) and a second set of epilogue warps were built and gave nothing at these sizes.
 // With few tokens dx has few tiles and a long contraction: it is cut into parts (GLU_DX_PARTS, the slowest tile index),
 // whose fp32 sums k_add_parts adds in order.

@@ -328,8 +328,8 @@ struct RowShared {
 };
 
 // A row is read once: bound by memory, closely followed by the issue slots (7 instructions a logit: unpacking, fma, exponential,
-// two sums, maximum).  8192 x 50257 bfloat16 in 146-154 us (5.4-5.6 TB/s), 1333 x 32000 fp32 with five alternatives in
-// 37 us, one row of 50257 with eight in 9 us.  Each thread keeps (m, s, u) of its own elements, rescaled when its largest logit grows, in
+// two sums, maximum).  8192 x 50257 bfloat16 in 145-153 us (5.4-5.7 TB/s), 1333 x 32000 fp32 with five alternatives in
+// 35 us, one row of 50257 with eight in 8.1 us, without in 4.0 (in a graph).  Each thread keeps (m, s, u) of its own elements, rescaled when its largest logit grows, in
 // batches of kUnroll 16-byte words; the parts are joined through shuffles and shared memory, and between the CTAs of a cluster (a row is
 // split over 1 to 8 CTAs, so that few rows still fill the GPU) through distributed shared memory.
 //
@@ -546,7 +546,7 @@ struct GradArgs {
   int* status;
 };
 
-// One read and one write of every logit: bound by memory (8192 x 50257 bfloat16 in 281 us, 5.9 TB/s).  A CTA takes a row or
+// One read and one write of every logit: bound by memory (8192 x 50257 bfloat16 in 278-281 us, 5.9 TB/s).  A CTA takes a row or
 // an even part of it: seven CTAs to a row, each with its own set-up, took 303 us.
 template <typename T> struct Out;   // packs results the way Words unpacks logits
 template <> struct Out<float> {
@@ -623,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 8) k_logprobs_grad(const GradArgs a,
   // the row's words dealt evenly to its CTAs
   const unsigned per = (words + chunks - 1) / chunks, end = min(words, (chunk + 1) * per);
   const long long hit_word = y < (long long)lead || y >= (long long)tail ? -1 : (y - lead) / n;
-  // neither the logits nor the gradient are needed again soon (streaming accesses: 310 -> 293 us at 8192 x 50257)
+  // neither the logits nor the gradient are needed again soon (streaming accesses: 310 -> 293 us at 8192 x 50257, when the rest took longer)
   const auto words_at = [&](unsigned i, auto count) {
     constexpr int N = decltype(count)::value;
     uint4 raw[N];
