@@ -35,6 +35,9 @@ EXPORTS = (
     "cocodc_lm_embed", "cocodc_lm_embed_grad", "cocodc_lm_embed_grad_workspace",
     "cocodc_lm_glu", "cocodc_lm_glu_grad", "cocodc_lm_glu_grad_workspace",
     "cocodc_lm_logprobs", "cocodc_lm_logprobs_grad", "cocodc_lm_submit",
+    "cocodc_lm_norm", "cocodc_lm_norm_grad", "cocodc_lm_norm_grad_workspace",
+    "cocodc_lm_head", "cocodc_lm_head_workspace", "cocodc_lm_head_grad", "cocodc_lm_head_grad_workspace",
+    "cocodc_lm_adam_create", "cocodc_lm_adam_destroy", "cocodc_lm_adamw",
 )
 NOALLOC_MAX_K, NOALLOC_MAX_SEGMENTS = 64, 64
 
@@ -57,6 +60,12 @@ class _Hyper(ctypes.Structure):
                 ("reserved", ctypes.c_int32), ("H", ctypes.c_int64), ("tau", ctypes.c_int64),
                 ("outer_lr", ctypes.c_float), ("momentum", ctypes.c_float),
                 ("lam", ctypes.c_float), ("alpha", ctypes.c_float)]
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("p", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [
+        ("n", ctypes.c_int64), ("grad_type", ctypes.c_int32), ("copy_type", ctypes.c_int32), ("decay", ctypes.c_float),
+        ("reserved", ctypes.c_int32)]
 
 
 @dataclass
@@ -130,8 +139,19 @@ def _load() -> ctypes.CDLL:
     lib.cocodc_lm_logprobs.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, i32, vp, vp, vp]
     lib.cocodc_lm_logprobs_grad.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, i64, vp]
     lib.cocodc_lm_submit.argtypes = [vp, ctypes.c_char_p]
+    lib.cocodc_lm_norm.argtypes = [vp, vp, i32, i64, vp, i64, i32, vp, i32, i64, i64, f32, vp, i64, vp, i32, i64, vp, i64, vp, vp]
+    lib.cocodc_lm_norm_grad.argtypes = [vp, vp, i32, i64, vp, i32, i64, vp, i32, vp, i64, i64, vp, i64, vp, i64, vp, i32, i32, vp, u64, vp]
+    lib.cocodc_lm_norm_grad_workspace.argtypes = [i64, i64]
+    lib.cocodc_lm_head.argtypes = [vp, i32, vp, i64, vp, i64, i64, i64, i64, vp, i32, f32, vp, vp, vp, u64, vp]
+    lib.cocodc_lm_head_grad.argtypes = [vp, i32, vp, i64, vp, i64, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, i64, vp, i32, i64, i32,
+                                        vp, u64, vp]
+    lib.cocodc_lm_head_workspace.argtypes = lib.cocodc_lm_head_grad_workspace.argtypes = [i64, i64, i64]
+    lib.cocodc_lm_adam_create.argtypes = [ctypes.POINTER(vp), vp, ctypes.POINTER(_Tensor), i64, i32]
+    lib.cocodc_lm_adam_destroy.argtypes = [vp]
+    lib.cocodc_lm_adamw.argtypes = [vp, vp, f64, f64, f64, f64, i64, vp, vp, vp, i64, vp]
     other = {"cocodc_launch_count": i64, "cocodc_status_string": ctypes.c_char_p, "cocodc_lm_launch_count": i64,
-             "cocodc_lm_embed_grad_workspace": u64, "cocodc_lm_glu_grad_workspace": u64}
+             "cocodc_lm_embed_grad_workspace": u64, "cocodc_lm_glu_grad_workspace": u64, "cocodc_lm_norm_grad_workspace": u64,
+             "cocodc_lm_head_workspace": u64, "cocodc_lm_head_grad_workspace": u64}
     for name, restype in other.items():
         getattr(lib, name).restype = restype
     for name in EXPORTS:
@@ -372,12 +392,15 @@ class Context:
 
 ACT_SILU, ACT_GELU = 0, 1
 LM_MAX_TOP = 32
+LM_ADAM_BLOCK = 256
+E4M3 = 3                                                 # COCODC_E4M3: torch.float8_e4m3fn
 _ACTS = {"silu": ACT_SILU, "gelu": ACT_GELU, ACT_SILU: ACT_SILU, ACT_GELU: ACT_GELU}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
 # records of cocodc_lm_submit: the operator's number, then its arguments (q: pointer or integer, d: scale)
-_EMBED, _EMBED_GRAD, _GLU, _GLU_GRAD, _LOGPROBS, _LOGPROBS_GRAD = (
-    struct.Struct("=" + f).pack for f in ("9qd4q", "9qd7q", "17q", "24q", "8qd7q", "8qd7q"))
+_EMBED, _EMBED_GRAD, _GLU, _GLU_GRAD, _LOGPROBS, _LOGPROBS_GRAD, _NORM, _NORM_GRAD, _HEAD, _HEAD_GRAD, _ADAMW = (
+    struct.Struct("=" + f).pack for f in ("9qd4q", "9qd7q", "17q", "24q", "8qd7q", "8qd7q", "11qd9q", "22q", "11qd5q", "11qd12q",
+                                          "2q4d6q"))
 _submit = _lib.cocodc_lm_submit
 
 
@@ -434,6 +457,55 @@ def _one_type(*tensors) -> int:
 def _sized(name: str, rows: int, cols: int, want_rows: int, want_cols: int) -> None:
     if rows != want_rows or cols != want_cols:
         raise ValueError(f"{name} must be {want_rows} x {want_cols}, not {rows} x {cols}")
+
+
+class AdamTensors:
+    """Owns a cocodc_lm_adam: the tensors of a model as cocodc_lm_adamw steps them.
+
+    params: packed float32 tensors; grads of any type; m and v float32, or float8_e4m3fn with their scales (m_scales, v_scales: one
+    float32 for every 256 elements, begun at zero like m and v); decay: a number or one for each tensor; copies: 16-bit tensors
+    (or None each) that receive the stepped parameters.  The tensors are kept alive and have to stay where they are."""
+
+    def __init__(self, ops: "LmOps", params, grads, m, v, decay=0.0, copies=None, m_scales=None, v_scales=None):
+        self._h = ctypes.c_void_p()
+        params, grads, m, v = (list(x) for x in (params, grads, m, v))
+        count = len(params)
+        fill = lambda x: [None] * count if x is None else list(x)  # noqa: E731
+        copies, m_scales, v_scales = fill(copies), fill(m_scales), fill(v_scales)
+        decay = list(decay) if isinstance(decay, Sequence) else [float(decay)] * count
+        lists = (params, grads, m, v, copies, m_scales, v_scales, decay)
+        if any(len(x) != count for x in lists):
+            raise ValueError("one of every list is needed for each tensor")
+        self.tensors, self.count = lists, count
+        state = torch.float32 if count == 0 or m[0] is None else m[0].dtype
+        if state not in (torch.float32, torch.float8_e4m3fn):
+            raise ValueError(f"states of type {state} are not supported (float32, float8_e4m3fn)")
+        self.state_bits = 8 if state is torch.float8_e4m3fn else 32
+        table = (_Tensor * max(1, count))()
+        for i, (p, g, a, b, c, ms, vs, d) in enumerate(zip(*lists)):
+            ops._on_device(p, g, a, b, c, ms, vs)
+            n = p.numel()
+            if g.numel() != n or not g.is_contiguous():
+                raise ValueError(f"grads[{i}] must be packed, of {n} elements")
+            if c is not None and (c.numel() != n or not c.is_contiguous() or c.dtype not in (torch.bfloat16, torch.float16)):
+                raise ValueError(f"copies[{i}] must be packed, bfloat16 or float16, of {n} elements")
+            blocks = (n + LM_ADAM_BLOCK - 1) // LM_ADAM_BLOCK
+            table[i] = _Tensor(_vector(p, f"params[{i}]", n, torch.float32), g.data_ptr(), _vector(a, f"m[{i}]", n, state),
+                               _vector(b, f"v[{i}]", n, state), _vector(ms, f"m_scales[{i}]", blocks, torch.float32),
+                               _vector(vs, f"v_scales[{i}]", blocks, torch.float32), 0 if c is None else c.data_ptr(), n, _type(g),
+                               0 if c is None else _type(c), float(d), 0)
+        _check(_lib.cocodc_lm_adam_create(ctypes.byref(self._h), ops._h, table, count, self.state_bits), "cocodc_lm_adam_create")
+
+    def close(self) -> None:
+        if self._h:
+            _lib.cocodc_lm_adam_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class LmOps:
@@ -615,3 +687,131 @@ class LmOps:
                                                _vector(dentropy, "dentropy", T, f32), dp, ds, self._stream(stream)))
         if code:
             raise CocodcError(code, "cocodc_lm_logprobs_grad")
+
+    def cocodc_lm_norm(self, x, weight, y, residual=None, total=None, rstd=None, y_scale=None, eps: float = 1e-6, stream=None) -> None:
+        """total = x + residual (both or neither; total may be residual); y = total / rms(total) * weight, or of x.  y of type
+        float8_e4m3fn takes y_scale: [T] or [T, 1] for a scale per row, [T, ceil(D / 128)] for one per 128 columns."""
+        self._on_device(x, weight, y, residual, total, rstd, y_scale)
+        xp, xs, T, D = _matrix(x, "x")
+        yp, ys, rows, cols = _matrix(y, "y")
+        if rows != T or cols != D:
+            _sized("y", rows, cols, T, D)
+        rp = tp = kind = 0
+        rs = ts = D
+        if residual is not None or total is not None:
+            kinds = set()
+            for name, t in (("residual", residual), ("total", total)):
+                if t is not None:                            # one without the other is refused by the call
+                    p, st, r, c = _matrix(t, name)
+                    _sized(name, r, c, T, D)
+                    kinds.add(_type(t))
+                    if name == "residual":
+                        rp, rs = p, st
+                    else:
+                        tp, ts = p, st
+            if len(kinds) > 1:
+                raise ValueError("residual and total must have one type")
+            kind = kinds.pop()
+        group = 0
+        y_type = E4M3 if y.dtype is torch.float8_e4m3fn else _type(y)
+        if y_scale is not None:
+            groups = (D + 127) // 128
+            shape = tuple(y_scale.shape)
+            if shape == (T, groups) and groups > 1:
+                group = 128
+            elif shape not in ((T,), (T, 1)):
+                raise ValueError(f"y_scale must be {T}, {T} x 1 or {T} x {groups}, not {shape}")
+            sp = _vector(y_scale, "y_scale", y_scale.numel(), torch.float32)
+        else:
+            sp = 0
+        code = _submit(self._h, _NORM(6, xp, _type(x), xs, rp, rs, kind, _vector(weight, "weight", D, weight.dtype), _type(weight), T, D, eps,
+                                      tp, ts, yp, y_type, ys, sp, group, _vector(rstd, "rstd", T, torch.float32), self._stream(stream)))
+        if code:
+            raise CocodcError(code, "cocodc_lm_norm")
+
+    def cocodc_lm_norm_grad(self, dy, total, weight, rstd, dx=None, dweight=None, dtotal=None, accumulate: bool = False, workspace=None,
+                            stream=None) -> None:
+        """dx = the gradient of total through the norm, plus dtotal (the one that reaches it otherwise; dx may be dtotal);
+        dweight (+)= the weight's.  total and rstd are what cocodc_lm_norm wrote (total: x where it had no residual)."""
+        self._on_device(dy, total, weight, rstd, dx, dweight, dtotal)
+        yp, ys, T, D = _matrix(dy, "dy")
+        kind = _type(total)
+
+        def take(t, name):
+            if t is None:
+                return 0, D
+            p, stride, r, c = _matrix(t, name)
+            if r != T or c != D:
+                _sized(name, r, c, T, D)
+            if _type(t) != kind:
+                raise ValueError("total, dtotal and dx must have one type")
+            return p, stride
+
+        (tp, ts), (dtp, dts), (xp, xs) = take(total, "total"), take(dtotal, "dtotal"), take(dx, "dx")
+        wp = size = 0
+        if dweight is not None:
+            w = self._scratch(workspace, _lib.cocodc_lm_norm_grad_workspace(T, D), stream)
+            wp, size = w.data_ptr(), w.numel() * w.element_size()
+        code = _submit(self._h, _NORM_GRAD(7, yp, _type(dy), ys, tp, kind, ts, _vector(weight, "weight", D, weight.dtype), _type(weight),
+                                           _vector(rstd, "rstd", T, torch.float32), T, D, dtp, dts, xp, xs,
+                                           0 if dweight is None else _vector(dweight, "dweight", D, dweight.dtype),
+                                           0 if dweight is None else _type(dweight), bool(accumulate), wp, size, self._stream(stream)))
+        if code:
+            raise CocodcError(code, "cocodc_lm_norm_grad")
+
+    def cocodc_lm_head(self, x, table, targets, logp, lse=None, scale: float = 1.0, workspace=None, stream=None) -> None:
+        """Log probability of targets[t] (0 where it is negative) and log-sum-exp of the logits scale * x table^T, which are not kept.
+        targets and logp may both be None."""
+        self._on_device(x, table, targets, logp, lse)
+        xp, xs, T, D = _matrix(x, "x")
+        wp, ws, V, cols = _matrix(table, "table")
+        if cols != D:
+            _sized("table", V, cols, V, D)
+        kind = _one_type(x, table)
+        tp, tt = _ids(targets, "targets", T) if targets is not None else (0, 0)
+        w = self._scratch(workspace, _lib.cocodc_lm_head_workspace(T, D, V), stream)
+        f32 = torch.float32
+        code = _submit(self._h, _HEAD(8, kind, xp, xs, wp, ws, T, D, V, tp, tt, scale, _vector(logp, "logp", T, f32), _vector(lse, "lse", T, f32),
+                                      w.data_ptr(), w.numel() * w.element_size(), self._stream(stream)))
+        if code:
+            raise CocodcError(code, "cocodc_lm_head")
+
+    def cocodc_lm_head_grad(self, x, table, targets, lse, dlogp, dlse, dx=None, dtable=None, scale: float = 1.0, accumulate: bool = False,
+                            workspace=None, stream=None) -> None:
+        """dx and dtable of cocodc_lm_head from d/dlogp and d/dlse (None for zero) and the lse that it wrote; either output may be None.
+        dtable of x's type or float32, added to what it holds with accumulate."""
+        self._on_device(x, table, targets, lse, dlogp, dlse, dx, dtable)
+        xp, xs, T, D = _matrix(x, "x")
+        wp, ws, V, cols = _matrix(table, "table")
+        if cols != D:
+            _sized("table", V, cols, V, D)
+        kind = _one_type(x, table, dx)
+        tp, tt = _ids(targets, "targets", T) if targets is not None else (0, 0)
+        dxp = dtp = dtt = 0
+        dxs = dts = D
+        if dx is not None:
+            dxp, dxs, r, c = _matrix(dx, "dx")
+            _sized("dx", r, c, T, D)
+        if dtable is not None:
+            dtp, dts, r, c = _matrix(dtable, "dtable")
+            _sized("dtable", r, c, V, D)
+            dtt = _type(dtable)
+        w = self._scratch(workspace, _lib.cocodc_lm_head_grad_workspace(T, D, V), stream)
+        f32 = torch.float32
+        code = _submit(self._h, _HEAD_GRAD(9, kind, xp, xs, wp, ws, T, D, V, tp, tt, scale, _vector(lse, "lse", T, f32),
+                                           _vector(dlogp, "dlogp", T, f32), _vector(dlse, "dlse", T, f32), dxp, dxs, dtp, dtt, dts,
+                                           bool(accumulate), w.data_ptr(), w.numel() * w.element_size(), self._stream(stream)))
+        if code:
+            raise CocodcError(code, "cocodc_lm_head_grad")
+
+    def cocodc_lm_adamw(self, plan: AdamTensors, lr: float, step: int = 0, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
+                        step_at=None, grad_scale=None, lr_scale=None, seed: int = 0, stream=None) -> None:
+        """One AdamW step of the plan's tensors.  step counts from 1; step_at (int64), grad_scale and lr_scale (float32) are device
+        scalars, for captured steps, clipping and schedules; seed is the one of the random rounding of 8-bit states."""
+        self._on_device(step_at, grad_scale, lr_scale)
+        f32 = torch.float32
+        code = _submit(self._h, _ADAMW(10, plan._h.value or 0, lr, beta1, beta2, eps, step, _vector(step_at, "step_at", 1, torch.int64),
+                                       _vector(grad_scale, "grad_scale", 1, f32), _vector(lr_scale, "lr_scale", 1, f32), seed,
+                                       self._stream(stream)))
+        if code:
+            raise CocodcError(code, "cocodc_lm_adamw")

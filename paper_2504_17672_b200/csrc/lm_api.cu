@@ -102,6 +102,11 @@ cocodc_status cocodc_lm_submit(cocodc_lm* lm, const void* record) {
     case COCODC_LM_GLU_GRAD: return call(cocodc_lm_glu_grad, lm, r);
     case COCODC_LM_LOGPROBS: return call(cocodc_lm_logprobs, lm, r);
     case COCODC_LM_LOGPROBS_GRAD: return call(cocodc_lm_logprobs_grad, lm, r);
+    case COCODC_LM_NORM: return call(cocodc_lm_norm, lm, r);
+    case COCODC_LM_NORM_GRAD: return call(cocodc_lm_norm_grad, lm, r);
+    case COCODC_LM_HEAD: return call(cocodc_lm_head, lm, r);
+    case COCODC_LM_HEAD_GRAD: return call(cocodc_lm_head_grad, lm, r);
+    case COCODC_LM_ADAMW: return call(cocodc_lm_adamw, lm, r);
   }
   return COCODC_ERR_INVALID_ARG;
 }

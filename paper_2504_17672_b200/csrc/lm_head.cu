@@ -1,0 +1,431 @@
+// The output head with its loss, without keeping the logits, and its gradient (include/cocodc_lm.h).
+
+#include "lm_common.cuh"
+#include "lm_plain.cuh"
+
+#include <type_traits>
+
+using namespace cocodc_lm_impl;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kMostScale = 1e30f;
+constexpr int kSms = 148;                            // of a B200 (workspace sizes are asked for without a handle)
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
+
+// Logits are taken in base 2 (times scale log2 e).  A strip of a row's logits leaves its largest one and the sum of 2^(z - largest): (m, s).
+struct Stats { float m, s; };
+__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }   // nothing but -Inf: the sum is then 0
+__device__ __forceinline__ Stats join(Stats a, Stats b) {
+  const float m = fmaxf(a.m, b.m), k = shift_of(m);
+  return Stats{m, a.s * fast_exp2(a.m - k) + b.s * fast_exp2(b.m - k)};
+}
+
+// Columns of a strip: what a tile of the product covers, a multiple of 16 up to 256.  Tiles times their width in rounds of one per SM,
+// plus what a tile costs beside its products, come out smallest.
+int strip_width(int64_t T, int64_t V) {
+  const int64_t rows = up(T, 128);
+  int best = 256;
+  int64_t least = INT64_MAX;
+  for (int w = 256; w >= 16; w -= 16) {
+    const int64_t cost = up(rows * up(V, w), kSms) * (w + 24);
+    if (cost < least) {
+      least = cost;
+      best = w;
+    }
+  }
+  return best;
+}
+
+struct HeadArgs {
+  long long T, V;
+  int width;
+  long long strips;
+  float scale2;                                      // scale * log2 e
+  const void* targets;
+  int targets64;
+  float2* stats;                                     // [strip][T]
+  float* picked;                                     // [T]: the target's logit, base 2
+};
+__device__ __forceinline__ long long raw_target(const void* targets, int is64, long long t) {
+  return is64 ? static_cast<const long long*>(targets)[t] : (long long)static_cast<const int*>(targets)[t];
+}
+
+// Any strides: 64 rows and a strip for each block, in pieces of 64 columns.
+template <typename E>
+__global__ void __launch_bounds__(256) k_head_plain(const HeadArgs a, const Operand<E> x, const Operand<E> w, long long D) {
+  wait_for_previous();
+  may_follow();
+  __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
+  const long long strip = blockIdx.x % a.strips, t0 = blockIdx.x / a.strips * kTile, v0 = strip * a.width, v1 = min(a.V, v0 + a.width);
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  Stats own[4];
+  long long target[4];
+  for (int i = 0; i < 4; ++i) {
+    own[i] = Stats{-INFINITY, 0.f};
+    const long long t = t0 + ty * 4 + i;
+    target[i] = a.targets && t < a.T ? raw_target(a.targets, a.targets64, t) : -1;
+  }
+  for (long long v = v0; v < v1; v += kTile) {
+    float c[4][4] = {};
+    accumulate(c, x, w, t0, a.T, v, v1, D, sa, sb);
+    for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < 4; ++j) {
+        const long long col = v + tx * 4 + j, t = t0 + ty * 4 + i;
+        if (col >= v1 || t >= a.T) continue;
+        const float z = c[i][j] * a.scale2;
+        const float m = fmaxf(own[i].m, z), k = shift_of(m);
+        own[i] = Stats{m, own[i].s * fast_exp2(own[i].m - k) + fast_exp2(z - k)};
+        if (col == target[i]) a.picked[t] = z;
+      }
+  }
+  for (int i = 0; i < 4; ++i) {
+    for (int o = 8; o; o >>= 1) {
+      const float m = __shfl_xor_sync(~0u, own[i].m, o), s = __shfl_xor_sync(~0u, own[i].s, o);
+      own[i] = join(own[i], Stats{m, s});
+    }
+    const long long t = t0 + ty * 4 + i;
+    if (tx == 0 && t < a.T) a.stats[strip * a.T + t] = make_float2(own[i].m, own[i].s);
+  }
+}
+
+// The strips of a row joined.  R rows for a block of 256 threads, 256 / R threads for a row.
+template <int R> __global__ void __launch_bounds__(256) k_head_join(const HeadArgs a, float* logp, float* lse, int* status) {
+  wait_for_previous();
+  may_follow();
+  constexpr int kParts = 256 / R;
+  __shared__ Stats cell[kParts][R];
+  const int r = threadIdx.x % R, part = threadIdx.x / R;
+  const long long t = (long long)blockIdx.x * R + r;
+  Stats all{-INFINITY, 0.f};
+  if (t < a.T) {
+#pragma unroll 4
+    for (long long i = part; i < a.strips; i += kParts) {
+      const float2 v = a.stats[i * a.T + t];
+      all = join(all, Stats{v.x, v.y});
+    }
+  }
+  cell[part][r] = all;
+  __syncthreads();
+  for (int n = kParts / 2; n; n >>= 1) {
+    if (part < n) cell[part][r] = join(cell[part][r], cell[part + n][r]);
+    __syncthreads();
+  }
+  if (part || t >= a.T) return;
+  all = cell[0][r];
+  const float log2sum = shift_of(all.m) + log2f(all.s);
+  if (lse) lse[t] = log2sum * kLn2;
+  if (!logp) return;
+  const long long y = token_at(a.targets, a.targets64, t, a.V, status);
+  logp[t] = y < 0 ? 0.f : (log2sum == -INFINITY ? -INFINITY : (a.picked[t] - log2sum) * kLn2);
+}
+
+// ---- gradient -------------------------------------------------------------------------------------
+// The power of two that half-precision dz is taken at: factor[0], and its inverse.
+__global__ void __launch_bounds__(1024) k_head_factor(const HeadArgs a, const float* dlogp, const float* dlse, float* factor) {
+  wait_for_previous();
+  may_follow();
+  __shared__ unsigned cell[32];
+  unsigned most = 0;
+  for (long long t = threadIdx.x; t < a.T; t += 1024) {
+    float v = dlse ? fabsf(dlse[t]) : 0.f;
+    if (dlogp && raw_target(a.targets, a.targets64, t) >= 0) v += fabsf(dlogp[t]);
+    if (v < INFINITY) most = max(most, __float_as_uint(v));         // not NaN either
+  }
+  most = __reduce_max_sync(~0u, most);
+  if (threadIdx.x % 32 == 0) cell[threadIdx.x / 32] = most;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int i = 1; i < 32; ++i) most = max(most, cell[i]);
+  int e = most ? 9 - ilogbf(__uint_as_float(most)) : 0;
+  e = max(-120, min(120, e));
+  factor[0] = ldexpf(1.f, e);
+  factor[1] = ldexpf(1.f, -e);
+}
+
+struct DzArgs {
+  long long T, V;
+  float scale2;
+  const void* targets;
+  int targets64;
+  const float *lse, *dlogp, *dlse, *factor;          // factor NULL: 1
+  long long v0, v1;                                  // the piece
+  void* dz;                                          // [T][pitch]
+  long long pitch;
+  int* status;
+};
+// What a row's dz needs: p's factor, what the target gets on top, and lse in base 2.
+struct RowOf { float slope, hit, lse2; long long y; };
+__device__ __forceinline__ RowOf row_of(const DzArgs& a, long long t) {
+  RowOf r{0.f, 0.f, 0.f, -1};
+  const float f = a.factor ? a.factor[0] : 1.f;
+  if (a.targets) r.y = token_at(a.targets, a.targets64, t, a.V, a.status);
+  const float up = r.y >= 0 ? a.dlogp[t] * f : 0.f, dl = a.dlse ? a.dlse[t] * f : 0.f, lse = a.lse[t];
+  if ((up == 0.f && dl == 0.f) || lse == -INFINITY) {               // nothing: whatever p is, it counts for nothing
+    r.y = -1;
+    r.lse2 = INFINITY;
+    return r;
+  }
+  r.slope = dl - up;
+  r.hit = up;
+  r.lse2 = lse == INFINITY ? __uint_as_float(0x7fc00000u) : lse * kLog2e;
+  return r;
+}
+__device__ __forceinline__ float dz_of(const RowOf& r, float z2, bool target) {
+  if (r.lse2 == INFINITY) return 0.f;
+  return fmaf(fast_exp2(z2 - r.lse2), r.slope, target ? r.hit : 0.f);
+}
+
+template <typename E>
+__global__ void __launch_bounds__(256) k_head_dz_plain(const DzArgs a, const Operand<E> x, const Operand<E> w, long long D) {
+  wait_for_previous();
+  may_follow();
+  __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
+  const long long tiles = (a.v1 - a.v0 + kTile - 1) / kTile;
+  const long long v = a.v0 + blockIdx.x % tiles * kTile, t0 = blockIdx.x / tiles * kTile;
+  float c[4][4] = {};
+  accumulate(c, x, w, t0, a.T, v, a.v1, D, sa, sb);
+  for (int i = 0; i < 4; ++i) {
+    const long long t = t0 + threadIdx.x / 16 * 4 + i;
+    if (t >= a.T) continue;
+    const RowOf r = row_of(a, t);
+    for (int j = 0; j < 4; ++j) {
+      const long long col = v + threadIdx.x % 16 * 4 + j;
+      if (col < a.v1) static_cast<E*>(a.dz)[t * a.pitch + col - a.v0] = from_f32<E>(dz_of(r, c[i][j] * a.scale2, col == r.y));
+    }
+  }
+}
+
+// Where a product goes: fp32 sums that other pieces of the vocabulary share, or the output.
+struct Out {
+  void* out;
+  int type, accumulate;
+  long long ld;
+  float* sums;                                       // [rows][cols], or NULL
+  int add, last;                                     // add what the sums hold; the sums are complete and go to the output
+  const float* factor;
+  float scale;
+};
+template <typename E> __device__ __forceinline__ void deliver(const Out& o, long long r, long long c, long long cols, float v) {
+  if (o.sums && o.add) v += o.sums[r * cols + c];
+  if (o.sums && !o.last) {
+    o.sums[r * cols + c] = v;
+    return;
+  }
+  v *= o.factor ? o.factor[1] * o.scale : o.scale;
+  if (o.type == COCODC_F32) {
+    float* p = static_cast<float*>(o.out) + r * o.ld + c;
+    *p = o.accumulate ? *p + v : v;
+  } else {
+    E* p = static_cast<E*>(o.out) + r * o.ld + c;
+    *p = from_f32<E>(o.accumulate ? to_f32(*p) + v : v);
+  }
+}
+
+template <typename E>
+__global__ void __launch_bounds__(256) k_head_product_plain(const Operand<E> A, const Operand<E> B, long long M, long long N, long long K, const Out o) {
+  wait_for_previous();
+  may_follow();
+  __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
+  const long long tiles = (N + kTile - 1) / kTile;
+  const long long n0 = blockIdx.x % tiles * kTile, m0 = blockIdx.x / tiles * kTile;
+  float c[4][4] = {};
+  accumulate(c, A, B, m0, M, n0, N, K, sa, sb);
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < 4; ++j) {
+      const long long m = m0 + threadIdx.x / 16 * 4 + i, n = n0 + threadIdx.x % 16 * 4 + j;
+      if (m < M && n < N) deliver<E>(o, m, n, N, c[i][j]);
+    }
+}
+
+template <typename O> __global__ void __launch_bounds__(256) k_head_zero(O* out, long long ld, long long rows, long long cols) {
+  wait_for_previous();
+  may_follow();
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (long long)gridDim.x * 256)
+    out[i / cols * ld + i % cols] = from_f32<O>(0.f);
+}
+
+// Columns of a piece of the vocabulary in the gradient: dz of a piece takes at most kPieceBytes, as long as that leaves 1024 columns.
+constexpr int64_t kPieceBytes = int64_t(1) << 28, kLeastPiece = 1024;
+int64_t piece_width(int64_t T, int64_t V) {
+  int64_t w = T > 0 ? kPieceBytes / 2 / T / 256 * 256 : V;
+  if (w < kLeastPiece) w = kLeastPiece;
+  if (w >= V) return up(V, 8) * 8;
+  const int64_t pieces = up(V, w);
+  return up(up(V, pieces), 256) * 256;
+}
+
+template <typename F> cocodc_status with_half(int32_t type, F&& f) { return type == COCODC_BF16 ? f(__nv_bfloat16()) : f(__half()); }
+
+bool sizes_ok(int64_t T, int64_t D, int64_t V) {
+  const int64_t most = int64_t(1) << 48;             // elements of a matrix: byte counts stay far inside 64 bits
+  return T >= 0 && T <= INT32_MAX && D >= 1 && D <= INT32_MAX && V >= 1 && V <= (int64_t(1) << 30) && T <= most / D && V <= most / D;
+}
+// a grid of tiles of `t` x `n` in one dimension
+bool grid_of(int64_t rows, int64_t t, int64_t cols, int64_t n, unsigned* out) {
+  const int64_t blocks = up(rows, t) * up(cols, n);
+  *out = (unsigned)blocks;
+  return blocks <= INT32_MAX;
+}
+
+struct GradLayout { uint64_t sums, dz, bytes; int64_t width; };
+GradLayout grad_layout(int64_t T, int64_t D, int64_t V) {
+  GradLayout l{};
+  l.width = piece_width(T, V);
+  l.sums = 256;
+  l.dz = l.sums + (l.width < V ? (uint64_t)up(T * D, 64) * 256 : 0);
+  l.bytes = l.dz + (uint64_t)T * (uint64_t)l.width * 2;
+  return l;
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t cocodc_lm_head_workspace(int64_t T, int64_t D, int64_t V) {
+  if (!sizes_ok(T, D, V)) return 0;
+  return 16 + (uint64_t)T * 4 + 16 + (uint64_t)up(V, strip_width(T, V)) * (uint64_t)T * sizeof(float2);
+}
+
+cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t x_stride, const void* table, int64_t table_stride,
+                             int64_t T, int64_t D, int64_t V, const void* targets, int32_t targets_type, float scale,
+                             float* logp, float* lse, void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!lm || (type != COCODC_BF16 && type != COCODC_F16) || !sizes_ok(T, D, V) || x_stride < D || !sane(x_stride) || table_stride < D ||
+      !sane(table_stride) || !(scale > 0.f && scale <= kMostScale) || (targets && targets_type != COCODC_I32 && targets_type != COCODC_I64))
+    return COCODC_ERR_INVALID_ARG;
+  if (!logp != !targets || (!logp && !lse)) return T == 0 ? COCODC_OK : COCODC_ERR_INVALID_ARG;
+  if (T == 0) return COCODC_OK;
+  if (!x || !table || !workspace || workspace_bytes < cocodc_lm_head_workspace(T, D, V)) return COCODC_ERR_INVALID_ARG;
+  const int ib = targets ? index_bytes(targets_type) : 4;
+  if (!on_boundary(x, 2) || !on_boundary(table, 2) || !on_boundary(targets, ib) || !on_boundary(logp, 4) || !on_boundary(lse, 4) ||
+      !on_boundary(workspace, 16))
+    return COCODC_ERR_ALIGNMENT;
+  const Span in[3] = {span(x, T, x_stride, D, 2), span(table, V, table_stride, D, 2), span(targets, 1, T, T, ib)};
+  const Span out[3] = {span(logp, 1, T, T, 4), span(lse, 1, T, T, 4), span(workspace, 1, (int64_t)workspace_bytes, (int64_t)workspace_bytes, 1)};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 3; ++j)
+      if (meet(out[i], in[j])) return COCODC_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return COCODC_ERR_ALIAS;
+  }
+  DeviceScope scope(lm->device);
+  if (!scope.ok) return COCODC_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  HeadArgs a{};
+  a.T = T;
+  a.V = V;
+  a.width = strip_width(T, V);
+  a.strips = up(V, a.width);
+  a.scale2 = scale * kLog2e;
+  a.targets = targets;
+  a.targets64 = targets_type == COCODC_I64;
+  a.picked = static_cast<float*>(workspace);
+  a.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + up(T, 4) * 16);
+  unsigned grid;
+  if (!grid_of(T, kTile, V, a.width, &grid)) return COCODC_ERR_INVALID_ARG;
+  const cocodc_status status = with_half(type, [&](auto e) {
+    using E = decltype(e);
+    const Operand<E> xo{static_cast<const E*>(x), x_stride, 1}, wo{static_cast<const E*>(table), table_stride, 1};
+    return start(lm, k_head_plain<E>, grid, 256, 0, st, 1, a, xo, wo, (long long)D);
+  });
+  if (status != COCODC_OK) return status;
+  return T < 4 * kSms ? start(lm, k_head_join<1>, (unsigned)T, 256, 0, st, 1, a, logp, lse, lm->d_status)
+                      : start(lm, k_head_join<32>, (unsigned)up(T, 32), 256, 0, st, 1, a, logp, lse, lm->d_status);
+}
+
+uint64_t cocodc_lm_head_grad_workspace(int64_t T, int64_t D, int64_t V) { return sizes_ok(T, D, V) ? grad_layout(T, D, V).bytes : 0; }
+
+cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, int64_t x_stride, const void* table,
+                                  int64_t table_stride, int64_t T, int64_t D, int64_t V, const void* targets, int32_t targets_type,
+                                  float scale, const float* lse, const float* dlogp, const float* dlse, void* dx, int64_t dx_stride,
+                                  void* dtable, int32_t dtable_type, int64_t dtable_stride, int32_t accumulate, void* workspace,
+                                  uint64_t workspace_bytes, void* stream) {
+  if (!lm || (type != COCODC_BF16 && type != COCODC_F16) || !sizes_ok(T, D, V) || x_stride < D || !sane(x_stride) || table_stride < D ||
+      !sane(table_stride) || !(scale > 0.f && scale <= kMostScale) || (targets && targets_type != COCODC_I32 && targets_type != COCODC_I64) ||
+      (dx && (dx_stride < D || !sane(dx_stride))) ||
+      (dtable && (dtable_stride < D || !sane(dtable_stride) || (dtable_type != type && dtable_type != COCODC_F32))))
+    return COCODC_ERR_INVALID_ARG;
+  if (!dx && !dtable) return T == 0 ? COCODC_OK : COCODC_ERR_INVALID_ARG;
+  if (T > 0 && (!x || !table || !lse || !dlogp != !targets || (!dlogp && !dlse) || !workspace ||
+                workspace_bytes < cocodc_lm_head_grad_workspace(T, D, V)))
+    return COCODC_ERR_INVALID_ARG;
+  const int ib = targets ? index_bytes(targets_type) : 4, wb = dtable_type == COCODC_F32 ? 4 : 2;
+  if (!on_boundary(x, 2) || !on_boundary(table, 2) || !on_boundary(dx, 2) || !on_boundary(dtable, wb) || !on_boundary(targets, ib) ||
+      !on_boundary(lse, 4) || !on_boundary(dlogp, 4) || !on_boundary(dlse, 4) || !on_boundary(workspace, 16))
+    return COCODC_ERR_ALIGNMENT;
+  const Span in[6] = {span(x, T, x_stride, D, 2), span(table, V, table_stride, D, 2), span(targets, 1, T, T, ib), span(lse, 1, T, T, 4),
+                      span(dlogp, 1, T, T, 4), span(dlse, 1, T, T, 4)};
+  const Span out[3] = {span(dx, T, dx_stride, D, 2), span(dtable, V, dtable_stride, D, wb),
+                       T > 0 ? span(workspace, 1, (int64_t)workspace_bytes, (int64_t)workspace_bytes, 1) : Span{0, 0, 0, 0}};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 6; ++j)
+      if (meet(out[i], in[j])) return COCODC_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return COCODC_ERR_ALIAS;
+  }
+  DeviceScope scope(lm->device);
+  if (!scope.ok) return COCODC_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return with_half(type, [&](auto e) {
+    using E = decltype(e);
+    if (T == 0) {
+      if (!dtable || accumulate) return COCODC_OK;
+      const unsigned blocks = (unsigned)(up(V * D, 1024) < 65535 ? up(V * D, 1024) : 65535);
+      return dtable_type == COCODC_F32
+                 ? start(lm, k_head_zero<float>, blocks, 256, 0, st, 1, static_cast<float*>(dtable), (long long)dtable_stride, (long long)V, (long long)D)
+                 : start(lm, k_head_zero<E>, blocks, 256, 0, st, 1, static_cast<E*>(dtable), (long long)dtable_stride, (long long)V, (long long)D);
+    }
+    const GradLayout l = grad_layout(T, D, V);
+    char* ws = static_cast<char*>(workspace);
+    DzArgs d{};
+    d.T = T;
+    d.V = V;
+    d.scale2 = scale * kLog2e;
+    d.targets = targets;
+    d.targets64 = targets_type == COCODC_I64;
+    d.lse = lse;
+    d.dlogp = dlogp;
+    d.dlse = dlse;
+    d.dz = ws + l.dz;
+    d.pitch = l.width;
+    d.status = lm->d_status;
+    if (type == COCODC_F16) {
+      d.factor = reinterpret_cast<float*>(ws);
+      HeadArgs h{};
+      h.T = T;
+      h.V = V;
+      h.targets = targets;
+      h.targets64 = d.targets64;
+      const cocodc_status s = start(lm, k_head_factor, 1, 1024, 0, st, 1, h, dlogp, dlse, reinterpret_cast<float*>(ws));
+      if (s != COCODC_OK) return s;
+    }
+    unsigned g1, g2, g3;
+    if (!grid_of(T, kTile, l.width, kTile, &g1) || !grid_of(T, kTile, D, kTile, &g2) || !grid_of(l.width, kTile, D, kTile, &g3))
+      return COCODC_ERR_INVALID_ARG;
+    const E *xe = static_cast<const E*>(x), *we = static_cast<const E*>(table), *dz = reinterpret_cast<const E*>(ws + l.dz);
+    for (int64_t v0 = 0; v0 < V; v0 += l.width) {
+      d.v0 = v0;
+      d.v1 = v0 + l.width < V ? v0 + l.width : V;
+      const long long w = d.v1 - v0;
+      grid_of(T, kTile, w, kTile, &g1);
+      cocodc_status s = start(lm, k_head_dz_plain<E>, g1, 256, 0, st, 1, d, Operand<E>{xe, x_stride, 1}, Operand<E>{we, table_stride, 1}, (long long)D);
+      if (s != COCODC_OK) return s;
+      if (dtable) {
+        grid_of(w, kTile, D, kTile, &g3);
+        const Out o{static_cast<char*>(dtable) + v0 * dtable_stride * wb, dtable_type, accumulate ? 1 : 0, dtable_stride, nullptr, 0, 1, d.factor, scale};
+        s = start(lm, k_head_product_plain<E>, g3, 256, 0, st, 1, Operand<E>{dz, 1, d.pitch}, Operand<E>{xe, 1, x_stride}, w, (long long)D, (long long)T, o);
+        if (s != COCODC_OK) return s;
+      }
+      if (dx) {
+        const Out o{dx, type, 0, dx_stride, l.width < V ? reinterpret_cast<float*>(ws + l.sums) : nullptr, v0 > 0, d.v1 == V, d.factor, scale};
+        s = start(lm, k_head_product_plain<E>, g2, 256, 0, st, 1, Operand<E>{dz, d.pitch, 1}, Operand<E>{we + v0 * table_stride, 1, table_stride},
+                  (long long)T, (long long)D, w, o);
+        if (s != COCODC_OK) return s;
+      }
+    }
+    return COCODC_OK;
+  });
+}
+
+}  // extern "C"

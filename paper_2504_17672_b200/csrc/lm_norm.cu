@@ -1,0 +1,632 @@
+// The root-mean-square norm with the residual's addition and its gradient (include/cocodc_lm.h).
+
+#include "lm_common.cuh"
+
+#include <type_traits>
+
+using namespace cocodc_lm_impl;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kMost8 = 448.f, kLeastScale = 1e-30f;
+
+// ---- elements ----------------------------------------------------------------------------------------
+// Eight elements of a row as they lie in memory, fetched before they are needed.
+template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Raw8<T> fetch8(const T* p) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.q[i] = load16(p + i * (16 / sizeof(T)));
+  return r;
+}
+__device__ __forceinline__ void widen(const Raw8<float>& r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[4 * i] = __uint_as_float(r.q[i].x);
+    v[4 * i + 1] = __uint_as_float(r.q[i].y);
+    v[4 * i + 2] = __uint_as_float(r.q[i].z);
+    v[4 * i + 3] = __uint_as_float(r.q[i].w);
+  }
+}
+template <typename T> __device__ __forceinline__ void widen(const Raw8<T>& r, float (&v)[8]) {
+  const unsigned w[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      v[2 * i] = f.x;
+      v[2 * i + 1] = f.y;
+    }
+  }
+}
+template <typename T> __device__ __forceinline__ unsigned narrow2(float a, float b) {
+  if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const unsigned*>(&v);
+  } else {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const unsigned*>(&v);
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    *reinterpret_cast<uint4*>(p) = make_uint4(narrow2<T>(v[0], v[1]), narrow2<T>(v[2], v[3]), narrow2<T>(v[4], v[5]), narrow2<T>(v[6], v[7]));
+  }
+}
+// two numbers to the nearest e4m3, the first in the lower byte
+__device__ __forceinline__ unsigned narrow_e4m3(float a, float b) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ float load_as(const void* p, int type, long long i) {
+  return type == COCODC_F32    ? static_cast<const float*>(p)[i]
+         : type == COCODC_BF16 ? to_f32(static_cast<const __nv_bfloat16*>(p)[i])
+                               : to_f32(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_as(void* p, int type, long long i, float v) {
+  if (type == COCODC_F32) static_cast<float*>(p)[i] = v;
+  else if (type == COCODC_BF16) static_cast<__nv_bfloat16*>(p)[i] = from_f32<__nv_bfloat16>(v);
+  else if (type == COCODC_F16) static_cast<__half*>(p)[i] = from_f32<__half>(v);
+  else static_cast<unsigned char*>(p)[i] = (unsigned char)narrow_e4m3(v, 0.f);
+}
+
+// ---- a row in registers ---------------------------------------------------------------------------------
+// G threads hold a row, 8 P columns each; a block of 256 threads takes 256 / G rows at a time and strides on.  Where rows start on
+// 16-byte boundaries (WIDE) a thread's columns are packs of eight, otherwise single ones G apart, so that neighbours
+// read neighbours either way.
+template <int G, int P, bool WIDE> struct Row {
+  static constexpr int kRows = kThreads / G;
+  static __device__ __forceinline__ int column(int p, int i) {
+    const int t = threadIdx.x % G;
+    return WIDE ? (p * G + t) * 8 + i : (p * 8 + i) * G + t;
+  }
+};
+// One row's share of a thread: raw words while they are on their way.
+template <typename T, int G, int P, bool WIDE> struct Piece {
+  Raw8<T> raw[WIDE ? P : 1];
+  T one[WIDE ? 1 : P * 8];
+  // columns behind the row's end are zero
+  __device__ __forceinline__ void fetch(const T* row, int D) {
+    using R = Row<G, P, WIDE>;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if constexpr (WIDE) {
+        const int c = R::column(p, 0);
+        if (c + 8 <= D) {
+          raw[p] = fetch8(row + c);
+        } else {
+          alignas(16) T v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = c + i < D ? row[c + i] : from_f32<T>(0.f);
+          raw[p] = *reinterpret_cast<const Raw8<T>*>(v);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = R::column(p, i);
+          one[p * 8 + i] = c < D ? row[c] : from_f32<T>(0.f);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int p, float (&v)[8]) const {
+    if constexpr (WIDE) {
+      widen(raw[p], v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = to_f32(one[p * 8 + i]);
+    }
+  }
+};
+template <typename T, int G, int P, bool WIDE> __device__ __forceinline__ void put(T* row, int D, int p, const float (&v)[8]) {
+  using R = Row<G, P, WIDE>;
+  if (WIDE && R::column(p, 0) + 8 <= D) {
+    store8(row + R::column(p, 0), v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (R::column(p, i) < D) row[R::column(p, i)] = from_f32<T>(v[i]);
+  }
+}
+
+// Sums or maxima over the G threads of a row.  Above a warp they meet in shared memory, in two buffers in turn: one barrier each, for all
+// threads of the block.
+template <int G> struct Join {
+  float (*cell)[kThreads / 32];
+  int turn = 0;
+  template <typename F> __device__ __forceinline__ float operator()(float v, F f) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(~0u, v, o));
+    if constexpr (G > 32) {
+      if (threadIdx.x % 32 == 0) cell[turn][threadIdx.x / 32] = v;
+      __syncthreads();
+      const int first = threadIdx.x / G * (G / 32);
+      v = cell[turn][first];
+#pragma unroll
+      for (int i = 1; i < G / 32; ++i) v = f(v, cell[turn][first + i]);
+      turn ^= 1;
+    }
+    return v;
+  }
+};
+struct Plus { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Most { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+
+struct NormArgs {
+  const void *x, *residual, *weight;
+  long long x_stride, r_stride, t_stride, y_stride;
+  long long T;
+  int D, weight_type, y_type, groups;   // groups: scales of a row (0: y is not in 8 bits)
+  float eps;
+  void *total, *y;
+  float *y_scale, *rstd;
+};
+
+__device__ __forceinline__ float rms_scale(float sum, int D, float eps) { return 1.f / sqrtf(sum / D + eps); }
+__device__ __forceinline__ float scale_8(float most) { return fmaxf(most * (1.f / kMost8), kLeastScale); }
+
+template <typename X, typename S, int G, int P, bool WIDE>
+__global__ void __launch_bounds__(kThreads) k_norm(const NormArgs a) {
+  wait_for_previous();
+  may_follow();
+  using R = Row<G, P, WIDE>;
+  __shared__ float cell[2][kThreads / 32];
+  __shared__ unsigned most[R::kRows][G * P * 8 / 128 + 1];
+  Join<G> join{cell};
+  const int D = a.D;
+  float w[P][8];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[p][i] = R::column(p, i) < D ? load_as(a.weight, a.weight_type, R::column(p, i)) : 0.f;
+  const int mine = threadIdx.x / G;
+  Piece<X, G, P, WIDE> x;
+  Piece<S, G, P, WIDE> r;
+  const auto fetch = [&](long long row) {
+    if (row >= a.T) row = a.T - 1;                                  // a row that another thread group has too: nothing is written for it
+    x.fetch(static_cast<const X*>(a.x) + row * a.x_stride, D);
+    if (a.residual) r.fetch(static_cast<const S*>(a.residual) + row * a.r_stride, D);
+  };
+  const long long step = (long long)gridDim.x * R::kRows;
+  long long row0 = (long long)blockIdx.x * R::kRows;
+  fetch(row0 + mine);
+  for (; row0 < a.T; row0 += step) {
+    const long long row = row0 + mine;
+    const bool in = row < a.T;
+    float v[P][8], sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      x.get(p, v[p]);
+      if (a.residual) {
+        float u[8];
+        r.get(p, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i] + u[i]));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(v[p][i], v[p][i], sum);
+    }
+    if (in && a.residual) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) put<S, G, P, WIDE>(static_cast<S*>(a.total) + row * a.t_stride, D, p, v[p]);
+    }
+    if (row0 + step < a.T) fetch(row + step);                       // on its way while this row is finished
+    const float rstd = rms_scale(join(sum, Plus()), D, a.eps);
+    if (in && a.rstd && threadIdx.x % G == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[p][i] = v[p][i] * rstd * w[p][i];
+    if (a.groups == 0) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        if (!in) continue;
+        if (a.y_type == COCODC_F32) put<float, G, P, WIDE>(static_cast<float*>(a.y) + row * a.y_stride, D, p, v[p]);
+        else if (a.y_type == COCODC_BF16) put<__nv_bfloat16, G, P, WIDE>(static_cast<__nv_bfloat16*>(a.y) + row * a.y_stride, D, p, v[p]);
+        else put<__half, G, P, WIDE>(static_cast<__half*>(a.y) + row * a.y_stride, D, p, v[p]);
+      }
+      continue;
+    }
+    // 8 bits: largest magnitudes of the row or of its groups (as whole numbers: the order of the updates changes nothing)
+    const int groups = a.groups;
+    if (groups > 1) {
+      for (int i = threadIdx.x % G; i < groups; i += G) most[mine][i] = 0;
+      if (G > 32) __syncthreads(); else __syncwarp();
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        if constexpr (WIDE) {
+          float m = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[p][i]));
+          if (R::column(p, 0) < D) atomicMax(&most[mine][R::column(p, 0) / 128], __float_as_uint(m));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (R::column(p, i) < D && !isnan(v[p][i])) atomicMax(&most[mine][R::column(p, i) / 128], __float_as_uint(fabsf(v[p][i])));
+        }
+      }
+      if (G > 32) __syncthreads(); else __syncwarp();
+      if (in)
+        for (int i = threadIdx.x % G; i < groups; i += G) a.y_scale[row * groups + i] = scale_8(__uint_as_float(most[mine][i]));
+    } else {
+      float m = 0.f;
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[p][i]));
+      m = join(m, Most());
+      if (threadIdx.x % G == 0) {
+        most[mine][0] = __float_as_uint(m);
+        if (in) a.y_scale[row] = scale_8(m);
+      }
+      if (G > 32) __syncthreads(); else __syncwarp();
+    }
+    unsigned char* y = static_cast<unsigned char*>(a.y) + row * a.y_stride;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if (!in) continue;
+      if (WIDE && R::column(p, 0) + 8 <= D) {
+        const float inv = 1.f / scale_8(__uint_as_float(most[mine][groups > 1 ? R::column(p, 0) / 128 : 0]));
+        unsigned lo = narrow_e4m3(v[p][0] * inv, v[p][1] * inv) | narrow_e4m3(v[p][2] * inv, v[p][3] * inv) << 16;
+        unsigned hi = narrow_e4m3(v[p][4] * inv, v[p][5] * inv) | narrow_e4m3(v[p][6] * inv, v[p][7] * inv) << 16;
+        *reinterpret_cast<uint2*>(y + R::column(p, 0)) = make_uint2(lo, hi);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = R::column(p, i);
+          if (c < D) y[c] = (unsigned char)narrow_e4m3(v[p][i] * (1.f / scale_8(__uint_as_float(most[mine][groups > 1 ? c / 128 : 0]))), 0.f);
+        }
+      }
+    }
+    if (G > 32) __syncthreads(); else __syncwarp();                 // before the next row's maxima
+  }
+}
+
+// Rows too long for registers: read again after their sum is known; one block a row.
+template <typename X, typename S> __global__ void __launch_bounds__(kThreads) k_norm_long(const NormArgs a) {
+  wait_for_previous();
+  may_follow();
+  __shared__ float cell[2][kThreads / 32];
+  Join<kThreads> join{cell};
+  for (long long row = blockIdx.x; row < a.T; row += gridDim.x) {
+    const X* x = static_cast<const X*>(a.x) + row * a.x_stride;
+    const S* r = static_cast<const S*>(a.residual) + row * a.r_stride;
+    S* total = static_cast<S*>(a.total) + row * a.t_stride;
+    const auto value = [&](int c) { return a.residual ? to_f32(total[c]) : to_f32(x[c]); };
+    float sum = 0.f;
+    for (int c = threadIdx.x; c < a.D; c += kThreads) {
+      if (a.residual) total[c] = from_f32<S>(to_f32(x[c]) + to_f32(r[c]));
+      sum = fmaf(value(c), value(c), sum);
+    }
+    const float rstd = rms_scale(join(sum, Plus()), a.D, a.eps);
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+    const auto result = [&](int c) { return value(c) * rstd * load_as(a.weight, a.weight_type, c); };
+    if (a.groups == 0) {
+      for (int c = threadIdx.x; c < a.D; c += kThreads) store_as(a.y, a.y_type, row * a.y_stride + c, result(c));
+      continue;
+    }
+    const auto finish = [&](int from, int to, float scale, int at, int pace) {
+      const float inv = 1.f / scale;
+      for (int c = from + at; c < to; c += pace) store_as(a.y, COCODC_E4M3, row * a.y_stride + c, result(c) * inv);
+    };
+    if (a.groups == 1) {
+      float m = 0.f;
+      for (int c = threadIdx.x; c < a.D; c += kThreads) m = fmaxf(m, fabsf(result(c)));
+      const float scale = scale_8(join(m, Most()));
+      if (threadIdx.x == 0) a.y_scale[row] = scale;
+      finish(0, a.D, scale, threadIdx.x, kThreads);
+      continue;
+    }
+    // a warp takes a group at a time; the columns of its lanes are not those that they summed
+    __syncthreads();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    for (int g = warp; g < a.groups; g += kThreads / 32) {
+      const int from = g * 128, to = min(a.D, from + 128);
+      float m = 0.f;
+      for (int c = from + lane; c < to; c += 32) m = fmaxf(m, fabsf(result(c)));
+#pragma unroll
+      for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+      const float scale = scale_8(m);
+      if (lane == 0) a.y_scale[row * a.groups + g] = scale;
+      finish(from, to, scale, lane, 32);
+    }
+  }
+}
+
+struct NormGradArgs {
+  const void *dy, *total, *weight, *dtotal;
+  long long dy_stride, t_stride, dt_stride, dx_stride;
+  long long T;
+  int D, weight_type;
+  const float* rstd;
+  void* dx;
+  float* parts;             // [blocks][D]: the blocks' sums of dweight, or NULL
+};
+
+template <typename Y, typename S, int G, int P, bool WIDE>
+__global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
+  wait_for_previous();
+  may_follow();
+  using R = Row<G, P, WIDE>;
+  __shared__ float cell[2][kThreads / 32];
+  extern __shared__ float shared_parts[];                           // [kRows][D] where a block has more than one row at a time
+  Join<G> join{cell};
+  const int D = a.D;
+  float w[P][8], dw[P][8] = {};
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[p][i] = R::column(p, i) < D ? load_as(a.weight, a.weight_type, R::column(p, i)) : 0.f;
+  const int mine = threadIdx.x / G;
+  Piece<Y, G, P, WIDE> dy;
+  Piece<S, G, P, WIDE> s, dt;
+  float rstd = 0.f;
+  const auto fetch = [&](long long row) {
+    const bool in = row < a.T;
+    if (!in) row = a.T - 1;
+    dy.fetch(static_cast<const Y*>(a.dy) + row * a.dy_stride, D);
+    s.fetch(static_cast<const S*>(a.total) + row * a.t_stride, D);
+    if (a.dtotal) dt.fetch(static_cast<const S*>(a.dtotal) + row * a.dt_stride, D);
+    rstd = a.rstd[row];
+  };
+  const long long step = (long long)gridDim.x * R::kRows;
+  long long row0 = (long long)blockIdx.x * R::kRows;
+  if (row0 < a.T) fetch(row0 + mine);
+  for (; row0 < a.T; row0 += step) {
+    const long long row = row0 + mine;
+    const bool in = row < a.T;
+    const float k = rstd;
+    float g[P][8], h[P][8], sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      dy.get(p, g[p]);
+      s.get(p, h[p]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        h[p][i] *= k;
+        if (in) dw[p][i] = fmaf(g[p][i], h[p][i], dw[p][i]);
+        g[p][i] *= w[p][i];
+        sum = fmaf(g[p][i], h[p][i], sum);
+      }
+    }
+    const float mean = join(sum, Plus()) / D;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      float u[8] = {};
+      if (a.dtotal) dt.get(p, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[p][i] = fmaf(k, fmaf(-h[p][i], mean, g[p][i]), u[i]);
+    }
+    if (row0 + step < a.T) fetch(row + step);
+    if (in && a.dx)
+#pragma unroll
+      for (int p = 0; p < P; ++p) put<S, G, P, WIDE>(static_cast<S*>(a.dx) + row * a.dx_stride, D, p, g[p]);
+  }
+  if (!a.parts) return;
+  float* out = a.parts + (long long)blockIdx.x * D;
+  if constexpr (R::kRows == 1) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (R::column(p, i) < D) out[R::column(p, i)] = dw[p][i];
+  } else {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (R::column(p, i) < D) shared_parts[mine * D + R::column(p, i)] = dw[p][i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < D; c += kThreads) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < R::kRows; ++i) sum += shared_parts[i * D + c];
+      out[c] = sum;
+    }
+  }
+}
+
+// Rows too long for registers; the block's sums of dweight stay in memory.
+template <typename Y, typename S> __global__ void __launch_bounds__(kThreads) k_norm_grad_long(const NormGradArgs a) {
+  wait_for_previous();
+  may_follow();
+  __shared__ float cell[2][kThreads / 32];
+  Join<kThreads> join{cell};
+  float* part = a.parts ? a.parts + (long long)blockIdx.x * a.D : nullptr;
+  if (part)
+    for (int c = threadIdx.x; c < a.D; c += kThreads) part[c] = 0.f;
+  for (long long row = blockIdx.x; row < a.T; row += gridDim.x) {
+    const Y* dy = static_cast<const Y*>(a.dy) + row * a.dy_stride;
+    const S* s = static_cast<const S*>(a.total) + row * a.t_stride;
+    const S* dt = static_cast<const S*>(a.dtotal) + row * a.dt_stride;
+    S* dx = static_cast<S*>(a.dx) + row * a.dx_stride;
+    const float k = a.rstd[row];
+    float sum = 0.f;
+    for (int c = threadIdx.x; c < a.D; c += kThreads) {
+      const float g = to_f32(dy[c]), h = to_f32(s[c]) * k;
+      if (part) part[c] = fmaf(g, h, part[c]);
+      sum = fmaf(g * load_as(a.weight, a.weight_type, c), h, sum);
+    }
+    const float mean = join(sum, Plus()) / a.D;
+    if (a.dx)
+      for (int c = threadIdx.x; c < a.D; c += kThreads) {
+        const float g = to_f32(dy[c]) * load_as(a.weight, a.weight_type, c), h = to_f32(s[c]) * k;
+        dx[c] = from_f32<S>(fmaf(k, fmaf(-h, mean, g), a.dtotal ? to_f32(dt[c]) : 0.f));
+      }
+  }
+}
+
+// The blocks' sums of dweight added in order: a block takes 32 columns, its eight warps every eighth part.
+__global__ void __launch_bounds__(kThreads) k_norm_weight(const float* parts, int count, int D, void* out, int type, int accumulate) {
+  wait_for_previous();
+  may_follow();
+  __shared__ float cell[kThreads / 32][32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const long long c = (long long)blockIdx.x * 32 + lane;
+  float sum = 0.f;
+  if (c < D) {
+#pragma unroll 8
+    for (int i = warp; i < count; i += kThreads / 32) sum += parts[(long long)i * D + c];
+  }
+  cell[warp][lane] = sum;
+  __syncthreads();
+  if (warp || c >= D) return;
+  sum = accumulate ? load_as(out, type, c) : 0.f;
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) sum += cell[i][lane];
+  store_as(out, type, c, sum);
+}
+
+constexpr int kLongest = 8192;                      // columns that 256 threads hold
+constexpr int kGradBlocks = 592;                    // at most, four for each SM of a B200 (the workspace's size is asked for without a handle)
+
+// Calls f with the element types (x and the sum) that two type codes stand for.
+template <typename F> cocodc_status with_types(int32_t x, int32_t s, F&& f) {
+  if (x == COCODC_F32) return f(float(), float());
+  if (x == COCODC_BF16) return s == COCODC_F32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
+  return s == COCODC_F32 ? f(__half(), float()) : f(__half(), __half());
+}
+template <int N> using Int = std::integral_constant<int, N>;
+
+unsigned grid_for(const cocodc_lm* lm, int64_t T, int rows, int per_sm) {
+  const int64_t blocks = (T + rows - 1) / rows, most = (int64_t)lm->sm_count * per_sm;
+  return (unsigned)(blocks < most ? blocks : most);
+}
+
+// Calls f(threads of a row, packs of a thread).  Few rows: as many threads as a row can use.
+template <typename F> cocodc_status with_shape(const cocodc_lm* lm, int64_t T, int64_t D, bool wide, F&& f) {
+  if (!wide) return D <= 1024 && T > lm->sm_count ? f(Int<32>(), Int<4>(), std::false_type()) : f(Int<256>(), Int<4>(), std::false_type());
+  const std::true_type w;
+  if (T <= 2 * lm->sm_count) return D <= 2048 ? f(Int<256>(), Int<1>(), w) : f(Int<256>(), Int<4>(), w);
+  if (D <= 512) return f(Int<32>(), Int<2>(), w);
+  if (D <= 1024) return f(Int<32>(), Int<4>(), w);
+  if (D <= 2048) return f(Int<128>(), Int<2>(), w);
+  if (D <= 4096) return f(Int<128>(), Int<4>(), w);
+  return f(Int<256>(), Int<4>(), w);
+}
+
+}  // namespace
+
+extern "C" {
+
+cocodc_status cocodc_lm_norm(cocodc_lm* lm, const void* x, int32_t x_type, int64_t x_stride, const void* residual,
+                             int64_t residual_stride, int32_t sum_type, const void* weight, int32_t weight_type, int64_t T,
+                             int64_t D, float eps, void* total, int64_t total_stride, void* y, int32_t y_type, int64_t y_stride,
+                             float* y_scale, int64_t scale_group, float* rstd, void* stream) {
+  const bool eight = y_type == COCODC_E4M3, sum = residual || total;
+  if (!lm || !known_type(x_type) || !known_type(weight_type) || !(known_type(y_type) || eight) || !sane(T) || D < 1 || D > INT32_MAX ||
+      !(eps >= 0.f && eps <= 3.4e38f) || x_stride < D || !sane(x_stride) || y_stride < D || !sane(y_stride) ||
+      (eight ? (scale_group != 0 && scale_group != 128) : scale_group != 0))
+    return COCODC_ERR_INVALID_ARG;
+  if (sum && ((sum_type != x_type && sum_type != COCODC_F32) || residual_stride < D || !sane(residual_stride) || total_stride < D ||
+              !sane(total_stride)))
+    return COCODC_ERR_INVALID_ARG;
+  if (T == 0) return COCODC_OK;
+  if (!x || !weight || !y || !residual != !total || !eight != !y_scale) return COCODC_ERR_INVALID_ARG;
+  const int xb = type_bytes(x_type), sb = sum ? type_bytes(sum_type) : xb, yb = eight ? 1 : type_bytes(y_type), wb = type_bytes(weight_type);
+  if (!on_boundary(x, xb) || !on_boundary(residual, sb) || !on_boundary(total, sb) || !on_boundary(y, yb) || !on_boundary(weight, wb) ||
+      !on_boundary(y_scale, 4) || !on_boundary(rstd, 4))
+    return COCODC_ERR_ALIGNMENT;
+  const int64_t groups = eight ? (scale_group ? (D + 127) / 128 : 1) : 0;
+  const Span in[3] = {span(x, T, x_stride, D, xb), span(residual, T, residual_stride, D, sb), span(weight, 1, D, D, wb)};
+  const Span out[4] = {span(total, T, total_stride, D, sb), span(y, T, y_stride, D, yb), span(y_scale, T, groups, groups, 4), span(rstd, 1, T, T, 4)};
+  const bool in_place = residual && total == residual && total_stride == residual_stride;
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 3; ++j)
+      if (!(in_place && i == 0 && j == 1) && meet(out[i], in[j])) return COCODC_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return COCODC_ERR_ALIAS;
+  }
+  DeviceScope scope(lm->device);
+  if (!scope.ok) return COCODC_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const NormArgs a{x, residual, weight, x_stride, residual_stride, total_stride, y_stride, T, (int)D, weight_type, y_type, (int)groups, eps,
+                   total, y, y_scale, rstd};
+  const bool wide = rows_aligned(x, x_stride, xb) && (!sum || (rows_aligned(residual, residual_stride, sb) && rows_aligned(total, total_stride, sb))) &&
+                    (eight ? on_boundary(y, 8) && y_stride % 8 == 0 : rows_aligned(y, y_stride, yb));
+  return with_types(x_type, sum ? sum_type : x_type, [&](auto xt, auto s) {
+    using X = decltype(xt);
+    using S = decltype(s);
+    if (D > kLongest) return start(lm, k_norm_long<X, S>, grid_for(lm, T, 1, 8), kThreads, 0, st, 1, a);
+    return with_shape(lm, T, D, wide, [&](auto g, auto p, auto w) {
+      constexpr int G = decltype(g)::value, P = decltype(p)::value;
+      return start(lm, k_norm<X, S, G, P, decltype(w)::value>, grid_for(lm, T, kThreads / G, 4), kThreads, 0, st, 1, a);
+    });
+  });
+}
+
+uint64_t cocodc_lm_norm_grad_workspace(int64_t T, int64_t D) {
+  if (!sane(T) || D < 1 || D > INT32_MAX) return 0;
+  return 16 + (uint64_t)(T < kGradBlocks ? T : kGradBlocks) * (uint64_t)D * sizeof(float);
+}
+
+cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type, int64_t dy_stride, const void* total,
+                                  int32_t total_type, int64_t total_stride, const void* weight, int32_t weight_type,
+                                  const float* rstd, int64_t T, int64_t D, const void* dtotal, int64_t dtotal_stride, void* dx,
+                                  int64_t dx_stride, void* dweight, int32_t dweight_type, int32_t accumulate, void* workspace,
+                                  uint64_t workspace_bytes, void* stream) {
+  if (!lm || !known_type(dy_type) || (total_type != dy_type && total_type != COCODC_F32) || !known_type(weight_type) || !sane(T) || D < 1 ||
+      D > INT32_MAX || dy_stride < D || !sane(dy_stride) || total_stride < D || !sane(total_stride) ||
+      (dtotal && (dtotal_stride < D || !sane(dtotal_stride))) || (dx && (dx_stride < D || !sane(dx_stride))) ||
+      (dweight && !known_type(dweight_type)))
+    return COCODC_ERR_INVALID_ARG;
+  if (!dx && !dweight) return T == 0 ? COCODC_OK : COCODC_ERR_INVALID_ARG;
+  if (T > 0 && (!dy || !total || !weight || !rstd)) return COCODC_ERR_INVALID_ARG;
+  if (dweight && (!workspace || workspace_bytes < cocodc_lm_norm_grad_workspace(T, D))) return COCODC_ERR_INVALID_ARG;
+  const int yb = type_bytes(dy_type), sb = type_bytes(total_type), wb = type_bytes(weight_type), db = dweight ? type_bytes(dweight_type) : 4;
+  if (!on_boundary(dy, yb) || !on_boundary(total, sb) || !on_boundary(dtotal, sb) || !on_boundary(dx, sb) || !on_boundary(weight, wb) ||
+      !on_boundary(dweight, db) || !on_boundary(rstd, 4) || (dweight && !on_boundary(workspace, 16)))
+    return COCODC_ERR_ALIGNMENT;
+  const Span in[5] = {span(dy, T, dy_stride, D, yb), span(total, T, total_stride, D, sb), span(weight, 1, D, D, wb), span(rstd, 1, T, T, 4),
+                      span(dtotal, T, dtotal_stride, D, sb)};
+  const Span out[3] = {span(dx, T, dx_stride, D, sb), span(dweight, 1, D, D, db),
+                       dweight ? span(workspace, 1, (int64_t)workspace_bytes, (int64_t)workspace_bytes, 1) : Span{0, 0, 0, 0}};
+  const bool in_place = dx && dx == dtotal && dx_stride == dtotal_stride;
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 5; ++j)
+      if (!(in_place && i == 0 && j == 4) && meet(out[i], in[j])) return COCODC_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return COCODC_ERR_ALIAS;
+  }
+  if (T == 0 && (!dweight || accumulate)) return COCODC_OK;
+  DeviceScope scope(lm->device);
+  if (!scope.ok) return COCODC_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const NormGradArgs a{dy, total, weight, dtotal, dy_stride, total_stride, dtotal_stride, dx_stride, T, (int)D, weight_type, rstd, dx,
+                       dweight ? static_cast<float*>(workspace) : nullptr};
+  const bool wide = rows_aligned(dy, dy_stride, yb) && rows_aligned(total, total_stride, sb) && (!dtotal || rows_aligned(dtotal, dtotal_stride, sb)) &&
+                    (!dx || rows_aligned(dx, dx_stride, sb));
+  unsigned blocks = 0;
+  cocodc_status status = COCODC_OK;
+  if (T > 0) {
+    status = with_types(dy_type, total_type, [&](auto yt, auto s) {
+      using Y = decltype(yt);
+      using S = decltype(s);
+      if (D > kLongest) {
+        blocks = grid_for(lm, T, 1, 4);
+        if (blocks > kGradBlocks) blocks = kGradBlocks;
+        return start(lm, k_norm_grad_long<Y, S>, blocks, kThreads, 0, st, 1, a);
+      }
+      return with_shape(lm, T, D, wide, [&](auto g, auto p, auto w) {
+        constexpr int G = decltype(g)::value, P = decltype(p)::value;
+        blocks = grid_for(lm, T, kThreads / G, 4);
+        if (blocks > kGradBlocks) blocks = kGradBlocks;
+        const unsigned shared = dweight && G < kThreads ? kThreads / G * (unsigned)D * 4 : 0;
+        return start(lm, k_norm_grad<Y, S, G, P, decltype(w)::value>, blocks, kThreads, shared, st, 1, a);
+      });
+    });
+  }
+  if (status != COCODC_OK || !dweight) return status;
+  return start(lm, k_norm_weight, (unsigned)((D + 31) / 32), kThreads, 0, st, 1, static_cast<const float*>(workspace), (int)blocks, (int)D, dweight,
+               dweight_type, accumulate ? 1 : 0);
+}
+
+}  // extern "C"
