@@ -23,6 +23,7 @@ namespace cocodc_lm_impl {
 // attribute is per device and outlives the handle).
 bool embed_prepare();
 bool glu_prepare();
+bool head_prepare();
 
 struct DeviceScope {
   int prev = -1;

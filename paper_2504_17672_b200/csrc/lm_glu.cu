@@ -290,18 +290,6 @@ uint64_t part_bytes(int64_t T, int64_t D, int64_t F) {
 int64_t scratch_pitch(int64_t F) { return (F + 7) / 8 * 8; }
 
 // ---- tensor-core path: host side ----------------------------------------------------------------
-std::atomic<EncodeTiled> g_encode{nullptr};
-
-template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t stride, int64_t rows, int64_t cols, int box_rows) {
-  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-  return g_encode.load()(map, IsBf16<E>::v ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                         const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-
 template <typename E, int MODE, int ACT, int BN> cocodc_status run_tc(cocodc_lm* lm, const TcArgs& a, cudaStream_t st) {
   const long long tiles = (long long)a.m_tiles * a.n_tiles * a.matrices, most = lm->sm_count;
   if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;

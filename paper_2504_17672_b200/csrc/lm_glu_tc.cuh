@@ -42,11 +42,6 @@ struct TcArgs {
   int* status;
 };
 
-constexpr int kTcThreads = 192;
-constexpr int kBM = 128, kBK = 64;
-constexpr unsigned kABytes = kBM * kBK * 2;
-constexpr unsigned kSlab = 64 * kBK * 2;            // an MN-major operand's 64 columns of m or n: 64 k rows of 128 bytes
-constexpr unsigned kOutBytes = 32 * 128;            // one warp's staged output: 32 rows of 64 columns
 template <int BN> struct TcShape {
   static constexpr unsigned kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
   // one CTA per SM; wide tiles stage their outputs for TMA stores, narrow ones write them from registers
@@ -112,13 +107,6 @@ __device__ __forceinline__ void store_row(const TcArgs& a, int what, int x, int 
     }
   }
 }
-// 32 columns (packed in pairs) of the thread's row into columns half*32.. of the staged tile, swizzled as the copy expects
-__device__ __forceinline__ void stage32(unsigned buf, int row, int half, const unsigned (&v)[16]) {
-  for (int q = 0; q < 4; ++q)
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + row * 128 + (((half * 4 + q) ^ (row & 7)) << 4)),
-                 "r"(v[4 * q]), "r"(v[4 * q + 1]), "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
-}
-
 template <typename E, int MODE, int ACT, int BN>
 __global__ void __launch_bounds__(kTcThreads, 1) k_glu_tc(const __grid_constant__ TcArgs a) {
   extern __shared__ unsigned char dyn[];

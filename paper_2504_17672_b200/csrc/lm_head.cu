@@ -1,6 +1,6 @@
 // The output head with its loss, without keeping the logits, and its gradient (include/cocodc_lm.h).
 
-#include "lm_common.cuh"
+#include "lm_head_tc.cuh"
 #include "lm_plain.cuh"
 
 #include <type_traits>
@@ -9,26 +9,17 @@ using namespace cocodc_lm_impl;
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kMostScale = 1e30f;
 constexpr int kSms = 148;                            // of a B200 (workspace sizes are asked for without a handle)
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 
-// Logits are taken in base 2 (times scale log2 e).  A strip of a row's logits leaves its largest one and the sum of 2^(z - largest): (m, s).
-struct Stats { float m, s; };
-__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }   // nothing but -Inf: the sum is then 0
-__device__ __forceinline__ Stats join(Stats a, Stats b) {
-  const float m = fmaxf(a.m, b.m), k = shift_of(m);
-  return Stats{m, a.s * fast_exp2(a.m - k) + b.s * fast_exp2(b.m - k)};
-}
-
-// Columns of a strip: what a tile of the product covers, a multiple of 16 up to 256.  Tiles times their width in rounds of one per SM,
-// plus what a tile costs beside its products, come out smallest.
-int strip_width(int64_t T, int64_t V) {
-  const int64_t rows = up(T, 128);
+// Columns of a tile of logits: multiples of `step` up to 256.  Tiles times their width in rounds of one per SM, plus what a tile
+// costs beside its products, come out smallest.
+int tile_width(int64_t T, int64_t V, int step) {
+  const int64_t rows = up(T, kBM);
   int best = 256;
   int64_t least = INT64_MAX;
-  for (int w = 256; w >= 16; w -= 16) {
+  for (int w = 256; w >= step; w -= step) {
     const int64_t cost = up(rows * up(V, w), kSms) * (w + 24);
     if (cost < least) {
       least = cost;
@@ -37,20 +28,7 @@ int strip_width(int64_t T, int64_t V) {
   }
   return best;
 }
-
-struct HeadArgs {
-  long long T, V;
-  int width;
-  long long strips;
-  float scale2;                                      // scale * log2 e
-  const void* targets;
-  int targets64;
-  float2* stats;                                     // [strip][T]
-  float* picked;                                     // [T]: the target's logit, base 2
-};
-__device__ __forceinline__ long long raw_target(const void* targets, int is64, long long t) {
-  return is64 ? static_cast<const long long*>(targets)[t] : (long long)static_cast<const int*>(targets)[t];
-}
+int strip_width(int64_t T, int64_t V) { return tile_width(T, V, 16); }
 
 // Any strides: 64 rows and a strip for each block, in pieces of 64 columns.
 template <typename E>
@@ -144,39 +122,6 @@ __global__ void __launch_bounds__(1024) k_head_factor(const HeadArgs a, const fl
   factor[1] = ldexpf(1.f, -e);
 }
 
-struct DzArgs {
-  long long T, V;
-  float scale2;
-  const void* targets;
-  int targets64;
-  const float *lse, *dlogp, *dlse, *factor;          // factor NULL: 1
-  long long v0, v1;                                  // the piece
-  void* dz;                                          // [T][pitch]
-  long long pitch;
-  int* status;
-};
-// What a row's dz needs: p's factor, what the target gets on top, and lse in base 2.
-struct RowOf { float slope, hit, lse2; long long y; };
-__device__ __forceinline__ RowOf row_of(const DzArgs& a, long long t) {
-  RowOf r{0.f, 0.f, 0.f, -1};
-  const float f = a.factor ? a.factor[0] : 1.f;
-  if (a.targets) r.y = token_at(a.targets, a.targets64, t, a.V, a.status);
-  const float up = r.y >= 0 ? a.dlogp[t] * f : 0.f, dl = a.dlse ? a.dlse[t] * f : 0.f, lse = a.lse[t];
-  if ((up == 0.f && dl == 0.f) || lse == -INFINITY) {               // nothing: whatever p is, it counts for nothing
-    r.y = -1;
-    r.lse2 = INFINITY;
-    return r;
-  }
-  r.slope = dl - up;
-  r.hit = up;
-  r.lse2 = lse == INFINITY ? __uint_as_float(0x7fc00000u) : lse * kLog2e;
-  return r;
-}
-__device__ __forceinline__ float dz_of(const RowOf& r, float z2, bool target) {
-  if (r.lse2 == INFINITY) return 0.f;
-  return fmaf(fast_exp2(z2 - r.lse2), r.slope, target ? r.hit : 0.f);
-}
-
 template <typename E>
 __global__ void __launch_bounds__(256) k_head_dz_plain(const DzArgs a, const Operand<E> x, const Operand<E> w, long long D) {
   wait_for_previous();
@@ -197,16 +142,6 @@ __global__ void __launch_bounds__(256) k_head_dz_plain(const DzArgs a, const Ope
   }
 }
 
-// Where a product goes: fp32 sums that other pieces of the vocabulary share, or the output.
-struct Out {
-  void* out;
-  int type, accumulate;
-  long long ld;
-  float* sums;                                       // [rows][cols], or NULL
-  int add, last;                                     // add what the sums hold; the sums are complete and go to the output
-  const float* factor;
-  float scale;
-};
 template <typename E> __device__ __forceinline__ void deliver(const Out& o, long long r, long long c, long long cols, float v) {
   if (o.sums && o.add) v += o.sums[r * cols + c];
   if (o.sums && !o.last) {
@@ -269,17 +204,71 @@ bool grid_of(int64_t rows, int64_t t, int64_t cols, int64_t n, unsigned* out) {
   return blocks <= INT32_MAX;
 }
 
+// Parts of dx's contraction where its tiles are few: as many as there are SMs for each tile, with at least 16 k-blocks to a part.
+int dx_width(int64_t D) { return D >= 256 ? 256 : (int)up(D, 64) * 64; }
+int dx_parts(int64_t T, int64_t D, int64_t width) {
+  if (T < 1) return 1;
+  const int64_t tiles = up(T, kBM) * up(D, dx_width(D)), parts = kSms / tiles, most = up(width, kBK) / 16;
+  const int64_t p = parts < most ? parts : most;
+  return p < 2 ? 1 : (int)p;
+}
+
 struct GradLayout { uint64_t sums, dz, bytes; int64_t width; };
 GradLayout grad_layout(int64_t T, int64_t D, int64_t V) {
   GradLayout l{};
   l.width = piece_width(T, V);
+  const int parts = dx_parts(T, D, l.width);
   l.sums = 256;
-  l.dz = l.sums + (l.width < V ? (uint64_t)up(T * D, 64) * 256 : 0);
+  // whole tiles of 128 x dx_width for each part; the kernels for any strides need T x D of it
+  l.dz = l.sums + (l.width < V || parts > 1 ? (uint64_t)parts * (uint64_t)up(T, kBM) * (uint64_t)up(D, dx_width(D)) * kBM * dx_width(D) * 4 : 0);
   l.bytes = l.dz + (uint64_t)T * (uint64_t)l.width * 2;
   return l;
 }
 
+// ---- tensor-core path: host side ----------------------------------------------------------------
+bool map_f32(CUtensorMap* map, const void* p, int64_t stride, int64_t rows, int64_t cols) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 4};
+  const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+  return g_encode.load()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+int a_rows(int64_t T) { return T >= kBM ? kBM : (int)up(T, 8) * 8; }
+
+template <typename E, int MODE> cocodc_status run_tc(cocodc_lm* lm, HeadTc& c, cudaStream_t st) {
+  const long long tiles = MODE == HEAD_PRODUCTS ? (long long)c.job[0].tiles + c.job[1].tiles : (long long)c.m_tiles * c.n_tiles;
+  if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;
+  c.status = lm->d_status;
+  return start(lm, k_head_tc<E, MODE>, (unsigned)(tiles < lm->sm_count ? tiles : lm->sm_count), kTcThreads, kHeadSmem, st, 1, c);
+}
+// A tile of logits: x [T][D] by rows of the table.
+template <typename E>
+bool logit_maps(HeadTc* c, const void* x, int64_t x_stride, const void* table, int64_t table_stride, int64_t T, int64_t D, int64_t V, int width) {
+  c->width = width;
+  c->a_bytes = a_rows(T) * kBK * 2;
+  c->m_tiles = (int)up(T, kBM);
+  c->k_blocks = (int)up(D, kBK);
+  return map_of<E>(&c->a[0], x, x_stride, T, D, a_rows(T)) && map_of<E>(&c->b[0], table, table_stride, V, D, width);
+}
+
 }  // namespace
+
+namespace cocodc_lm_impl {
+bool head_prepare() {
+  bool ok = true;
+  const auto allow = [&](auto kernel) {
+    ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem) == cudaSuccess;
+  };
+  const auto allow_type = [&](auto e) {
+    using E = decltype(e);
+    allow(k_head_tc<E, HEAD_STATS>);
+    allow(k_head_tc<E, HEAD_DZ>);
+    allow(k_head_tc<E, HEAD_PRODUCTS>);
+  };
+  allow_type(__nv_bfloat16());
+  allow_type(__half());
+  return ok;
+}
+}  // namespace cocodc_lm_impl
 
 extern "C" {
 
@@ -322,10 +311,18 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
   a.targets64 = targets_type == COCODC_I64;
   a.picked = static_cast<float*>(workspace);
   a.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + up(T, 4) * 16);
+  const bool tensor = rows_aligned(x, x_stride, 2) && rows_aligned(table, table_stride, 2);
   unsigned grid;
   if (!grid_of(T, kTile, V, a.width, &grid)) return COCODC_ERR_INVALID_ARG;
   const cocodc_status status = with_half(type, [&](auto e) {
     using E = decltype(e);
+    if (tensor) {
+      HeadTc c{};
+      c.h = a;
+      c.n_tiles = (int)a.strips;
+      if (!logit_maps<E>(&c, x, x_stride, table, table_stride, T, D, V, a.width)) return COCODC_ERR_CUDA;
+      return run_tc<E, HEAD_STATS>(lm, c, st);
+    }
     const Operand<E> xo{static_cast<const E*>(x), x_stride, 1}, wo{static_cast<const E*>(table), table_stride, 1};
     return start(lm, k_head_plain<E>, grid, 256, 0, st, 1, a, xo, wo, (long long)D);
   });
@@ -403,24 +400,62 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
     unsigned g1, g2, g3;
     if (!grid_of(T, kTile, l.width, kTile, &g1) || !grid_of(T, kTile, D, kTile, &g2) || !grid_of(l.width, kTile, D, kTile, &g3))
       return COCODC_ERR_INVALID_ARG;
+    const bool tensor = rows_aligned(x, x_stride, 2) && rows_aligned(table, table_stride, 2) && (!dx || rows_aligned(dx, dx_stride, 2)) &&
+                        (!dtable || rows_aligned(dtable, dtable_stride, wb));
+    if (up(T, kBM) * up(D, 64) > INT32_MAX / kSms || up(l.width, kBM) * up(D, 64) > INT32_MAX / 4) return COCODC_ERR_INVALID_ARG;
+    const int parts = tensor ? dx_parts(T, D, l.width) : 1;
     const E *xe = static_cast<const E*>(x), *we = static_cast<const E*>(table), *dz = reinterpret_cast<const E*>(ws + l.dz);
     for (int64_t v0 = 0; v0 < V; v0 += l.width) {
       d.v0 = v0;
       d.v1 = v0 + l.width < V ? v0 + l.width : V;
       const long long w = d.v1 - v0;
+      const Out ow{static_cast<char*>(dtable) + v0 * dtable_stride * wb, dtable_type, accumulate ? 1 : 0, dtable_stride, nullptr, 0, 1, d.factor, scale};
+      const Out ox{dx, type, 0, dx_stride, l.width < V || parts > 1 ? reinterpret_cast<float*>(ws + l.sums) : nullptr, v0 > 0,
+                   d.v1 == V && parts == 1, d.factor, scale};
+      if (tensor) {
+        HeadTc c{};
+        c.d = d;
+        c.first_row = v0;
+        const int width = tile_width(T, w, 64);
+        c.n_tiles = (int)up(w, width);
+        if (!logit_maps<E>(&c, x, x_stride, table, table_stride, T, D, V, width) || !map_of<E>(&c.c[0], d.dz, d.pitch, T, w, 32)) return COCODC_ERR_CUDA;
+        cocodc_status s = run_tc<E, HEAD_DZ>(lm, c, st);
+        if (s != COCODC_OK) return s;
+        c.width = dx_width(D);
+        const int n_tiles = (int)up(D, c.width);
+        if (dtable) {
+          HeadJob& j = c.job[0];
+          j = HeadJob{(int)up(w, kBM), n_tiles, (int)up(T, kBK), 1, (int)up(w, kBM) * n_tiles, (int)w, (int)D, kABytes, ow};
+          if (!map_of<E>(&c.a[0], d.dz, d.pitch, T, w, kBK) || !map_of<E>(&c.b[0], x, x_stride, T, D, kBK) ||
+              !(wb == 4 ? map_f32(&c.c[0], ow.out, dtable_stride, w, D) : map_of<E>(&c.c[0], ow.out, dtable_stride, w, D, 32)))
+            return COCODC_ERR_CUDA;
+        }
+        if (dx) {
+          HeadJob& j = c.job[1];
+          const int tiles = (int)up(T, kBM) * n_tiles;
+          j = HeadJob{(int)up(T, kBM), n_tiles, (int)up(w, kBK), parts, tiles * parts, (int)T, (int)D, c.a_bytes, ox};
+          if (!map_of<E>(&c.a[1], d.dz, d.pitch, T, w, a_rows(T)) || !map_of<E>(&c.b[1], table, table_stride, V, D, kBK) ||
+              !map_of<E>(&c.c[1], dx, dx_stride, T, D, 32))
+            return COCODC_ERR_CUDA;
+        }
+        s = run_tc<E, HEAD_PRODUCTS>(lm, c, st);
+        if (s != COCODC_OK) return s;
+        if (dx && parts > 1 && d.v1 == V)
+          s = start(lm, k_head_add<E>, (unsigned)(c.job[1].m_tiles * n_tiles * (kBM / 8)), 256, 0, st, 1, c);
+        if (s != COCODC_OK) return s;
+        continue;
+      }
       grid_of(T, kTile, w, kTile, &g1);
       cocodc_status s = start(lm, k_head_dz_plain<E>, g1, 256, 0, st, 1, d, Operand<E>{xe, x_stride, 1}, Operand<E>{we, table_stride, 1}, (long long)D);
       if (s != COCODC_OK) return s;
       if (dtable) {
         grid_of(w, kTile, D, kTile, &g3);
-        const Out o{static_cast<char*>(dtable) + v0 * dtable_stride * wb, dtable_type, accumulate ? 1 : 0, dtable_stride, nullptr, 0, 1, d.factor, scale};
-        s = start(lm, k_head_product_plain<E>, g3, 256, 0, st, 1, Operand<E>{dz, 1, d.pitch}, Operand<E>{xe, 1, x_stride}, w, (long long)D, (long long)T, o);
+        s = start(lm, k_head_product_plain<E>, g3, 256, 0, st, 1, Operand<E>{dz, 1, d.pitch}, Operand<E>{xe, 1, x_stride}, w, (long long)D, (long long)T, ow);
         if (s != COCODC_OK) return s;
       }
       if (dx) {
-        const Out o{dx, type, 0, dx_stride, l.width < V ? reinterpret_cast<float*>(ws + l.sums) : nullptr, v0 > 0, d.v1 == V, d.factor, scale};
         s = start(lm, k_head_product_plain<E>, g2, 256, 0, st, 1, Operand<E>{dz, d.pitch, 1}, Operand<E>{we + v0 * table_stride, 1, table_stride},
-                  (long long)T, (long long)D, w, o);
+                  (long long)T, (long long)D, w, ox);
         if (s != COCODC_OK) return s;
       }
     }

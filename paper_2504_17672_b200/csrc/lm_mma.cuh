@@ -93,6 +93,7 @@ __device__ __forceinline__ void tmem_load32(float (&v)[32], unsigned addr) {
         "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
         "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
+#pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -123,9 +124,33 @@ template <> __device__ __forceinline__ unsigned pack2<__half>(float a, float b) 
   return *reinterpret_cast<const unsigned*>(&v);
 }
 
+// Tiles of the tensor-core kernels
+constexpr int kTcThreads = 192;
+constexpr int kBM = 128, kBK = 64;
+constexpr unsigned kABytes = kBM * kBK * 2;
+constexpr unsigned kSlab = 64 * kBK * 2;            // an MN-major operand's 64 columns of m or n: 64 k rows of 128 bytes
+constexpr unsigned kOutBytes = 32 * 128;            // one warp's staged output: 32 rows of 64 columns
+
+// 32 columns (packed in pairs) of the thread's row into columns half*32.. of the staged tile, swizzled as the copy expects
+__device__ __forceinline__ void stage32(unsigned buf, int row, int half, const unsigned (&v)[16]) {
+  for (int q = 0; q < 4; ++q)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + row * 128 + (((half * 4 + q) ^ (row & 7)) << 4)),
+                 "r"(v[4 * q]), "r"(v[4 * q + 1]), "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
+}
+
 // Host: a row-major matrix of 16-bit elements as a tensor map with boxes of 64 columns (128 bytes, swizzled) x `rows`.
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+inline std::atomic<EncodeTiled> g_encode{nullptr};     // found at creation of a handle
+
+template <typename E> bool map_of(CUtensorMap* map, const void* p, int64_t stride, int64_t rows, int64_t cols, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return g_encode.load()(map, IsBf16<E>::v ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                         const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 }  // namespace cocodc_lm_impl

@@ -171,7 +171,7 @@ def test_plan_refuses_also(B, lib, handle):
     assert create(B, lib, handle, [tensor(B, **s), tensor(B, at=4, m_scale=A[8] + 12, v_scale=A[10])], bits=8) == B.ERR_ALIAS
 
 
-@pytest.mark.parametrize("sizes", [(1, 1, 1), (1, 2048, 32000), (8192, 2048, 32000), (2 ** 31 - 1, 1, 2 ** 30), (77, 2 ** 31 - 1, 2 ** 17), (2 ** 31 - 1, 2 ** 17, 2 ** 30)])
+@pytest.mark.parametrize("sizes", [(0, 1, 1), (0, 64, 100), (1, 1, 1), (1, 2048, 32000), (8192, 2048, 32000), (2 ** 31 - 1, 1, 2 ** 30), (77, 2 ** 31 - 1, 2 ** 17), (2 ** 31 - 1, 2 ** 17, 2 ** 30)])
 def test_workspace_sizes(lib, sizes):
     T, D, V = sizes
     assert lib.cocodc_lm_head_workspace(T, D, V) >= 4 * T + 8 * T * ((V + 255) // 256)
