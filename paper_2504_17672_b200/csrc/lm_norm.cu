@@ -79,39 +79,28 @@ __device__ __forceinline__ void store_as(void* p, int type, long long i, float v
 }
 
 // ---- a row in registers ---------------------------------------------------------------------------------
-// G threads hold a row, 8 P columns each; a block of 256 threads takes 256 / G rows at a time and strides on.  Where rows start on
-// 16-byte boundaries (WIDE) a thread's columns are packs of eight, otherwise single ones G apart, so that neighbours
-// read neighbours either way.
-template <int G, int P, bool WIDE> struct Row {
-  static constexpr int kRows = kThreads / G;
-  static __device__ __forceinline__ int column(int p, int i) {
-    const int t = threadIdx.x % G;
-    return WIDE ? (p * G + t) * 8 + i : (p * 8 + i) * G + t;
-  }
+// A group of G threads (whole warps, as many as the row's columns fill) holds a row, 8 P columns each; a block has as many groups as
+// make 256 threads, and each strides on by itself.  Where rows are whole packs of eight columns on 16-byte boundaries (WIDE) a thread's columns are such
+// packs, otherwise single ones G apart, so that neighbours read neighbours either way.
+template <int P, bool WIDE> struct Row {
+  int G, t;                                          // threads of the group, this one's number
+  __device__ __forceinline__ int column(int p, int i) const { return WIDE ? (p * G + t) * 8 + i : (p * 8 + i) * G + t; }
 };
 // One row's share of a thread: raw words while they are on their way.
-template <typename T, int G, int P, bool WIDE> struct Piece {
+template <typename T, int P, bool WIDE> struct Piece {
   Raw8<T> raw[WIDE ? P : 1];
   T one[WIDE ? 1 : P * 8];
   // columns behind the row's end are zero
-  __device__ __forceinline__ void fetch(const T* row, int D) {
-    using R = Row<G, P, WIDE>;
+  __device__ __forceinline__ void fetch(const Row<P, WIDE>& r, const T* row, int D) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       if constexpr (WIDE) {
-        const int c = R::column(p, 0);
-        if (c + 8 <= D) {
-          raw[p] = fetch8(row + c);
-        } else {
-          alignas(16) T v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = c + i < D ? row[c + i] : from_f32<T>(0.f);
-          raw[p] = *reinterpret_cast<const Raw8<T>*>(v);
-        }
+        const int c = r.column(p, 0);
+        raw[p] = c < D ? fetch8(row + c) : Raw8<T>{};
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int c = R::column(p, i);
+          const int c = r.column(p, i);
           one[p * 8 + i] = c < D ? row[c] : from_f32<T>(0.f);
         }
       }
@@ -126,31 +115,60 @@ template <typename T, int G, int P, bool WIDE> struct Piece {
     }
   }
 };
-template <typename T, int G, int P, bool WIDE> __device__ __forceinline__ void put(T* row, int D, int p, const float (&v)[8]) {
-  using R = Row<G, P, WIDE>;
-  if (WIDE && R::column(p, 0) + 8 <= D) {
-    store8(row + R::column(p, 0), v);
+template <typename T, int P, bool WIDE> __device__ __forceinline__ void put(const Row<P, WIDE>& r, T* row, int D, int p, const float (&v)[8]) {
+  if (WIDE) {
+    if (r.column(p, 0) < D) store8(row + r.column(p, 0), v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (R::column(p, i) < D) row[R::column(p, i)] = from_f32<T>(v[i]);
+      if (r.column(p, i) < D) row[r.column(p, i)] = from_f32<T>(v[i]);
   }
 }
+template <int P, bool WIDE> __device__ __forceinline__ void put_type(const Row<P, WIDE>& r, void* y, int type, long long at, int D, int p, const float (&v)[8]) {
+  if (type == COCODC_F32) put<float>(r, static_cast<float*>(y) + at, D, p, v);
+  else if (type == COCODC_BF16) put<__nv_bfloat16>(r, static_cast<__nv_bfloat16*>(y) + at, D, p, v);
+  else put<__half>(r, static_cast<__half*>(y) + at, D, p, v);
+}
+// The weights of a thread's columns, read once for all of its rows.
+template <int P, bool WIDE> __device__ __forceinline__ void fetch_weight(const Row<P, WIDE>& r, const void* w, int type, int D, float (&v)[P][8]) {
+  const auto take = [&](auto e) {
+    using T = decltype(e);
+    const T* p0 = static_cast<const T*>(w);
+    if (WIDE && (reinterpret_cast<unsigned long long>(w) & 15) == 0) {
+      Piece<T, P, WIDE> x;
+      x.fetch(r, p0, D);
+#pragma unroll
+      for (int p = 0; p < P; ++p) x.get(p, v[p]);
+    } else {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[p][i] = r.column(p, i) < D ? to_f32(p0[r.column(p, i)]) : 0.f;
+    }
+  };
+  if (type == COCODC_F32) take(float());
+  else if (type == COCODC_BF16) take(__nv_bfloat16());
+  else take(__half());
+}
 
-// Sums or maxima over the G threads of a row.  Above a warp they meet in shared memory, in two buffers in turn: one barrier each, for all
-// threads of the block.
-template <int G> struct Join {
-  float (*cell)[kThreads / 32];
+// Sums or maxima over the threads of a row's group.  Above a warp they meet in shared memory, in two buffers in turn: one barrier of
+// the group each.
+struct Join {
+  float (*cell)[kThreads / 32];                      // [2][...]
+  int group, G;
   int turn = 0;
+  __device__ __forceinline__ void barrier() const {
+    __syncwarp();
+    if (G > 32) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(G) : "memory");
+  }
   template <typename F> __device__ __forceinline__ float operator()(float v, F f) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(~0u, v, o));
-    if constexpr (G > 32) {
+    if (G > 32) {
+      const int first = group * (G / 32);
       if (threadIdx.x % 32 == 0) cell[turn][threadIdx.x / 32] = v;
-      __syncthreads();
-      const int first = threadIdx.x / G * (G / 32);
+      barrier();
       v = cell[turn][first];
-#pragma unroll
       for (int i = 1; i < G / 32; ++i) v = f(v, cell[turn][first + i]);
       turn ^= 1;
     }
@@ -164,7 +182,7 @@ struct NormArgs {
   const void *x, *residual, *weight;
   long long x_stride, r_stride, t_stride, y_stride;
   long long T;
-  int D, weight_type, y_type, groups;   // groups: scales of a row (0: y is not in 8 bits)
+  int D, G, weight_type, y_type, groups;   // G: threads of a row; groups: scales of a row (0: y is not in 8 bits)
   float eps;
   void *total, *y;
   float *y_scale, *rstd;
@@ -173,120 +191,109 @@ struct NormArgs {
 __device__ __forceinline__ float rms_scale(float sum, int D, float eps) { return 1.f / sqrtf(sum / D + eps); }
 __device__ __forceinline__ float scale_8(float most) { return fmaxf(most * (1.f / kMost8), kLeastScale); }
 
-template <typename X, typename S, int G, int P, bool WIDE>
-__global__ void __launch_bounds__(kThreads) k_norm(const NormArgs a) {
+// Registers: 24 P for the row and its weights, and what is on its way of the next row.
+template <typename X, typename S, int P, bool WIDE>
+__global__ void __launch_bounds__(kThreads, P == 4 ? 1 : P == 2 || !WIDE ? 2 : 3) k_norm(const NormArgs a) {
   wait_for_previous();
   may_follow();
-  using R = Row<G, P, WIDE>;
   __shared__ float cell[2][kThreads / 32];
-  __shared__ unsigned most[R::kRows][G * P * 8 / 128 + 1];
-  Join<G> join{cell};
+  __shared__ unsigned most[WIDE ? 1 : kThreads * P * 8 / 128 + kThreads / 32];   // a group's largest magnitudes: column order is not the threads'
+  const int group = threadIdx.x / a.G;
+  const Row<P, WIDE> r{a.G, (int)threadIdx.x % a.G};
+  Join join{cell, group, a.G};
   const int D = a.D;
   float w[P][8];
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[p][i] = R::column(p, i) < D ? load_as(a.weight, a.weight_type, R::column(p, i)) : 0.f;
-  const int mine = threadIdx.x / G;
-  Piece<X, G, P, WIDE> x;
-  Piece<S, G, P, WIDE> r;
+  fetch_weight(r, a.weight, a.weight_type, D, w);
+  Piece<X, P, WIDE> x;
+  Piece<S, P, WIDE> u;
   const auto fetch = [&](long long row) {
-    if (row >= a.T) row = a.T - 1;                                  // a row that another thread group has too: nothing is written for it
-    x.fetch(static_cast<const X*>(a.x) + row * a.x_stride, D);
-    if (a.residual) r.fetch(static_cast<const S*>(a.residual) + row * a.r_stride, D);
+    x.fetch(r, static_cast<const X*>(a.x) + row * a.x_stride, D);
+    if (a.residual) u.fetch(r, static_cast<const S*>(a.residual) + row * a.r_stride, D);
   };
-  const long long step = (long long)gridDim.x * R::kRows;
-  long long row0 = (long long)blockIdx.x * R::kRows;
-  fetch(row0 + mine);
-  for (; row0 < a.T; row0 += step) {
-    const long long row = row0 + mine;
-    const bool in = row < a.T;
+  const int rows = blockDim.x / a.G;
+  const long long step = (long long)gridDim.x * rows;
+  long long row = (long long)blockIdx.x * rows + group;
+  if (row < a.T) fetch(row);
+  for (; row < a.T; row += step) {
     float v[P][8], sum = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       x.get(p, v[p]);
       if (a.residual) {
-        float u[8];
-        r.get(p, u);
+        float q[8];
+        u.get(p, q);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i] + u[i]));
+        for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i] + q[i]));
+        put<S>(r, static_cast<S*>(a.total) + row * a.t_stride, D, p, v[p]);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(v[p][i], v[p][i], sum);
     }
-    if (in && a.residual) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) put<S, G, P, WIDE>(static_cast<S*>(a.total) + row * a.t_stride, D, p, v[p]);
-    }
-    if (row0 + step < a.T) fetch(row + step);                       // on its way while this row is finished
+    if (row + step < a.T) fetch(row + step);                        // on its way while this row is finished
     const float rstd = rms_scale(join(sum, Plus()), D, a.eps);
-    if (in && a.rstd && threadIdx.x % G == 0) a.rstd[row] = rstd;
+    if (a.rstd && r.t == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[p][i] = v[p][i] * rstd * w[p][i];
     if (a.groups == 0) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        if (!in) continue;
-        if (a.y_type == COCODC_F32) put<float, G, P, WIDE>(static_cast<float*>(a.y) + row * a.y_stride, D, p, v[p]);
-        else if (a.y_type == COCODC_BF16) put<__nv_bfloat16, G, P, WIDE>(static_cast<__nv_bfloat16*>(a.y) + row * a.y_stride, D, p, v[p]);
-        else put<__half, G, P, WIDE>(static_cast<__half*>(a.y) + row * a.y_stride, D, p, v[p]);
-      }
+      for (int p = 0; p < P; ++p) put_type(r, a.y, a.y_type, row * a.y_stride, D, p, v[p]);
       continue;
     }
-    // 8 bits: largest magnitudes of the row or of its groups (as whole numbers: the order of the updates changes nothing)
-    const int groups = a.groups;
-    if (groups > 1) {
-      for (int i = threadIdx.x % G; i < groups; i += G) most[mine][i] = 0;
-      if (G > 32) __syncthreads(); else __syncwarp();
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        if constexpr (WIDE) {
-          float m = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[p][i]));
-          if (R::column(p, 0) < D) atomicMax(&most[mine][R::column(p, 0) / 128], __float_as_uint(m));
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (R::column(p, i) < D && !isnan(v[p][i])) atomicMax(&most[mine][R::column(p, i) / 128], __float_as_uint(fabsf(v[p][i])));
-        }
-      }
-      if (G > 32) __syncthreads(); else __syncwarp();
-      if (in)
-        for (int i = threadIdx.x % G; i < groups; i += G) a.y_scale[row * groups + i] = scale_8(__uint_as_float(most[mine][i]));
-    } else {
-      float m = 0.f;
+    unsigned char* y = static_cast<unsigned char*>(a.y) + row * a.y_stride;
+    float top = 0.f;
+    if (a.groups == 1) {
 #pragma unroll
       for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[p][i]));
-      m = join(m, Most());
-      if (threadIdx.x % G == 0) {
-        most[mine][0] = __float_as_uint(m);
-        if (in) a.y_scale[row] = scale_8(m);
-      }
-      if (G > 32) __syncthreads(); else __syncwarp();
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[p][i]));
+      top = scale_8(join(top, Most()));
+      if (r.t == 0) a.y_scale[row] = top;
     }
-    unsigned char* y = static_cast<unsigned char*>(a.y) + row * a.y_stride;
+    if constexpr (WIDE) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if (!in) continue;
-      if (WIDE && R::column(p, 0) + 8 <= D) {
-        const float inv = 1.f / scale_8(__uint_as_float(most[mine][groups > 1 ? R::column(p, 0) / 128 : 0]));
-        unsigned lo = narrow_e4m3(v[p][0] * inv, v[p][1] * inv) | narrow_e4m3(v[p][2] * inv, v[p][3] * inv) << 16;
-        unsigned hi = narrow_e4m3(v[p][4] * inv, v[p][5] * inv) | narrow_e4m3(v[p][6] * inv, v[p][7] * inv) << 16;
-        *reinterpret_cast<uint2*>(y + R::column(p, 0)) = make_uint2(lo, hi);
-      } else {
+      for (int p = 0; p < P; ++p) {
+        const int c = r.column(p, 0);
+        float scale = top;
+        if (a.groups > 1) {                                         // sixteen neighbours hold 128 columns
+          scale = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int c = R::column(p, i);
-          if (c < D) y[c] = (unsigned char)narrow_e4m3(v[p][i] * (1.f / scale_8(__uint_as_float(most[mine][groups > 1 ? c / 128 : 0]))), 0.f);
+          for (int i = 0; i < 8; ++i) scale = fmaxf(scale, fabsf(v[p][i]));
+#pragma unroll
+          for (int o = 8; o; o >>= 1) scale = fmaxf(scale, __shfl_xor_sync(~0u, scale, o));
+          scale = scale_8(scale);
+          if (r.t % 16 == 0 && c < D) a.y_scale[row * a.groups + c / 128] = scale;
+        }
+        const float inv = 1.f / scale;
+        if (c < D) {
+          const unsigned lo = narrow_e4m3(v[p][0] * inv, v[p][1] * inv) | narrow_e4m3(v[p][2] * inv, v[p][3] * inv) << 16;
+          const unsigned hi = narrow_e4m3(v[p][4] * inv, v[p][5] * inv) | narrow_e4m3(v[p][6] * inv, v[p][7] * inv) << 16;
+          *reinterpret_cast<uint2*>(y + c) = make_uint2(lo, hi);
         }
       }
+    } else {
+      unsigned* mine = most + group * ((kThreads * P * 8 / 128) / rows + 1);
+      if (a.groups > 1) {                                           // as whole numbers: the order of the updates changes nothing
+        for (int i = r.t; i < a.groups; i += a.G) mine[i] = 0;
+        join.barrier();
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (r.column(p, i) < D && !isnan(v[p][i])) atomicMax(&mine[r.column(p, i) / 128], __float_as_uint(fabsf(v[p][i])));
+        join.barrier();
+        for (int i = r.t; i < a.groups; i += a.G) a.y_scale[row * a.groups + i] = scale_8(__uint_as_float(mine[i]));
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = r.column(p, i);
+          if (c < D) y[c] = (unsigned char)narrow_e4m3(v[p][i] * (1.f / (a.groups > 1 ? scale_8(__uint_as_float(mine[c / 128])) : top)), 0.f);
+        }
+      if (a.groups > 1) join.barrier();                             // before the next row's maxima
     }
-    if (G > 32) __syncthreads(); else __syncwarp();                 // before the next row's maxima
   }
 }
 
@@ -295,7 +302,7 @@ template <typename X, typename S> __global__ void __launch_bounds__(kThreads) k_
   wait_for_previous();
   may_follow();
   __shared__ float cell[2][kThreads / 32];
-  Join<kThreads> join{cell};
+  Join join{cell, 0, kThreads};
   for (long long row = blockIdx.x; row < a.T; row += gridDim.x) {
     const X* x = static_cast<const X*>(a.x) + row * a.x_stride;
     const S* r = static_cast<const S*>(a.residual) + row * a.r_stride;
@@ -345,44 +352,37 @@ struct NormGradArgs {
   const void *dy, *total, *weight, *dtotal;
   long long dy_stride, t_stride, dt_stride, dx_stride;
   long long T;
-  int D, weight_type;
+  int D, G, weight_type;
   const float* rstd;
   void* dx;
   float* parts;             // [blocks][D]: the blocks' sums of dweight, or NULL
 };
 
-template <typename Y, typename S, int G, int P, bool WIDE>
-__global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
+template <typename Y, typename S, int P, bool WIDE>
+__global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const NormGradArgs a) {
   wait_for_previous();
   may_follow();
-  using R = Row<G, P, WIDE>;
   __shared__ float cell[2][kThreads / 32];
-  extern __shared__ float shared_parts[];                           // [kRows][D] where a block has more than one row at a time
-  Join<G> join{cell};
+  extern __shared__ float shared_parts[];                           // [rows of the block][D] where it has more than one
+  const int group = threadIdx.x / a.G, rows = blockDim.x / a.G;
+  const Row<P, WIDE> r{a.G, (int)threadIdx.x % a.G};
+  Join join{cell, group, a.G};
   const int D = a.D;
   float w[P][8], dw[P][8] = {};
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[p][i] = R::column(p, i) < D ? load_as(a.weight, a.weight_type, R::column(p, i)) : 0.f;
-  const int mine = threadIdx.x / G;
-  Piece<Y, G, P, WIDE> dy;
-  Piece<S, G, P, WIDE> s, dt;
+  fetch_weight(r, a.weight, a.weight_type, D, w);
+  Piece<Y, P, WIDE> dy;
+  Piece<S, P, WIDE> s, dt;
   float rstd = 0.f;
   const auto fetch = [&](long long row) {
-    const bool in = row < a.T;
-    if (!in) row = a.T - 1;
-    dy.fetch(static_cast<const Y*>(a.dy) + row * a.dy_stride, D);
-    s.fetch(static_cast<const S*>(a.total) + row * a.t_stride, D);
-    if (a.dtotal) dt.fetch(static_cast<const S*>(a.dtotal) + row * a.dt_stride, D);
+    dy.fetch(r, static_cast<const Y*>(a.dy) + row * a.dy_stride, D);
+    s.fetch(r, static_cast<const S*>(a.total) + row * a.t_stride, D);
+    if (a.dtotal) dt.fetch(r, static_cast<const S*>(a.dtotal) + row * a.dt_stride, D);
     rstd = a.rstd[row];
   };
-  const long long step = (long long)gridDim.x * R::kRows;
-  long long row0 = (long long)blockIdx.x * R::kRows;
-  if (row0 < a.T) fetch(row0 + mine);
-  for (; row0 < a.T; row0 += step) {
-    const long long row = row0 + mine;
-    const bool in = row < a.T;
+  const long long step = (long long)gridDim.x * rows;
+  long long row = (long long)blockIdx.x * rows + group;
+  if (row < a.T) fetch(row);
+  for (; row < a.T; row += step) {
     const float k = rstd;
     float g[P][8], h[P][8], sum = 0.f;
 #pragma unroll
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         h[p][i] *= k;
-        if (in) dw[p][i] = fmaf(g[p][i], h[p][i], dw[p][i]);
+        dw[p][i] = fmaf(g[p][i], h[p][i], dw[p][i]);
         g[p][i] *= w[p][i];
         sum = fmaf(g[p][i], h[p][i], sum);
       }
@@ -405,32 +405,26 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) g[p][i] = fmaf(k, fmaf(-h[p][i], mean, g[p][i]), u[i]);
     }
-    if (row0 + step < a.T) fetch(row + step);
-    if (in && a.dx)
+    if (row + step < a.T) fetch(row + step);
+    if (a.dx) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) put<S, G, P, WIDE>(static_cast<S*>(a.dx) + row * a.dx_stride, D, p, g[p]);
+      for (int p = 0; p < P; ++p) put<S>(r, static_cast<S*>(a.dx) + row * a.dx_stride, D, p, g[p]);
+    }
   }
   if (!a.parts) return;
   float* out = a.parts + (long long)blockIdx.x * D;
-  if constexpr (R::kRows == 1) {
+  float* mine = rows == 1 ? out : shared_parts + group * D;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (R::column(p, i) < D) out[R::column(p, i)] = dw[p][i];
-  } else {
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (R::column(p, i) < D) shared_parts[mine * D + R::column(p, i)] = dw[p][i];
-    __syncthreads();
-    for (int c = threadIdx.x; c < D; c += kThreads) {
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < R::kRows; ++i) sum += shared_parts[i * D + c];
-      out[c] = sum;
-    }
+    for (int i = 0; i < 8; ++i)
+      if (r.column(p, i) < D) mine[r.column(p, i)] = dw[p][i];
+  if (rows == 1) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < D; c += blockDim.x) {
+    float sum = 0.f;
+    for (int i = 0; i < rows; ++i) sum += shared_parts[i * D + c];
+    out[c] = sum;
   }
 }
 
@@ -439,7 +433,7 @@ template <typename Y, typename S> __global__ void __launch_bounds__(kThreads) k_
   wait_for_previous();
   may_follow();
   __shared__ float cell[2][kThreads / 32];
-  Join<kThreads> join{cell};
+  Join join{cell, 0, kThreads};
   float* part = a.parts ? a.parts + (long long)blockIdx.x * a.D : nullptr;
   if (part)
     for (int c = threadIdx.x; c < a.D; c += kThreads) part[c] = 0.f;
@@ -464,28 +458,29 @@ template <typename Y, typename S> __global__ void __launch_bounds__(kThreads) k_
   }
 }
 
-// The blocks' sums of dweight added in order: a block takes 32 columns, its eight warps every eighth part.
-__global__ void __launch_bounds__(kThreads) k_norm_weight(const float* parts, int count, int D, void* out, int type, int accumulate) {
+// The blocks' sums of dweight added in order: a block takes 32 columns, each of its 32 warps every 32nd part.
+__global__ void __launch_bounds__(1024) k_norm_weight(const float* parts, int count, int D, void* out, int type, int accumulate) {
   wait_for_previous();
   may_follow();
-  __shared__ float cell[kThreads / 32][32];
+  __shared__ float cell[32][33];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const long long c = (long long)blockIdx.x * 32 + lane;
   float sum = 0.f;
   if (c < D) {
 #pragma unroll 8
-    for (int i = warp; i < count; i += kThreads / 32) sum += parts[(long long)i * D + c];
+    for (int i = warp; i < count; i += 32) sum += parts[(long long)i * D + c];
   }
   cell[warp][lane] = sum;
   __syncthreads();
   if (warp || c >= D) return;
   sum = accumulate ? load_as(out, type, c) : 0.f;
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) sum += cell[i][lane];
+  for (int i = 0; i < 32; ++i) sum += cell[i][lane];
   store_as(out, type, c, sum);
 }
 
-constexpr int kLongest = 8192;                      // columns that 256 threads hold
+// Columns that 256 threads hold: 32 each in packs, 8 one by one (more take more registers than there are)
+int64_t longest(bool wide) { return wide ? 8192 : 2048; }
 constexpr int kGradBlocks = 592;                    // at most, four for each SM of a B200 (the workspace's size is asked for without a handle)
 
 // Calls f with the element types (x and the sum) that two type codes stand for.
@@ -500,17 +495,34 @@ unsigned grid_for(const cocodc_lm* lm, int64_t T, int rows, int per_sm) {
   const int64_t blocks = (T + rows - 1) / rows, most = (int64_t)lm->sm_count * per_sm;
   return (unsigned)(blocks < most ? blocks : most);
 }
+// Blocks of a kernel that an SM holds, by registers (shared memory never limits these kernels).  A kernel's number is asked for once.
+int per_sm(std::atomic<int>& known, const void* kernel, int threads) {
+  int regs = known.load(std::memory_order_relaxed);
+  if (regs == 0) {
+    cudaFuncAttributes f;
+    if (cudaFuncGetAttributes(&f, kernel) != cudaSuccess) {
+      cudaGetLastError();
+      return 1;
+    }
+    regs = (f.numRegs + 7) / 8 * 8;
+    known.store(regs, std::memory_order_relaxed);
+  }
+  const int blocks = 65536 / (regs * threads), most = 2048 / threads;
+  return blocks < 1 ? 1 : blocks < most ? blocks : most;
+}
 
-// Calls f(threads of a row, packs of a thread).  Few rows: as many threads as a row can use.
+// Calls f(packs of a thread, whether wide, threads of a row, rows of a block).  Two packs a thread: registers for two blocks and more on an SM, with
+// the next row on its way; one where rows are few and their latency is what counts.
 template <typename F> cocodc_status with_shape(const cocodc_lm* lm, int64_t T, int64_t D, bool wide, F&& f) {
-  if (!wide) return D <= 1024 && T > lm->sm_count ? f(Int<32>(), Int<4>(), std::false_type()) : f(Int<256>(), Int<4>(), std::false_type());
-  const std::true_type w;
-  if (T <= 2 * lm->sm_count) return D <= 2048 ? f(Int<256>(), Int<1>(), w) : f(Int<256>(), Int<4>(), w);
-  if (D <= 512) return f(Int<32>(), Int<2>(), w);
-  if (D <= 1024) return f(Int<32>(), Int<4>(), w);
-  if (D <= 2048) return f(Int<128>(), Int<2>(), w);
-  if (D <= 4096) return f(Int<128>(), Int<4>(), w);
-  return f(Int<256>(), Int<4>(), w);
+  const auto go = [&](auto p) {
+    constexpr int P = decltype(p)::value;
+    const int G = (int)((D + 8 * P * 32 - 1) / (8 * P * 32)) * 32, rows = G >= kThreads ? 1 : kThreads / G;
+    if constexpr (P == 1)
+      if (!wide) return f(p, std::false_type(), G, rows);
+    return f(p, std::true_type(), G, rows);
+  };
+  if (!wide || D <= 256 || (T <= 2 * lm->sm_count && D <= 2048)) return go(Int<1>());
+  return D <= 4096 ? go(Int<2>()) : go(Int<4>());
 }
 
 }  // namespace
@@ -548,17 +560,19 @@ cocodc_status cocodc_lm_norm(cocodc_lm* lm, const void* x, int32_t x_type, int64
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const NormArgs a{x, residual, weight, x_stride, residual_stride, total_stride, y_stride, T, (int)D, weight_type, y_type, (int)groups, eps,
+  NormArgs a{x, residual, weight, x_stride, residual_stride, total_stride, y_stride, T, (int)D, 0, weight_type, y_type, (int)groups, eps,
                    total, y, y_scale, rstd};
-  const bool wide = rows_aligned(x, x_stride, xb) && (!sum || (rows_aligned(residual, residual_stride, sb) && rows_aligned(total, total_stride, sb))) &&
+  const bool wide = D % 8 == 0 && rows_aligned(x, x_stride, xb) && (!sum || (rows_aligned(residual, residual_stride, sb) && rows_aligned(total, total_stride, sb))) &&
                     (eight ? on_boundary(y, 8) && y_stride % 8 == 0 : rows_aligned(y, y_stride, yb));
   return with_types(x_type, sum ? sum_type : x_type, [&](auto xt, auto s) {
     using X = decltype(xt);
     using S = decltype(s);
-    if (D > kLongest) return start(lm, k_norm_long<X, S>, grid_for(lm, T, 1, 8), kThreads, 0, st, 1, a);
-    return with_shape(lm, T, D, wide, [&](auto g, auto p, auto w) {
-      constexpr int G = decltype(g)::value, P = decltype(p)::value;
-      return start(lm, k_norm<X, S, G, P, decltype(w)::value>, grid_for(lm, T, kThreads / G, 4), kThreads, 0, st, 1, a);
+    if (D > longest(wide)) return start(lm, k_norm_long<X, S>, grid_for(lm, T, 1, 8), kThreads, 0, st, 1, a);
+    return with_shape(lm, T, D, wide, [&](auto p, auto w, int G, int rows) {
+      static std::atomic<int> regs{0};
+      const auto kernel = k_norm<X, S, decltype(p)::value, decltype(w)::value>;
+      a.G = G;
+      return start(lm, kernel, grid_for(lm, T, rows, per_sm(regs, reinterpret_cast<const void*>(kernel), G * rows)), G * rows, 0, st, 1, a);
     });
   });
 }
@@ -600,9 +614,9 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const NormGradArgs a{dy, total, weight, dtotal, dy_stride, total_stride, dtotal_stride, dx_stride, T, (int)D, weight_type, rstd, dx,
+  NormGradArgs a{dy, total, weight, dtotal, dy_stride, total_stride, dtotal_stride, dx_stride, T, (int)D, 0, weight_type, rstd, dx,
                        dweight ? static_cast<float*>(workspace) : nullptr};
-  const bool wide = rows_aligned(dy, dy_stride, yb) && rows_aligned(total, total_stride, sb) && (!dtotal || rows_aligned(dtotal, dtotal_stride, sb)) &&
+  const bool wide = D % 8 == 0 && rows_aligned(dy, dy_stride, yb) && rows_aligned(total, total_stride, sb) && (!dtotal || rows_aligned(dtotal, dtotal_stride, sb)) &&
                     (!dx || rows_aligned(dx, dx_stride, sb));
   unsigned blocks = 0;
   cocodc_status status = COCODC_OK;
@@ -610,22 +624,23 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
     status = with_types(dy_type, total_type, [&](auto yt, auto s) {
       using Y = decltype(yt);
       using S = decltype(s);
-      if (D > kLongest) {
+      if (D > longest(wide)) {
         blocks = grid_for(lm, T, 1, 4);
         if (blocks > kGradBlocks) blocks = kGradBlocks;
         return start(lm, k_norm_grad_long<Y, S>, blocks, kThreads, 0, st, 1, a);
       }
-      return with_shape(lm, T, D, wide, [&](auto g, auto p, auto w) {
-        constexpr int G = decltype(g)::value, P = decltype(p)::value;
-        blocks = grid_for(lm, T, kThreads / G, 4);
+      return with_shape(lm, T, D, wide, [&](auto p, auto w, int G, int rows) {
+        static std::atomic<int> regs{0};
+        const auto kernel = k_norm_grad<Y, S, decltype(p)::value, decltype(w)::value>;
+        a.G = G;
+        blocks = grid_for(lm, T, rows, per_sm(regs, reinterpret_cast<const void*>(kernel), G * rows));
         if (blocks > kGradBlocks) blocks = kGradBlocks;
-        const unsigned shared = dweight && G < kThreads ? kThreads / G * (unsigned)D * 4 : 0;
-        return start(lm, k_norm_grad<Y, S, G, P, decltype(w)::value>, blocks, kThreads, shared, st, 1, a);
+        return start(lm, kernel, blocks, G * rows, dweight && rows > 1 ? rows * (unsigned)D * 4 : 0, st, 1, a);
       });
     });
   }
   if (status != COCODC_OK || !dweight) return status;
-  return start(lm, k_norm_weight, (unsigned)((D + 31) / 32), kThreads, 0, st, 1, static_cast<const float*>(workspace), (int)blocks, (int)D, dweight,
+  return start(lm, k_norm_weight, (unsigned)((D + 31) / 32), 1024, 0, st, 1, static_cast<const float*>(workspace), (int)blocks, (int)D, dweight,
                dweight_type, accumulate ? 1 : 0);
 }
 
