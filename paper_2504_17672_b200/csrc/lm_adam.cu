@@ -13,7 +13,6 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnit = COCODC_LM_ADAM_BLOCK;          // elements that a warp takes at a time and that share a scale: 8 for each lane
-constexpr int kTileUnits = 16;                       // a block's share: 4096 elements of one tensor
 constexpr float kMost8 = 448.f, kLeastScale = 1e-30f;
 __device__ __forceinline__ float scale_8(unsigned most) { return fmaxf(__fmul_rn(__uint_as_float(most), 1.f / kMost8), kLeastScale); }
 
@@ -26,25 +25,26 @@ struct Tensor {                                      // as the kernel reads it
   long long n;
   int grad_type, copy_type;
   float decay;
+  int position;                                      // in the plan
   int wide;                                          // every array starts where vector accesses may
+  long long first;                                   // number of its first unit among all tensors' units
 };
-struct Tile { int tensor, first; };                  // first: its first unit
 
 }  // namespace
 
 struct cocodc_lm_adam {
   int device = 0, bits = 32;
-  long long tiles = 0;
+  long long units = 0;
+  int count = 0;
   Tensor* d_tensors = nullptr;
-  Tile* d_tiles = nullptr;
 };
 
 namespace {
 
 struct AdamArgs {
-  const Tensor* tensors;
-  const Tile* tiles;
-  long long count;
+  const Tensor* tensors;                             // those with elements; `position` of each is its place in the plan
+  int count;
+  long long units;
   float b1, c1, b2, c2, eps;                         // c = 1 - b
   double lr, beta1, beta2;
   long long step;
@@ -62,13 +62,11 @@ __device__ __forceinline__ unsigned mix(unsigned x) {
 }
 constexpr unsigned kGolden = 0x9E3779B9u;
 
-// x in [0, 448] to an e4m3 code, up with probability (what is cut off) / (spacing): bits holds 16 random ones.  From 2^-6 on
-// they are added below the three bits of mantissa that stay; below, the codes are multiples of 2^-9.
-__device__ __forceinline__ unsigned round_8(float x, unsigned bits) {
-  const unsigned cut = ((__float_as_uint(x) + (bits << 4)) >> 20) - (120u << 3);
-  const float u = __uint_as_float(0x3f800000u | bits << 7) - 1.f;
-  const unsigned whole = __float_as_uint(__fadd_rz(fmaf(x, 512.f, u), 8388608.f)) & 15u;      // floor of a number below 16
-  return x < 0.015625f ? whole : cut;
+// A number x of a unit's largest magnitude 448 to an e4m3 code in the highest byte, without its sign: up with probability (what is cut off) /
+// (spacing).  Times 2^-120 the exponents of e4m3 are those of fp32, numbers below its smallest normal one too (2^-126 here and there), so that the
+// code is what stands above the lowest 20 bits; 16 random bits, here bytes 1 and 2, are added to those.  x may be 448 + 3 ulp: no carry comes of it.
+__device__ __forceinline__ unsigned code_of(float x, unsigned random) {
+  return (__float_as_uint(__fmul_rn(x, 0x1p-120f)) << 4) + random;
 }
 __device__ __forceinline__ float2 widen_e4m3(unsigned short v) {
   unsigned h;
@@ -98,15 +96,97 @@ __device__ __forceinline__ unsigned load4(const void* p) {
   asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));
   return v;
 }
-// finite magnitudes as whole numbers, whose order is theirs; 0 for the others
-__device__ __forceinline__ unsigned magnitude(float x) {
+// the larger magnitude; NaN if one is
+__device__ __forceinline__ float larger(float a, float b) {
+  float v;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(a), "f"(fabsf(b)));
+  return v;
+}
+__device__ __forceinline__ float inverse(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ unsigned finite_magnitude(float x) {
   const unsigned b = __float_as_uint(x) & 0x7fffffffu;
   return b < 0x7f800000u ? b : 0u;
 }
 
-// A warp takes a unit: lane l has its elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3, so that neighbours read neighbours in
-// every width.  Read once, written once: bound by memory.
-template <bool EIGHT> __global__ void __launch_bounds__(kThreads) k_adamw(const AdamArgs a) {
+// A unit's numbers on their way: lane l has its elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3, so that neighbours read neighbours in
+// every width.
+template <bool EIGHT> struct RawUnit {
+  uint4 p[2], g[2];
+  uint4 m[EIGHT ? 1 : 2], v[EIGHT ? 1 : 2];          // EIGHT: codes in x and y
+  float ms, vs;
+};
+template <bool EIGHT> __device__ __forceinline__ void fetch(RawUnit<EIGHT>& r, const Tensor& t, long long unit, int lane) {
+  const long long base = unit * kUnit + lane * 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const long long i = base + h * 128;
+    r.p[h] = load16(t.p + i);
+    if (t.grad_type == COCODC_F32) {
+      r.g[h] = load16(static_cast<const float*>(t.grad) + i);
+    } else {
+      const uint2 q = load8(static_cast<const unsigned short*>(t.grad) + i);
+      r.g[h].x = q.x;
+      r.g[h].y = q.y;
+    }
+    if (EIGHT) {
+      (h ? r.m[0].y : r.m[0].x) = load4(static_cast<const unsigned char*>(t.m) + i);
+      (h ? r.v[0].y : r.v[0].x) = load4(static_cast<const unsigned char*>(t.v) + i);
+    } else {
+      r.m[h] = load16(static_cast<const float*>(t.m) + i);
+      r.v[h] = load16(static_cast<const float*>(t.v) + i);
+    }
+  }
+  if (EIGHT) {
+    r.ms = t.m_scale[unit];
+    r.vs = t.v_scale[unit];
+  }
+}
+__device__ __forceinline__ void spread4(const uint4& r, float* v) {
+  v[0] = __uint_as_float(r.x);
+  v[1] = __uint_as_float(r.y);
+  v[2] = __uint_as_float(r.z);
+  v[3] = __uint_as_float(r.w);
+}
+template <bool EIGHT>
+__device__ __forceinline__ void spread(const RawUnit<EIGHT>& r, int grad_type, float (&p)[8], float (&g)[8], float (&m)[8], float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    spread4(r.p[h], p + 4 * h);
+    float* pg = g + 4 * h;
+    if (grad_type == COCODC_F32) {
+      spread4(r.g[h], pg);
+    } else if (grad_type == COCODC_BF16) {
+      pg[0] = __uint_as_float(r.g[h].x << 16);
+      pg[1] = __uint_as_float(r.g[h].x & 0xffff0000u);
+      pg[2] = __uint_as_float(r.g[h].y << 16);
+      pg[3] = __uint_as_float(r.g[h].y & 0xffff0000u);
+    } else {
+      const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&r.g[h].x)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&r.g[h].y));
+      pg[0] = f0.x;
+      pg[1] = f0.y;
+      pg[2] = f1.x;
+      pg[3] = f1.y;
+    }
+    if (EIGHT) {
+      const unsigned cm = h ? r.m[0].y : r.m[0].x, cv = h ? r.v[0].y : r.v[0].x;
+      const float2 m0 = widen_e4m3((unsigned short)cm), m1 = widen_e4m3((unsigned short)(cm >> 16));
+      const float2 v0 = widen_e4m3((unsigned short)cv), v1 = widen_e4m3((unsigned short)(cv >> 16));
+      m[4 * h] = m0.x; m[4 * h + 1] = m0.y; m[4 * h + 2] = m1.x; m[4 * h + 3] = m1.y;
+      v[4 * h] = v0.x; v[4 * h + 1] = v0.y; v[4 * h + 2] = v1.x; v[4 * h + 3] = v1.y;
+    } else {
+      spread4(r.m[h], m + 4 * h);
+      spread4(r.v[h], v + 4 * h);
+    }
+  }
+}
+
+// Read once, written once: bound by memory.  The units of all tensors form one row, of which each block takes an equal part and its warps one unit
+// in turn: a warp walks from tensor to tensor, and the next unit's numbers are on their way while it works on one.
+template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 2) k_adamw(const AdamArgs a) {
   wait_for_previous();
   may_follow();
   __shared__ float factors[2];
@@ -122,170 +202,170 @@ template <bool EIGHT> __global__ void __launch_bounds__(kThreads) k_adamw(const 
     factors[1] = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)step)));
     shared_lr = lr;
   }
-  __syncthreads();
-  const float k1 = factors[0], k2 = factors[1], gs = a.grad_scale ? *a.grad_scale : 1.f;
-  const double lr = shared_lr;
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const unsigned step_bits = (unsigned)(a.step_at ? *a.step_at : a.step);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  for (long long at = blockIdx.x; at < a.count; at += gridDim.x) {
-    const Tile tile = a.tiles[at];
-    const Tensor t = a.tensors[tile.tensor];
-    const float keep = (float)(1.0 - lr * (double)t.decay);
-    const long long units = (t.n + kUnit - 1) / kUnit;
-    for (long long unit = (long long)tile.first + warp; unit < min(units, (long long)tile.first + kTileUnits); unit += kWarps) {
-      const long long base = unit * kUnit;
-      const int here = (int)min((long long)kUnit, t.n - base);
-      const bool wide = t.wide && here == kUnit;
-      float p[8], g[8], m[8], v[8];
-      float ms = 0.f, vs = 0.f;
+  const long long last = a.units * (blockIdx.x + 1) / gridDim.x;
+  long long unit = a.units * blockIdx.x / gridDim.x + warp;
+  // the tensor of the warp's first unit: the last one that begins at or before it
+  int at = 0;
+  for (int n = a.count; n > 1;) {
+    const int half = n / 2;
+    if (a.tensors[at + half].first <= unit) at += half;
+    n -= half;
+  }
+  long long behind = a.tensors[at].first + (a.tensors[at].n + kUnit - 1) / kUnit;      // the unit behind the tensor's last
+  const auto whole = [&](const Tensor& t, long long u) { return t.wide && (u - t.first + 1) * kUnit <= t.n; };
+  RawUnit<EIGHT> raw;
+  if (unit < last && whole(a.tensors[at], unit)) fetch(raw, a.tensors[at], unit - a.tensors[at].first, lane);
+  __syncthreads();
+  const float k1 = factors[0], k2 = factors[1];
+  while (unit < last) {
+    const Tensor& t = a.tensors[at];
+    const long long own = unit - t.first, base = own * kUnit;
+    const bool wide = whole(t, unit);
+    const float keep = (float)(1.0 - shared_lr * (double)t.decay);
+    float p[8], g[8], m[8], v[8], ms = 0.f, vs = 0.f;
+    const int here = (int)min((long long)kUnit, t.n - base);
+    if (wide) {
+      spread(raw, t.grad_type, p, g, m, v);
+      ms = raw.ms;
+      vs = raw.vs;
+    } else {
       if (EIGHT) {
-        ms = t.m_scale[unit];
-        vs = t.v_scale[unit];
+        ms = t.m_scale[own];
+        vs = t.v_scale[own];
       }
-      if (wide) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const long long i = base + h * 128 + lane * 4;
-          const uint4 rp = load16(t.p + i);
-          uint4 rg, rm, rv;
-          if (t.grad_type == COCODC_F32) {
-            rg = load16(static_cast<const float*>(t.grad) + i);
-          } else {
-            const uint2 q = load8(static_cast<const unsigned short*>(t.grad) + i);
-            rg = make_uint4(q.x, q.y, 0, 0);
-          }
-          if (EIGHT) {
-            rm.x = load4(static_cast<const unsigned char*>(t.m) + i);
-            rv.x = load4(static_cast<const unsigned char*>(t.v) + i);
-          } else {
-            rm = load16(static_cast<const float*>(t.m) + i);
-            rv = load16(static_cast<const float*>(t.v) + i);
-          }
-          float *pp = p + 4 * h, *pg = g + 4 * h, *pm = m + 4 * h, *pv = v + 4 * h;
-          pp[0] = __uint_as_float(rp.x); pp[1] = __uint_as_float(rp.y); pp[2] = __uint_as_float(rp.z); pp[3] = __uint_as_float(rp.w);
-          if (t.grad_type == COCODC_F32) {
-            pg[0] = __uint_as_float(rg.x); pg[1] = __uint_as_float(rg.y); pg[2] = __uint_as_float(rg.z); pg[3] = __uint_as_float(rg.w);
-          } else if (t.grad_type == COCODC_BF16) {
-            pg[0] = __uint_as_float(rg.x << 16); pg[1] = __uint_as_float(rg.x & 0xffff0000u);
-            pg[2] = __uint_as_float(rg.y << 16); pg[3] = __uint_as_float(rg.y & 0xffff0000u);
-          } else {
-            const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&rg.x)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&rg.y));
-            pg[0] = f0.x; pg[1] = f0.y; pg[2] = f1.x; pg[3] = f1.y;
-          }
-          if (EIGHT) {
-            const float2 m0 = widen_e4m3((unsigned short)rm.x), m1 = widen_e4m3((unsigned short)(rm.x >> 16));
-            const float2 v0 = widen_e4m3((unsigned short)rv.x), v1 = widen_e4m3((unsigned short)(rv.x >> 16));
-            pm[0] = m0.x; pm[1] = m0.y; pm[2] = m1.x; pm[3] = m1.y;
-            pv[0] = v0.x; pv[1] = v0.y; pv[2] = v1.x; pv[3] = v1.y;
-          } else {
-            pm[0] = __uint_as_float(rm.x); pm[1] = __uint_as_float(rm.y); pm[2] = __uint_as_float(rm.z); pm[3] = __uint_as_float(rm.w);
-            pv[0] = __uint_as_float(rv.x); pv[1] = __uint_as_float(rv.y); pv[2] = __uint_as_float(rv.z); pv[3] = __uint_as_float(rv.w);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int o = e / 4 * 128 + lane * 4 + e % 4;
-          p[e] = g[e] = m[e] = v[e] = 0.f;
-          if (o >= here) continue;
-          p[e] = t.p[base + o];
-          g[e] = load_grad(t.grad, t.grad_type, base + o);
-          if (EIGHT) {
-            m[e] = widen_e4m3(static_cast<const unsigned char*>(t.m)[base + o]).x;
-            v[e] = widen_e4m3(static_cast<const unsigned char*>(t.v)[base + o]).x;
-          } else {
-            m[e] = static_cast<const float*>(t.m)[base + o];
-            v[e] = static_cast<const float*>(t.v)[base + o];
-          }
-        }
-      }
-      float root[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
+        const int o = e / 4 * 128 + lane * 4 + e % 4;
+        p[e] = g[e] = m[e] = v[e] = 0.f;
+        if (o >= here) continue;
+        p[e] = t.p[base + o];
+        g[e] = load_grad(t.grad, t.grad_type, base + o);
         if (EIGHT) {
-          m[e] = __fmul_rn(m[e], ms);
-          v[e] = __fmul_rn(v[e], vs);
-          v[e] = __fmul_rn(v[e], v[e]);
+          m[e] = widen_e4m3(static_cast<const unsigned char*>(t.m)[base + o]).x;
+          v[e] = widen_e4m3(static_cast<const unsigned char*>(t.v)[base + o]).x;
+        } else {
+          m[e] = static_cast<const float*>(t.m)[base + o];
+          v[e] = static_cast<const float*>(t.v)[base + o];
         }
-        const float gr = __fmul_rn(g[e], gs);
-        m[e] = __fadd_rn(__fmul_rn(m[e], a.b1), __fmul_rn(gr, a.c1));
-        v[e] = __fadd_rn(__fmul_rn(v[e], a.b2), __fmul_rn(__fmul_rn(gr, a.c2), gr));
-        root[e] = __fsqrt_rn(v[e]);
-        p[e] = __fadd_rn(__fmul_rn(p[e], keep), -__fdividef(__fmul_rn(m[e], k1), __fadd_rn(__fmul_rn(root[e], k2), a.eps)));
       }
-      unsigned mc[8], vc[8];
+    }
+    // the next unit's
+    const int now = at;
+    unit += kWarps;
+    while (unit < last && unit >= behind) {
+      ++at;
+      behind = a.tensors[at].first + (a.tensors[at].n + kUnit - 1) / kUnit;
+    }
+    if (unit < last && whole(a.tensors[at], unit)) fetch(raw, a.tensors[at], unit - a.tensors[at].first, lane);
+    float root[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
       if (EIGHT) {
-        unsigned top_m = 0, top_v = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int o = e / 4 * 128 + lane * 4 + e % 4;
-          if (o < here) {
-            top_m = max(top_m, magnitude(m[e]));
-            top_v = max(top_v, magnitude(root[e]));
-          }
-        }
-        top_m = __reduce_max_sync(~0u, top_m);
-        top_v = __reduce_max_sync(~0u, top_v);
-        ms = scale_8(top_m);
-        vs = scale_8(top_v);
-        const float im = __fdiv_rn(1.f, ms), iv = __fdiv_rn(1.f, vs);
-        unsigned key = mix(a.seed + kGolden) ^ step_bits;
-        key = mix(key + kGolden) ^ (unsigned)tile.tensor;
-        key = mix(key + kGolden) ^ (unsigned)unit;
-        key = mix(key + kGolden);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const unsigned bits = mix(key + (unsigned)(e / 4 * 128 + lane * 4 + e % 4) * kGolden);
-          mc[e] = round_8(fminf(__fmul_rn(fabsf(m[e]), im), kMost8), bits & 0xffffu) | (__float_as_uint(m[e]) >> 24 & 0x80u);
-          vc[e] = round_8(fminf(__fmul_rn(root[e], iv), kMost8), bits >> 16);
-          if (root[e] > 0.f) vc[e] = max(vc[e], 1u);
-          if (magnitude(m[e]) == 0 && m[e] != 0.f) mc[e] = 0x7f;
-          if (magnitude(root[e]) == 0 && root[e] != 0.f) vc[e] = 0x7f;
-        }
-        if (lane == 0) {
-          t.m_scale[unit] = ms;
-          t.v_scale[unit] = vs;
-        }
+        m[e] = __fmul_rn(m[e], ms);
+        v[e] = __fmul_rn(v[e], vs);
+        v[e] = __fmul_rn(v[e], v[e]);
       }
-      if (wide) {
+      const float gr = __fmul_rn(g[e], gs);
+      m[e] = __fadd_rn(__fmul_rn(m[e], a.b1), __fmul_rn(gr, a.c1));
+      v[e] = __fadd_rn(__fmul_rn(v[e], a.b2), __fmul_rn(__fmul_rn(gr, a.c2), gr));
+      root[e] = __fsqrt_rn(v[e]);
+      p[e] = __fadd_rn(__fmul_rn(p[e], keep), -__fmul_rn(__fmul_rn(m[e], k1), inverse(__fadd_rn(__fmul_rn(root[e], k2), a.eps))));
+    }
+    unsigned mc[2], vc[2];                             // codes of four elements each
+    if (EIGHT) {
+      float top_m = 0.f, top_v = 0.f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const long long i = base + h * 128 + lane * 4;
-          const float *pp = p + 4 * h, *pm = m + 4 * h, *pv = v + 4 * h;
-          *reinterpret_cast<float4*>(t.p + i) = make_float4(pp[0], pp[1], pp[2], pp[3]);
-          if (EIGHT) {
-            const unsigned *qm = mc + 4 * h, *qv = vc + 4 * h;
-            *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(t.m) + i) = qm[0] | qm[1] << 8 | qm[2] << 16 | qm[3] << 24;
-            *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(t.v) + i) = qv[0] | qv[1] << 8 | qv[2] << 16 | qv[3] << 24;
-          } else {
-            *reinterpret_cast<float4*>(static_cast<float*>(t.m) + i) = make_float4(pm[0], pm[1], pm[2], pm[3]);
-            *reinterpret_cast<float4*>(static_cast<float*>(t.v) + i) = make_float4(pv[0], pv[1], pv[2], pv[3]);
-          }
-          if (t.copy)
-            *reinterpret_cast<uint2*>(static_cast<unsigned short*>(t.copy) + i) =
-                make_uint2(narrow2(t.copy_type, pp[0], pp[1]), narrow2(t.copy_type, pp[2], pp[3]));
-        }
-      } else {
+      for (int e = 0; e < 8; ++e) {
+        top_m = larger(top_m, m[e]);
+        top_v = larger(top_v, root[e]);
+      }
+      unsigned most_m = __reduce_max_sync(~0u, __float_as_uint(top_m)), most_v = __reduce_max_sync(~0u, __float_as_uint(top_v));
+      const bool odd = max(most_m, most_v) >= 0x7f800000u;             // a number that is not finite, somewhere in the unit
+      if (odd) {
+        most_m = most_v = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int o = e / 4 * 128 + lane * 4 + e % 4;
-          if (o >= here) continue;
-          t.p[base + o] = p[e];
-          if (EIGHT) {
-            static_cast<unsigned char*>(t.m)[base + o] = (unsigned char)mc[e];
-            static_cast<unsigned char*>(t.v)[base + o] = (unsigned char)vc[e];
-          } else {
-            static_cast<float*>(t.m)[base + o] = m[e];
-            static_cast<float*>(t.v)[base + o] = v[e];
-          }
-          if (t.copy) static_cast<unsigned short*>(t.copy)[base + o] = (unsigned short)narrow2(t.copy_type, p[e], 0.f);
+          most_m = max(most_m, finite_magnitude(m[e]));
+          most_v = max(most_v, finite_magnitude(root[e]));
         }
+        most_m = __reduce_max_sync(~0u, most_m);
+        most_v = __reduce_max_sync(~0u, most_v);
+      }
+      ms = scale_8(most_m);
+      vs = scale_8(most_v);
+      const float im = __fdiv_rn(1.f, ms), iv = __fdiv_rn(1.f, vs);
+      unsigned key = mix(a.seed + kGolden) ^ step_bits;
+      key = mix(key + kGolden) ^ (unsigned)a.tensors[now].position;
+      key = mix(key + kGolden) ^ (unsigned)own;
+      key = mix(key + kGolden) + (unsigned)(lane * 4) * kGolden;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        unsigned cm[4], cv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = h * 4 + i;
+          const unsigned bits = mix(key + (unsigned)(h * 128 + i) * kGolden);
+          cm[i] = code_of(__fmul_rn(m[e], im), __byte_perm(bits, 0, 0x4104));
+          // a root above zero (none is below 2^-75) stays above zero
+          cv[i] = max(code_of(__fmul_rn(root[e], iv), __byte_perm(bits, 0, 0x4324)), min(__float_as_uint(root[e]), 1u << 24));
+          if (odd) {
+            if (finite_magnitude(m[e]) == 0 && m[e] != 0.f) cm[i] = 0x7f000000u;
+            if (finite_magnitude(root[e]) == 0 && root[e] != 0.f) cv[i] = 0x7f000000u;
+          }
+        }
+        const auto pack = [](const unsigned* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
+        unsigned sign[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sign[i] = __float_as_uint(m[h * 4 + i]);
+        mc[h] = (pack(cm) & 0x7f7f7f7fu) | (pack(sign) & 0x80808080u);
+        vc[h] = pack(cv);
+      }
+    }
+    const Tensor& d = a.tensors[now];
+    if (EIGHT && lane == 0) {
+      d.m_scale[own] = ms;
+      d.v_scale[own] = vs;
+    }
+    if (wide) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const long long i = base + h * 128 + lane * 4;
+        const float *pp = p + 4 * h, *pm = m + 4 * h, *pv = v + 4 * h;
+        *reinterpret_cast<float4*>(d.p + i) = make_float4(pp[0], pp[1], pp[2], pp[3]);
+        if (EIGHT) {
+          *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(d.m) + i) = mc[h];
+          *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(d.v) + i) = vc[h];
+        } else {
+          *reinterpret_cast<float4*>(static_cast<float*>(d.m) + i) = make_float4(pm[0], pm[1], pm[2], pm[3]);
+          *reinterpret_cast<float4*>(static_cast<float*>(d.v) + i) = make_float4(pv[0], pv[1], pv[2], pv[3]);
+        }
+        if (d.copy)
+          *reinterpret_cast<uint2*>(static_cast<unsigned short*>(d.copy) + i) =
+              make_uint2(narrow2(d.copy_type, pp[0], pp[1]), narrow2(d.copy_type, pp[2], pp[3]));
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int o = e / 4 * 128 + lane * 4 + e % 4;
+        if (o >= here) continue;
+        d.p[base + o] = p[e];
+        if (EIGHT) {
+          static_cast<unsigned char*>(d.m)[base + o] = (unsigned char)(mc[e / 4] >> e % 4 * 8);
+          static_cast<unsigned char*>(d.v)[base + o] = (unsigned char)(vc[e / 4] >> e % 4 * 8);
+        } else {
+          static_cast<float*>(d.m)[base + o] = m[e];
+          static_cast<float*>(d.v)[base + o] = v[e];
+        }
+        if (d.copy) static_cast<unsigned short*>(d.copy)[base + o] = (unsigned short)narrow2(d.copy_type, p[e], 0.f);
       }
     }
   }
 }
 
-cocodc_status check(const cocodc_lm_tensor* tensors, int64_t count, int32_t bits, std::vector<Tensor>& out, std::vector<Tile>& tiles) {
+cocodc_status check(const cocodc_lm_tensor* tensors, int64_t count, int32_t bits, std::vector<Tensor>& out, long long* total) {
   struct Array { Span s; bool written; };
   std::vector<Array> arrays;
   const int state = bits == 8 ? 1 : 4;
@@ -310,8 +390,8 @@ cocodc_status check(const cocodc_lm_tensor* tensors, int64_t count, int32_t bits
     arrays.push_back({span(t.grad, 1, t.n, t.n, gb), false});
     const bool wide = on_boundary(t.p, 16) && on_boundary(t.grad, gb == 4 ? 16 : 8) && on_boundary(t.m, 4 * state) && on_boundary(t.v, 4 * state) &&
                       on_boundary(t.copy, 8);
-    out.push_back({t.p, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, t.grad_type, t.copy_type, t.decay, wide ? 1 : 0});
-    for (int64_t u = 0; u < units; u += kTileUnits) tiles.push_back({(int)i, (int)u});
+    if (units) out.push_back({t.p, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, t.grad_type, t.copy_type, t.decay, (int)i, wide ? 1 : 0, *total});
+    *total += units;
   }
   // in order of their first bytes, an array that is written begins behind all before it, a gradient behind all written ones before it
   std::sort(arrays.begin(), arrays.end(), [](const Array& x, const Array& y) { return x.s.lo < y.s.lo; });
@@ -335,24 +415,22 @@ cocodc_status cocodc_lm_adam_create(cocodc_lm_adam** out, cocodc_lm* lm, const c
   if (!lm || count < 0 || count > (1 << 20) || (count && !tensors) || (state_bits != 32 && state_bits != 8)) return COCODC_ERR_INVALID_ARG;
   try {
     std::vector<Tensor> t;
-    std::vector<Tile> tiles;
-    const cocodc_status status = check(tensors, count, state_bits, t, tiles);
+    long long units = 0;
+    const cocodc_status status = check(tensors, count, state_bits, t, &units);
     if (status != COCODC_OK) return status;
     DeviceScope scope(lm->device);
     if (!scope.ok) return COCODC_ERR_CUDA;
     cocodc_lm_adam* plan = new cocodc_lm_adam();
     plan->device = lm->device;
     plan->bits = state_bits;
-    plan->tiles = (long long)tiles.size();
-    if (plan->tiles) {
+    plan->units = units;
+    plan->count = (int)t.size();
+    if (units) {
       const bool ok = cudaMalloc(&plan->d_tensors, t.size() * sizeof(Tensor)) == cudaSuccess &&
-                      cudaMalloc(&plan->d_tiles, tiles.size() * sizeof(Tile)) == cudaSuccess &&
-                      cudaMemcpy(plan->d_tensors, t.data(), t.size() * sizeof(Tensor), cudaMemcpyHostToDevice) == cudaSuccess &&
-                      cudaMemcpy(plan->d_tiles, tiles.data(), tiles.size() * sizeof(Tile), cudaMemcpyHostToDevice) == cudaSuccess;
+                      cudaMemcpy(plan->d_tensors, t.data(), t.size() * sizeof(Tensor), cudaMemcpyHostToDevice) == cudaSuccess;
       if (!ok) {
         cudaGetLastError();
         cudaFree(plan->d_tensors);
-        cudaFree(plan->d_tiles);
         delete plan;
         return COCODC_ERR_CUDA;
       }
@@ -367,8 +445,7 @@ cocodc_status cocodc_lm_adam_create(cocodc_lm_adam** out, cocodc_lm* lm, const c
 cocodc_status cocodc_lm_adam_destroy(cocodc_lm_adam* plan) {
   if (!plan) return COCODC_OK;
   DeviceScope scope(plan->device);
-  bool ok = scope.ok && cudaFree(plan->d_tensors) == cudaSuccess;
-  ok = scope.ok && cudaFree(plan->d_tiles) == cudaSuccess && ok;
+  const bool ok = scope.ok && cudaFree(plan->d_tensors) == cudaSuccess;
   delete plan;
   return ok ? COCODC_OK : COCODC_ERR_CUDA;
 }
@@ -379,13 +456,13 @@ cocodc_status cocodc_lm_adamw(cocodc_lm* lm, const cocodc_lm_adam* plan, double 
       !(eps >= 0 && eps <= 1) || (!step_at && step < 1))
     return COCODC_ERR_INVALID_ARG;
   if (!on_boundary(step_at, 8) || !on_boundary(grad_scale, 4) || !on_boundary(lr_scale, 4)) return COCODC_ERR_ALIGNMENT;
-  if (plan->tiles == 0) return COCODC_OK;
+  if (plan->units == 0) return COCODC_OK;
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
-  const AdamArgs a{plan->d_tensors, plan->d_tiles, plan->tiles, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
+  const AdamArgs a{plan->d_tensors, plan->count, plan->units, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
                    lr, beta1, beta2, step, reinterpret_cast<const long long*>(step_at), grad_scale, lr_scale, (unsigned)seed, lm->d_status};
-  const long long most = (long long)lm->sm_count * 4;
-  const unsigned grid = (unsigned)(plan->tiles < most ? plan->tiles : most);
+  const long long blocks = (plan->units + kWarps - 1) / kWarps, most = (long long)lm->sm_count * (plan->bits == 8 ? 3 : 2);
+  const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return plan->bits == 8 ? start(lm, k_adamw<true>, grid, kThreads, 0, st, 1, a) : start(lm, k_adamw<false>, grid, kThreads, 0, st, 1, a);
 }
