@@ -11,7 +11,7 @@ using namespace cocodc_lm_impl;
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kUnit = COCODC_LM_ADAM_BLOCK;          // elements that a warp takes at a time and that share a scale: 8 for each lane
 constexpr float kMost8 = 448.f, kLeastScale = 1e-30f;
 __device__ __forceinline__ float scale_8(unsigned most) { return fmaxf(__fmul_rn(__uint_as_float(most), 1.f / kMost8), kLeastScale); }
@@ -62,12 +62,35 @@ __device__ __forceinline__ unsigned mix(unsigned x) {
 }
 constexpr unsigned kGolden = 0x9E3779B9u;
 
-// A number x of a unit's largest magnitude 448 to an e4m3 code in the highest byte, without its sign: up with probability (what is cut off) /
-// (spacing).  Times 2^-120 the exponents of e4m3 are those of fp32, numbers below its smallest normal one too (2^-126 here and there), so that the
-// code is what stands above the lowest 20 bits; 16 random bits, here bytes 1 and 2, are added to those.  x may be 448 + 3 ulp: no carry comes of it.
-__device__ __forceinline__ unsigned code_of(float x, unsigned random) {
-  return (__float_as_uint(__fmul_rn(x, 0x1p-120f)) << 4) + random;
+// ---- pairs of fp32 numbers: one instruction for two, each rounded on its own --------------------------
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
+  f32x2 v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
 }
+__device__ __forceinline__ float2 halves(f32x2 v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 v;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ f32x2 both(float x) { return pair_of(x, x); }
+// one by one: the two instructions of a packed product and sum come out of the assembler as one, which rounds once
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  const float2 x = halves(a), y = halves(b);
+  return pair_of(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
+}
+
+// A number times 2^-120 (a unit's largest magnitude was brought to 448 before) to an e4m3 code in the highest byte, without its sign: up with
+// probability (what is cut off) / (spacing).  There the exponents of e4m3 are those of fp32, below its smallest normal number too (2^-126
+// here and there), so that the code is what stands above the lowest 20 bits; 16 random bits, here bytes 1 and 2, are added to
+// those.  The number may be 448 + 3 ulp: no carry comes of it.
+__device__ __forceinline__ unsigned code_of(float x, unsigned random) { return (__float_as_uint(x) << 4) + random; }
 __device__ __forceinline__ float2 widen_e4m3(unsigned short v) {
   unsigned h;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(v));
@@ -78,13 +101,13 @@ __device__ __forceinline__ float load_grad(const void* p, int type, long long i)
          : type == COCODC_BF16 ? to_f32(static_cast<const __nv_bfloat16*>(p)[i])
                                : to_f32(static_cast<const __half*>(p)[i]);
 }
-__device__ __forceinline__ unsigned narrow2(int type, float a, float b) {
+__device__ __forceinline__ unsigned narrow2(int type, float2 v) {
   if (type == COCODC_BF16) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const unsigned*>(&v);
+    const __nv_bfloat162 h = __float22bfloat162_rn(v);
+    return *reinterpret_cast<const unsigned*>(&h);
   }
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const unsigned*>(&v);
+  const __half2 h = __float22half2_rn(v);
+  return *reinterpret_cast<const unsigned*>(&h);
 }
 __device__ __forceinline__ uint2 load8(const void* p) {
   uint2 v;
@@ -112,81 +135,161 @@ __device__ __forceinline__ unsigned finite_magnitude(float x) {
   return b < 0x7f800000u ? b : 0u;
 }
 
-// A unit's numbers on their way: lane l has its elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3, so that neighbours read neighbours in
-// every width.
+// A lane's eight elements of a unit: 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3, so that neighbours read neighbours in every width.
+struct Eight { f32x2 p[4], m[4], v[4], g[4]; };
+__device__ __forceinline__ int place(int e, int lane) { return e / 4 * 128 + lane * 4 + e % 4; }
+
+// A unit's numbers on their way.
 template <bool EIGHT> struct RawUnit {
   uint4 p[2], g[2];
   uint4 m[EIGHT ? 1 : 2], v[EIGHT ? 1 : 2];          // EIGHT: codes in x and y
   float ms, vs;
 };
-template <bool EIGHT> __device__ __forceinline__ void fetch(RawUnit<EIGHT>& r, const Tensor& t, long long unit, int lane) {
-  const long long base = unit * kUnit + lane * 4;
+// A lane's addresses in a unit of the tensor (first: the unit's first element + 4 l).
+struct At {
+  float* p;
+  const char* g;
+  char *m, *v, *c;
+  float *ms, *vs;
+};
+constexpr int kAhead = kWarps * kUnit;               // elements from a warp's unit to its next
+template <bool EIGHT, int AHEAD> __device__ __forceinline__ void fetch(RawUnit<EIGHT>& r, const At& a, int grad_type) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const long long i = base + h * 128;
-    r.p[h] = load16(t.p + i);
-    if (t.grad_type == COCODC_F32) {
-      r.g[h] = load16(static_cast<const float*>(t.grad) + i);
+    const int i = AHEAD + h * 128;
+    r.p[h] = load16(a.p + i);
+    if (grad_type == COCODC_F32) {
+      r.g[h] = load16(a.g + i * 4);
     } else {
-      const uint2 q = load8(static_cast<const unsigned short*>(t.grad) + i);
+      const uint2 q = load8(a.g + i * 2);
       r.g[h].x = q.x;
       r.g[h].y = q.y;
     }
     if (EIGHT) {
-      (h ? r.m[0].y : r.m[0].x) = load4(static_cast<const unsigned char*>(t.m) + i);
-      (h ? r.v[0].y : r.v[0].x) = load4(static_cast<const unsigned char*>(t.v) + i);
+      (h ? r.m[0].y : r.m[0].x) = load4(a.m + i);
+      (h ? r.v[0].y : r.v[0].x) = load4(a.v + i);
     } else {
-      r.m[h] = load16(static_cast<const float*>(t.m) + i);
-      r.v[h] = load16(static_cast<const float*>(t.v) + i);
+      r.m[h] = load16(a.m + i * 4);
+      r.v[h] = load16(a.v + i * 4);
     }
   }
   if (EIGHT) {
-    r.ms = t.m_scale[unit];
-    r.vs = t.v_scale[unit];
+    r.ms = a.ms[AHEAD / kUnit];
+    r.vs = a.vs[AHEAD / kUnit];
   }
 }
-__device__ __forceinline__ void spread4(const uint4& r, float* v) {
-  v[0] = __uint_as_float(r.x);
-  v[1] = __uint_as_float(r.y);
-  v[2] = __uint_as_float(r.z);
-  v[3] = __uint_as_float(r.w);
+__device__ __forceinline__ void spread4(const uint4& r, f32x2* v) {
+  v[0] = pair_of(__uint_as_float(r.x), __uint_as_float(r.y));
+  v[1] = pair_of(__uint_as_float(r.z), __uint_as_float(r.w));
 }
-template <bool EIGHT>
-__device__ __forceinline__ void spread(const RawUnit<EIGHT>& r, int grad_type, float (&p)[8], float (&g)[8], float (&m)[8], float (&v)[8]) {
+template <bool EIGHT> __device__ __forceinline__ void spread(const RawUnit<EIGHT>& r, int grad_type, Eight& x) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    spread4(r.p[h], p + 4 * h);
-    float* pg = g + 4 * h;
+    spread4(r.p[h], x.p + 2 * h);
     if (grad_type == COCODC_F32) {
-      spread4(r.g[h], pg);
-    } else if (grad_type == COCODC_BF16) {
-      pg[0] = __uint_as_float(r.g[h].x << 16);
-      pg[1] = __uint_as_float(r.g[h].x & 0xffff0000u);
-      pg[2] = __uint_as_float(r.g[h].y << 16);
-      pg[3] = __uint_as_float(r.g[h].y & 0xffff0000u);
+      spread4(r.g[h], x.g + 2 * h);
     } else {
-      const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&r.g[h].x)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&r.g[h].y));
-      pg[0] = f0.x;
-      pg[1] = f0.y;
-      pg[2] = f1.x;
-      pg[3] = f1.y;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const unsigned w = i ? r.g[h].y : r.g[h].x;
+        if (grad_type == COCODC_BF16) {
+          x.g[2 * h + i] = pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        } else {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+          x.g[2 * h + i] = pair_of(f.x, f.y);
+        }
+      }
     }
     if (EIGHT) {
       const unsigned cm = h ? r.m[0].y : r.m[0].x, cv = h ? r.v[0].y : r.v[0].x;
-      const float2 m0 = widen_e4m3((unsigned short)cm), m1 = widen_e4m3((unsigned short)(cm >> 16));
-      const float2 v0 = widen_e4m3((unsigned short)cv), v1 = widen_e4m3((unsigned short)(cv >> 16));
-      m[4 * h] = m0.x; m[4 * h + 1] = m0.y; m[4 * h + 2] = m1.x; m[4 * h + 3] = m1.y;
-      v[4 * h] = v0.x; v[4 * h + 1] = v0.y; v[4 * h + 2] = v1.x; v[4 * h + 3] = v1.y;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 fm = widen_e4m3((unsigned short)(cm >> 16 * i)), fv = widen_e4m3((unsigned short)(cv >> 16 * i));
+        x.m[2 * h + i] = pair_of(fm.x, fm.y);
+        x.v[2 * h + i] = pair_of(fv.x, fv.y);
+      }
     } else {
-      spread4(r.m[h], m + 4 * h);
-      spread4(r.v[h], v + 4 * h);
+      spread4(r.m[h], x.m + 2 * h);
+      spread4(r.v[h], x.v + 2 * h);
     }
   }
 }
 
-// Read once, written once: bound by memory.  The units of all tensors form one row, of which each block takes an equal part and its warps one unit
-// in turn: a warp walks from tensor to tensor, and the next unit's numbers are on their way while it works on one.
-template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 2) k_adamw(const AdamArgs a) {
+// The step of a lane's eight elements.  EIGHT: m and v come as codes, which ms and vs scale, and leave as codes of four elements each with new scales.
+struct Factors { f32x2 gs, b1, c1, b2, c2, k1, k2, eps, keep; };
+template <bool EIGHT>
+__device__ __forceinline__ void step_of(Eight& x, const Factors& f, float& ms, float& vs, unsigned key, unsigned (&mc)[2], unsigned (&vc)[2]) {
+  f32x2 root[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (EIGHT) {
+      x.m[i] = mul2(x.m[i], both(ms));
+      x.v[i] = mul2(x.v[i], both(vs));
+      x.v[i] = mul2(x.v[i], x.v[i]);
+    }
+    const f32x2 g = mul2(x.g[i], f.gs);
+    x.m[i] = add2(mul2(x.m[i], f.b1), mul2(g, f.c1));
+    x.v[i] = add2(mul2(x.v[i], f.b2), mul2(mul2(g, f.c2), g));
+    const float2 v = halves(x.v[i]);
+    root[i] = pair_of(__fsqrt_rn(v.x), __fsqrt_rn(v.y));
+    const float2 d = halves(add2(mul2(root[i], f.k2), f.eps));
+    x.p[i] = add2(mul2(x.p[i], f.keep), mul2(mul2(x.m[i], f.k1), pair_of(inverse(d.x), inverse(d.y))));        // k1 is negative
+  }
+  if constexpr (!EIGHT) return;
+  float top_m = 0.f, top_v = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 m = halves(x.m[i]), r = halves(root[i]);
+    top_m = larger(larger(top_m, m.x), m.y);
+    top_v = larger(larger(top_v, r.x), r.y);
+  }
+  unsigned most_m = __reduce_max_sync(~0u, __float_as_uint(top_m)), most_v = __reduce_max_sync(~0u, __float_as_uint(top_v));
+  const bool odd = max(most_m, most_v) >= 0x7f800000u;               // a number that is not finite, somewhere in the unit
+  if (odd) {
+    most_m = most_v = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 m = halves(x.m[i]), r = halves(root[i]);
+      most_m = max(most_m, max(finite_magnitude(m.x), finite_magnitude(m.y)));
+      most_v = max(most_v, max(finite_magnitude(r.x), finite_magnitude(r.y)));
+    }
+    most_m = __reduce_max_sync(~0u, most_m);
+    most_v = __reduce_max_sync(~0u, most_v);
+  }
+  ms = scale_8(most_m);
+  vs = scale_8(most_v);
+  const f32x2 im = both(__frcp_rn(ms)), iv = both(__frcp_rn(vs)), low = both(0x1p-120f);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    unsigned cm[4], cv[4], sign[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 m = halves(x.m[2 * h + i]), r = halves(root[2 * h + i]);
+      const float2 y = halves(mul2(mul2(x.m[2 * h + i], im), low)), z = halves(mul2(mul2(root[2 * h + i], iv), low));
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int n = 2 * i + j;
+        const unsigned bits = mix(key + (unsigned)(h * 128 + n) * kGolden);
+        cm[n] = code_of(j ? y.y : y.x, __byte_perm(bits, 0, 0x4104));
+        // a root above zero (none is below 2^-75) stays above zero
+        cv[n] = max(code_of(j ? z.y : z.x, __byte_perm(bits, 0, 0x4324)), min(__float_as_uint(j ? r.y : r.x), 1u << 24));
+        sign[n] = __float_as_uint(j ? m.y : m.x);
+        if (odd) {
+          if (finite_magnitude(j ? m.y : m.x) == 0 && (j ? m.y : m.x) != 0.f) cm[n] = 0x7f000000u;
+          if (finite_magnitude(j ? r.y : r.x) == 0 && (j ? r.y : r.x) != 0.f) cv[n] = 0x7f000000u;
+        }
+      }
+    }
+    const auto pack = [](const unsigned* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
+    mc[h] = (pack(cm) & 0x7f7f7f7fu) | (pack(sign) & 0x80808080u);
+    vc[h] = pack(cv);
+  }
+}
+
+// Read once, written once: bound by memory, with states in 8 bits nearly as much by instructions (some 65 an element).  The units of all tensors
+// form one row, of which each block takes an equal part and its warps one unit in turn: a warp walks from tensor to tensor, and the next unit's
+// numbers are on their way while it works on one.
+template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 4 : 3) k_adamw(const AdamArgs a) {
   wait_for_previous();
   may_follow();
   __shared__ float factors[2];
@@ -208,37 +311,85 @@ template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 2)
   const long long last = a.units * (blockIdx.x + 1) / gridDim.x;
   long long unit = a.units * blockIdx.x / gridDim.x + warp;
   // the tensor of the warp's first unit: the last one that begins at or before it
-  int at = 0;
+  int number = 0;
   for (int n = a.count; n > 1;) {
     const int half = n / 2;
-    if (a.tensors[at + half].first <= unit) at += half;
+    if (a.tensors[number + half].first <= unit) number += half;
     n -= half;
   }
-  long long behind = a.tensors[at].first + (a.tensors[at].n + kUnit - 1) / kUnit;      // the unit behind the tensor's last
-  const auto whole = [&](const Tensor& t, long long u) { return t.wide && (u - t.first + 1) * kUnit <= t.n; };
-  RawUnit<EIGHT> raw;
-  if (unit < last && whole(a.tensors[at], unit)) fetch(raw, a.tensors[at], unit - a.tensors[at].first, lane);
   __syncthreads();
-  const float k1 = factors[0], k2 = factors[1];
-  while (unit < last) {
-    const Tensor& t = a.tensors[at];
-    const long long own = unit - t.first, base = own * kUnit;
-    const bool wide = whole(t, unit);
-    const float keep = (float)(1.0 - shared_lr * (double)t.decay);
-    float p[8], g[8], m[8], v[8], ms = 0.f, vs = 0.f;
-    const int here = (int)min((long long)kUnit, t.n - base);
-    if (wide) {
-      spread(raw, t.grad_type, p, g, m, v);
-      ms = raw.ms;
-      vs = raw.vs;
-    } else {
-      if (EIGHT) {
-        ms = t.m_scale[own];
-        vs = t.v_scale[own];
+  Factors f;
+  f.gs = both(gs);
+  f.b1 = both(a.b1);
+  f.c1 = both(a.c1);
+  f.b2 = both(a.b2);
+  f.c2 = both(a.c2);
+  f.k1 = both(-factors[0]);
+  f.k2 = both(factors[1]);
+  f.eps = both(a.eps);
+  for (; unit < last; ++number) {
+    const Tensor t = a.tensors[number];
+    const long long units = (t.n + kUnit - 1) / kUnit, end = min(last, t.first + units) - t.first;
+    const long long wide_end = t.wide ? min(end, t.n / kUnit) : 0;     // units before this one are whole and aligned
+    long long own = unit - t.first;
+    if (own >= end) continue;
+    f.keep = both((float)(1.0 - shared_lr * (double)t.decay));
+    unsigned seed = mix(a.seed + kGolden) ^ step_bits;
+    seed = mix((mix(seed + kGolden) ^ (unsigned)t.position) + kGolden);
+    const auto key_of = [&](long long u) { return mix((seed ^ (unsigned)u) + kGolden) + (unsigned)(lane * 4) * kGolden; };
+    RawUnit<EIGHT> raw;
+    Eight x;
+    unsigned mc[2], vc[2];
+    float ms = 0.f, vs = 0.f;
+    if (own < wide_end) {
+      const long long i = own * kUnit + lane * 4;
+      const int gb = t.grad_type == COCODC_F32 ? 4 : 2, sb = EIGHT ? 1 : 4;
+      At at{t.p + i, static_cast<const char*>(t.grad) + i * gb, static_cast<char*>(t.m) + i * sb, static_cast<char*>(t.v) + i * sb,
+            t.copy ? static_cast<char*>(t.copy) + i * 2 : nullptr, EIGHT ? t.m_scale + own : nullptr, EIGHT ? t.v_scale + own : nullptr};
+      fetch<EIGHT, 0>(raw, at, t.grad_type);
+      for (; own < wide_end; own += kWarps) {
+        spread(raw, t.grad_type, x);
+        ms = raw.ms;
+        vs = raw.vs;
+        if (own + kWarps < wide_end) fetch<EIGHT, kAhead>(raw, at, t.grad_type);
+        step_of<EIGHT>(x, f, ms, vs, key_of(own), mc, vc);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float2 p0 = halves(x.p[2 * h]), p1 = halves(x.p[2 * h + 1]);
+          *reinterpret_cast<float4*>(at.p + h * 128) = make_float4(p0.x, p0.y, p1.x, p1.y);
+          if (EIGHT) {
+            *reinterpret_cast<unsigned*>(at.m + h * 128) = mc[h];
+            *reinterpret_cast<unsigned*>(at.v + h * 128) = vc[h];
+          } else {
+            const float2 m0 = halves(x.m[2 * h]), m1 = halves(x.m[2 * h + 1]), v0 = halves(x.v[2 * h]), v1 = halves(x.v[2 * h + 1]);
+            *reinterpret_cast<float4*>(at.m + h * 512) = make_float4(m0.x, m0.y, m1.x, m1.y);
+            *reinterpret_cast<float4*>(at.v + h * 512) = make_float4(v0.x, v0.y, v1.x, v1.y);
+          }
+          if (at.c) *reinterpret_cast<uint2*>(at.c + h * 256) = make_uint2(narrow2(t.copy_type, p0), narrow2(t.copy_type, p1));
+        }
+        if (EIGHT && lane == 0) {
+          *at.ms = ms;
+          *at.vs = vs;
+        }
+        at.p += kAhead;
+        at.g += kAhead * gb;
+        at.m += kAhead * sb;
+        at.v += kAhead * sb;
+        if (at.c) at.c += kAhead * 2;
+        if (EIGHT) {
+          at.ms += kWarps;
+          at.vs += kWarps;
+        }
       }
+    }
+    // a last unit that is not whole, or a tensor that is not aligned: element by element
+    for (; own < end; own += kWarps) {
+      const long long base = own * kUnit;
+      const int here = (int)min((long long)kUnit, t.n - base);
+      float p[8], g[8], m[8], v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int o = e / 4 * 128 + lane * 4 + e % 4;
+        const int o = place(e, lane);
         p[e] = g[e] = m[e] = v[e] = 0.f;
         if (o >= here) continue;
         p[e] = t.p[base + o];
@@ -251,117 +402,40 @@ template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 2)
           v[e] = static_cast<const float*>(t.v)[base + o];
         }
       }
-    }
-    // the next unit's
-    const int now = at;
-    unit += kWarps;
-    while (unit < last && unit >= behind) {
-      ++at;
-      behind = a.tensors[at].first + (a.tensors[at].n + kUnit - 1) / kUnit;
-    }
-    if (unit < last && whole(a.tensors[at], unit)) fetch(raw, a.tensors[at], unit - a.tensors[at].first, lane);
-    float root[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
       if (EIGHT) {
-        m[e] = __fmul_rn(m[e], ms);
-        v[e] = __fmul_rn(v[e], vs);
-        v[e] = __fmul_rn(v[e], v[e]);
+        ms = t.m_scale[own];
+        vs = t.v_scale[own];
       }
-      const float gr = __fmul_rn(g[e], gs);
-      m[e] = __fadd_rn(__fmul_rn(m[e], a.b1), __fmul_rn(gr, a.c1));
-      v[e] = __fadd_rn(__fmul_rn(v[e], a.b2), __fmul_rn(__fmul_rn(gr, a.c2), gr));
-      root[e] = __fsqrt_rn(v[e]);
-      p[e] = __fadd_rn(__fmul_rn(p[e], keep), -__fmul_rn(__fmul_rn(m[e], k1), inverse(__fadd_rn(__fmul_rn(root[e], k2), a.eps))));
-    }
-    unsigned mc[2], vc[2];                             // codes of four elements each
-    if (EIGHT) {
-      float top_m = 0.f, top_v = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x.p[i] = pair_of(p[2 * i], p[2 * i + 1]);
+        x.g[i] = pair_of(g[2 * i], g[2 * i + 1]);
+        x.m[i] = pair_of(m[2 * i], m[2 * i + 1]);
+        x.v[i] = pair_of(v[2 * i], v[2 * i + 1]);
+      }
+      step_of<EIGHT>(x, f, ms, vs, key_of(own), mc, vc);
+      if (EIGHT && lane == 0) {
+        t.m_scale[own] = ms;
+        t.v_scale[own] = vs;
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        top_m = larger(top_m, m[e]);
-        top_v = larger(top_v, root[e]);
-      }
-      unsigned most_m = __reduce_max_sync(~0u, __float_as_uint(top_m)), most_v = __reduce_max_sync(~0u, __float_as_uint(top_v));
-      const bool odd = max(most_m, most_v) >= 0x7f800000u;             // a number that is not finite, somewhere in the unit
-      if (odd) {
-        most_m = most_v = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          most_m = max(most_m, finite_magnitude(m[e]));
-          most_v = max(most_v, finite_magnitude(root[e]));
-        }
-        most_m = __reduce_max_sync(~0u, most_m);
-        most_v = __reduce_max_sync(~0u, most_v);
-      }
-      ms = scale_8(most_m);
-      vs = scale_8(most_v);
-      const float im = __fdiv_rn(1.f, ms), iv = __fdiv_rn(1.f, vs);
-      unsigned key = mix(a.seed + kGolden) ^ step_bits;
-      key = mix(key + kGolden) ^ (unsigned)a.tensors[now].position;
-      key = mix(key + kGolden) ^ (unsigned)own;
-      key = mix(key + kGolden) + (unsigned)(lane * 4) * kGolden;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        unsigned cm[4], cv[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = h * 4 + i;
-          const unsigned bits = mix(key + (unsigned)(h * 128 + i) * kGolden);
-          cm[i] = code_of(__fmul_rn(m[e], im), __byte_perm(bits, 0, 0x4104));
-          // a root above zero (none is below 2^-75) stays above zero
-          cv[i] = max(code_of(__fmul_rn(root[e], iv), __byte_perm(bits, 0, 0x4324)), min(__float_as_uint(root[e]), 1u << 24));
-          if (odd) {
-            if (finite_magnitude(m[e]) == 0 && m[e] != 0.f) cm[i] = 0x7f000000u;
-            if (finite_magnitude(root[e]) == 0 && root[e] != 0.f) cv[i] = 0x7f000000u;
-          }
-        }
-        const auto pack = [](const unsigned* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
-        unsigned sign[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sign[i] = __float_as_uint(m[h * 4 + i]);
-        mc[h] = (pack(cm) & 0x7f7f7f7fu) | (pack(sign) & 0x80808080u);
-        vc[h] = pack(cv);
-      }
-    }
-    const Tensor& d = a.tensors[now];
-    if (EIGHT && lane == 0) {
-      d.m_scale[own] = ms;
-      d.v_scale[own] = vs;
-    }
-    if (wide) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const long long i = base + h * 128 + lane * 4;
-        const float *pp = p + 4 * h, *pm = m + 4 * h, *pv = v + 4 * h;
-        *reinterpret_cast<float4*>(d.p + i) = make_float4(pp[0], pp[1], pp[2], pp[3]);
-        if (EIGHT) {
-          *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(d.m) + i) = mc[h];
-          *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(d.v) + i) = vc[h];
-        } else {
-          *reinterpret_cast<float4*>(static_cast<float*>(d.m) + i) = make_float4(pm[0], pm[1], pm[2], pm[3]);
-          *reinterpret_cast<float4*>(static_cast<float*>(d.v) + i) = make_float4(pv[0], pv[1], pv[2], pv[3]);
-        }
-        if (d.copy)
-          *reinterpret_cast<uint2*>(static_cast<unsigned short*>(d.copy) + i) =
-              make_uint2(narrow2(d.copy_type, pp[0], pp[1]), narrow2(d.copy_type, pp[2], pp[3]));
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int o = e / 4 * 128 + lane * 4 + e % 4;
+        const int o = place(e, lane);
         if (o >= here) continue;
-        d.p[base + o] = p[e];
+        const float2 pp = halves(x.p[e / 2]), pm = halves(x.m[e / 2]), pv = halves(x.v[e / 2]);
+        const float q = e % 2 ? pp.y : pp.x;
+        t.p[base + o] = q;
         if (EIGHT) {
-          static_cast<unsigned char*>(d.m)[base + o] = (unsigned char)(mc[e / 4] >> e % 4 * 8);
-          static_cast<unsigned char*>(d.v)[base + o] = (unsigned char)(vc[e / 4] >> e % 4 * 8);
+          static_cast<unsigned char*>(t.m)[base + o] = (unsigned char)(mc[e / 4] >> e % 4 * 8);
+          static_cast<unsigned char*>(t.v)[base + o] = (unsigned char)(vc[e / 4] >> e % 4 * 8);
         } else {
-          static_cast<float*>(d.m)[base + o] = m[e];
-          static_cast<float*>(d.v)[base + o] = v[e];
+          static_cast<float*>(t.m)[base + o] = e % 2 ? pm.y : pm.x;
+          static_cast<float*>(t.v)[base + o] = e % 2 ? pv.y : pv.x;
         }
-        if (d.copy) static_cast<unsigned short*>(d.copy)[base + o] = (unsigned short)narrow2(d.copy_type, p[e], 0.f);
+        if (t.copy) static_cast<unsigned short*>(t.copy)[base + o] = (unsigned short)narrow2(t.copy_type, make_float2(q, 0.f));
       }
     }
+    unit = t.first + own;
   }
 }
 
@@ -461,7 +535,7 @@ cocodc_status cocodc_lm_adamw(cocodc_lm* lm, const cocodc_lm_adam* plan, double 
   if (!scope.ok) return COCODC_ERR_CUDA;
   const AdamArgs a{plan->d_tensors, plan->count, plan->units, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
                    lr, beta1, beta2, step, reinterpret_cast<const long long*>(step_at), grad_scale, lr_scale, (unsigned)seed, lm->d_status};
-  const long long blocks = (plan->units + kWarps - 1) / kWarps, most = (long long)lm->sm_count * (plan->bits == 8 ? 3 : 2);
+  const long long blocks = (plan->units + kWarps - 1) / kWarps, most = (long long)lm->sm_count * (plan->bits == 8 ? 4 : 3);
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return plan->bits == 8 ? start(lm, k_adamw<true>, grid, kThreads, 0, st, 1, a) : start(lm, k_adamw<false>, grid, kThreads, 0, st, 1, a);
