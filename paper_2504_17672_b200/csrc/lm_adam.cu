@@ -286,6 +286,8 @@ __device__ __forceinline__ void step_of(Eight& x, const Factors& f, float& ms, f
   }
 }
 
+constexpr int kSoon = 3;                             // units of a warp
+
 // Read once, written once: bound by memory, with states in 8 bits nearly as much by instructions (some 65 an element).  The units of all tensors
 // form one row, of which each block takes an equal part and its warps one unit in turn: a warp walks from tensor to tensor, and the next unit's
 // numbers are on their way while it works on one.
@@ -347,7 +349,18 @@ template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 4 : 3)
       At at{t.p + i, static_cast<const char*>(t.grad) + i * gb, static_cast<char*>(t.m) + i * sb, static_cast<char*>(t.v) + i * sb,
             t.copy ? static_cast<char*>(t.copy) + i * 2 : nullptr, EIGHT ? t.m_scale + own : nullptr, EIGHT ? t.v_scale + own : nullptr};
       fetch<EIGHT, 0>(raw, at, t.grad_type);
+      // states in 8 bits: 2 KB a unit and warp are too few on their way, and registers for more there are none.  The lines of later units are brought to
+      // L2 by a lane each: 8 of the parameters, up to 8 of the gradients, 2 of each state.
+      const int line = lane < 8 ? lane : lane < 16 ? lane - 8 : lane < 18 ? lane - 16 : lane - 18;
+      const int width = lane < 8 ? 4 : lane < 16 ? gb : sb;
+      const char* soon = lane < 8 ? reinterpret_cast<const char*>(t.p) : lane < 16 ? static_cast<const char*>(t.grad) : lane < 18 ? static_cast<const char*>(t.m) : static_cast<const char*>(t.v);
+      soon += (own + kSoon * kWarps) * kUnit * width + line * 128;
+      const bool helps = EIGHT && lane < 20 && line * 128 < kUnit * width;
       for (; own < wide_end; own += kWarps) {
+        if (EIGHT) {
+          if (helps && own + kSoon * kWarps < wide_end) asm volatile("prefetch.global.L2 [%0];" ::"l"(soon));
+          soon += kAhead * width;
+        }
         spread(raw, t.grad_type, x);
         ms = raw.ms;
         vs = raw.vs;
