@@ -238,7 +238,7 @@ template <typename E, int MODE> cocodc_status run_tc(cocodc_lm* lm, HeadTc& c, c
   const long long tiles = MODE == HEAD_PRODUCTS ? (long long)c.job[0].tiles + c.job[1].tiles : (long long)c.m_tiles * c.n_tiles;
   if (tiles > INT32_MAX / 2) return COCODC_ERR_INVALID_ARG;
   c.status = lm->d_status;
-  return start(lm, k_head_tc<E, MODE>, (unsigned)(tiles < lm->sm_count ? tiles : lm->sm_count), kTcThreads, kHeadSmem, st, 1, c);
+  return start(lm, k_head_tc<E, MODE>, (unsigned)(tiles < lm->sm_count ? tiles : lm->sm_count), kHeadThreads, kHeadSmem, st, 1, c);
 }
 // A tile of logits: x [T][D] by rows of the table.
 template <typename E>
@@ -274,7 +274,7 @@ extern "C" {
 
 uint64_t cocodc_lm_head_workspace(int64_t T, int64_t D, int64_t V) {
   if (!sizes_ok(T, D, V)) return 0;
-  return 16 + (uint64_t)T * 4 + 16 + (uint64_t)up(V, strip_width(T, V)) * (uint64_t)T * sizeof(float2);
+  return 16 + (uint64_t)T * 4 + 16 + (uint64_t)up(V, strip_width(T, V)) * 2 * (uint64_t)T * sizeof(float2);
 }
 
 cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t x_stride, const void* table, int64_t table_stride,
@@ -305,7 +305,7 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
   a.T = T;
   a.V = V;
   a.width = strip_width(T, V);
-  a.strips = up(V, a.width);
+  a.strips = up(V, a.width);                          // parts of a row's statistics: one for each strip, on the tensor cores two
   a.scale2 = scale * kLog2e;
   a.targets = targets;
   a.targets64 = targets_type == COCODC_I64;
@@ -320,6 +320,7 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
       HeadTc c{};
       c.h = a;
       c.n_tiles = (int)a.strips;
+      a.strips *= 2;
       if (!logit_maps<E>(&c, x, x_stride, table, table_stride, T, D, V, a.width)) return COCODC_ERR_CUDA;
       return run_tc<E, HEAD_STATS>(lm, c, st);
     }
@@ -416,6 +417,7 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
         HeadTc c{};
         c.d = d;
         c.first_row = v0;
+        c.counter = reinterpret_cast<int*>(ws + 64);
         const int width = tile_width(T, w, 64);
         c.n_tiles = (int)up(w, width);
         if (!logit_maps<E>(&c, x, x_stride, table, table_stride, T, D, V, width) || !map_of<E>(&c.c[0], d.dz, d.pitch, T, w, 32)) return COCODC_ERR_CUDA;
@@ -438,6 +440,7 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
               !map_of<E>(&c.c[1], dx, dx_stride, T, D, 32))
             return COCODC_ERR_CUDA;
         }
+        c.first = c.job[1].tiles && (!c.job[0].tiles || (c.job[1].k_blocks + parts - 1) / parts > c.job[0].k_blocks) ? 1 : 0;
         s = run_tc<E, HEAD_PRODUCTS>(lm, c, st);
         if (s != COCODC_OK) return s;
         if (dx && parts > 1 && d.v1 == V)

@@ -3,11 +3,12 @@
 // Persistent, 128 x (up to 256) tiles, k-blocks of 64, the roles of the gated block's kernel:
 //   warp 0   producer: TMA copies of the operands' tiles into a ring of shared-memory stages
 //   warp 1   issuer: tcgen05.mma of each stage into one of two TMEM accumulators of 256 columns
-//   warps 2-5 epilogue, while the other accumulator fills; a thread has a row of the tile
+//   warps 2-9 epilogue, while the other accumulator fills; a thread has a row of the tile, two of them share it
 // STATS     a tile of x W^T is reduced where it lies: each thread finds its row's largest logit and the sum of powers of two among the
 //           tile's columns, and picks the target's logit; 8 bytes a row and tile leave the chip instead of 512.
 // DZ        the same product; the epilogue forms dz from the row's lse and factors and writes it in 16 bits, 64 staged columns at a time.
-// PRODUCTS  dtable = dz^T x and dx = dz W of one piece in one launch: a tile's number tells which of the two it belongs to.  dx's sums over
+// PRODUCTS  dtable = dz^T x and dx = dz W of one piece in one launch: a tile's number tells which of the two it belongs to.  Tiles differ in
+//           length, so that a block takes the next one when it is ready (a counter that DZ set back), the long ones first.  dx's sums over
 //           the pieces of the vocabulary (and over parts of its contraction, where its tiles are few) stay in fp32 in an order of
 //           their own, in which 32 lanes' accesses are 512 consecutive bytes.
 #pragma once
@@ -33,17 +34,21 @@ struct HeadTc {
   HeadArgs h;
   DzArgs d;
   HeadJob job[2];                 // dtable, dx
+  int first;                      // which of them has the longer tiles: its come first
+  int* counter;                   // tiles taken beyond one for each block; DZ sets it to 0
   long long first_row;            // of the piece, in the table
   int* status;
 };
 
-constexpr int kHeadStages = 4;
-constexpr unsigned kHeadStage = kABytes + 256 * kBK * 2, kHeadSmem = 1024 + kHeadStages * kHeadStage + 4 * 2 * kOutBytes;
+constexpr int kHeadStages = 4, kHeadEpilogue = 8, kHeadThreads = 64 + kHeadEpilogue * 32;
+constexpr int kTileRing = 4;      // tiles that the producer may be ahead
+constexpr unsigned kHeadStage = kABytes + 256 * kBK * 2, kHeadSmem = 1024 + kHeadStages * kHeadStage + kHeadEpilogue * kOutBytes;
 // Tiles of consecutive rows that go through one column of tiles in turn (as in the gated block).
 template <int MODE> constexpr int kHeadGroup = MODE == HEAD_PRODUCTS ? 8 : 32;
 
 struct HeadShared {
-  unsigned long long full[kHeadStages], empty[kHeadStages], acc_full[2], acc_empty[2], drain;
+  unsigned long long full[kHeadStages], empty[kHeadStages], acc_full[2], acc_empty[2], tile_full[kTileRing], tile_empty[kTileRing], drain;
+  int tile[kTileRing];
   unsigned tmem;
   int stop;
 };
@@ -54,9 +59,9 @@ template <int MODE> __device__ __forceinline__ HeadTile head_tile(const HeadTc& 
   int m_tiles = a.m_tiles, n_tiles = a.n_tiles;
   t.kb1 = a.k_blocks;
   if (MODE == HEAD_PRODUCTS) {
-    t.kind = tile >= a.job[0].tiles;
+    t.kind = tile < a.job[a.first].tiles ? a.first : 1 - a.first;
     const HeadJob& j = a.job[t.kind];
-    if (t.kind) tile -= a.job[0].tiles;
+    if (t.kind != a.first) tile -= a.job[a.first].tiles;
     m_tiles = j.m_tiles;
     n_tiles = j.n_tiles;
     const int per = m_tiles * n_tiles;
@@ -133,7 +138,7 @@ __device__ __forceinline__ void emit(const Out& o, const CUtensorMap* map, int r
 }
 
 template <typename E, int MODE>
-__global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant__ HeadTc a) {
+__global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_constant__ HeadTc a) {
   extern __shared__ unsigned char dyn[];
   __shared__ HeadShared sh;
   const unsigned base = (smem_addr(dyn) + 1023u) & ~1023u;
@@ -148,7 +153,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(smem_addr(&sh.acc_full[i]), 1);
-      bar_init(smem_addr(&sh.acc_empty[i]), 4);
+      bar_init(smem_addr(&sh.acc_empty[i]), kHeadEpilogue);
+    }
+    for (int i = 0; i < kTileRing; ++i) {
+      bar_init(smem_addr(&sh.tile_full[i]), 1);
+      bar_init(smem_addr(&sh.tile_empty[i]), 1 + kHeadEpilogue);
     }
     bar_init(smem_addr(&sh.drain), 1);
     sh.stop = 0;
@@ -162,13 +171,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant
   may_follow();
   const unsigned tmem = sh.tmem;
   volatile int* stop = &sh.stop;
+  if (MODE == HEAD_DZ && blockIdx.x == 0 && threadIdx.x == 0) *a.counter = 0;
+
+  // The block's n-th tile: -1 behind the last, -2 when a wait gave up.  PRODUCTS: as the producer published it; who has read it gives its place back.
+  const auto nth_tile = [&](int n) -> int {
+    if (MODE != HEAD_PRODUCTS) {
+      const long long tile = blockIdx.x + (long long)n * gridDim.x;
+      return tile < tiles ? (int)tile : -1;
+    }
+    const int slot = n % kTileRing;
+    if (!bar_wait(smem_addr(&sh.tile_full[slot]), (unsigned)(n / kTileRing) & 1, stop)) return -2;
+    return *reinterpret_cast<volatile int*>(&sh.tile[slot]);
+  };
+  const auto tile_read = [&](int n) {
+    if (MODE == HEAD_PRODUCTS) bar_arrive(smem_addr(&sh.tile_empty[n % kTileRing]));
+  };
 
   if (warp == 0) {
     if (lane == 0) {
       long long it = 0;
       bool ok = true;
       const int slabs = a.width / 64;
-      for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+      int next = blockIdx.x;
+      for (int n = 0; ok; ++n) {
+        int tile = next;
+        if (MODE == HEAD_PRODUCTS) {
+          const int slot = n % kTileRing;
+          if (tile >= tiles) tile = -1;
+          else next = gridDim.x + atomicAdd(a.counter, 1);            // comes while this tile is fetched
+          ok = bar_wait(smem_addr(&sh.tile_empty[slot]), ((unsigned)(n / kTileRing) & 1) ^ 1, stop);
+          if (!ok) break;
+          *reinterpret_cast<volatile int*>(&sh.tile[slot]) = tile;
+          bar_arrive(smem_addr(&sh.tile_full[slot]));
+        } else {
+          tile = nth_tile(n);
+        }
+        if (tile < 0) break;
         const HeadTile t = head_tile<MODE>(a, tile);
         const int m0 = t.m * kBM, n0 = t.n * a.width;
         const unsigned bytes = MODE == HEAD_PRODUCTS ? a.job[t.kind].a_bytes + slabs * kSlab : a.a_bytes + a.width * kBK * 2;
@@ -201,9 +239,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant
   } else if (warp == 1) {
     if (lane == 0) {
       long long it = 0;
-      int turn = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++turn) {
+      for (int turn = 0; ok; ++turn) {
+        const int tile = nth_tile(turn);
+        tile_read(turn);
+        if (tile < 0) {
+          ok = tile == -1;
+          break;
+        }
         const HeadTile t = head_tile<MODE>(a, tile);
         const bool a_mn = MODE == HEAD_PRODUCTS && t.kind == 0;
         constexpr bool b_mn = MODE == HEAD_PRODUCTS;
@@ -231,11 +274,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant
       }
     }
   } else {
-    const int quarter = warp & 3, e = warp - 2;
-    const unsigned out = staging + e * 2 * kOutBytes;
-    int turn = 0, sent = 0;
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
+    // a warp reaches the 32 TMEM lanes of its number modulo 4; of two such warps one takes the even, one the odd pieces of the columns
+    const int quarter = warp & 3, part = (warp - 2) / 4;
+    const unsigned buf = staging + (warp - 2) * kOutBytes;
+    for (int turn = 0;; ++turn) {
       const int acc = turn & 1;
+      const int tile = nth_tile(turn);
+      if (!__all_sync(~0u, tile >= 0)) break;          // every lane has read it
+      if (lane == 0) tile_read(turn);
       const HeadTile t = head_tile<MODE>(a, tile);
       const int row0 = t.m * kBM + quarter * 32, n0 = t.n * a.width;
       const unsigned src = tmem + acc * 256 + ((unsigned)(quarter * 32) << 16);
@@ -254,7 +300,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant
         const int cols = (int)min((long long)a.width, a.h.V - n0);
         const int hit = target >= n0 && target < n0 + cols ? (int)(target - n0) : -1;
         float m = -INFINITY, s = 0.f;
-        for (int col = 0; col < cols; col += 32) {
+        for (int col = part * 32; col < cols; col += 64) {
           float v[32];
           tmem_load32(v, src + col);
           tmem_wait_loads();
@@ -280,7 +326,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant
             if (at >= 0 && at < 32 && row < a.h.T) a.h.picked[row] = picked * a.h.scale2;
           }
         }
-        if (row < a.h.T) a.h.stats[(long long)t.n * a.h.T + row] = make_float2(m * a.h.scale2, s);
+        if (row < a.h.T) a.h.stats[(2ll * t.n + part) * a.h.T + row] = make_float2(m * a.h.scale2, s);
       } else if constexpr (MODE == HEAD_DZ) {
         const int cols = (int)min((long long)a.width, a.d.v1 - a.d.v0 - n0);
         const bool nothing = r.lse2 == INFINITY;
@@ -290,67 +336,65 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_head_tc(const __grid_constant
         o.type = COCODC_BF16;
         o.ld = a.d.pitch;
         if (row0 < a.d.T)
-          for (int p = 0; p < 2 * ((cols + 63) / 64); ++p) {
-            const int col = p * 32, half = p & 1;
-            const unsigned buf = out + (sent & 1) * kOutBytes;
-            if (half == 0) {
-              if (lane == 0) store_wait_read<1>();
-              __syncwarp();
-            }
-            float v[32];
-            tmem_load32(v, src + col);
-            tmem_wait_loads();
+          for (int x0 = part * 64; x0 < cols; x0 += 128) {
+            if (lane == 0) store_wait_read<0>();
+            __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = fast_exp2(fmaf(v[i], a.d.scale2, -r.lse2)) * r.slope;
-            if (__any_sync(~0u, hit >= col && hit < col + 32)) {
+            for (int half = 0; half < 2; ++half) {
+              const int col = x0 + half * 32;
+              float v[32];
+              tmem_load32(v, src + col);
+              tmem_wait_loads();
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                v[i] += i == (int)(hit - col) ? r.hit : 0.f;
-            }
-            if (nothing) {
+              for (int i = 0; i < 32; ++i) v[i] = fast_exp2(fmaf(v[i], a.d.scale2, -r.lse2)) * r.slope;
+              if (__any_sync(~0u, hit >= col && hit < col + 32)) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                for (int i = 0; i < 32; ++i) v[i] += i == (int)(hit - col) ? r.hit : 0.f;
+              }
+              if (nothing) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+              }
+              emit<E>(o, &a.c[0], (int)a.d.T, (int)(a.d.v1 - a.d.v0), n0 + col, row0, half, buf, lane, v);
             }
-            emit<E>(o, &a.c[0], (int)a.d.T, (int)(a.d.v1 - a.d.v0), n0 + col, row0, half, buf, lane, v);
-            sent += half;
           }
       } else {
         const HeadJob& j = a.job[t.kind];
         const Out& o = j.o;
         const float scale = o.factor ? o.factor[1] * o.scale : o.scale;
-        const bool keep = o.sums && !o.last;
+        const bool keep = o.sums && !o.last, whole = o.type == COCODC_F32;   // 32 columns of fp32 are a staged tile of their own
         if (row0 < j.rows)
-          for (int p = 0; p < a.width / 32; ++p) {
-            const int col = p * 32, half = p & 1, x = n0 + col;
-            const bool whole = o.type == COCODC_F32;   // 32 columns are a staged tile of their own
-            if ((whole ? x : x - 32 * half) >= j.cols) break;
-            float v[32];
-            tmem_load32(v, src + col);
-            tmem_wait_loads();
-            float4* sums = sums_at(o, t.number, a.width, col, quarter * 32 + lane);
-            if (o.sums && o.add) {
+          for (int x0 = part * 64; x0 < a.width && n0 + x0 < j.cols; x0 += 128) {
+            for (int half = 0; half < 2; ++half) {
+              const int col = x0 + half * 32, x = n0 + col;
+              if (whole && x >= j.cols) break;
+              float v[32];
+              tmem_load32(v, src + col);
+              tmem_wait_loads();
+              float4* sums = sums_at(o, t.number, a.width, col, quarter * 32 + lane);
+              if (o.sums && o.add) {
 #pragma unroll
-              for (int q = 0; q < 8; ++q) {
-                const float4 u = sums[q * kBM];
-                v[4 * q] += u.x;
-                v[4 * q + 1] += u.y;
-                v[4 * q + 2] += u.z;
-                v[4 * q + 3] += u.w;
+                for (int q = 0; q < 8; ++q) {
+                  const float4 u = sums[q * kBM];
+                  v[4 * q] += u.x;
+                  v[4 * q + 1] += u.y;
+                  v[4 * q + 2] += u.z;
+                  v[4 * q + 3] += u.w;
+                }
               }
-            }
-            if (keep) {
+              if (keep) {
 #pragma unroll
-              for (int q = 0; q < 8; ++q) sums[q * kBM] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-              continue;
-            }
+                for (int q = 0; q < 8; ++q) sums[q * kBM] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                continue;
+              }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= scale;
-            if (whole || half == 0) {
-              if (lane == 0) store_wait_read<1>();
-              __syncwarp();
+              for (int i = 0; i < 32; ++i) v[i] *= scale;
+              if (whole || half == 0) {
+                if (lane == 0) store_wait_read<0>();
+                __syncwarp();
+              }
+              emit<E>(o, &a.c[t.kind], j.rows, j.cols, x, row0, half, buf, lane, v);
             }
-            emit<E>(o, &a.c[t.kind], j.rows, j.cols, x, row0, half, out + (sent & 1) * kOutBytes, lane, v);
-            sent += whole ? 1 : half;
           }
       }
       tc_fence_before();
@@ -375,7 +419,7 @@ template <typename E> __global__ void __launch_bounds__(256) k_head_add(const __
   may_follow();
   const HeadJob& j = a.job[1];
   const int per = j.m_tiles * j.n_tiles, tile = blockIdx.x / (kBM / 8), row = blockIdx.x % (kBM / 8) * 8 + threadIdx.x % 8;
-  const HeadTile t = head_tile<HEAD_PRODUCTS>(a, a.job[0].tiles + tile);
+  const HeadTile t = head_tile<HEAD_PRODUCTS>(a, (a.first == 1 ? 0 : a.job[0].tiles) + tile);
   const int y = t.m * kBM + row;
   if (y >= j.rows) return;
   const float scale = j.o.factor ? j.o.factor[1] * j.o.scale : j.o.scale;
