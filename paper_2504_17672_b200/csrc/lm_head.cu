@@ -197,7 +197,7 @@ constexpr int64_t kPieceBytes = int64_t(1) << 28, kLeastPiece = 1024;
 int64_t piece_width(int64_t T, int64_t V) {
   int64_t w = T > 0 ? kPieceBytes / 2 / T / 256 * 256 : V;
   if (w < kLeastPiece) w = kLeastPiece;
-  if (w >= V) return up(V, 8) * 8;
+  if (w >= V) return up(V, 64) * 64;
   const int64_t pieces = up(V, w);
   return up(up(V, pieces), 256) * 256;
 }
@@ -242,6 +242,15 @@ bool map_f32(CUtensorMap* map, const void* p, int64_t stride, int64_t rows, int6
   const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
   return g_encode.load()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The same memory as slabs of 64 columns, `count` of which (64 rows each) a copy brings at once: an MN-major operand of k-blocks of 64 in one
+// copy instead of two or four.  For rows of whole slabs.
+template <typename E> bool map_slabs(CUtensorMap* map, const void* p, int64_t stride, int64_t rows, int64_t cols, int count) {
+  const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(cols / 64)}, strides[2] = {(cuuint64_t)stride * 2, 128};
+  const cuuint32_t box[3] = {64, (cuuint32_t)kBK, (cuuint32_t)count}, steps[3] = {1, 1, 1};
+  return g_encode.load()(map, IsBf16<E>::v ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims,
+                         strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 int a_rows(int64_t T) { return T >= kBM ? kBM : (int)up(T, 8) * 8; }
 
@@ -435,10 +444,14 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
         if (s != COCODC_OK) return s;
         c.width = dx_width(D);
         const int n_tiles = (int)up(D, c.width);
+        c.slabs = D % 64 == 0 ? c.width / 64 : 1;
+        const auto map_b = [&](CUtensorMap* map, const void* p, int64_t stride, int64_t rows) {
+          return c.slabs > 1 ? map_slabs<E>(map, p, stride, rows, D, c.slabs) : map_of<E>(map, p, stride, rows, D, kBK);
+        };
         if (dtable) {
           HeadJob& j = c.job[0];
           j = HeadJob{(int)up(w, kBM), n_tiles, (int)up(T, kBK), 1, (int)up(w, kBM) * n_tiles, (int)w, (int)D, kABytes, ow};
-          if (!map_of<E>(&c.a[0], d.dz, d.pitch, T, w, kBK) || !map_of<E>(&c.b[0], x, x_stride, T, D, kBK) ||
+          if (!map_slabs<E>(&c.a[0], d.dz, d.pitch, T, up(w, 64) * 64, kBM / 64) || !map_b(&c.b[0], x, x_stride, T) ||
               !(wb == 4 ? map_f32(&c.c[0], ow.out, dtable_stride, w, D) : map_of<E>(&c.c[0], ow.out, dtable_stride, w, D, 32)))
             return COCODC_ERR_CUDA;
         }
@@ -446,7 +459,7 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
           HeadJob& j = c.job[1];
           const int tiles = (int)up(T, kBM) * n_tiles;
           j = HeadJob{(int)up(T, kBM), n_tiles, (int)up(w, kBK), parts, tiles * parts, (int)T, (int)D, c.a_bytes, ox};
-          if (!map_of<E>(&c.a[1], d.dz, d.pitch, T, w, a_rows(T)) || !map_of<E>(&c.b[1], table, table_stride, V, D, kBK) ||
+          if (!map_of<E>(&c.a[1], d.dz, d.pitch, T, w, a_rows(T)) || !map_b(&c.b[1], table, table_stride, V) ||
               !map_of<E>(&c.c[1], dx, dx_stride, T, D, 32))
             return COCODC_ERR_CUDA;
         }

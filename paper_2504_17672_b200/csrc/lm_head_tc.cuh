@@ -31,6 +31,7 @@ struct HeadTc {
   int m_tiles, n_tiles, k_blocks; // STATS, DZ
   int width;                      // columns of a tile
   unsigned a_bytes;
+  int slabs;                      // PRODUCTS: slabs of 64 columns that one copy brings: all of a tile, or one (see map_slabs)
   HeadArgs h;
   DzArgs d;
   HeadJob job[2];                 // dtable, dx
@@ -83,6 +84,12 @@ template <int MODE> __device__ __forceinline__ HeadTile head_tile(const HeadTc& 
 __device__ __forceinline__ void tma_add(const CUtensorMap* map, int x, int y, unsigned src) {
   asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%1, %2}], [%3];"
                ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+
+// Slabs of 64 columns (from number `slab` on) of 64 rows, one behind the other.
+__device__ __forceinline__ void tma_load_slabs(unsigned dst, const CUtensorMap* map, int row, int slab, unsigned bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(slab), "r"(bar) : "memory");
 }
 
 // The sums of a tile: 32 columns (col, col + 1, ...) of a thread's row
@@ -219,12 +226,13 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
           if (MODE != HEAD_PRODUCTS) {
             tma_load(sa, &a.a[0], k0, m0, full);
             tma_load(sb, &a.b[0], k0, (int)a.first_row + n0, full);
-          } else if (t.kind == 0) {
-            for (int i = 0; i < kBM / 64; ++i) tma_load(sa + i * kSlab, &a.a[0], m0 + i * 64, k0, full);
-            for (int i = 0; i < slabs; ++i) tma_load(sb + i * kSlab, &a.b[0], n0 + i * 64, k0, full);
           } else {
-            tma_load(sa, &a.a[1], k0, m0, full);
-            for (int i = 0; i < slabs; ++i) tma_load(sb + i * kSlab, &a.b[1], n0 + i * 64, (int)a.first_row + k0, full);
+            if (t.kind == 0) tma_load_slabs(sa, &a.a[0], k0, m0 / 64, full);
+            else tma_load(sa, &a.a[1], k0, m0, full);
+            const int row = t.kind == 0 ? k0 : (int)a.first_row + k0;
+            if (a.slabs > 1) tma_load_slabs(sb, &a.b[t.kind], row, n0 / 64, full);
+            else
+              for (int i = 0; i < slabs; ++i) tma_load(sb + i * kSlab, &a.b[t.kind], n0 + i * 64, row, full);
           }
         }
       }
