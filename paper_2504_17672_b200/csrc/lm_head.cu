@@ -68,18 +68,33 @@ __global__ void __launch_bounds__(256) k_head_plain(const HeadArgs a, const Oper
   }
 }
 
-// The strips of a row joined: 32 threads a row, read by eight rows at a time (two times 197 strips of 1333 rows took 21 us with eight threads a row).
-constexpr int kJoinRows = 8;
-__global__ void __launch_bounds__(32 * kJoinRows) k_head_join(const HeadArgs a, float* logp, float* lse, int* status) {
+// The strips of a row joined: eight rows a block, 32 threads each, that read by eight rows at a time (two times 197 strips of 1333 rows took 21 us with
+// eight threads a row); few rows: one a block, all its threads, so that one round of loads does.
+__device__ __forceinline__ Stats join_warp(Stats v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float m = __shfl_xor_sync(~0u, v.m, o), s = __shfl_xor_sync(~0u, v.s, o);
+    v = join(v, Stats{m, s});
+  }
+  return v;
+}
+template <int ROWS> __global__ void __launch_bounds__(256) k_head_join(const HeadArgs a, float* logp, float* lse, int* status) {
   wait_for_previous();
   may_follow();
-  constexpr int R = kJoinRows, kParts = 32;
-  __shared__ Stats cell[R][kParts + 1];
-  const long long t = (long long)blockIdx.x * R + threadIdx.x % R;
+  constexpr int kParts = 256 / ROWS;
+  __shared__ Stats cell[8][33];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const long long t = (long long)blockIdx.x * ROWS + threadIdx.x % ROWS, row = (long long)blockIdx.x * ROWS + (ROWS == 1 ? 0 : warp);
+  long long y = -1;
+  float picked = 0.f;
+  if (lane == 0 && row < a.T && (ROWS > 1 || warp == 0)) {            // on its way beside the strips
+    if (logp) y = token_at(a.targets, a.targets64, row, a.V, status);
+    if (y >= 0) picked = a.picked[row];
+  }
   Stats all{-INFINITY, 0.f};
   if (t < a.T) {
-    for (long long i = threadIdx.x / R; i < a.strips; i += 8 * kParts) {
-      float2 v[8];                                    // together on their way
+    for (long long i = threadIdx.x / ROWS; i < a.strips; i += 8 * kParts) {
+      float2 v[8];                                                    // together on their way
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = i + k * kParts < a.strips ? a.stats[(i + k * kParts) * a.T + t] : make_float2(-INFINITY, 0.f);
       float m = all.m;
@@ -92,22 +107,22 @@ __global__ void __launch_bounds__(32 * kJoinRows) k_head_join(const HeadArgs a, 
       all = Stats{m, s};
     }
   }
-  cell[threadIdx.x % R][threadIdx.x / R] = all;
-  __syncthreads();
-  const int lane = threadIdx.x % 32;
-  const long long row = (long long)blockIdx.x * R + threadIdx.x / 32;
-  all = cell[threadIdx.x / 32][lane];
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const float m = __shfl_xor_sync(~0u, all.m, o), s = __shfl_xor_sync(~0u, all.s, o);
-    all = join(all, Stats{m, s});
+  if (ROWS == 1) {
+    all = join_warp(all);
+    if (lane == 0) cell[0][warp] = all;
+    __syncthreads();
+    if (warp) return;
+    all = lane < 8 ? cell[0][lane] : Stats{-INFINITY, 0.f};
+  } else {
+    cell[threadIdx.x % ROWS][threadIdx.x / ROWS] = all;
+    __syncthreads();
+    all = cell[warp][lane];
   }
+  all = join_warp(all);
   if (lane || row >= a.T) return;
   const float log2sum = shift_of(all.m) + log2f(all.s);
   if (lse) lse[row] = log2sum * kLn2;
-  if (!logp) return;
-  const long long y = token_at(a.targets, a.targets64, row, a.V, status);
-  logp[row] = y < 0 ? 0.f : (log2sum == -INFINITY ? -INFINITY : (a.picked[row] - log2sum) * kLn2);
+  if (logp) logp[row] = y < 0 ? 0.f : (log2sum == -INFINITY ? -INFINITY : (picked - log2sum) * kLn2);
 }
 
 // ---- gradient -------------------------------------------------------------------------------------
@@ -348,7 +363,8 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
     return start(lm, k_head_plain<E>, grid, 256, 0, st, 1, a, xo, wo, (long long)D);
   });
   if (status != COCODC_OK) return status;
-  return start(lm, k_head_join, (unsigned)up(T, kJoinRows), 32 * kJoinRows, 0, st, 1, a, logp, lse, lm->d_status);
+  return T <= 2 * kSms ? start(lm, k_head_join<1>, (unsigned)T, 256, 0, st, 1, a, logp, lse, lm->d_status)
+                       : start(lm, k_head_join<8>, (unsigned)up(T, 8), 256, 0, st, 1, a, logp, lse, lm->d_status);
 }
 
 uint64_t cocodc_lm_head_grad_workspace(int64_t T, int64_t D, int64_t V) { return sizes_ok(T, D, V) ? grad_layout(T, D, V).bytes : 0; }
