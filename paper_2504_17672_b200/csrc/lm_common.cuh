@@ -24,6 +24,7 @@ namespace cocodc_lm_impl {
 bool embed_prepare();
 bool glu_prepare();
 bool head_prepare();
+bool norm_prepare();
 
 struct DeviceScope {
   int prev = -1;

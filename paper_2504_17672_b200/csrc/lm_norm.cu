@@ -1,6 +1,6 @@
 // The root-mean-square norm with the residual's addition and its gradient (include/cocodc_lm.h).
 
-#include "lm_common.cuh"
+#include "lm_mma.cuh"
 
 #include <type_traits>
 
@@ -52,14 +52,22 @@ template <typename T> __device__ __forceinline__ unsigned narrow2(float a, float
     return *reinterpret_cast<const unsigned*>(&v);
   }
 }
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+template <typename T> __device__ __forceinline__ Raw8<T> narrow8(const float (&v)[8]) {
+  Raw8<T> r;
   if constexpr (sizeof(T) == 4) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      r.q[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
   } else {
-    *reinterpret_cast<uint4*>(p) = make_uint4(narrow2<T>(v[0], v[1]), narrow2<T>(v[2], v[3]), narrow2<T>(v[4], v[5]), narrow2<T>(v[6], v[7]));
+    r.q[0] = make_uint4(narrow2<T>(v[0], v[1]), narrow2<T>(v[2], v[3]), narrow2<T>(v[4], v[5]), narrow2<T>(v[6], v[7]));
   }
+  return r;
 }
+template <typename T> __device__ __forceinline__ void store_raw(T* p, const Raw8<T>& r) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = r.q[i];
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) { store_raw(p, narrow8<T>(v)); }
 // two numbers to the nearest e4m3, the first in the lower byte
 __device__ __forceinline__ unsigned narrow_e4m3(float a, float b) {
   unsigned short r;
@@ -86,35 +94,54 @@ template <int P, bool WIDE> struct Row {
   int G, t;                                          // threads of the group, this one's number
   __device__ __forceinline__ int column(int p, int i) const { return WIDE ? (p * G + t) * 8 + i : (p * 8 + i) * G + t; }
 };
-// One row's share of a thread: raw words while they are on their way.
-template <typename T, int P, bool WIDE> struct Piece {
-  Raw8<T> raw[WIDE ? P : 1];
-  T one[WIDE ? 1 : P * 8];
-  // columns behind the row's end are zero
-  __device__ __forceinline__ void fetch(const Row<P, WIDE>& r, const T* row, int D) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if constexpr (WIDE) {
-        const int c = r.column(p, 0);
-        raw[p] = c < D ? fetch8(row + c) : Raw8<T>{};
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int c = r.column(p, i);
-          one[p * 8 + i] = c < D ? row[c] : from_f32<T>(0.f);
-        }
-      }
-    }
+// Rows on their way (WIDE): a ring of stages in shared memory for each group, filled by bulk copies of whole rows, up to three arrays' rows to a stage.
+// A stage is read into registers before the row's sum is joined, and filled again right after.  A wait that gives up lets its
+// thread go on (the group's barriers need all of them) without writing anything.
+constexpr int kMostStages = 4;
+struct Ring {
+  unsigned base, bar, bytes, stages, turn, issued;
+  volatile int* stop;
+  bool ok;
+  __device__ __forceinline__ unsigned stage() const { return base + turn % stages * bytes; }
+  __device__ __forceinline__ unsigned barrier() const { return bar + turn % stages * 8; }
+  // the copies in flight land before the block leaves its shared memory
+  __device__ __forceinline__ void give_up(int* status) const {
+    record(status, COCODC_ERR_TIMEOUT);
+    for (unsigned i = issued > stages ? issued - stages : 0; i < issued; ++i) bar_drain(bar + i % stages * 8, (i / stages) & 1);
   }
-  __device__ __forceinline__ void get(int p, float (&v)[8]) const {
-    if constexpr (WIDE) {
-      widen(raw[p], v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = to_f32(one[p * 8 + i]);
-    }
-  }
+  __device__ __forceinline__ void wait() { ok = bar_wait(barrier(), (turn / stages) & 1, stop) && ok; }
 };
+__device__ __forceinline__ Ring ring_of(unsigned char* memory, unsigned long long (*bars)[kMostStages], int* stop, int group, unsigned bytes, unsigned stages) {
+  return Ring{smem_addr(memory) + group * stages * bytes, smem_addr(&bars[group][0]), bytes, stages, 0, 0, stop, true};
+}
+__device__ __forceinline__ void ring_start(unsigned long long (*bars)[kMostStages], int* stop) {
+  if (threadIdx.x < kThreads / 32 * kMostStages) bar_init(smem_addr(&bars[0][0]) + threadIdx.x * 8, 1);
+  if (threadIdx.x == 0) *stop = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncthreads();
+}
+template <typename T> __device__ __forceinline__ Raw8<T> staged8(unsigned at) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.q[i].x), "=r"(r.q[i].y), "=r"(r.q[i].z), "=r"(r.q[i].w) : "r"(at + i * 16));
+  return r;
+}
+
+// Pack p of a row: from its place in a stage (WIDE), or from memory.  Columns behind the row's end are zero.
+template <typename T, int P, bool WIDE>
+__device__ __forceinline__ void get(const Row<P, WIDE>& r, unsigned staged, const T* row, int D, int p, float (&v)[8]) {
+  if constexpr (WIDE) {
+    const int c = r.column(p, 0);
+    if (c < D) widen(staged8<T>(staged + c * (unsigned)sizeof(T)), v);
+    else
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = r.column(p, i) < D ? to_f32(row[r.column(p, i)]) : 0.f;
+  }
+}
 template <typename T, int P, bool WIDE> __device__ __forceinline__ void put(const Row<P, WIDE>& r, T* row, int D, int p, const float (&v)[8]) {
   if (WIDE) {
     if (r.column(p, 0) < D) store8(row + r.column(p, 0), v);
@@ -135,10 +162,12 @@ template <int P, bool WIDE> __device__ __forceinline__ void fetch_weight(const R
     using T = decltype(e);
     const T* p0 = static_cast<const T*>(w);
     if (WIDE && (reinterpret_cast<unsigned long long>(w) & 15) == 0) {
-      Piece<T, P, WIDE> x;
-      x.fetch(r, p0, D);
 #pragma unroll
-      for (int p = 0; p < P; ++p) x.get(p, v[p]);
+      for (int p = 0; p < P; ++p)
+        if (r.column(p, 0) < D) widen(fetch8(p0 + r.column(p, 0)), v[p]);
+        else
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[p][i] = 0.f;
     } else {
 #pragma unroll
       for (int p = 0; p < P; ++p)
@@ -182,55 +211,88 @@ struct NormArgs {
   const void *x, *residual, *weight;
   long long x_stride, r_stride, t_stride, y_stride;
   long long T;
-  int D, G, weight_type, y_type, groups;   // G: threads of a row; groups: scales of a row (0: y is not in 8 bits)
+  int D, G, stages, weight_type, y_type, groups;   // G: threads of a row; groups: scales of a row (0: y is not in 8 bits)
   float eps;
   void *total, *y;
   float *y_scale, *rstd;
+  int* status;
 };
 
-__device__ __forceinline__ float rms_scale(float sum, int D, float eps) { return 1.f / sqrtf(sum / D + eps); }
+// 2 ulp from the approximate root, 1 from the reciprocal of D
+__device__ __forceinline__ float rms_scale(float sum, float inv_d, float eps) { return rsqrtf(fmaf(sum, inv_d, eps)); }
 __device__ __forceinline__ float scale_8(float most) { return fmaxf(most * (1.f / kMost8), kLeastScale); }
 
-// Registers: 24 P for the row and its weights, and what is on its way of the next row.
 template <typename X, typename S, int P, bool WIDE>
-__global__ void __launch_bounds__(kThreads, P == 4 ? 1 : P == 2 || !WIDE ? 2 : 3) k_norm(const NormArgs a) {
-  wait_for_previous();
-  may_follow();
+__global__ void __launch_bounds__(kThreads, P == 4 ? 2 : 3) k_norm(const NormArgs a) {
+  extern __shared__ __align__(128) unsigned char memory[];
   __shared__ float cell[2][kThreads / 32];
+  __shared__ unsigned long long bars[kThreads / 32][kMostStages];
+  __shared__ int shared_stop;
   __shared__ unsigned most[WIDE ? 1 : kThreads * P * 8 / 128 + kThreads / 32];   // a group's largest magnitudes: column order is not the threads'
   const int group = threadIdx.x / a.G;
   const Row<P, WIDE> r{a.G, (int)threadIdx.x % a.G};
   Join join{cell, group, a.G};
   const int D = a.D;
-  float w[P][8];
-  fetch_weight(r, a.weight, a.weight_type, D, w);
-  Piece<X, P, WIDE> x;
-  Piece<S, P, WIDE> u;
-  const auto fetch = [&](long long row) {
-    x.fetch(r, static_cast<const X*>(a.x) + row * a.x_stride, D);
-    if (a.residual) u.fetch(r, static_cast<const S*>(a.residual) + row * a.r_stride, D);
-  };
+  const float inv_d = 1.f / D;
+  const unsigned x_bytes = D * (unsigned)sizeof(X), s_bytes = a.residual ? D * (unsigned)sizeof(S) : 0;
+  Ring ring = ring_of(memory, bars, &shared_stop, group, x_bytes + s_bytes, a.stages);
+  if (WIDE) ring_start(bars, &shared_stop);
+  wait_for_previous();
+  may_follow();
   const int rows = blockDim.x / a.G;
   const long long step = (long long)gridDim.x * rows;
   long long row = (long long)blockIdx.x * rows + group;
-  if (row < a.T) fetch(row);
+  const X* const x = static_cast<const X*>(a.x);
+  const S* const u = static_cast<const S*>(a.residual);
+  const auto fetch = [&](long long t, unsigned stage, unsigned bar) {
+    bar_expect(bar, x_bytes + s_bytes);
+    bulk_load(stage, x + t * a.x_stride, x_bytes, bar);
+    if (u) bulk_load(stage + x_bytes, u + t * a.r_stride, s_bytes, bar);
+  };
+  if (WIDE && r.t == 0)
+    for (; ring.issued < ring.stages && row + ring.issued * step < a.T; ++ring.issued)
+      fetch(row + ring.issued * step, ring.base + ring.issued * ring.bytes, ring.bar + ring.issued * 8);
+  float w[P][8];
+  fetch_weight(r, a.weight, a.weight_type, D, w);
   for (; row < a.T; row += step) {
+    if (WIDE) ring.wait();
+    const unsigned stage = ring.stage();
     float v[P][8], sum = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      x.get(p, v[p]);
-      if (a.residual) {
+      get(r, stage, x + row * a.x_stride, D, p, v[p]);
+      if (u) {
         float q[8];
-        u.get(p, q);
+        get(r, stage + x_bytes, u + row * a.r_stride, D, p, q);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i] + q[i]));
-        put<S>(r, static_cast<S*>(a.total) + row * a.t_stride, D, p, v[p]);
+        for (int i = 0; i < 8; ++i) v[p][i] += q[i];
+        S* const to = static_cast<S*>(a.total) + row * a.t_stride;
+        if constexpr (WIDE) {                                       // rounded by pairs, once for the store and for what follows
+          const Raw8<S> sum8 = narrow8<S>(v[p]);
+          if (ring.ok && r.column(p, 0) < D) store_raw(to + r.column(p, 0), sum8);
+          widen(sum8, v[p]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i]));
+          put<S>(r, to, D, p, v[p]);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(v[p][i], v[p][i], sum);
     }
-    if (row + step < a.T) fetch(row + step);                        // on its way while this row is finished
-    const float rstd = rms_scale(join(sum, Plus()), D, a.eps);
+    const float rstd = rms_scale(join(sum, Plus()), inv_d, a.eps);
+    if (WIDE) {                                                     // all of the group have read the stage
+      __syncwarp();
+      if (r.t == 0 && ring.ok && row + a.stages * step < a.T) {
+        fetch(row + a.stages * step, stage, ring.barrier());
+        ++ring.issued;
+      }
+      ++ring.turn;
+    }
+    if (!ring.ok) {
+      if (a.groups == 1) join(0.f, Most());                         // the group's barrier
+      continue;
+    }
     if (a.rstd && r.t == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int p = 0; p < P; ++p)
@@ -265,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : P == 2 || !WIDE ? 2 : 3
           scale = scale_8(scale);
           if (r.t % 16 == 0 && c < D) a.y_scale[row * a.groups + c / 128] = scale;
         }
-        const float inv = 1.f / scale;
+        const float inv = __fdividef(1.f, scale);
         if (c < D) {
           const unsigned lo = narrow_e4m3(v[p][0] * inv, v[p][1] * inv) | narrow_e4m3(v[p][2] * inv, v[p][3] * inv) << 16;
           const unsigned hi = narrow_e4m3(v[p][4] * inv, v[p][5] * inv) | narrow_e4m3(v[p][6] * inv, v[p][7] * inv) << 16;
@@ -295,6 +357,7 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : P == 2 || !WIDE ? 2 : 3
       if (a.groups > 1) join.barrier();                             // before the next row's maxima
     }
   }
+  if (WIDE && !ring.ok && r.t == 0) ring.give_up(a.status);
 }
 
 // Rows too long for registers: read again after their sum is known; one block a row.
@@ -313,7 +376,7 @@ template <typename X, typename S> __global__ void __launch_bounds__(kThreads) k_
       if (a.residual) total[c] = from_f32<S>(to_f32(x[c]) + to_f32(r[c]));
       sum = fmaf(value(c), value(c), sum);
     }
-    const float rstd = rms_scale(join(sum, Plus()), a.D, a.eps);
+    const float rstd = rms_scale(join(sum, Plus()), 1.f / a.D, a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     const auto result = [&](int c) { return value(c) * rstd * load_as(a.weight, a.weight_type, c); };
     if (a.groups == 0) {
@@ -352,43 +415,55 @@ struct NormGradArgs {
   const void *dy, *total, *weight, *dtotal;
   long long dy_stride, t_stride, dt_stride, dx_stride;
   long long T;
-  int D, G, weight_type;
+  int D, G, stages, weight_type;
   const float* rstd;
   void* dx;
   float* parts;             // [blocks][D]: the blocks' sums of dweight, or NULL
+  int* status;
 };
 
 template <typename Y, typename S, int P, bool WIDE>
 __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const NormGradArgs a) {
-  wait_for_previous();
-  may_follow();
+  extern __shared__ __align__(128) unsigned char memory[];
   __shared__ float cell[2][kThreads / 32];
-  extern __shared__ float shared_parts[];                           // [rows of the block][D] where it has more than one
+  __shared__ unsigned long long bars[kThreads / 32][kMostStages];
+  __shared__ int shared_stop;
   const int group = threadIdx.x / a.G, rows = blockDim.x / a.G;
   const Row<P, WIDE> r{a.G, (int)threadIdx.x % a.G};
   Join join{cell, group, a.G};
   const int D = a.D;
-  float w[P][8], dw[P][8] = {};
-  fetch_weight(r, a.weight, a.weight_type, D, w);
-  Piece<Y, P, WIDE> dy;
-  Piece<S, P, WIDE> s, dt;
-  float rstd = 0.f;
-  const auto fetch = [&](long long row) {
-    dy.fetch(r, static_cast<const Y*>(a.dy) + row * a.dy_stride, D);
-    s.fetch(r, static_cast<const S*>(a.total) + row * a.t_stride, D);
-    if (a.dtotal) dt.fetch(r, static_cast<const S*>(a.dtotal) + row * a.dt_stride, D);
-    rstd = a.rstd[row];
-  };
+  const float inv_d = 1.f / D;
+  const unsigned y_bytes = D * (unsigned)sizeof(Y), s_bytes = D * (unsigned)sizeof(S), all = y_bytes + s_bytes * (a.dtotal ? 2 : 1);
+  Ring ring = ring_of(memory, bars, &shared_stop, group, all, a.stages);
+  if (WIDE) ring_start(bars, &shared_stop);
+  wait_for_previous();
+  may_follow();
   const long long step = (long long)gridDim.x * rows;
   long long row = (long long)blockIdx.x * rows + group;
-  if (row < a.T) fetch(row);
+  const Y* const dy = static_cast<const Y*>(a.dy);
+  const S *const s = static_cast<const S*>(a.total), *const dt = static_cast<const S*>(a.dtotal);
+  const auto fetch = [&](long long t, unsigned stage, unsigned bar) {
+    bar_expect(bar, all);
+    bulk_load(stage, dy + t * a.dy_stride, y_bytes, bar);
+    bulk_load(stage + y_bytes, s + t * a.t_stride, s_bytes, bar);
+    if (dt) bulk_load(stage + y_bytes + s_bytes, dt + t * a.dt_stride, s_bytes, bar);
+  };
+  if (WIDE && r.t == 0)
+    for (; ring.issued < ring.stages && row + ring.issued * step < a.T; ++ring.issued)
+      fetch(row + ring.issued * step, ring.base + ring.issued * ring.bytes, ring.bar + ring.issued * 8);
+  float w[P][8], dw[P][8] = {};
+  fetch_weight(r, a.weight, a.weight_type, D, w);
+  float next = row < a.T ? a.rstd[row] : 0.f;
   for (; row < a.T; row += step) {
-    const float k = rstd;
+    const float k = next;
+    if (row + step < a.T) next = a.rstd[row + step];
+    if (WIDE) ring.wait();
+    const unsigned stage = ring.stage();
     float g[P][8], h[P][8], sum = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      dy.get(p, g[p]);
-      s.get(p, h[p]);
+      get(r, stage, dy + row * a.dy_stride, D, p, g[p]);
+      get(r, stage + y_bytes, s + row * a.t_stride, D, p, h[p]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         h[p][i] *= k;
@@ -397,23 +472,30 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const No
         sum = fmaf(g[p][i], h[p][i], sum);
       }
     }
-    const float mean = join(sum, Plus()) / D;
+    const float mean = join(sum, Plus()) * inv_d;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      float u[8] = {};
-      if (a.dtotal) dt.get(p, u);
+      float q[8] = {};
+      if (dt) get(r, stage + y_bytes + s_bytes, dt + row * a.dt_stride, D, p, q);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[p][i] = fmaf(k, fmaf(-h[p][i], mean, g[p][i]), u[i]);
+      for (int i = 0; i < 8; ++i) g[p][i] = fmaf(k, fmaf(-h[p][i], mean, g[p][i]), q[i]);
+      if (a.dx && ring.ok) put<S>(r, static_cast<S*>(a.dx) + row * a.dx_stride, D, p, g[p]);
     }
-    if (row + step < a.T) fetch(row + step);
-    if (a.dx) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) put<S>(r, static_cast<S*>(a.dx) + row * a.dx_stride, D, p, g[p]);
+    if (WIDE) {
+      join.barrier();                                               // all of the group have read the stage
+      if (r.t == 0 && ring.ok && row + a.stages * step < a.T) {
+        fetch(row + a.stages * step, stage, ring.barrier());
+        ++ring.issued;
+      }
+      ++ring.turn;
     }
   }
+  if (WIDE && !ring.ok && r.t == 0) ring.give_up(a.status);
+  float* const shared_parts = reinterpret_cast<float*>(memory);      // [rows of the block][D] where it has more than one
   if (!a.parts) return;
   float* out = a.parts + (long long)blockIdx.x * D;
   float* mine = rows == 1 ? out : shared_parts + group * D;
+  if (rows > 1) __syncthreads();                                     // the stages have been read
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -489,14 +571,15 @@ template <typename F> cocodc_status with_types(int32_t x, int32_t s, F&& f) {
   if (x == COCODC_BF16) return s == COCODC_F32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
   return s == COCODC_F32 ? f(__half(), float()) : f(__half(), __half());
 }
+constexpr unsigned kSharedOfSm = 227 * 1024;
 template <int N> using Int = std::integral_constant<int, N>;
 
 unsigned grid_for(const cocodc_lm* lm, int64_t T, int rows, int per_sm) {
   const int64_t blocks = (T + rows - 1) / rows, most = (int64_t)lm->sm_count * per_sm;
   return (unsigned)(blocks < most ? blocks : most);
 }
-// Blocks of a kernel that an SM holds, by registers (shared memory never limits these kernels).  A kernel's number is asked for once.
-int per_sm(std::atomic<int>& known, const void* kernel, int threads) {
+// Blocks of a kernel that an SM holds, by registers and shared memory.  A kernel's registers are asked for once.
+int per_sm(std::atomic<int>& known, const void* kernel, int threads, unsigned shared) {
   int regs = known.load(std::memory_order_relaxed);
   if (regs == 0) {
     cudaFuncAttributes f;
@@ -507,12 +590,13 @@ int per_sm(std::atomic<int>& known, const void* kernel, int threads) {
     regs = (f.numRegs + 7) / 8 * 8;
     known.store(regs, std::memory_order_relaxed);
   }
-  const int blocks = 65536 / (regs * threads), most = 2048 / threads;
+  const int by_regs = 65536 / (regs * threads), by_memory = (int)(kSharedOfSm / (shared + 2048)), most = 2048 / threads;
+  const int blocks = by_regs < by_memory ? by_regs : by_memory;
   return blocks < 1 ? 1 : blocks < most ? blocks : most;
 }
 
-// Calls f(packs of a thread, whether wide, threads of a row, rows of a block).  Two packs a thread: registers for two blocks and more on an SM, with
-// the next row on its way; one where rows are few and their latency is what counts.
+// Calls f(packs of a thread, whether wide, threads of a row, rows of a block).  Two packs a thread leave registers for two blocks and more on an SM;
+// one where rows are few and their latency is what counts.
 template <typename F> cocodc_status with_shape(const cocodc_lm* lm, int64_t T, int64_t D, bool wide, F&& f) {
   const auto go = [&](auto p) {
     constexpr int P = decltype(p)::value;
@@ -524,8 +608,53 @@ template <typename F> cocodc_status with_shape(const cocodc_lm* lm, int64_t T, i
   if (!wide || D <= 256 || (T <= 2 * lm->sm_count && D <= 2048)) return go(Int<1>());
   return D <= 4096 ? go(Int<2>()) : go(Int<4>());
 }
+// Stages of a group's ring: what the loads of an SM need to be on their way at a time, but no more than there are rows.
+int stages_for(unsigned bytes, int rows, int blocks_by_regs, int64_t T, unsigned grid_rows) {
+  const unsigned share = kSharedOfSm / blocks_by_regs - 2048;
+  int n = (int)(share / (bytes * rows));
+  n = n > kMostStages ? kMostStages : n < 2 ? 2 : n;
+  const int64_t each = (T + grid_rows - 1) / grid_rows;
+  return each < n ? (int)(each < 1 ? 1 : each) : n;
+}
+
+// Starts a kernel that walks over rows with a ring of `bytes` a row (0: none).
+template <typename K, typename A>
+cocodc_status start_rows(cocodc_lm* lm, std::atomic<int>& regs, K kernel, A& a, int G, int rows, unsigned bytes, unsigned more, int most_blocks, unsigned* blocks,
+                         cudaStream_t st) {
+  const int by_regs = per_sm(regs, reinterpret_cast<const void*>(kernel), G * rows, more);
+  a.G = G;
+  a.stages = bytes ? stages_for(bytes, rows, by_regs, a.T, (unsigned)rows * by_regs * lm->sm_count) : 1;
+  unsigned shared = bytes * rows * a.stages;
+  if (shared < more) shared = more;
+  *blocks = grid_for(lm, a.T, rows, per_sm(regs, reinterpret_cast<const void*>(kernel), G * rows, shared));
+  if (*blocks > (unsigned)most_blocks) *blocks = (unsigned)most_blocks;
+  return start(lm, kernel, *blocks, G * rows, shared, st, 1, a);
+}
 
 }  // namespace
+
+namespace cocodc_lm_impl {
+bool norm_prepare() {
+  bool ok = true;
+  const auto allow = [&](auto kernel) {
+    ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedOfSm - 4096) == cudaSuccess;
+  };
+  for (int32_t x : {COCODC_F32, COCODC_BF16, COCODC_F16})
+    for (int32_t s : {x, (int32_t)COCODC_F32})
+      with_types(x, s, [&](auto xt, auto st) {
+        using X = decltype(xt);
+        using S = decltype(st);
+        allow(k_norm<X, S, 1, true>);
+        allow(k_norm<X, S, 2, true>);
+        allow(k_norm<X, S, 4, true>);
+        allow(k_norm_grad<X, S, 1, true>);
+        allow(k_norm_grad<X, S, 2, true>);
+        allow(k_norm_grad<X, S, 4, true>);
+        return COCODC_OK;
+      });
+  return ok;
+}
+}  // namespace cocodc_lm_impl
 
 extern "C" {
 
@@ -560,8 +689,8 @@ cocodc_status cocodc_lm_norm(cocodc_lm* lm, const void* x, int32_t x_type, int64
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  NormArgs a{x, residual, weight, x_stride, residual_stride, total_stride, y_stride, T, (int)D, 0, weight_type, y_type, (int)groups, eps,
-                   total, y, y_scale, rstd};
+  NormArgs a{x, residual, weight, x_stride, residual_stride, total_stride, y_stride, T, (int)D, 0, 0, weight_type, y_type, (int)groups, eps,
+                   total, y, y_scale, rstd, lm->d_status};
   const bool wide = D % 8 == 0 && rows_aligned(x, x_stride, xb) && (!sum || (rows_aligned(residual, residual_stride, sb) && rows_aligned(total, total_stride, sb))) &&
                     (eight ? on_boundary(y, 8) && y_stride % 8 == 0 : rows_aligned(y, y_stride, yb));
   return with_types(x_type, sum ? sum_type : x_type, [&](auto xt, auto s) {
@@ -570,9 +699,9 @@ cocodc_status cocodc_lm_norm(cocodc_lm* lm, const void* x, int32_t x_type, int64
     if (D > longest(wide)) return start(lm, k_norm_long<X, S>, grid_for(lm, T, 1, 8), kThreads, 0, st, 1, a);
     return with_shape(lm, T, D, wide, [&](auto p, auto w, int G, int rows) {
       static std::atomic<int> regs{0};
-      const auto kernel = k_norm<X, S, decltype(p)::value, decltype(w)::value>;
-      a.G = G;
-      return start(lm, kernel, grid_for(lm, T, rows, per_sm(regs, reinterpret_cast<const void*>(kernel), G * rows)), G * rows, 0, st, 1, a);
+      unsigned blocks;
+      return start_rows(lm, regs, k_norm<X, S, decltype(p)::value, decltype(w)::value>, a, G, rows,
+                        decltype(w)::value ? (unsigned)D * (unsigned)(sizeof(X) + (sum ? sizeof(S) : 0)) : 0, 0, INT32_MAX, &blocks, st);
     });
   });
 }
@@ -614,8 +743,8 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  NormGradArgs a{dy, total, weight, dtotal, dy_stride, total_stride, dtotal_stride, dx_stride, T, (int)D, 0, weight_type, rstd, dx,
-                       dweight ? static_cast<float*>(workspace) : nullptr};
+  NormGradArgs a{dy, total, weight, dtotal, dy_stride, total_stride, dtotal_stride, dx_stride, T, (int)D, 0, 0, weight_type, rstd, dx,
+                       dweight ? static_cast<float*>(workspace) : nullptr, lm->d_status};
   const bool wide = D % 8 == 0 && rows_aligned(dy, dy_stride, yb) && rows_aligned(total, total_stride, sb) && (!dtotal || rows_aligned(dtotal, dtotal_stride, sb)) &&
                     (!dx || rows_aligned(dx, dx_stride, sb));
   unsigned blocks = 0;
@@ -631,11 +760,9 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
       }
       return with_shape(lm, T, D, wide, [&](auto p, auto w, int G, int rows) {
         static std::atomic<int> regs{0};
-        const auto kernel = k_norm_grad<Y, S, decltype(p)::value, decltype(w)::value>;
-        a.G = G;
-        blocks = grid_for(lm, T, rows, per_sm(regs, reinterpret_cast<const void*>(kernel), G * rows));
-        if (blocks > kGradBlocks) blocks = kGradBlocks;
-        return start(lm, kernel, blocks, G * rows, dweight && rows > 1 ? rows * (unsigned)D * 4 : 0, st, 1, a);
+        return start_rows(lm, regs, k_norm_grad<Y, S, decltype(p)::value, decltype(w)::value>, a, G, rows,
+                          decltype(w)::value ? (unsigned)D * (unsigned)(sizeof(Y) + sizeof(S) * (dtotal ? 2 : 1)) : 0,
+                          dweight && rows > 1 ? rows * (unsigned)D * 4 : 0, kGradBlocks, &blocks, st);
       });
     });
   }
