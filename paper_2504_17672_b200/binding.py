@@ -696,34 +696,28 @@ class LmOps:
         yp, ys, rows, cols = _matrix(y, "y")
         if rows != T or cols != D:
             _sized("y", rows, cols, T, D)
-        rp = tp = kind = 0
+        rp = tp = kind = sp = group = 0
         rs = ts = D
-        if residual is not None or total is not None:
-            kinds = set()
-            for name, t in (("residual", residual), ("total", total)):
-                if t is not None:                            # one without the other is refused by the call
-                    p, st, r, c = _matrix(t, name)
-                    _sized(name, r, c, T, D)
-                    kinds.add(_type(t))
-                    if name == "residual":
-                        rp, rs = p, st
-                    else:
-                        tp, ts = p, st
-            if len(kinds) > 1:
+        if residual is not None:                             # one without the other is refused by the call
+            kind = _type(residual)
+            rp, rs, rows, cols = _matrix(residual, "residual")
+            if rows != T or cols != D:
+                _sized("residual", rows, cols, T, D)
+        if total is not None:
+            if residual is not None and total.dtype is not residual.dtype:
                 raise ValueError("residual and total must have one type")
-            kind = kinds.pop()
-        group = 0
+            kind = _type(total)
+            tp, ts, rows, cols = _matrix(total, "total")
+            if rows != T or cols != D:
+                _sized("total", rows, cols, T, D)
         y_type = E4M3 if y.dtype is torch.float8_e4m3fn else _type(y)
         if y_scale is not None:
-            groups = (D + 127) // 128
-            shape = tuple(y_scale.shape)
+            groups, shape = (D + 127) // 128, tuple(y_scale.shape)
             if shape == (T, groups) and groups > 1:
                 group = 128
             elif shape not in ((T,), (T, 1)):
                 raise ValueError(f"y_scale must be {T}, {T} x 1 or {T} x {groups}, not {shape}")
             sp = _vector(y_scale, "y_scale", y_scale.numel(), torch.float32)
-        else:
-            sp = 0
         code = _submit(self._h, _NORM(6, xp, _type(x), xs, rp, rs, kind, _vector(weight, "weight", D, weight.dtype), _type(weight), T, D, eps,
                                       tp, ts, yp, y_type, ys, sp, group, _vector(rstd, "rstd", T, torch.float32), self._stream(stream)))
         if code:
