@@ -76,6 +76,26 @@ template <typename T> __device__ __forceinline__ void store_raw(T* p, const Raw8
   for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = r.q[i];
 }
 template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) { store_raw(p, narrow8<T>(v)); }
+// x + u, rounded to u's type: of one 16-bit type by pairs, otherwise in fp32 and then by pairs
+template <typename X, typename S> __device__ __forceinline__ Raw8<S> sum8(const Raw8<X>& x, const Raw8<S>& u) {
+  if constexpr (std::is_same_v<X, S> && sizeof(S) == 2) {
+    using Two = std::conditional_t<std::is_same_v<S, __half>, __half2, __nv_bfloat162>;
+    const auto add = [](unsigned a, unsigned b) {
+      const Two v = __hadd2(*reinterpret_cast<const Two*>(&a), *reinterpret_cast<const Two*>(&b));
+      return *reinterpret_cast<const unsigned*>(&v);
+    };
+    Raw8<S> r;
+    r.q[0] = make_uint4(add(x.q[0].x, u.q[0].x), add(x.q[0].y, u.q[0].y), add(x.q[0].z, u.q[0].z), add(x.q[0].w, u.q[0].w));
+    return r;
+  } else {
+    float v[8], q[8];
+    widen(x, v);
+    widen(u, q);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += q[i];
+    return narrow8<S>(v);
+  }
+}
 // two numbers to the nearest e4m3, the first in the lower byte
 __device__ __forceinline__ unsigned narrow_e4m3(float a, float b) {
   unsigned short r;
@@ -105,7 +125,7 @@ template <int P, bool WIDE> struct Row {
 // Rows on their way (WIDE): a ring of stages in shared memory for each group, filled by bulk copies of whole rows, up to three arrays' rows to a stage.
 // A stage is read into registers before the row's sum is joined, and filled again right after.  A wait that gives up lets its
 // thread go on (the group's barriers need all of them) without writing anything.
-constexpr int kMostStages = 4;
+constexpr int kMostStages = 3;
 struct Ring {
   unsigned base, bar, bytes, stages, turn, issued;
   volatile int* stop;
@@ -188,6 +208,8 @@ template <int P, bool WIDE> __device__ __forceinline__ void fetch_weight(const R
   else take(__half());
 }
 
+struct Plus { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Most { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 // Sums or maxima over the threads of a row's group.  Above a warp they meet in shared memory, in two buffers in turn: one barrier of
 // the group each.
 struct Join {
@@ -205,16 +227,19 @@ struct Join {
       const int first = group * (G / 32);
       if (threadIdx.x % 32 == 0) cell[turn][threadIdx.x / 32] = v;
       barrier();
-      v = cell[turn][first];
-      for (int i = 1; i < G / 32; ++i) v = f(v, cell[turn][first + i]);
+      if (G == 64) {
+        v = f(cell[turn][first], cell[turn][first + 1]);
+      } else {
+        v = cell[turn][first + min((int)threadIdx.x % 8, G / 32 - 1)];
+        if constexpr (std::is_same_v<F, Plus>) v = (int)threadIdx.x % 8 < G / 32 ? v : 0.f;
+#pragma unroll
+        for (int o = 4; o; o >>= 1) v = f(v, __shfl_xor_sync(~0u, v, o));
+      }
       turn ^= 1;
     }
     return v;
   }
 };
-struct Plus { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
-struct Most { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-
 struct NormArgs {
   const void *x, *residual, *weight;
   long long x_stride, r_stride, t_stride, y_stride;
@@ -265,24 +290,31 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 2 : 3) k_norm(const NormArg
   for (; row < a.T; row += step) {
     if (WIDE) ring.wait();
     const unsigned stage = ring.stage();
+    S* const total = static_cast<S*>(a.total) + row * a.t_stride;
     float v[P][8], sum = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      get(r, stage, x + row * a.x_stride, D, p, v[p]);
-      if (u) {
-        float q[8];
-        get(r, stage + x_bytes, u + row * a.r_stride, D, p, q);
+      if constexpr (WIDE) {
+        const int c = r.column(p, 0);
+        const unsigned at = stage + c * (unsigned)sizeof(X);
+        if (c >= D) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[p][i] += q[i];
-        S* const to = static_cast<S*>(a.total) + row * a.t_stride;
-        if constexpr (WIDE) {                                       // rounded by pairs, once for the store and for what follows
-          const Raw8<S> sum8 = narrow8<S>(v[p]);
-          if (ring.ok && r.column(p, 0) < D) store_raw(to + r.column(p, 0), sum8);
-          widen(sum8, v[p]);
+          for (int i = 0; i < 8; ++i) v[p][i] = 0.f;
+        } else if (u) {
+          const Raw8<S> both = sum8(staged8<X>(at), staged8<S>(stage + x_bytes + c * (unsigned)sizeof(S)));
+          if (ring.ok) store_raw(total + c, both);
+          widen(both, v[p]);
         } else {
+          widen(staged8<X>(at), v[p]);
+        }
+      } else {
+        get(r, stage, x + row * a.x_stride, D, p, v[p]);
+        if (u) {
+          float q[8];
+          get(r, stage, u + row * a.r_stride, D, p, q);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i]));
-          put<S>(r, to, D, p, v[p]);
+          for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i] + q[i]));
+          put<S>(r, total, D, p, v[p]);
         }
       }
 #pragma unroll
