@@ -296,6 +296,7 @@ bool head_prepare() {
   const auto allow_type = [&](auto e) {
     using E = decltype(e);
     allow(k_head_tc<E, HEAD_STATS>);
+    allow(k_head_tc<E, HEAD_LONG>);
     allow(k_head_tc<E, HEAD_DZ>);
     allow(k_head_tc<E, HEAD_PRODUCTS>);
   };
@@ -355,9 +356,10 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
       HeadTc c{};
       c.h = a;
       c.n_tiles = (int)a.strips;
+      c.parts = (int)up(up(D, kBK), kPartBlocks);
       a.strips *= 2;
       if (!logit_maps<E>(&c, x, x_stride, table, table_stride, T, D, V, a.width)) return COCODC_ERR_CUDA;
-      return run_tc<E, HEAD_STATS>(lm, c, st);
+      return c.k_blocks >= kLongBlocks ? run_tc<E, HEAD_LONG>(lm, c, st) : run_tc<E, HEAD_STATS>(lm, c, st);
     }
     const Operand<E> xo{static_cast<const E*>(x), x_stride, 1}, wo{static_cast<const E*>(table), table_stride, 1};
     return start(lm, k_head_plain<E>, grid, 256, 0, st, 1, a, xo, wo, (long long)D);

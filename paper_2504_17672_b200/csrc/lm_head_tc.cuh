@@ -5,7 +5,10 @@
 //   warp 1   issuer: tcgen05.mma of each stage into one of two TMEM accumulators of 256 columns
 //   warps 2-9 epilogue, while the other accumulator fills; a thread has a row of the tile, two of them share it
 // STATS     a tile of x W^T is reduced where it lies: each thread finds its row's largest logit and the sum of powers of two among the
-//           tile's columns, and picks the target's logit; 8 bytes a row and tile leave the chip instead of 512.
+//           tile's columns, and picks the target's logit; 8 bytes a row and tile leave the chip instead of 512.  The tensor cores cut the sums that
+//           they accumulate instead of rounding them, always towards zero: the log-sum-exp of 2048 products came out 6e-7 to 1.4e-6 too small.  So long
+//           contractions (LONG, from kLongBlocks k-blocks on) are accumulated in parts of at most kPartBlocks, which the epilogue adds in registers: a
+//           quarter of that error at 2048, as good as sums in fp32, for 3 % of the time.
 // DZ        the same product; the epilogue forms dz from the row's lse and factors and writes it in 16 bits, 64 staged columns at a time.
 // PRODUCTS  dtable = dz^T x and dx = dz W of one piece in one launch: a tile's number tells which of the two it belongs to.  Tiles differ in
 //           length, so that a block takes the next one when it is ready (a counter that DZ set back), the long ones first.  dx's sums over
@@ -18,7 +21,7 @@
 
 namespace cocodc_lm_impl {
 
-enum { HEAD_STATS = 0, HEAD_DZ = 1, HEAD_PRODUCTS = 2 };
+enum { HEAD_STATS = 0, HEAD_DZ = 1, HEAD_PRODUCTS = 2, HEAD_LONG = 3 };
 
 struct HeadJob {             // one of the two products of HEAD_PRODUCTS
   int m_tiles, n_tiles, k_blocks, splits, tiles;
@@ -28,7 +31,8 @@ struct HeadJob {             // one of the two products of HEAD_PRODUCTS
 };
 struct HeadTc {
   CUtensorMap a[2], b[2], c[2];   // STATS, DZ: x, table, dz; PRODUCTS: dtable's and dx's operands and outputs
-  int m_tiles, n_tiles, k_blocks; // STATS, DZ
+  int m_tiles, n_tiles, k_blocks; // STATS, LONG, DZ
+  int parts;                      // LONG: accumulations of a tile
   int width;                      // columns of a tile
   unsigned a_bytes;
   int slabs;                      // PRODUCTS: slabs of 64 columns that one copy brings: all of a tile, or one (see map_slabs)
@@ -42,6 +46,7 @@ struct HeadTc {
 };
 
 constexpr int kHeadStages = 4, kHeadEpilogue = 8, kHeadThreads = 64 + kHeadEpilogue * 32;
+constexpr int kPartBlocks = 8, kLongBlocks = 17;
 constexpr int kTileRing = 4;      // tiles that the producer may be ahead
 constexpr unsigned kHeadStage = kABytes + 256 * kBK * 2, kHeadSmem = 1024 + kHeadStages * kHeadStage + kHeadEpilogue * kOutBytes;
 // Tiles of consecutive rows that go through one column of tiles in turn (as in the gated block).
@@ -247,6 +252,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
   } else if (warp == 1) {
     if (lane == 0) {
       long long it = 0;
+      int sum = 0;                                     // accumulations so far
       bool ok = true;
       for (int turn = 0; ok; ++turn) {
         const int tile = nth_tile(turn);
@@ -259,22 +265,25 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
         const bool a_mn = MODE == HEAD_PRODUCTS && t.kind == 0;
         constexpr bool b_mn = MODE == HEAD_PRODUCTS;
         const unsigned idesc = instr_desc<E>(kBM, a.width, a_mn, b_mn);
-        const int acc = turn & 1;
-        ok = bar_wait(smem_addr(&sh.acc_empty[acc]), (unsigned)((turn >> 1) & 1) ^ 1, stop);
-        tc_fence_after();
-        for (int kb = t.kb0; ok && kb < t.kb1; ++kb, ++it) {
-          const int s = (int)(it % kHeadStages);
-          ok = bar_wait(smem_addr(&sh.full[s]), (unsigned)((it / kHeadStages) & 1), stop);
-          if (!ok) break;
+        const int parts = MODE == HEAD_LONG ? a.parts : 1;
+        for (int q = 0; ok && q < parts; ++q, ++sum) {
+          const int acc = sum & 1, first = MODE == HEAD_LONG ? t.kb1 * q / parts : t.kb0, last = MODE == HEAD_LONG ? t.kb1 * (q + 1) / parts : t.kb1;
+          ok = bar_wait(smem_addr(&sh.acc_empty[acc]), (unsigned)((sum >> 1) & 1) ^ 1, stop);
           tc_fence_after();
-          const unsigned sa = base + s * kHeadStage, sb = sa + kABytes;
-          const unsigned long long da = tile_desc(sa, a_mn ? kSlab : 16), db = tile_desc(sb, b_mn ? kSlab : 16);
-          const unsigned ka = a_mn ? 2048 >> 4 : 32 >> 4;   // 16 k: 32 bytes along a K-major row, 16 rows of an MN-major tile
-          constexpr unsigned kb16 = b_mn ? 2048 >> 4 : 32 >> 4;
-          for (int k = 0; k < kBK / 16; ++k) tc_mma(tmem + acc * 256, da + k * ka, db + k * kb16, idesc, kb > t.kb0 || k > 0);
-          tc_commit(smem_addr(&sh.empty[s]));
+          for (int kb = first; ok && kb < last; ++kb, ++it) {
+            const int s = (int)(it % kHeadStages);
+            ok = bar_wait(smem_addr(&sh.full[s]), (unsigned)((it / kHeadStages) & 1), stop);
+            if (!ok) break;
+            tc_fence_after();
+            const unsigned sa = base + s * kHeadStage, sb = sa + kABytes;
+            const unsigned long long da = tile_desc(sa, a_mn ? kSlab : 16), db = tile_desc(sb, b_mn ? kSlab : 16);
+            const unsigned ka = a_mn ? 2048 >> 4 : 32 >> 4;   // 16 k: 32 bytes along a K-major row, 16 rows of an MN-major tile
+            constexpr unsigned kb16 = b_mn ? 2048 >> 4 : 32 >> 4;
+            for (int k = 0; k < kBK / 16; ++k) tc_mma(tmem + acc * 256, da + k * ka, db + k * kb16, idesc, kb > first || k > 0);
+            tc_commit(smem_addr(&sh.empty[s]));
+          }
+          if (ok) tc_commit(smem_addr(&sh.acc_full[acc]));
         }
-        if (ok) tc_commit(smem_addr(&sh.acc_full[acc]));
       }
       if (!ok) {
         tc_commit(smem_addr(&sh.drain));
@@ -285,33 +294,27 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
     // a warp reaches the 32 TMEM lanes of its number modulo 4; of two such warps one takes the even, one the odd pieces of the columns
     const int quarter = warp & 3, part = (warp - 2) / 4;
     const unsigned buf = staging + (warp - 2) * kOutBytes;
+    int sum = 0;
     for (int turn = 0;; ++turn) {
-      const int acc = turn & 1;
       const int tile = nth_tile(turn);
       if (!__all_sync(~0u, tile >= 0)) break;          // every lane has read it
       if (lane == 0) tile_read(turn);
       const HeadTile t = head_tile<MODE>(a, tile);
       const int row0 = t.m * kBM + quarter * 32, n0 = t.n * a.width;
-      const unsigned src = tmem + acc * 256 + ((unsigned)(quarter * 32) << 16);
       const long long row = row0 + lane;
       // what the row needs is on its way while the tile's products run
       long long target = -1;
       RowOf r{};
-      if (MODE == HEAD_STATS && a.h.targets && row < a.h.T) target = raw_target(a.h.targets, a.h.targets64, row);
+      if ((MODE == HEAD_STATS || MODE == HEAD_LONG) && a.h.targets && row < a.h.T) target = raw_target(a.h.targets, a.h.targets64, row);
       if (MODE == HEAD_DZ && row < a.d.T) {
         r = row_of(a.d, row);
         target = r.y;
       }
-      if (!__all_sync(~0u, bar_wait(smem_addr(&sh.acc_full[acc]), (unsigned)((turn >> 1) & 1), stop))) break;
-      tc_fence_after();
-      if constexpr (MODE == HEAD_STATS) {
+      if constexpr (MODE == HEAD_STATS || MODE == HEAD_LONG) {
         const int cols = (int)min((long long)a.width, a.h.V - n0);
         const int hit = target >= n0 && target < n0 + cols ? (int)(target - n0) : -1;
         float m = -INFINITY, s = 0.f;
-        for (int col = part * 32; col < cols; col += 64) {
-          float v[32];
-          tmem_load32(v, src + col);
-          tmem_wait_loads();
+        const auto reduce = [&](float (&v)[32], int col) {
           if (cols - col < 32) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -333,9 +336,57 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
               if (i == at) picked = v[i];
             if (at >= 0 && at < 32 && row < a.h.T) a.h.picked[row] = picked * a.h.scale2;
           }
+        };
+        float z[MODE == HEAD_LONG ? 4 : 1][32];         // LONG: sums of the parts; the thread's columns are the pieces part, part + 2, ... of 32
+        const int parts = MODE == HEAD_LONG ? a.parts : 1;
+        bool ok = true;
+        for (int q = 0; ok && q < parts; ++q, ++sum) {
+          const int acc = sum & 1;
+          ok = __all_sync(~0u, bar_wait(smem_addr(&sh.acc_full[acc]), (unsigned)((sum >> 1) & 1), stop));
+          if (!ok) break;
+          tc_fence_after();
+          const unsigned src = tmem + acc * 256 + ((unsigned)(quarter * 32) << 16);
+          if constexpr (MODE == HEAD_LONG) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              const int col = (2 * p + part) * 32;
+              if (col >= cols) continue;
+              if (q == 0) {
+                tmem_load32(z[p], src + col);
+                tmem_wait_loads();
+              } else {
+                float v[32];
+                tmem_load32(v, src + col);
+                tmem_wait_loads();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) z[p][i] += v[i];
+              }
+            }
+          } else {
+            for (int col = part * 32; col < cols; col += 64) {
+              tmem_load32(z[0], src + col);
+              tmem_wait_loads();
+              reduce(z[0], col);
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(smem_addr(&sh.acc_empty[acc]));
+        }
+        if (!ok) break;
+        if constexpr (MODE == HEAD_LONG) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+            if ((2 * p + part) * 32 < cols) reduce(z[p], (2 * p + part) * 32);
         }
         if (row < a.h.T) a.h.stats[(2ll * t.n + part) * a.h.T + row] = make_float2(m * a.h.scale2, s);
-      } else if constexpr (MODE == HEAD_DZ) {
+        continue;
+      }
+      const int acc = turn & 1;
+      const unsigned src = tmem + acc * 256 + ((unsigned)(quarter * 32) << 16);
+      if (!__all_sync(~0u, bar_wait(smem_addr(&sh.acc_full[acc]), (unsigned)((turn >> 1) & 1), stop))) break;
+      tc_fence_after();
+      if constexpr (MODE == HEAD_DZ) {
         const int cols = (int)min((long long)a.width, a.d.v1 - a.d.v0 - n0);
         const bool nothing = r.lse2 == INFINITY;
         const long long hit = target < 0 ? -1 : target - a.d.v0 - n0;
