@@ -183,7 +183,7 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
  *   lse[t]  = log sum_j exp(z_j)
  *   logp[t] = z_y - lse, y = targets[t]; 0 where y < 0
  *   x [T][D]; table W [V][D]; both BF16 or both F16.  0 < scale <= 1e30.  logp (with targets) and lse: fp32, packed, one may be NULL.
- * Products accumulate in fp32 and the logits are not rounded to fewer bits.  A row whose logits hold a NaN or +Inf has NaN in lse and logp;
+ * Products accumulate in fp32 (on the tensor cores in parts of at most 1024, which are added in fp32) and the logits are not rounded to fewer bits.  A row whose logits hold a NaN or +Inf has NaN in lse and logp;
  * -Inf counts as probability 0, and a row of nothing but -Inf has lse = -Inf and log probabilities -Inf.
  * T <= 2^31 - 1, D <= 2^31 - 1, V <= 2^30, T D and V D <= 2^48.
  */
@@ -199,8 +199,8 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
  * dlogp is NULL (with targets NULL) or dlse is NULL for "zero"; dlogp[t] is not used where y < 0.  A row whose lse is -Inf or that gets nothing (both
  * factors 0) adds nothing, a row whose lse is NaN or +Inf gives NaN.
  * dz is rounded to x's type between the steps, as tensor cores take it (F16: times a power of two that takes the largest |dlogp| + |dlse|
- * to between 2^9 and 2^10, so that small probabilities do not underflow); the products accumulate in fp32.  The workspace holds dz of one piece, at most
- * a fixed number of bytes beyond 1024 columns, and fp32 sums of dx.  T = 0 sets dtable to zero (accumulate: leaves it).
+ * to between 2^9 and 2^10, so that small probabilities do not underflow); the products accumulate in fp32.  The workspace holds dz of one piece (of at most
+ * 2^28 bytes, or 1024 columns), and fp32 sums of dx.  T = 0 sets dtable to zero (accumulate: leaves it).
  */
 uint64_t cocodc_lm_head_grad_workspace(int64_t T, int64_t D, int64_t V);
 cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, int64_t x_stride, const void* table,
@@ -236,7 +236,8 @@ typedef struct {
 typedef struct cocodc_lm_adam cocodc_lm_adam;   /* a plan: belongs to the handle's device */
 
 /* state_bits is 32 or 8, count <= 2^20.  tensors is host memory.  Errors: INVALID_ARG, ALIGNMENT (of the element types), ALIAS (two of all
- * the arrays overlap, gradients with one another excepted), NOMEM, CUDA.  destroy waits for the device. */
+ * the arrays overlap, gradients with one another excepted), NOMEM, CUDA.  create allocates, and neither is for a stream that is being captured; a captured
+ * step reads the plan, which has to live as long as its graph.  destroy waits for the device. */
 cocodc_status cocodc_lm_adam_create(cocodc_lm_adam** out, cocodc_lm* lm, const cocodc_lm_tensor* tensors, int64_t count, int32_t state_bits);
 cocodc_status cocodc_lm_adam_destroy(cocodc_lm_adam* plan);
 

@@ -43,15 +43,6 @@ template <typename T> __device__ __forceinline__ void widen(const Raw8<T>& r, fl
     }
   }
 }
-template <typename T> __device__ __forceinline__ unsigned narrow2(float a, float b) {
-  if constexpr (std::is_same_v<T, __nv_bfloat16>) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const unsigned*>(&v);
-  } else {
-    const __half2 v = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const unsigned*>(&v);
-  }
-}
 template <typename T> __device__ __forceinline__ Raw8<T> narrow8(const float (&v)[8]) {
   Raw8<T> r;
   if constexpr (sizeof(T) == 4) {
@@ -59,7 +50,7 @@ template <typename T> __device__ __forceinline__ Raw8<T> narrow8(const float (&v
     for (int i = 0; i < 2; ++i)
       r.q[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
   } else {
-    r.q[0] = make_uint4(narrow2<T>(v[0], v[1]), narrow2<T>(v[2], v[3]), narrow2<T>(v[4], v[5]), narrow2<T>(v[6], v[7]));
+    r.q[0] = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
   }
   return r;
 }
