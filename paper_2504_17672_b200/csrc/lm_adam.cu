@@ -46,6 +46,7 @@ struct AdamArgs {
   int count;
   long long units;
   float b1, c1, b2, c2, eps;                         // c = 1 - b
+  float k1, k2;                                      // where the step and the rate are known on the host
   double lr, beta1, beta2;
   long long step;
   const long long* step_at;
@@ -297,29 +298,29 @@ template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 4 : 3)
   __shared__ float factors[2];
   __shared__ double shared_lr;
   if (threadIdx.x == 0) {
-    long long step = a.step_at ? *a.step_at : a.step;
-    if (step < 1) {
-      record(a.status, COCODC_ERR_INVALID_ARG);
-      step = 1;
+    factors[0] = a.k1;
+    factors[1] = a.k2;
+    shared_lr = a.lr;
+    if (a.step_at || a.lr_scale) {
+      long long step = a.step_at ? *a.step_at : a.step;
+      if (step < 1) {
+        record(a.status, COCODC_ERR_INVALID_ARG);
+        step = 1;
+      }
+      if (a.lr_scale) shared_lr = a.lr * (double)*a.lr_scale;
+      factors[0] = (float)(shared_lr / (1.0 - pow(a.beta1, (double)step)));
+      factors[1] = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)step)));
     }
-    const double lr = a.lr_scale ? a.lr * (double)*a.lr_scale : a.lr;
-    factors[0] = (float)(lr / (1.0 - pow(a.beta1, (double)step)));
-    factors[1] = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)step)));
-    shared_lr = lr;
   }
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const unsigned step_bits = (unsigned)(a.step_at ? *a.step_at : a.step);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const long long last = a.units * (blockIdx.x + 1) / gridDim.x;
-  long long unit = a.units * blockIdx.x / gridDim.x + warp;
-  // the tensor of the warp's first unit: the last one that begins at or before it
-  int number = 0;
-  for (int n = a.count; n > 1;) {
-    const int half = n / 2;
-    if (a.tensors[number + half].first <= unit) number += half;
-    n -= half;
-  }
-  __syncthreads();
+  const long long from = a.units * blockIdx.x / gridDim.x;
+  long long unit = from + warp;
+  // the tensor of the block's first unit: the last one that begins at or before it (all looked at together: a search by halves waits for a load at each)
+  int number = -1;
+  for (int i = 0; i < a.count; i += kThreads) number += __syncthreads_count(i + (int)threadIdx.x < a.count && a.tensors[i + threadIdx.x].first <= from);
   Factors f;
   f.gs = both(gs);
   f.b1 = both(a.b1);
@@ -547,7 +548,7 @@ cocodc_status cocodc_lm_adamw(cocodc_lm* lm, const cocodc_lm_adam* plan, double 
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   const AdamArgs a{plan->d_tensors, plan->count, plan->units, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
-                   lr, beta1, beta2, step, reinterpret_cast<const long long*>(step_at), grad_scale, lr_scale, (unsigned)seed, lm->d_status};
+                   (float)(lr / (1.0 - std::pow(beta1, (double)step))), (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step))), lr, beta1, beta2, step, reinterpret_cast<const long long*>(step_at), grad_scale, lr_scale, (unsigned)seed, lm->d_status};
   const long long blocks = (plan->units + kWarps - 1) / kWarps, most = (long long)lm->sm_count * (plan->bits == 8 ? 4 : 3);
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
