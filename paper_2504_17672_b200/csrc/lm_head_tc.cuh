@@ -14,6 +14,12 @@
 //           length, so that a block takes the next one when it is ready (a counter that DZ set back), the long ones first.  dx's sums over
 //           the pieces of the vocabulary (and over parts of its contraction, where its tiles are few) stay in fp32 in an order of
 //           their own, in which 32 lanes' accesses are 512 consecutive bytes.
+// Measured alone (ncu), tensor pipe: 8192 x 2048 x 32000 LONG 758 us (1.42 PFLOP/s, 77 %; without parts 704 us, 83 %), DZ of 16128 columns 370-376 us
+// (81 %), PRODUCTS of them 768 us (1.41 PFLOP/s, 84 %; with two and four copies for an MN-major operand's slabs 864 us, 66 %).  Back to back the power cap
+// lowers the clock: 890-905 us forward, 2.74 ms backward.  dx and dtable in a launch each took 405 + 372 us, together 743.  Bringing
+// tiles to L2 ahead of time made all of it slower (PRODUCTS 864 -> 925 us); what feeds the tensor cores is the way from L2, 49 KB a k-block.
+// 1333 x 768 x 50257: 94 us (15 rounds of tiles for 14.6).  One row of 2048 x 32000: 29 us, 20 of which are the table's bytes; 4 are the start and
+// end of the kernel, 2 the joining one.
 #pragma once
 
 #include "lm_head.cuh"

