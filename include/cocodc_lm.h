@@ -183,7 +183,8 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
  *   lse[t]  = log sum_j exp(z_j)
  *   logp[t] = z_y - lse, y = targets[t]; 0 where y < 0
  *   x [T][D]; table W [V][D]; both BF16 or both F16.  0 < scale <= 1e30.  logp (with targets) and lse: fp32, packed, one may be NULL.
- * Products accumulate in fp32 (on the tensor cores in parts of at most 1024, which are added in fp32) and the logits are not rounded to fewer bits.  A row whose logits hold a NaN or +Inf has NaN in lse and logp;
+ * Products accumulate in fp32 (on the tensor cores in parts of at most 1024, which are added in fp32) and the logits are not rounded to fewer bits.  A row whose logits hold a NaN or +Inf (a product or
+ * sum beyond fp32's range is one) has NaN in lse and logp;
  * -Inf counts as probability 0, and a row of nothing but -Inf has lse = -Inf and log probabilities -Inf.
  * T <= 2^31 - 1, D <= 2^31 - 1, V <= 2^30, T D and V D <= 2^48.
  */
@@ -197,7 +198,8 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
  *   dz[t][j] = scale * ( dlogp[t] * (1[j = y] - p_j) + dlse[t] * p_j ),  p_j = exp(z_j - lse[t])
  *   dx = dz W   [T][D] of x's type, or NULL        dtable = dz^T x   [V][D] of x's type or F32, or NULL (accumulate: added to what it holds)
  * dlogp is NULL (with targets NULL) or dlse is NULL for "zero"; dlogp[t] is not used where y < 0.  A row whose lse is -Inf or that gets nothing (both
- * factors 0) adds nothing, a row whose lse is NaN or +Inf gives NaN.
+ * factors 0, a target below 0 without dlse among them) has dz = 0, whatever its logits are; in dtable its x takes part as 0 x, so that x has to be
+ * finite there.  A row whose lse is NaN or +Inf gives NaN.
  * dz is rounded to x's type between the steps, as tensor cores take it (F16: times a power of two that takes the largest |dlogp| + |dlse|
  * to between 2^9 and 2^10, so that small probabilities do not underflow); the products accumulate in fp32.  The workspace holds dz of one piece (of at most
  * 2^28 bytes, or 1024 columns), and fp32 sums of dx.  T = 0 sets dtable to zero (accumulate: leaves it).
