@@ -485,7 +485,7 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
         s = run_tc<E, HEAD_PRODUCTS>(lm, c, st);
         if (s != COCODC_OK) return s;
         if (dx && parts > 1 && d.v1 == V)
-          s = start(lm, k_head_add<E>, (unsigned)(c.job[1].m_tiles * n_tiles * (kBM / 8)), 256, 0, st, 1, c);
+          s = start(lm, k_head_add<E>, dim3((unsigned)(c.job[1].m_tiles * n_tiles * (kBM / 8)), (unsigned)up(c.width, 128)), 256, 0, st, 1, c);
         if (s != COCODC_OK) return s;
         continue;
       }

@@ -326,14 +326,15 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
             for (int i = 0; i < 32; ++i)
               if (i >= cols - col) v[i] = -INFINITY;
           }
-          float most = v[0];
+          float most[4] = {v[0], v[1], v[2], v[3]}, sums[4] = {0.f, 0.f, 0.f, 0.f};       // four chains: one waits for itself
 #pragma unroll
-          for (int i = 1; i < 32; ++i) most = fmaxf(most, v[i]);
-          const float now = fmaxf(m, most), shift = shift_of(now) * a.h.scale2;
+          for (int i = 4; i < 32; ++i) most[i % 4] = fmaxf(most[i % 4], v[i]);
+          const float now = fmaxf(m, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]))), shift = shift_of(now) * a.h.scale2;
           s *= fast_exp2(fmaf(m, a.h.scale2, -shift));
           m = now;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) s += fast_exp2(fmaf(v[i], a.h.scale2, -shift));
+          for (int i = 0; i < 32; ++i) sums[i % 4] += fast_exp2(fmaf(v[i], a.h.scale2, -shift));
+          s += (sums[0] + sums[1]) + (sums[2] + sums[3]);
           const int at = hit - col;
           if (__any_sync(~0u, at >= 0 && at < 32)) {
             float picked = 0.f;
@@ -478,32 +479,32 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
   }
 }
 
-// The parts of dx's sums added in order, and out: a block takes eight rows of a tile.
+// The parts of dx's sums added in order, and out: a block takes eight rows and 128 columns of a tile.
 template <typename E> __global__ void __launch_bounds__(256) k_head_add(const __grid_constant__ HeadTc a) {
   wait_for_previous();
   may_follow();
   const HeadJob& j = a.job[1];
   const int per = j.m_tiles * j.n_tiles, tile = blockIdx.x / (kBM / 8), row = blockIdx.x % (kBM / 8) * 8 + threadIdx.x % 8;
   const HeadTile t = head_tile<HEAD_PRODUCTS>(a, (a.first == 1 ? 0 : a.job[0].tiles) + tile);
-  const int y = t.m * kBM + row;
-  if (y >= j.rows) return;
+  const int y = t.m * kBM + row, col = blockIdx.y * 128 + threadIdx.x / 8 * 4, x = t.n * a.width + col;
+  if (y >= j.rows || col >= a.width || x >= j.cols) return;
   const float scale = j.o.factor ? j.o.factor[1] * j.o.scale : j.o.scale;
-  for (int col = threadIdx.x / 8 * 4; col < a.width; col += 128) {
-    const int x = t.n * a.width + col;
-    if (x >= j.cols) break;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int z = 0; z < j.splits; ++z) {
-      const float4 v = *sums_at(j.o, z * per + tile, a.width, col, row);
-      sum.x += v.x;
-      sum.y += v.y;
-      sum.z += v.z;
-      sum.w += v.w;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int z = 0; z < j.splits; z += 4) {
+    float4 u[4];                                                      // together on their way
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = z + k < j.splits ? *sums_at(j.o, (z + k) * per + tile, a.width, col, row) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[0] += u[k].x;
+      v[1] += u[k].y;
+      v[2] += u[k].z;
+      v[3] += u[k].w;
     }
-    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
-    E* out = static_cast<E*>(j.o.out) + y * j.o.ld + x;
-    for (int i = 0; i < 4; ++i)
-      if (x + i < j.cols) out[i] = from_f32<E>(v[i] * scale);
   }
+  E* out = static_cast<E*>(j.o.out) + y * j.o.ld + x;
+  for (int i = 0; i < 4; ++i)
+    if (x + i < j.cols) out[i] = from_f32<E>(v[i] * scale);
 }
 
 }  // namespace cocodc_lm_impl

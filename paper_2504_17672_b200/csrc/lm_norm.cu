@@ -147,20 +147,32 @@ template <typename T> __device__ __forceinline__ Raw8<T> staged8(unsigned at) {
   return r;
 }
 
-// Pack p of a row: from its place in a stage (WIDE), or from memory.  Columns behind the row's end are zero.
-template <typename T, int P, bool WIDE>
-__device__ __forceinline__ void get(const Row<P, WIDE>& r, unsigned staged, const T* row, int D, int p, float (&v)[8]) {
-  if constexpr (WIDE) {
-    const int c = r.column(p, 0);
-    if (c < D) widen(staged8<T>(staged + c * (unsigned)sizeof(T)), v);
-    else
+// Pack p of a row from its place in a stage; columns behind the row's end are zero.
+template <typename T, int P> __device__ __forceinline__ void get(const Row<P, true>& r, unsigned staged, int D, int p, float (&v)[8]) {
+  const int c = r.column(p, 0);
+  if (c < D) widen(staged8<T>(staged + c * (unsigned)sizeof(T)), v);
+  else
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = r.column(p, i) < D ? to_f32(row[r.column(p, i)]) : 0.f;
-  }
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
 }
+// Rows that are not whole packs: a row's columns on their way in registers (gradient of 10392 x 601 bf16: 33 us, 60 without).
+template <typename T, int P, bool WIDE> struct Ahead {
+  T one[WIDE ? 1 : P * 8];
+  __device__ __forceinline__ void fetch(const Row<P, WIDE>& r, const T* row, int D) {
+    if constexpr (!WIDE) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) one[p * 8 + i] = r.column(p, i) < D ? row[r.column(p, i)] : from_f32<T>(0.f);
+    }
+  }
+  __device__ __forceinline__ void get(int p, float (&v)[8]) const {
+    if constexpr (!WIDE) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = to_f32(one[p * 8 + i]);
+    }
+  }
+};
 template <typename T, int P, bool WIDE> __device__ __forceinline__ void put(const Row<P, WIDE>& r, T* row, int D, int p, const float (&v)[8]) {
   if (WIDE) {
     if (r.column(p, 0) < D) store8(row + r.column(p, 0), v);
@@ -251,7 +263,7 @@ __device__ __forceinline__ float scale_8(float most) { return fmaxf(most * (1.f 
 // ten rounds of rows at 4099.  Measured: 65536 x 1024 bf16 with fp32 sums 128 us (6.3 TB/s, 96 % of the copy rate); 4099 x 3200 in
 // 8 bits 18.8 us (4.9 TB/s); one row of 2048 5.3 us alone with cold caches.
 template <typename X, typename S, int P, bool WIDE>
-__global__ void __launch_bounds__(kThreads, P == 4 ? 2 : 3) k_norm(const NormArgs a) {
+__global__ void __launch_bounds__(kThreads, P == 4 || !WIDE ? 2 : 3) k_norm(const NormArgs a) {
   extern __shared__ __align__(128) unsigned char memory[];
   __shared__ float cell[2][kThreads / 32];
   __shared__ unsigned long long bars[kThreads / 32][kMostStages];
@@ -282,6 +294,14 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 2 : 3) k_norm(const NormArg
       fetch(row + ring.issued * step, ring.base + ring.issued * ring.bytes, ring.bar + ring.issued * 8);
   float w[P][8];
   fetch_weight(r, a.weight, a.weight_type, D, w);
+  Ahead<X, P, WIDE> ahead_x;
+  Ahead<S, P, WIDE> ahead_u;
+  const auto fetch_ahead = [&](long long t) {
+    if (WIDE || t >= a.T) return;
+    ahead_x.fetch(r, x + t * a.x_stride, D);
+    if (u) ahead_u.fetch(r, u + t * a.r_stride, D);
+  };
+  fetch_ahead(row);
   for (; row < a.T; row += step) {
     if (WIDE) ring.wait();
     const unsigned stage = ring.stage();
@@ -303,10 +323,10 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 2 : 3) k_norm(const NormArg
           widen(staged8<X>(at), v[p]);
         }
       } else {
-        get(r, stage, x + row * a.x_stride, D, p, v[p]);
+        ahead_x.get(p, v[p]);
         if (u) {
           float q[8];
-          get(r, stage, u + row * a.r_stride, D, p, q);
+          ahead_u.get(p, q);
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[p][i] = to_f32(from_f32<S>(v[p][i] + q[i]));
           put<S>(r, total, D, p, v[p]);
@@ -315,6 +335,7 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 2 : 3) k_norm(const NormArg
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(v[p][i], v[p][i], sum);
     }
+    fetch_ahead(row + step);
     const float rstd = rms_scale(join(sum, Plus()), inv_d, a.eps);
     if (WIDE) {                                                     // all of the group have read the stage
       __syncwarp();
@@ -491,6 +512,15 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const No
   float w[P][8], dw[P][8] = {};
   fetch_weight(r, a.weight, a.weight_type, D, w);
   float next = row < a.T ? a.rstd[row] : 0.f;
+  Ahead<Y, P, WIDE> ahead_y;
+  Ahead<S, P, WIDE> ahead_s, ahead_t;
+  const auto fetch_ahead = [&](long long t) {
+    if (WIDE || t >= a.T) return;
+    ahead_y.fetch(r, dy + t * a.dy_stride, D);
+    ahead_s.fetch(r, s + t * a.t_stride, D);
+    if (dt) ahead_t.fetch(r, dt + t * a.dt_stride, D);
+  };
+  fetch_ahead(row);
   for (; row < a.T; row += step) {
     const float k = next;
     if (row + step < a.T) next = a.rstd[row + step];
@@ -499,8 +529,13 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const No
     float g[P][8], h[P][8], sum = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      get(r, stage, dy + row * a.dy_stride, D, p, g[p]);
-      get(r, stage + y_bytes, s + row * a.t_stride, D, p, h[p]);
+      if constexpr (WIDE) {
+        get<Y>(r, stage, D, p, g[p]);
+        get<S>(r, stage + y_bytes, D, p, h[p]);
+      } else {
+        ahead_y.get(p, g[p]);
+        ahead_s.get(p, h[p]);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         h[p][i] *= k;
@@ -513,9 +548,13 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const No
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       float q[8] = {};
-      if (dt) get(r, stage + y_bytes + s_bytes, dt + row * a.dt_stride, D, p, q);
+      if (dt) {
+        if constexpr (WIDE) get<S>(r, stage + y_bytes + s_bytes, D, p, q);
+        else ahead_t.get(p, q);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) g[p][i] = fmaf(k, fmaf(-h[p][i], mean, g[p][i]), q[i]);
+      if (p == P - 1) fetch_ahead(row + step);
       if (a.dx && ring.ok) put<S>(r, static_cast<S*>(a.dx) + row * a.dx_stride, D, p, g[p]);
     }
     if (WIDE) {
