@@ -115,7 +115,7 @@ template <int P, bool WIDE> struct Row {
 };
 // Rows on their way (WIDE): a ring of stages in shared memory for each group, filled by bulk copies of whole rows, up to three arrays' rows to a stage.
 // A stage is read into registers before the row's sum is joined, and filled again right after.  A wait that gives up lets its
-// thread go on (the group's barriers need all of them) without writing anything.
+// warp go on (the group's barriers need all of them) without writing anything.
 constexpr int kMostStages = 3;
 struct Ring {
   unsigned base, bar, bytes, stages, turn, issued;
@@ -128,7 +128,8 @@ struct Ring {
     record(status, COCODC_ERR_TIMEOUT);
     for (unsigned i = issued > stages ? issued - stages : 0; i < issued; ++i) bar_drain(bar + i % stages * 8, (i / stages) & 1);
   }
-  __device__ __forceinline__ void wait() { ok = bar_wait(barrier(), (turn / stages) & 1, stop) && ok; }
+  // one answer for a warp, whose lanes go on together
+  __device__ __forceinline__ void wait() { ok = __all_sync(~0u, bar_wait(barrier(), (turn / stages) & 1, stop)) && ok; }
 };
 __device__ __forceinline__ Ring ring_of(unsigned char* memory, unsigned long long (*bars)[kMostStages], int* stop, int group, unsigned bytes, unsigned stages) {
   return Ring{smem_addr(memory) + group * stages * bytes, smem_addr(&bars[group][0]), bytes, stages, 0, 0, stop, true};
@@ -260,7 +261,7 @@ __device__ __forceinline__ float scale_8(float most) { return fmaxf(most * (1.f 
 
 // Bound by memory: x and residual read, total and y written once.  Rows wait in shared memory rather than in registers (with the next row in
 // registers, two blocks of 128 registers an SM: 135 us), P = 2 leaves three blocks an SM; the 8-bit output costs 27 instructions an element and
-// ten rounds of rows at 4099.  Measured: 65536 x 1024 bf16 with fp32 sums 128 us (6.3 TB/s, 96 % of the copy rate); 4099 x 3200 in
+// seven rounds of rows at 4099.  Measured: 65536 x 1024 bf16 with fp32 sums 128 us (6.3 TB/s, 96 % of the copy rate); 4099 x 3200 in
 // 8 bits 18.8 us (4.9 TB/s); one row of 2048 5.3 us alone with cold caches.
 template <typename X, typename S, int P, bool WIDE>
 __global__ void __launch_bounds__(kThreads, P == 4 || !WIDE ? 2 : 3) k_norm(const NormArgs a) {
