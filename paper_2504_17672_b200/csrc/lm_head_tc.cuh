@@ -429,6 +429,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
         const Out& o = j.o;
         const float scale = o.factor ? o.factor[1] * o.scale : o.scale;
         const bool keep = o.sums && !o.last, whole = o.type == COCODC_F32;   // 32 columns of fp32 are a staged tile of their own
+        // the last piece of the vocabulary can have fewer k-blocks than dx has parts: no product ran for such a part, and the accumulator holds an older tile's
+        const bool empty = t.kb0 == t.kb1;
         if (row0 < j.rows)
           for (int x0 = part * 64; x0 < a.width && n0 + x0 < j.cols; x0 += 128) {
             for (int half = 0; half < 2; ++half) {
@@ -437,6 +439,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
               float v[32];
               tmem_load32(v, src + col);
               tmem_wait_loads();
+              if (empty) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+              }
               float4* sums = sums_at(o, t.number, a.width, col, quarter * 32 + lane);
               if (o.sums && o.add) {
 #pragma unroll
