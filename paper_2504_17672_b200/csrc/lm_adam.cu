@@ -519,7 +519,8 @@ cocodc_status cocodc_lm_adam_create(cocodc_lm_adam** out, cocodc_lm* lm, const c
     plan->count = (int)t.size();
     if (units) {
       const bool ok = cudaMalloc(&plan->d_tensors, t.size() * sizeof(Tensor)) == cudaSuccess &&
-                      cudaMemcpy(plan->d_tensors, t.data(), t.size() * sizeof(Tensor), cudaMemcpyHostToDevice) == cudaSuccess;
+                      cudaMemcpy(plan->d_tensors, t.data(), t.size() * sizeof(Tensor), cudaMemcpyHostToDevice) == cudaSuccess &&
+                      cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;   // the copy may return before it has arrived, and a step on another stream does not wait for it
       if (!ok) {
         cudaGetLastError();
         cudaFree(plan->d_tensors);
