@@ -430,6 +430,8 @@ cocodc_status cocodc_create(cocodc_ctx** ctx_out, const cocodc_partition* part, 
   ok = ok && cudaMemset(c->d_ticket, 0, sizeof(int)) == cudaSuccess;
   ok = ok && cudaMemset(c->d_pending, 0, sizeof(PendingScores)) == cudaSuccess;
   ok = ok && cudaMemset(c->d_hdr, 0, sizeof(PlanHeader)) == cudaSuccess;
+  // these may return before they have arrived, and calls on non-blocking streams do not wait for them
+  ok = ok && cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;
   c->inline_plan = (S <= kInlineSegs);
   if (c->inline_plan) {
     c->table.K = K;

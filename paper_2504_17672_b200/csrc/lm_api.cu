@@ -53,7 +53,8 @@ cocodc_status cocodc_lm_create(cocodc_lm** lm_out, int32_t device) {
   lm->device = device;
   bool ok = cudaDeviceGetAttribute(&lm->sm_count, cudaDevAttrMultiProcessorCount, device) == cudaSuccess;
   ok = ok && cudaMalloc(&lm->d_status, sizeof(int)) == cudaSuccess;
-  ok = ok && cudaMemset(lm->d_status, 0, sizeof(int)) == cudaSuccess;
+  // cudaMemset may return before it is done, and calls on other streams do not wait for it
+  ok = ok && cudaMemset(lm->d_status, 0, sizeof(int)) == cudaSuccess && cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;
   ok = ok && embed_prepare() && glu_prepare() && head_prepare() && norm_prepare();
   if (!ok) {
     cudaGetLastError();

@@ -1,11 +1,15 @@
 """Properties of the norm's, the output head's and the optimizer's host and device code that only their sources show."""
 
-from test_lm_sources_cpu import sources
+import os
+import re
+
+from test_lm_sources_cpu import ROOT
 
 
 def function(file, name):
     """The body of the last function of a source file whose definition begins with this text."""
-    (text,) = [t for f, t in sources() if f == file]
+    with open(os.path.join(ROOT, "paper_2504_17672_b200", "csrc", file)) as h:
+        text = re.sub(r"//[^\n]*", "", h.read())
     at = text.rindex(name)
     return text[at:text.index("\n}\n", at)]
 
@@ -15,3 +19,11 @@ def test_a_plan_is_on_the_device_when_it_is_handed_out():
     body = function("lm_adam.cu", "cocodc_status cocodc_lm_adam_create(")
     last = body.rindex("cudaMemcpy(")
     assert "cudaStreamSynchronize(cudaStreamLegacy)" in body[last:body.index("*out = plan;")]
+
+
+def test_a_handle_is_on_the_device_when_it_is_handed_out():
+    """Nor do they wait for cudaMemset on the default stream, which need not be done when it returns."""
+    for file, name, out in (("lm_api.cu", "cocodc_status cocodc_lm_create(", "*lm_out = lm;"), ("cocodc_api.cu", "cocodc_status cocodc_create(", "*ctx_out = c;")):
+        body = function(file, name)
+        last = max(body.rfind("cudaMemcpy("), body.rfind("cudaMemset("))
+        assert "cudaStreamSynchronize(cudaStreamLegacy)" in body[last:body.index(out)], file
