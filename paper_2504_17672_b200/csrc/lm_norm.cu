@@ -123,9 +123,8 @@ struct Ring {
   bool ok;
   __device__ __forceinline__ unsigned stage() const { return base + turn % stages * bytes; }
   __device__ __forceinline__ unsigned barrier() const { return bar + turn % stages * 8; }
-  // the copies in flight land before the block leaves its shared memory
-  __device__ __forceinline__ void give_up(int* status) const {
-    record(status, COCODC_ERR_TIMEOUT);
+  // the copies in flight land before the block leaves its shared memory (who issued them has waited for all of them as long as it is ok)
+  __device__ __forceinline__ void drain() const {
     for (unsigned i = issued > stages ? issued - stages : 0; i < issued; ++i) bar_drain(bar + i % stages * 8, (i / stages) & 1);
   }
   // one answer for a warp, whose lanes go on together
@@ -139,6 +138,12 @@ __device__ __forceinline__ void ring_start(unsigned long long (*bars)[kMostStage
   if (threadIdx.x == 0) *stop = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   __syncthreads();
+}
+// All threads of the block: a wait that gave up is recorded whichever warp's it was, since the group's others may have been in time.
+__device__ __forceinline__ void ring_end(const Ring& ring, bool issuer, int* status) {
+  if (issuer && !ring.ok) ring.drain();
+  __syncthreads();
+  if (threadIdx.x == 0 && *ring.stop) record(status, COCODC_ERR_TIMEOUT);
 }
 template <typename T> __device__ __forceinline__ Raw8<T> staged8(unsigned at) {
   Raw8<T> r;
@@ -414,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, P == 4 || !WIDE ? 2 : 3) k_norm(cons
       if (a.groups > 1) join.barrier();                             // before the next row's maxima
     }
   }
-  if (WIDE && !ring.ok && r.t == 0) ring.give_up(a.status);
+  if (WIDE) ring_end(ring, r.t == 0, a.status);
 }
 
 // Rows too long for registers: read again after their sum is known; one block a row.
@@ -567,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, P == 4 ? 1 : 2) k_norm_grad(const No
       ++ring.turn;
     }
   }
-  if (WIDE && !ring.ok && r.t == 0) ring.give_up(a.status);
+  if (WIDE) ring_end(ring, r.t == 0, a.status);
   float* const shared_parts = reinterpret_cast<float*>(memory);      // [rows of the block][D] where it has more than one
   if (!a.parts) return;
   float* out = a.parts + (long long)blockIdx.x * D;

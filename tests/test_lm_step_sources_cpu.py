@@ -27,3 +27,13 @@ def test_a_handle_is_on_the_device_when_it_is_handed_out():
         body = function(file, name)
         last = max(body.rfind("cudaMemcpy("), body.rfind("cudaMemset("))
         assert "cudaStreamSynchronize(cudaStreamLegacy)" in body[last:body.index(out)], file
+
+
+def test_the_norm_records_a_wait_that_gave_up_in_any_warp():
+    """Warps of a row give up by themselves: the flag that all of them raise is looked at when the whole block has come to its end."""
+    end = function("lm_norm.cu", "void ring_end(")
+    assert re.search(r"__syncthreads\(\);\s*if \(threadIdx.x == 0 && \*ring.stop\) record\(status, COCODC_ERR_TIMEOUT\);", end)
+    for kernel in ("k_norm(const", "k_norm_grad(const"):
+        body = function("lm_norm.cu", kernel)
+        assert re.search(r"^  if \(WIDE\) ring_end\(ring, r.t == 0, a.status\);$", body, re.M), kernel       # not in the rows' loop
+        assert "COCODC_ERR_TIMEOUT" not in body and "return" not in body[:body.index("ring_end(")].replace("if (WIDE || t >= a.T) return;", "")
