@@ -259,6 +259,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
     if (lane == 0) {
       long long it = 0;
       int sum = 0;                                     // accumulations so far
+      const int parts = MODE == HEAD_LONG ? a.parts : 1, each = a.k_blocks / parts, rest = a.k_blocks % parts;
       bool ok = true;
       for (int turn = 0; ok; ++turn) {
         const int tile = nth_tile(turn);
@@ -271,9 +272,15 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
         const bool a_mn = MODE == HEAD_PRODUCTS && t.kind == 0;
         constexpr bool b_mn = MODE == HEAD_PRODUCTS;
         const unsigned idesc = instr_desc<E>(kBM, a.width, a_mn, b_mn);
-        const int parts = MODE == HEAD_LONG ? a.parts : 1;
+        int last = t.kb0, over = 0;                     // LONG: part q ends at k-block floor(k_blocks (q + 1) / parts)
         for (int q = 0; ok && q < parts; ++q, ++sum) {
-          const int acc = sum & 1, first = MODE == HEAD_LONG ? t.kb1 * q / parts : t.kb0, last = MODE == HEAD_LONG ? t.kb1 * (q + 1) / parts : t.kb1;
+          const int acc = sum & 1, first = last;
+          last = t.kb1;
+          if (MODE == HEAD_LONG) {
+            over += rest;
+            last = first + each + (over >= parts);
+            if (over >= parts) over -= parts;
+          }
           ok = bar_wait(smem_addr(&sh.acc_empty[acc]), (unsigned)((sum >> 1) & 1) ^ 1, stop);
           tc_fence_after();
           for (int kb = first; ok && kb < last; ++kb, ++it) {
