@@ -317,7 +317,7 @@ template <bool EIGHT> __global__ void __launch_bounds__(kThreads, EIGHT ? 4 : 3)
     }
   }
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-  const unsigned step_bits = (unsigned)(a.step_at ? *a.step_at : a.step);
+  const unsigned step_bits = (unsigned)max(a.step_at ? *a.step_at : a.step, 1ll);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const long long last = a.units * (blockIdx.x + 1) / gridDim.x;
   const long long from = a.units * blockIdx.x / gridDim.x;

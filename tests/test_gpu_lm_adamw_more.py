@@ -2,7 +2,7 @@
 
 import pytest
 import torch
-from test_gpu_lm_adamw import E24, HYPER, gen, randn, states
+from test_gpu_lm_adamw import E24, E4M3, HYPER, gen, randn, states
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,24 @@ def test_a_plan_is_stepped_at_once_on_another_stream(B, ops):
     side.synchronize()
     assert torch.equal(m, want[0]) and torch.equal(v, want[1])
     assert bool(((p.double() - (want[3].double() - want[4].double())).abs() <= 8 * E24 * want[4].double().abs() + E24 * p.double().abs() + 1e-45).all())
+
+
+def test_a_step_below_one_is_step_one_for_the_random_bits_too(B):
+    ops = B.LmOps(0)
+    g = gen(32)
+    n = 2000
+    p, grad = randn(g, n), randn(g, n)
+
+    def stepped(**k):
+        q, m, v = p.clone(), torch.zeros(n, device="cuda").to(E4M3), torch.zeros(n, device="cuda").to(E4M3)
+        ms, vs = torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda")
+        ops.cocodc_lm_adamw(B.AdamTensors(ops, [q], [grad], [m], [v], m_scales=[ms], v_scales=[vs]), 1e-3, seed=5, **k)
+        return q, m.view(torch.uint8), v.view(torch.uint8), ms, vs
+
+    one = stepped(step=1)
+    assert ops.cocodc_lm_poll_status() == B.OK
+    for at in (0, -7):
+        other = stepped(step_at=torch.tensor([at], device="cuda"))
+        assert ops.cocodc_lm_poll_status() == B.ERR_INVALID_ARG
+        assert all(torch.equal(a, b) for a, b in zip(one, other))
+    assert not torch.equal(stepped(step=2)[1], one[1])
