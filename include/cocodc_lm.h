@@ -246,7 +246,8 @@ cocodc_status cocodc_lm_adam_destroy(cocodc_lm_adam* plan);
 /*
  * One step.  step >= 1 is the number of this step, or *step_at (device memory) where that is not NULL, so that a captured step can
  * be replayed; grad_scale and lr_scale are fp32 scalars in device memory (clipping, a schedule) or NULL for 1; the factor on lr is
- * lr * *lr_scale.  0 <= beta < 1, eps >= 0, lr finite.  A *step_at below 1 counts as 1 and records COCODC_ERR_INVALID_ARG.
+ * lr * *lr_scale.  0 <= beta < 1, lr finite, eps 0 or from 2^-126 to 2^125 (with eps = 0 an element whose v is 0 becomes NaN or infinite).  A *step_at
+ * below 1 counts as 1 and records COCODC_ERR_INVALID_ARG.
  */
 cocodc_status cocodc_lm_adamw(cocodc_lm* lm, const cocodc_lm_adam* plan, double lr, double beta1, double beta2, double eps, int64_t step,
                               const int64_t* step_at, const float* grad_scale, const float* lr_scale, int64_t seed, void* stream);

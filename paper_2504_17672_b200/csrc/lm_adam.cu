@@ -546,7 +546,7 @@ cocodc_status cocodc_lm_adam_destroy(cocodc_lm_adam* plan) {
 cocodc_status cocodc_lm_adamw(cocodc_lm* lm, const cocodc_lm_adam* plan, double lr, double beta1, double beta2, double eps, int64_t step,
                               const int64_t* step_at, const float* grad_scale, const float* lr_scale, int64_t seed, void* stream) {
   if (!lm || !plan || plan->device != lm->device || !std::isfinite(lr) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) ||
-      !(eps >= 0 && eps <= 1) || (!step_at && step < 1))
+      !(eps == 0 || (eps >= 0x1p-126 && eps <= 0x1p125)) || (!step_at && step < 1))         // a smaller eps would be 0 for the approximate inverse, with a larger one that is 0
     return COCODC_ERR_INVALID_ARG;
   if (!on_boundary(step_at, 8) || !on_boundary(grad_scale, 4) || !on_boundary(lr_scale, 4)) return COCODC_ERR_ALIGNMENT;
   if (plan->units == 0) return COCODC_OK;

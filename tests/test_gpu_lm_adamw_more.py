@@ -55,3 +55,19 @@ def test_a_step_below_one_is_step_one_for_the_random_bits_too(B):
         assert ops.cocodc_lm_poll_status() == B.ERR_INVALID_ARG
         assert all(torch.equal(a, b) for a, b in zip(one, other))
     assert not torch.equal(stepped(step=2)[1], one[1])
+
+
+@pytest.mark.parametrize("eps", [1.5, 1e6, 0.0, 2.0 ** -126])
+def test_any_eps(B, ops, eps):
+    g = gen(33)
+    n = 3000
+    p, grad, m = (randn(g, n) for _ in range(3))
+    v = randn(g, n).square()
+    m[1000:], v[1000:], grad[1000:] = 0, 0, 0                    # never used: stands still with any eps above zero
+    want = states(p, grad, m, v, 1e-2, 3, 0.0, 1.0, **{**HYPER, "eps": eps})
+    ops.cocodc_lm_adamw(B.AdamTensors(ops, [p], [grad], [m], [v]), 1e-2, step=3, eps=eps)
+    assert torch.equal(m, want[0]) and torch.equal(v, want[1])
+    used = slice(0, n if eps else 1000)
+    got, s = p[used].double(), want[4][used].double()
+    assert bool(((got - (want[3][used].double() - s)).abs() <= 8 * E24 * s.abs() + E24 * got.abs() + 1e-45).all())
+    assert eps or bool(torch.isnan(p[1000:]).all())              # 0 / 0
