@@ -232,7 +232,7 @@ typedef struct {
   void* copy;                       /* [n] BF16 or F16, or NULL */
   int64_t n;                        /* 0 <= n <= 2^38 */
   int32_t grad_type, copy_type;
-  float decay;                      /* of this tensor, >= 0 */
+  float decay;                      /* of this tensor, >= 0, finite */
   int32_t reserved;                 /* 0 */
 } cocodc_lm_tensor;
 typedef struct cocodc_lm_adam cocodc_lm_adam;   /* a plan: belongs to the handle's device */

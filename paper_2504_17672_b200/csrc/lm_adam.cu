@@ -464,7 +464,7 @@ cocodc_status check(const cocodc_lm_tensor* tensors, int64_t count, int32_t bits
   for (int64_t i = 0; i < count; ++i) {
     const cocodc_lm_tensor& t = tensors[i];
     if (t.n < 0 || t.n > (int64_t(1) << 38) || !known_type(t.grad_type) || (t.copy && t.copy_type != COCODC_BF16 && t.copy_type != COCODC_F16) ||
-        !(t.decay >= 0.f && t.decay <= 1e30f) || t.reserved != 0)
+        !(t.decay >= 0.f && std::isfinite(t.decay)) || t.reserved != 0)
       return COCODC_ERR_INVALID_ARG;
     const int64_t units = (t.n + kUnit - 1) / kUnit;
     if (t.n > 0 && (!t.p || !t.grad || !t.m || !t.v || (bits == 8 && (!t.m_scale || !t.v_scale)))) return COCODC_ERR_INVALID_ARG;

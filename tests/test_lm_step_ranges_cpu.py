@@ -28,3 +28,11 @@ def test_eps(B, lib, handle, empty, eps):  # noqa: F811
                                  dict(beta1=1.0), dict(beta2=-0.1), dict(lr=float("inf")), dict(step=0)])
 def test_refusals(B, lib, handle, empty, bad):  # noqa: F811
     assert adamw(lib, handle, empty, **bad) == B.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("decay", [0.0, 0.1, 1e30, 2e30, 3.4e38])
+def test_any_finite_decay(B, lib, handle, decay):  # noqa: F811
+    plan = ctypes.c_void_p()
+    code = lib.cocodc_lm_adam_create(ctypes.byref(plan), handle, (B._Tensor * 1)(tensor(B, decay=decay)), 1, 32)
+    assert code == (B.OK if plan else B.ERR_CUDA)                # past the checks: without a GPU the device is what fails
+    lib.cocodc_lm_adam_destroy(plan)
