@@ -518,10 +518,14 @@ cocodc_status cocodc_lm_adam_create(cocodc_lm_adam** out, cocodc_lm* lm, const c
     plan->units = units;
     plan->count = (int)t.size();
     if (units) {
-      const bool ok = cudaMalloc(&plan->d_tensors, t.size() * sizeof(Tensor)) == cudaSuccess &&
-                      cudaMemcpy(plan->d_tensors, t.data(), t.size() * sizeof(Tensor), cudaMemcpyHostToDevice) == cudaSuccess &&
-                      cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;   // the copy may return before it has arrived, and a step on another stream does not wait for it
-      if (!ok) {
+      const cocodc_status got = allocate(&plan->d_tensors, t.size() * sizeof(Tensor));
+      if (got != COCODC_OK) {
+        delete plan;
+        return got;
+      }
+      // the copy may return before it has arrived, and a step on another stream does not wait for it
+      if (cudaMemcpy(plan->d_tensors, t.data(), t.size() * sizeof(Tensor), cudaMemcpyHostToDevice) != cudaSuccess ||
+          cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {
         cudaGetLastError();
         cudaFree(plan->d_tensors);
         delete plan;

@@ -51,8 +51,12 @@ cocodc_status cocodc_lm_create(cocodc_lm** lm_out, int32_t device) {
   cocodc_lm* lm = new (std::nothrow) cocodc_lm();
   if (!lm) return COCODC_ERR_NOMEM;
   lm->device = device;
+  const cocodc_status got = cocodc_lm_impl::allocate(&lm->d_status, sizeof(int));
+  if (got != COCODC_OK) {
+    delete lm;
+    return got;
+  }
   bool ok = cudaDeviceGetAttribute(&lm->sm_count, cudaDevAttrMultiProcessorCount, device) == cudaSuccess;
-  ok = ok && cudaMalloc(&lm->d_status, sizeof(int)) == cudaSuccess;
   // cudaMemset may return before it is done, and calls on other streams do not wait for it
   ok = ok && cudaMemset(lm->d_status, 0, sizeof(int)) == cudaSuccess && cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;
   ok = ok && embed_prepare() && glu_prepare() && head_prepare() && norm_prepare();

@@ -66,6 +66,14 @@ inline cocodc_status start(cocodc_lm* lm, void (*kernel)(P...), dim3 grid, unsig
   return COCODC_OK;
 }
 
+// Memory that a handle or a plan keeps.
+template <typename T> inline cocodc_status allocate(T** p, size_t bytes) {
+  const cudaError_t e = cudaMalloc(p, bytes);
+  if (e == cudaSuccess) return COCODC_OK;
+  cudaGetLastError();
+  return e == cudaErrorMemoryAllocation ? COCODC_ERR_NOMEM : COCODC_ERR_CUDA;
+}
+
 inline bool known_type(int32_t t) { return t == COCODC_F32 || t == COCODC_BF16 || t == COCODC_F16; }
 inline int type_bytes(int32_t t) { return t == COCODC_F32 ? 4 : 2; }
 inline int index_bytes(int32_t t) { return t == COCODC_I32 ? 4 : 8; }

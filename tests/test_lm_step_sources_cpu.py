@@ -37,3 +37,11 @@ def test_the_norm_records_a_wait_that_gave_up_in_any_warp():
         body = function("lm_norm.cu", kernel)
         assert re.search(r"^  if \(WIDE\) ring_end\(ring, r.t == 0, a.status\);$", body, re.M), kernel       # not in the rows' loop
         assert "COCODC_ERR_TIMEOUT" not in body and "return" not in body[:body.index("ring_end(")].replace("if (WIDE || t >= a.T) return;", "")
+
+
+def test_no_memory_on_the_device_is_said_so():
+    """As the header lists it, and as cocodc_create answers."""
+    assert re.search(r"return e == cudaErrorMemoryAllocation \? COCODC_ERR_NOMEM : COCODC_ERR_CUDA;", function("lm_common.cuh", "inline cocodc_status allocate("))
+    for file, name in (("lm_adam.cu", "cocodc_status cocodc_lm_adam_create("), ("lm_api.cu", "cocodc_status cocodc_lm_create(")):
+        body = function(file, name)
+        assert "cudaMalloc" not in body and re.search(r"got = [\w:]*allocate\([^;]*;\s*if \(got != COCODC_OK\) \{\s*delete \w+;\s*return got;", body), file
