@@ -56,7 +56,7 @@ struct AdamArgs {
 };
 
 // One round of multiplications and shifts that spreads every bit over the word (the 32-bit finaliser with Appleby's constants).
-__device__ __forceinline__ unsigned mix(unsigned x) {
+__host__ __device__ __forceinline__ unsigned mix(unsigned x) {
   x = (x ^ x >> 16) * 0x85EBCA6Bu;
   x = (x ^ x >> 13) * 0xC2B2AE35u;
   return x ^ x >> 16;
@@ -557,7 +557,8 @@ cocodc_status cocodc_lm_adamw(cocodc_lm* lm, const cocodc_lm_adam* plan, double 
   DeviceScope scope(lm->device);
   if (!scope.ok) return COCODC_ERR_CUDA;
   const AdamArgs a{plan->d_tensors, plan->count, plan->units, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
-                   (float)(lr / (1.0 - std::pow(beta1, (double)step))), (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step))), lr, beta1, beta2, step, reinterpret_cast<const long long*>(step_at), grad_scale, lr_scale, (unsigned)seed, lm->d_status};
+                   (float)(lr / (1.0 - std::pow(beta1, (double)step))), (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step))), lr, beta1, beta2, step, reinterpret_cast<const long long*>(step_at), grad_scale, lr_scale,
+                   (unsigned)seed ^ mix((unsigned)((uint64_t)seed >> 32)), lm->d_status};
   const long long blocks = (plan->units + kWarps - 1) / kWarps, most = (long long)lm->sm_count * (plan->bits == 8 ? 4 : 3);
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   cudaStream_t st = static_cast<cudaStream_t>(stream);

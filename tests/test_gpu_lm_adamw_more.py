@@ -71,3 +71,21 @@ def test_any_eps(B, ops, eps):
     got, s = p[used].double(), want[4][used].double()
     assert bool(((got - (want[3][used].double() - s)).abs() <= 8 * E24 * s.abs() + E24 * got.abs() + 1e-45).all())
     assert eps or bool(torch.isnan(p[1000:]).all())              # 0 / 0
+
+
+def test_every_bit_of_the_seed_counts(B, ops):
+    g = gen(34)
+    n = 5000
+    grad = randn(g, n)
+
+    def codes(seed):
+        p, m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda").to(E4M3), torch.zeros(n, device="cuda").to(E4M3)
+        scales = [torch.zeros((n + 255) // 256, device="cuda") for _ in range(2)]
+        ops.cocodc_lm_adamw(B.AdamTensors(ops, [p], [grad], [m], [v], m_scales=[scales[0]], v_scales=[scales[1]]), 1e-3, step=1, seed=seed)
+        return m.view(torch.uint8).clone()
+
+    first = codes(5)
+    assert torch.equal(first, codes(5))
+    for seed in (5 + 2 ** 32, 5 + 2 ** 40, 5 - 2 ** 63, 5 - 2 ** 32):
+        # about half of the codes are rounded the other way with other bits
+        assert int((codes(seed) != first).sum()) > n // 8, seed
