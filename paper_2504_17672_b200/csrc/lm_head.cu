@@ -174,7 +174,7 @@ template <typename E> __device__ __forceinline__ void deliver(const Out& o, long
     o.sums[r * cols + c] = v;
     return;
   }
-  v *= o.factor ? o.factor[1] * o.scale : o.scale;
+  v = Back(o)(v);
   if (o.type == COCODC_F32) {
     float* p = static_cast<float*>(o.out) + r * o.ld + c;
     *p = o.accumulate ? *p + v : v;

@@ -71,5 +71,16 @@ struct Out {
   const float* factor;
   float scale;
 };
+// What the products are multiplied by at the end, in two steps where one number would leave fp32's range (and 0 times it be NaN).
+struct Back {
+  float one, two = 1.f;
+  __device__ __forceinline__ explicit Back(const Out& o) : one(o.factor ? o.factor[1] * o.scale : o.scale) {
+    if (!(one >= 0x1p-126f && one < INFINITY)) {
+      one = o.factor ? o.factor[1] : 1.f;
+      two = o.scale;
+    }
+  }
+  __device__ __forceinline__ float operator()(float v) const { return v * one * two; }
+};
 
 }  // namespace cocodc_lm_impl

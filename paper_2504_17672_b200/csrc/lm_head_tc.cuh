@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
       } else {
         const HeadJob& j = a.job[t.kind];
         const Out& o = j.o;
-        const float scale = o.factor ? o.factor[1] * o.scale : o.scale;
+        const Back back(o);
         const bool keep = o.sums && !o.last, whole = o.type == COCODC_F32;   // 32 columns of fp32 are a staged tile of their own
         // the last piece of the vocabulary can have fewer k-blocks than dx has parts: no product ran for such a part, and the accumulator holds an older tile's
         const bool empty = t.kb0 == t.kb1;
@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head_tc(const __grid_consta
                 continue;
               }
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] *= scale;
+              for (int i = 0; i < 32; ++i) v[i] = back(v[i]);
               if (whole || half == 0) {
                 if (lane == 0) store_wait_read<0>();
                 __syncwarp();
@@ -501,7 +501,7 @@ template <typename E> __global__ void __launch_bounds__(256) k_head_add(const __
   const HeadTile t = head_tile<HEAD_PRODUCTS>(a, (a.first == 1 ? 0 : a.job[0].tiles) + tile);
   const int y = t.m * kBM + row, col = blockIdx.y * 128 + threadIdx.x / 8 * 4, x = t.n * a.width + col;
   if (y >= j.rows || col >= a.width || x >= j.cols) return;
-  const float scale = j.o.factor ? j.o.factor[1] * j.o.scale : j.o.scale;
+  const Back back(j.o);
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   for (int z = 0; z < j.splits; z += 4) {
     float4 u[4];                                                      // together on their way
@@ -517,7 +517,7 @@ template <typename E> __global__ void __launch_bounds__(256) k_head_add(const __
   }
   E* out = static_cast<E*>(j.o.out) + y * j.o.ld + x;
   for (int i = 0; i < 4; ++i)
-    if (x + i < j.cols) out[i] = from_f32<E>(v[i] * scale);
+    if (x + i < j.cols) out[i] = from_f32<E>(back(v[i]));
 }
 
 }  // namespace cocodc_lm_impl
