@@ -186,7 +186,9 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
  * Products accumulate in fp32 (on the tensor cores in parts of at most 1024, which are added in fp32) and the logits are not rounded to fewer bits.  A row whose logits hold a NaN or +Inf (a product or
  * sum beyond fp32's range is one) has NaN in lse and logp;
  * -Inf counts as probability 0, and a row of nothing but -Inf has lse = -Inf and log probabilities -Inf.
- * T <= 2^31 - 1, D <= 2^31 - 1, V <= 2^30, T D and V D <= 2^48.
+ * T <= 2^31 - 1, D <= 2^31 - 1, V <= 2^30, T D and V D <= 2^48. Of these, sizes of more tiles than a launch takes are refused: ceil(T / 64) ceil(V / w) >= 2^31
+ * here (w from 16 to 256 by the sizes: a workspace of 2^41 bytes and more); in the gradient ceil(T / 128) ceil(D / 64) > 14510024, and
+ * ceil(w / 128) ceil(D / 64) >= 2^29 for pieces of w columns (below).
  */
 uint64_t cocodc_lm_head_workspace(int64_t T, int64_t D, int64_t V);
 cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t x_stride, const void* table, int64_t table_stride,

@@ -321,7 +321,9 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
     return COCODC_ERR_INVALID_ARG;
   if (!logp != !targets || (!logp && !lse)) return T == 0 ? COCODC_OK : COCODC_ERR_INVALID_ARG;
   if (T == 0) return COCODC_OK;
-  if (!x || !table || !workspace || workspace_bytes < cocodc_lm_head_workspace(T, D, V)) return COCODC_ERR_INVALID_ARG;
+  unsigned grid;                                      // of k_head_plain; k_head_tc has as many tiles at most
+  if (!x || !table || !workspace || workspace_bytes < cocodc_lm_head_workspace(T, D, V) || !grid_of(T, kTile, V, strip_width(T, V), &grid))
+    return COCODC_ERR_INVALID_ARG;
   const int ib = targets ? index_bytes(targets_type) : 4;
   if (!on_boundary(x, 2) || !on_boundary(table, 2) || !on_boundary(targets, ib) || !on_boundary(logp, 4) || !on_boundary(lse, 4) ||
       !on_boundary(workspace, 16))
@@ -348,8 +350,6 @@ cocodc_status cocodc_lm_head(cocodc_lm* lm, int32_t type, const void* x, int64_t
   a.picked = static_cast<float*>(workspace);
   a.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + up(T, 4) * 16);
   const bool tensor = rows_aligned(x, x_stride, 2) && rows_aligned(table, table_stride, 2);
-  unsigned grid;
-  if (!grid_of(T, kTile, V, a.width, &grid)) return COCODC_ERR_INVALID_ARG;
   const cocodc_status status = with_half(type, [&](auto e) {
     using E = decltype(e);
     if (tensor) {
@@ -385,6 +385,12 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
   if (T > 0 && (!x || !table || !lse || !dlogp != !targets || (!dlogp && !dlse) || !workspace ||
                 workspace_bytes < cocodc_lm_head_grad_workspace(T, D, V)))
     return COCODC_ERR_INVALID_ARG;
+  // grids of the kernels for any strides, tiles of the tensor-core kernel's products
+  const GradLayout l = T > 0 ? grad_layout(T, D, V) : GradLayout{};
+  unsigned g1 = 0, g2 = 0, g3 = 0;
+  if (T > 0 && (!grid_of(T, kTile, l.width, kTile, &g1) || !grid_of(T, kTile, D, kTile, &g2) || !grid_of(l.width, kTile, D, kTile, &g3) ||
+                up(T, kBM) * up(D, 64) > INT32_MAX / kSms || up(l.width, kBM) * up(D, 64) > INT32_MAX / 4))
+    return COCODC_ERR_INVALID_ARG;
   const int ib = targets ? index_bytes(targets_type) : 4, wb = dtable_type == COCODC_F32 ? 4 : 2;
   if (!on_boundary(x, 2) || !on_boundary(table, 2) || !on_boundary(dx, 2) || !on_boundary(dtable, wb) || !on_boundary(targets, ib) ||
       !on_boundary(lse, 4) || !on_boundary(dlogp, 4) || !on_boundary(dlse, 4) || !on_boundary(workspace, 16))
@@ -411,7 +417,6 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
                  ? start(lm, k_head_zero<float>, blocks, 256, 0, st, 1, static_cast<float*>(dtable), (long long)dtable_stride, (long long)V, (long long)D)
                  : start(lm, k_head_zero<E>, blocks, 256, 0, st, 1, static_cast<E*>(dtable), (long long)dtable_stride, (long long)V, (long long)D);
     }
-    const GradLayout l = grad_layout(T, D, V);
     char* ws = static_cast<char*>(workspace);
     DzArgs d{};
     d.T = T;
@@ -435,12 +440,8 @@ cocodc_status cocodc_lm_head_grad(cocodc_lm* lm, int32_t type, const void* x, in
       const cocodc_status s = start(lm, k_head_factor, 1, 1024, 0, st, 1, h, dlogp, dlse, reinterpret_cast<float*>(ws));
       if (s != COCODC_OK) return s;
     }
-    unsigned g1, g2, g3;
-    if (!grid_of(T, kTile, l.width, kTile, &g1) || !grid_of(T, kTile, D, kTile, &g2) || !grid_of(l.width, kTile, D, kTile, &g3))
-      return COCODC_ERR_INVALID_ARG;
     const bool tensor = rows_aligned(x, x_stride, 2) && rows_aligned(table, table_stride, 2) && (!dx || rows_aligned(dx, dx_stride, 2)) &&
                         (!dtable || rows_aligned(dtable, dtable_stride, wb));
-    if (up(T, kBM) * up(D, 64) > INT32_MAX / kSms || up(l.width, kBM) * up(D, 64) > INT32_MAX / 4) return COCODC_ERR_INVALID_ARG;
     const int parts = tensor ? dx_parts(T, D, l.width) : 1;
     const E *xe = static_cast<const E*>(x), *we = static_cast<const E*>(table), *dz = reinterpret_cast<const E*>(ws + l.dz);
     for (int64_t v0 = 0; v0 < V; v0 += l.width) {
