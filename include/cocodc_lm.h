@@ -183,7 +183,7 @@ cocodc_status cocodc_lm_norm_grad(cocodc_lm* lm, const void* dy, int32_t dy_type
  *   lse[t]  = log sum_j exp(z_j)
  *   logp[t] = z_y - lse, y = targets[t]; 0 where y < 0
  *   x [T][D]; table W [V][D]; both BF16 or both F16.  0 < scale <= 1e30.  logp (with targets) and lse: fp32, packed, one may be NULL.
- * Products accumulate in fp32 (on the tensor cores in parts of at most 1024, which are added in fp32) and the logits are not rounded to fewer bits.  A row whose logits hold a NaN or +Inf (a product or
+ * Products accumulate in fp32 (on the tensor cores, which cut instead of rounding, in parts of at most 704, which are added in fp32) and the logits are not rounded to fewer bits.  A row whose logits hold a NaN or +Inf (a product or
  * sum beyond fp32's range is one) has NaN in lse and logp;
  * -Inf counts as probability 0, and a row of nothing but -Inf has lse = -Inf and log probabilities -Inf.
  * T <= 2^31 - 1, D <= 2^31 - 1, V <= 2^30, T D and V D <= 2^48. Of these, sizes of more tiles than a launch takes are refused: ceil(T / 64) ceil(V / w) >= 2^31

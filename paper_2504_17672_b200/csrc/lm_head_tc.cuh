@@ -6,9 +6,9 @@
 //   warps 2-9 epilogue, while the other accumulator fills; a thread has a row of the tile, two of them share it
 // STATS     a tile of x W^T is reduced where it lies: each thread finds its row's largest logit and the sum of powers of two among the
 //           tile's columns, and picks the target's logit; 8 bytes a row and tile leave the chip instead of 512.  The tensor cores cut the sums that
-//           they accumulate instead of rounding them, always towards zero: the log-sum-exp of 2048 products came out 6e-7 to 1.4e-6 too small.  So long
-//           contractions (LONG, from kLongBlocks k-blocks on) are accumulated in parts of at most kPartBlocks, which the epilogue adds in registers: a
-//           quarter of that error at 2048, as good as sums in fp32, for 3 % of the time.
+//           they accumulate instead of rounding them, always towards zero: the log-sum-exp of 2048 products came out 7.5e-7 to 9.4e-7 too small on average, 4.6e-7 at
+//           1024.  So long contractions (LONG, from kLongBlocks k-blocks on) are accumulated in parts of at most kPartBlocks, which the epilogue adds in registers:
+//           1.8e-7 to 2.1e-7 from 1024 on (sums rounded in fp32: 3e-8 to 8e-8), for 3 % of the time.
 // DZ        the same product; the epilogue forms dz from the row's lse and factors and writes it in 16 bits, 64 staged columns at a time.
 // PRODUCTS  dtable = dz^T x and dx = dz W of one piece in one launch: a tile's number tells which of the two it belongs to.  Tiles differ in
 //           length, so that a block takes the next one when it is ready (a counter that DZ set back), the long ones first.  dx's sums over
@@ -52,7 +52,8 @@ struct HeadTc {
 };
 
 constexpr int kHeadStages = 4, kHeadEpilogue = 8, kHeadThreads = 64 + kHeadEpilogue * 32;
-constexpr int kPartBlocks = 8, kLongBlocks = 17;
+// Below 12 k-blocks the second accumulation costs more than 4 % (9 k-blocks: 270 -> 287 us, 12: 546 -> 562, 16: 452 -> 459 at 8192 rows) and the error is below 3e-7.
+constexpr int kPartBlocks = 8, kLongBlocks = 12;
 constexpr int kTileRing = 4;      // tiles that the producer may be ahead
 constexpr unsigned kHeadStage = kABytes + 256 * kBK * 2, kHeadSmem = 1024 + kHeadStages * kHeadStage + kHeadEpilogue * kOutBytes;
 // Tiles of consecutive rows that go through one column of tiles in turn (as in the gated block).
