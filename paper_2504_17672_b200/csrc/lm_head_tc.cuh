@@ -18,7 +18,7 @@
 // (81 %), PRODUCTS of them 768 us (1.41 PFLOP/s, 84 %; with two and four copies for an MN-major operand's slabs 864 us, 66 %).  Back to back the power cap
 // lowers the clock: 890-905 us forward, 2.74 ms backward.  dx and dtable in a launch each took 405 + 372 us, together 743.  Bringing
 // tiles to L2 ahead of time made all of it slower (PRODUCTS 864 -> 925 us); what feeds the tensor cores is the way from L2, 49 KB a k-block.
-// 1333 x 768 x 50257: 94 us (15 rounds of tiles for 14.6).  One row of 2048 x 32000: 29 us, 20 of which are the table's bytes; 4 are the start and
+// 1333 x 768 x 50257 LONG 99 us (15 rounds of tiles for 14.6; without parts 94).  One row of 2048 x 32000: 29 us, 20 of which are the table's bytes; 4 are the start and
 // end of the kernel, 2 the joining one.
 #pragma once
 

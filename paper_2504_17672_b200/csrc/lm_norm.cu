@@ -285,7 +285,7 @@ __device__ __forceinline__ float rms_scale(float sum, float inv_d, float eps) { 
 __device__ __forceinline__ float scale_8(float most) { return fmaxf(most * (1.f / kMost8), kLeastScale); }
 
 // Bound by memory: x and residual read, total and y written once.  Rows wait in shared memory rather than in registers (with the next row in
-// registers, two blocks of 128 registers an SM: 135 us), P = 2 leaves three blocks an SM; the 8-bit output costs 27 instructions an element and
+// registers, two blocks of 128 registers an SM: 135 us), P = 2 leaves three blocks an SM; the 8-bit output costs 28 instructions an element and
 // seven rounds of rows at 4099.  Measured: 65536 x 1024 bf16 with fp32 sums 128 us (6.3 TB/s, 96 % of the copy rate); 4099 x 3200 in
 // 8 bits 19.3 us (4.8 TB/s); one row of 2048 5.3 us alone with cold caches.
 template <typename X, typename S, int P, bool WIDE>
