@@ -673,7 +673,7 @@ template <typename F> cocodc_status with_types(int32_t x, int32_t s, F&& f) {
   if (x == COCODC_BF16) return s == COCODC_F32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
   return s == COCODC_F32 ? f(__half(), float()) : f(__half(), __half());
 }
-constexpr unsigned kSharedOfSm = 227 * 1024;
+constexpr unsigned kSharedOfSm = 227 * 1024, kMostShared = kSharedOfSm - 4096;      // of an SM; of a block, beside what the kernels declare
 template <int N> using Int = std::integral_constant<int, N>;
 
 unsigned grid_for(const cocodc_lm* lm, int64_t T, int rows, int per_sm) {
@@ -712,7 +712,7 @@ template <typename F> cocodc_status with_shape(const cocodc_lm* lm, int64_t T, i
 }
 // Stages of a group's ring: what the loads of an SM need to be on their way at a time, but no more than there are rows.
 int stages_for(unsigned bytes, int rows, int blocks_by_regs, int64_t T, unsigned grid_rows) {
-  const unsigned share = kSharedOfSm / blocks_by_regs - 2048;
+  const unsigned part = kSharedOfSm / blocks_by_regs - 2048, share = part < kMostShared ? part : kMostShared;
   int n = (int)(share / (bytes * rows));
   n = n > kMostStages ? kMostStages : n < 2 ? 2 : n;
   const int64_t each = (T + grid_rows - 1) / grid_rows;
@@ -744,7 +744,7 @@ namespace cocodc_lm_impl {
 bool norm_prepare() {
   bool ok = true;
   const auto allow = [&](auto kernel) {
-    ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedOfSm - 4096) == cudaSuccess;
+    ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) == cudaSuccess;
   };
   for (int32_t x : {COCODC_F32, COCODC_BF16, COCODC_F16})
     for (int32_t s : {x, (int32_t)COCODC_F32})

@@ -1,9 +1,10 @@
 """More of the norm: its output in 8 bits code by code, the accuracy of its scale.  Helpers and bounds of test_gpu_lm_norm.py."""
 
 import pytest
+import test_gpu_lm_norm as N
 import torch
 from test_gpu_lm_norm import E4M3, EPS, F32
-from test_gpu_lm_ops import gen, placed, put, randn
+from test_gpu_lm_ops import gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +58,9 @@ def test_codes_beside_an_infinite_one(ops, T, D, group):
     assert bool(torch.isnan(f[:, 130]).all())
     f[:, 130] = 0
     assert bool((f[:, spoiled] == 0).all()) and torch.equal(f[:, ~spoiled], want.float()[:, ~spoiled])
+
+
+@pytest.mark.parametrize("D,ty,ts", [(6344, F32, F32), (6400, F32, F32), (7616, torch.bfloat16, F32), (7680, torch.bfloat16, F32), (7680, torch.float16, F32)])
+def test_widths_whose_rings_fill_shared_memory(ops, D, ty, ts):
+    """Three rows of three arrays take all but a few hundred bytes of what a block may have, as soon as blocks have three rows or more."""
+    N.test_norm_grad(ops, 700, D, ty, ts, F32, F32, True)
