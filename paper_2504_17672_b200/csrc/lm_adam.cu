@@ -80,6 +80,11 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
   return v;
 }
+__device__ __forceinline__ f32x2 mul2_cut(f32x2 a, f32x2 b) {
+  f32x2 v;
+  asm("mul.rz.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
 __device__ __forceinline__ f32x2 both(float x) { return pair_of(x, x); }
 // one by one: the two instructions of a packed product and sum come out of the assembler as one, which rounds once
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
@@ -90,7 +95,7 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
 // A number times 2^-120 (a unit's largest magnitude was brought to 448 before) to an e4m3 code in the highest byte, without its sign: up with
 // probability (what is cut off) / (spacing).  There the exponents of e4m3 are those of fp32, below its smallest normal number too (2^-126
 // here and there), so that the code is what stands above the lowest 20 bits; 16 random bits, here bytes 1 and 2, are added to
-// those.  The number may be 448 + 3 ulp: no carry comes of it.
+// those.  Below that number the product with 2^-120 is cut, not rounded: rounded it could reach the next code without them.  The number may be 448 + 3 ulp: no carry comes of it.
 __device__ __forceinline__ unsigned code_of(float x, unsigned random) { return (__float_as_uint(x) << 4) + random; }
 __device__ __forceinline__ float2 widen_e4m3(unsigned short v) {
   unsigned h;
@@ -266,7 +271,7 @@ __device__ __forceinline__ void step_of(Eight& x, const Factors& f, float& ms, f
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float2 m = halves(x.m[2 * h + i]), r = halves(root[2 * h + i]);
-      const float2 y = halves(mul2(mul2(x.m[2 * h + i], im), low)), z = halves(mul2(mul2(root[2 * h + i], iv), low));
+      const float2 y = halves(mul2_cut(mul2(x.m[2 * h + i], im), low)), z = halves(mul2_cut(mul2(root[2 * h + i], iv), low));
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int n = 2 * i + j;

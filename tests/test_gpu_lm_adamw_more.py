@@ -2,7 +2,7 @@
 
 import pytest
 import torch
-from test_gpu_lm_adamw import E24, E4M3, HYPER, gen, randn, states
+from test_gpu_lm_adamw import E24, E4M3, HYPER, bits_of, gen, randn, states
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +89,24 @@ def test_every_bit_of_the_seed_counts(B, ops):
     for seed in (5 + 2 ** 32, 5 + 2 ** 40, 5 - 2 ** 63, 5 - 2 ** 32):
         # about half of the codes are rounded the other way with other bits
         assert int((codes(seed) != first).sum()) > n // 8, seed
+
+
+def test_small_codes_are_cut_exactly(B, ops):
+    """Below 2^-6 the 8-bit numbers are 2^-9 apart: floor(512 y + r / 65536) of them, y = value / scale in fp32, r 16 random bits.  Of so many values some come so near a
+    whole number that rounding any part of this would tell."""
+    g = gen(35)
+    n = 2 ** 24
+    grad = torch.exp2(-6.0 - 5 * torch.rand(n, generator=g, device="cuda"))
+    grad[::256] = 448.0                                            # the scale is 1
+    m, v = torch.zeros(n, device="cuda").to(E4M3), torch.zeros(n, device="cuda").to(E4M3)
+    scales = [torch.zeros(n // 256, device="cuda") for _ in range(2)]
+    plan = B.AdamTensors(ops, [torch.zeros(n, device="cuda")], [grad], [m], [v], m_scales=[scales[0]], v_scales=[scales[1]])
+    ops.cocodc_lm_adamw(plan, 0.0, step=1, beta1=0.0, beta2=0.0, seed=9)
+    r = bits_of(9, 1, 0, n)
+    root = torch.sqrt(grad * grad)
+    for codes, x, scale, bits in ((m, grad, scales[0], r & 0xFFFF), (v, root, scales[1], r >> 16)):
+        y = x * (1 / scale).repeat_interleave(256)
+        want = torch.floor(y.double() * 512 + bits.double() / 65536).clamp(min=1.0 if x is root else 0.0) / 512
+        small = y < 2.0 ** -6
+        assert int(small.sum()) > n // 2
+        assert torch.equal(codes.double()[small], want[small])
