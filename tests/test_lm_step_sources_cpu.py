@@ -45,3 +45,10 @@ def test_no_memory_on_the_device_is_said_so():
     for file, name in (("lm_adam.cu", "cocodc_status cocodc_lm_adam_create("), ("lm_api.cu", "cocodc_status cocodc_lm_create(")):
         body = function(file, name)
         assert "cudaMalloc" not in body and re.search(r"got = [\w:]*allocate\([^;]*;\s*if \(got != COCODC_OK\) \{\s*delete \w+;\s*return got;", body), file
+
+
+def test_long_rows_are_walked_without_a_step_past_31_bits():
+    """A row may have 2^31 - 1 columns: the step behind the last one leaves an int, and what comes then is below the end again."""
+    for kernel in ("k_norm_long(const", "k_norm_grad_long(const"):
+        body = function("lm_norm.cu", kernel)
+        assert body.count("(unsigned c = ") >= 3 and not re.search(r"\bint (c|from|to|at|pace)\b", body), kernel
