@@ -116,7 +116,7 @@ template <typename E>
 __device__ __forceinline__ void emit(const Out& o, const CUtensorMap* map, int rows, int cols, int x, int y, int half, unsigned buf, int lane, float (&v)[32]) {
   if (o.type == COCODC_F32) {
     float* row = static_cast<float*>(o.out) + (long long)(y + lane) * o.ld + x;
-    if (x + 32 <= cols || cols % 4 == 0) {
+    if (cols - x >= 32 || cols % 4 == 0) {
 #pragma unroll
       for (int q = 0; q < 8; ++q)
         asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((q ^ (lane & 7)) << 4)), "f"(v[4 * q]), "f"(v[4 * q + 1]),
@@ -137,7 +137,7 @@ __device__ __forceinline__ void emit(const Out& o, const CUtensorMap* map, int r
   }
   E* row = static_cast<E*>(o.out) + (long long)(y + lane) * o.ld + x;
   const int x0 = x - 32 * half;                       // of the staged tile
-  const bool by_copy = !o.accumulate && (x0 + 64 <= cols || cols % 8 == 0);
+  const bool by_copy = !o.accumulate && (cols - x0 >= 64 || cols % 8 == 0);
   if (by_copy) {
     unsigned packed[16];
 #pragma unroll

@@ -52,3 +52,9 @@ def test_long_rows_are_walked_without_a_step_past_31_bits():
     for kernel in ("k_norm_long(const", "k_norm_grad_long(const"):
         body = function("lm_norm.cu", kernel)
         assert body.count("(unsigned c = ") >= 3 and not re.search(r"\bint (c|from|to|at|pace)\b", body), kernel
+
+
+def test_ends_of_wide_rows_are_told_without_a_sum_past_31_bits():
+    """x0 + 64 is past an int for the last columns of a row of almost 2^31; what is left of the row is not."""
+    body = function("lm_head_tc.cuh", "void emit(")
+    assert "cols - x >= 32" in body and "cols - x0 >= 64" in body and not re.search(r"x0? \+ (32|64) <=", body)
