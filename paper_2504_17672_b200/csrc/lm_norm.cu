@@ -448,43 +448,43 @@ template <typename X, typename S> __global__ void __launch_bounds__(kThreads) k_
   may_follow();
   __shared__ float cell[2][kThreads / 32];
   Join join{cell, 0, kThreads};
-  const unsigned D = a.D;                            // of columns: they may go up to 2^31 - 1, and a step beyond
+  const int D = a.D;                                 // columns are counted from the row's end, -D to -1: D may be 2^31 - 1, and a step beyond it no int
   for (long long row = blockIdx.x; row < a.T; row += gridDim.x) {
-    const X* x = static_cast<const X*>(a.x) + row * a.x_stride;
-    const S* r = static_cast<const S*>(a.residual) + row * a.r_stride;
-    S* total = static_cast<S*>(a.total) + row * a.t_stride;
-    const auto value = [&](unsigned c) { return a.residual ? to_f32(total[c]) : to_f32(x[c]); };
+    const X* x = static_cast<const X*>(a.x) + row * a.x_stride + D;
+    const S* r = static_cast<const S*>(a.residual) + row * a.r_stride + D;
+    S* total = static_cast<S*>(a.total) + row * a.t_stride + D;
+    const auto value = [&](int c) { return a.residual ? to_f32(total[c]) : to_f32(x[c]); };
     float sum = 0.f;
-    for (unsigned c = threadIdx.x; c < D; c += kThreads) {
+    for (int c = (int)threadIdx.x - D; c < 0; c += kThreads) {
       if (a.residual) total[c] = from_f32<S>(to_f32(x[c]) + to_f32(r[c]));
       sum = fmaf(value(c), value(c), sum);
     }
     const float rstd = rms_scale(join(sum, Plus()), 1.f / a.D, a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
-    const auto result = [&](unsigned c) { return value(c) * rstd * load_as(a.weight, a.weight_type, c); };
+    const auto result = [&](int c) { return value(c) * rstd * load_as(a.weight, a.weight_type, (long long)D + c); };
     if (a.groups == 0) {
-      for (unsigned c = threadIdx.x; c < D; c += kThreads) store_as(a.y, a.y_type, row * a.y_stride + c, result(c));
+      for (int c = (int)threadIdx.x - D; c < 0; c += kThreads) store_as(a.y, a.y_type, row * a.y_stride + D + c, result(c));
       continue;
     }
-    const auto finish = [&](unsigned from, unsigned to, float scale, unsigned at, unsigned pace) {
+    const auto finish = [&](int from, int to, float scale, int at, int pace) {
       const Divide by(scale);
-      for (unsigned c = from + at; c < to; c += pace) store_as(a.y, COCODC_E4M3, row * a.y_stride + c, by(result(c)));
+      for (int c = from + at; c < to; c += pace) store_as(a.y, COCODC_E4M3, row * a.y_stride + D + c, by(result(c)));
     };
     if (a.groups == 1) {
       float m = 0.f;
-      for (unsigned c = threadIdx.x; c < D; c += kThreads) m = fmaxf(m, fabsf(result(c)));
+      for (int c = (int)threadIdx.x - D; c < 0; c += kThreads) m = fmaxf(m, fabsf(result(c)));
       const float scale = scale_8(join(m, Most()));
       if (threadIdx.x == 0) a.y_scale[row] = scale;
-      finish(0, D, scale, threadIdx.x, kThreads);
+      finish(-D, 0, scale, threadIdx.x, kThreads);
       continue;
     }
     // a warp takes a group at a time; the columns of its lanes are not those that they summed
     __syncthreads();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     for (int g = warp; g < a.groups; g += kThreads / 32) {
-      const unsigned from = g * 128u, to = min(D, from + 128);
+      const int from = g * 128 - D, to = min(0, from + 128);
       float m = 0.f;
-      for (unsigned c = from + lane; c < to; c += 32) m = fmaxf(m, fabsf(result(c)));
+      for (int c = from + lane; c < to; c += 32) m = fmaxf(m, fabsf(result(c)));
 #pragma unroll
       for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
       const float scale = scale_8(m);
@@ -619,26 +619,26 @@ template <typename Y, typename S> __global__ void __launch_bounds__(kThreads) k_
   may_follow();
   __shared__ float cell[2][kThreads / 32];
   Join join{cell, 0, kThreads};
-  const unsigned D = a.D;
-  float* part = a.parts ? a.parts + (long long)blockIdx.x * a.D : nullptr;
+  const int D = a.D;                                 // columns from the row's end, as in k_norm_long
+  float* part = a.parts ? a.parts + ((long long)blockIdx.x + 1) * D : nullptr;
   if (part)
-    for (unsigned c = threadIdx.x; c < D; c += kThreads) part[c] = 0.f;
+    for (int c = (int)threadIdx.x - D; c < 0; c += kThreads) part[c] = 0.f;
   for (long long row = blockIdx.x; row < a.T; row += gridDim.x) {
-    const Y* dy = static_cast<const Y*>(a.dy) + row * a.dy_stride;
-    const S* s = static_cast<const S*>(a.total) + row * a.t_stride;
-    const S* dt = static_cast<const S*>(a.dtotal) + row * a.dt_stride;
-    S* dx = static_cast<S*>(a.dx) + row * a.dx_stride;
+    const Y* dy = static_cast<const Y*>(a.dy) + row * a.dy_stride + D;
+    const S* s = static_cast<const S*>(a.total) + row * a.t_stride + D;
+    const S* dt = static_cast<const S*>(a.dtotal) + row * a.dt_stride + D;
+    S* dx = static_cast<S*>(a.dx) + row * a.dx_stride + D;
     const float k = a.rstd[row];
     float sum = 0.f;
-    for (unsigned c = threadIdx.x; c < D; c += kThreads) {
+    for (int c = (int)threadIdx.x - D; c < 0; c += kThreads) {
       const float g = to_f32(dy[c]), h = to_f32(s[c]) * k;
       if (part) part[c] = fmaf(g, h, part[c]);
-      sum = fmaf(g * load_as(a.weight, a.weight_type, c), h, sum);
+      sum = fmaf(g * load_as(a.weight, a.weight_type, (long long)D + c), h, sum);
     }
     const float mean = join(sum, Plus()) / a.D;
     if (a.dx)
-      for (unsigned c = threadIdx.x; c < D; c += kThreads) {
-        const float g = to_f32(dy[c]) * load_as(a.weight, a.weight_type, c), h = to_f32(s[c]) * k;
+      for (int c = (int)threadIdx.x - D; c < 0; c += kThreads) {
+        const float g = to_f32(dy[c]) * load_as(a.weight, a.weight_type, (long long)D + c), h = to_f32(s[c]) * k;
         dx[c] = from_f32<S>(fmaf(k, fmaf(-h, mean, g), a.dtotal ? to_f32(dt[c]) : 0.f));
       }
   }

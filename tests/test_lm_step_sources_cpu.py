@@ -48,10 +48,11 @@ def test_no_memory_on_the_device_is_said_so():
 
 
 def test_long_rows_are_walked_without_a_step_past_31_bits():
-    """A row may have 2^31 - 1 columns: the step behind the last one leaves an int, and what comes then is below the end again."""
+    """A row may have 2^31 - 1 columns: the step behind the last one leaves an int, and what comes then is below the end again.
+    So columns are counted from the row's end, up to 0."""
     for kernel in ("k_norm_long(const", "k_norm_grad_long(const"):
         body = function("lm_norm.cu", kernel)
-        assert body.count("(unsigned c = ") >= 3 and not re.search(r"\bint (c|from|to|at|pace)\b", body), kernel
+        assert body.count("for (int c = (int)threadIdx.x - D; c < 0; c += kThreads)") >= 3 and not re.search(r"c < (a\.)?D\b", body), kernel
 
 
 def test_ends_of_wide_rows_are_told_without_a_sum_past_31_bits():
